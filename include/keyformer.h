@@ -302,6 +302,138 @@ int kf_describe_decode(const kf_ctx* ctx, char* buf, size_t n);
 /* Number of kernel launches this context has enqueued so far. */
 int64_t kf_launch_count(const kf_ctx* ctx);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators around the generation step that need no context.  As above: device buffers and scratch belong to the
+ * caller, work is enqueued on `stream` of the current device, arguments are checked on the host before anything is
+ * enqueued, and nothing is allocated.  Scratch holds nothing between calls and need not be cleared; two calls that may run at
+ * the same time (other streams, other captured graphs) need scratch of their own.  Tensors of one call must not overlap
+ * unless they are the same argument.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+#define KF_TYPE_FP16 0
+#define KF_TYPE_BF16 1
+#define KF_TYPE_FP32 2
+
+/* ---- 4-bit caches.  A slot holds the K and the V row of one entry in kf_packed_slot_bytes(d) = 5d/4 bytes:
+ *   [0, d/2)      K codes, two features per byte, the even feature in the low nibble
+ *   [d/2, d)      V codes
+ *   [d, 9d/8)     K groups: for every 32 features two binary16 numbers, scale s and minimum m
+ *   [9d/8, 5d/4)  V groups
+ * A code c stands for the binary16 number s c + m (rounded once).  For a group with extremes lo and hi:
+ * s = (hi - lo) / 15 rounded down to binary16, m = lo, c = rint((x - lo) * (1 / s)) in binary32, at most 15 (0 if s is 0).
+ * A group that holds a NaN or an infinity reads back as NaN throughout. */
+int32_t kf_packed_slot_bytes(int32_t head_dim);   /* 0 if head_dim is not 64, 128 or 256 */
+
+/* Rows of a binary16 cache to slots, e.g. of a layer's kf_view_state after the prompt phase, and back.
+ *   d_K, d_V : DEVICE fp16 [units][n][d], 16-byte aligned;  d_cache : DEVICE [units][budget_k][5d/4], 16-byte aligned, budget_k >= n,
+ *              units * n * d <= 2^37
+ *   d_len    : DEVICE int32 [units] or NULL.  Row j of a unit is converted if j < d_len[unit]; the other slots (rows) and
+ *              those from n on are left as they were. */
+int kf_pack_cache(int64_t units, int32_t n, int32_t budget_k, int32_t head_dim, const void* d_K, const void* d_V,
+                  const int32_t* d_len, void* d_cache, void* stream);
+int kf_unpack_cache(int64_t units, int32_t n, int32_t budget_k, int32_t head_dim, const void* d_cache, const int32_t* d_len,
+                    void* d_K, void* d_V, void* stream);
+
+/* Arguments of kf_decode_step_packed: the quantities kf_decode_step takes from its context. */
+typedef struct kf_packed_step {
+  int32_t batch, n_heads;             /* B, H (B H <= 65535)                                                      */
+  int32_t n_kv_heads;                 /* Hkv: 0 or H, or H / Hkv in {2, 4, 8} query heads share a cache (see kf_config)   */
+  int32_t head_dim;                   /* d in {64, 128, 256}                                                      */
+  int32_t budget_k, recent_w;         /* k, w                                                                     */
+  int32_t layer;                      /* layer index (part of the noise coordinates)                              */
+  int32_t position;                   /* p: original position of the token being generated                        */
+  int32_t noise_mode, bias_mode;      /* KF_NOISE_*, KF_BIAS_*                                                    */
+  double  tau;                        /* temperature of this step (Eq. 12, computed by the caller)                */
+  uint64_t noise_seed;
+  float   logit_scale;                /* 0 => 1/sqrt(d)                                                           */
+  float   noise_const;                /* c of KF_NOISE_CONST                                                      */
+  float   noise_mu, noise_sigma;      /* KF_NOISE_GAUSS                                                           */
+  const float* d_alibi_slopes;        /* DEVICE [H] when bias_mode == KF_BIAS_ALIBI, else ignored                 */
+} kf_packed_step;
+
+/* One generation step of Algorithm 1 (as kf_decode_step, original positions, keys stored as they are to be multiplied)
+ * over a caller-held cache in 4 bits.  Cached rows take part as the values their codes stand for, the new token's own row
+ * as it was passed; it is quantised when it enters the cache.
+ *   d_cache  : DEVICE [B][Hkv][k][5d/4]       slots, updated in place (one replaced or appended per unit)
+ *   d_pos, d_acc, d_len : DEVICE int32 [B][Hkv][k], fp32 [B][Hkv][k], int32 [B][Hkv], updated in place
+ *   d_q, d_out : DEVICE fp16 [B][H][d];  d_knew, d_vnew : DEVICE fp16 [B][Hkv][d]
+ *   d_score_opt : DEVICE fp32 [B][Hkv][k+1] or NULL; z of the slots [0, len), the new token's at index len
+ *   d_slot_opt  : DEVICE int32 [B][Hkv] or NULL; the slot the new row went to, -1 if it was not stored (w = 0 and its own
+ *                 score was the smallest)
+ *   d_row_opt   : DEVICE fp16 [B][Hkv][2][d] or NULL; the new K and V row as the values their codes stand for
+ *   d_scratch   : DEVICE, kf_packed_scratch_bytes(args) bytes, 256-byte aligned (KF_ENOSPC if `scratch_bytes` is less)
+ * d_cache, d_q, d_knew, d_vnew, d_out must be 16-byte aligned.  A unit whose d_len entry is outside 0..k is skipped:
+ * nothing of it is read or written.  A non-finite value in a cached row makes the output of its unit NaN. */
+size_t kf_packed_scratch_bytes(const kf_packed_step* args);   /* 0 if the arguments are invalid */
+int kf_decode_step_packed(const kf_packed_step* args, void* d_cache, int32_t* d_pos, float* d_acc, int32_t* d_len,
+                          const void* d_q, const void* d_knew, const void* d_vnew, void* d_out, float* d_score_opt,
+                          int32_t* d_slot_opt, void* d_row_opt, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/* ---- From projection rows to what the prompt phase and the generation step take.  Per head of queries and keys:
+ *   norm     (KF_NORM_RMS)  x <- x * w / sqrt(mean(x^2) + eps), w = 1 where no weight is passed
+ *   rotation (R > 0)        pair i < R/2 of the first R features turned by position * base^(-2i/R); the pair is (2i, 2i+1)
+ *                           with KF_ROTARY_PAIRS (the embedding of kf_config.rotary_dims) or (i, i + R/2) with KF_ROTARY_HALVES
+ * and head-major rows; the values are only laid out.  Results are rounded once, to binary16 (beyond 65504: infinity). */
+#define KF_NORM_NONE 0
+#define KF_NORM_RMS  1
+#define KF_ROTARY_PAIRS  0
+#define KF_ROTARY_HALVES 1
+typedef struct kf_qk_norm_args {
+  int32_t batch, n_tokens;            /* B n < 2^31                                                               */
+  int32_t n_heads, n_kv_heads;        /* H, Hkv >= 1                                                              */
+  int32_t head_dim;                   /* d in {64, 128, 256}                                                      */
+  int32_t input_type;                 /* of the rows and the weights: KF_TYPE_FP16 or KF_TYPE_BF16                */
+  int64_t batch_stride, token_stride; /* of the rows, in elements, multiples of 8; token_stride >= (H + 2 Hkv) d  */
+  int32_t norm_mode;                  /* KF_NORM_*                                                                */
+  float   eps;                        /* >= 0                                                                     */
+  int32_t rotary_dims, rotary_style;  /* R: 0 or a power of two, 8 <= R <= d; KF_ROTARY_*                         */
+  float   rotary_base;                /* > 1 when R > 0                                                           */
+  int32_t position0;                  /* without d_positions token t of every row stands at position0 + t         */
+} kf_qk_norm_args;
+/*   d_qkv : DEVICE [B][n] rows of H query, Hkv key and Hkv value heads of d features
+ *   d_q_weight, d_k_weight : DEVICE [d] or NULL (only with KF_NORM_RMS);  d_positions : DEVICE int32 [B][n] or NULL
+ *   d_q : DEVICE fp16 [B][H][n][d];  d_k, d_v_opt : DEVICE fp16 [B][Hkv][n][d], d_v_opt may be NULL
+ * All but d_positions 16-byte aligned. */
+int kf_qk_norm_rotate(const kf_qk_norm_args* args, const void* d_qkv, const void* d_q_weight, const void* d_k_weight,
+                      const int32_t* d_positions, void* d_q, void* d_k, void* d_v_opt, void* stream);
+
+/* ---- Beam search (beams are batch rows).  Of the beams x vocabulary continuations of every request the `take` best by
+ *   value(b, t) = score_b + log softmax(logits_b)_t
+ * best first; equal values: the lower beam, then the lower token.  Values are formed in binary64, rounded to binary32.
+ *   - A logit that is NaN or +infinity counts as -infinity (a forbidden token).
+ *   - A beam that d_finished_opt marks (non-zero) goes on with pad_token alone, at value score_b; its logits are not read.
+ *   - A beam whose score is not finite, or whose logits are all forbidden, has value -infinity throughout.
+ *   Continuations at -infinity are returned only when there are no others left, in the order above. */
+typedef struct kf_beam_args {
+  int32_t batch, beams;               /* beams <= 32, batch * beams <= 65535                                      */
+  int32_t vocab, take;                /* take <= 64, take <= beams * vocab                                        */
+  int32_t logits_type;                /* KF_TYPE_*                                                                */
+  int32_t pad_token;                  /* 0 <= pad_token < vocab                                                   */
+  int64_t row_stride;                 /* elements between the rows of two beams, >= vocab                         */
+} kf_beam_args;
+/*   d_logits : DEVICE [B * beams] rows;  d_scores : DEVICE fp32 [B][beams];  d_finished_opt : DEVICE uint8 [B][beams] or NULL
+ *   d_out_scores fp32, d_out_parent, d_out_token int32 : DEVICE [B][take]; d_out_scores may not be d_scores
+ *   d_scratch : DEVICE, kf_beam_scratch_bytes(args) bytes, 256-byte aligned */
+size_t kf_beam_scratch_bytes(const kf_beam_args* args);
+int kf_beam_select(const kf_beam_args* args, const void* d_logits, const float* d_scores, const uint8_t* d_finished_opt,
+                   float* d_out_scores, int32_t* d_out_parent, int32_t* d_out_token, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/* State rows that follow their beam: in every buffer [outer][batch * beams][row_bytes], row (b, i) becomes what row
+ * (b, d_parent[b][i]) was before the call, in place.  A parent outside 0..beams-1 leaves its row as it is.
+ *   d_parent : DEVICE int32 [batch][beams].  At most 8 buffers; any row_bytes (multiples of 16 move fastest). */
+typedef struct kf_row_buffer {
+  void*   d_base;
+  int64_t row_bytes;
+  int64_t outer_stride;               /* bytes between two outer indices (layers), >= batch * beams * row_bytes; unused when outer is 1 */
+  int32_t outer;                      /* >= 1                                                                     */
+} kf_row_buffer;
+int kf_reorder_rows(const kf_row_buffer* buffers, int32_t n_buffers, int32_t batch, int32_t beams, const int32_t* d_parent, void* stream);
+
+/* The same for the caches of a context (K, V, positions, scores, entry counts, places): its batch rows are
+ * batch / beams requests of `beams` beams each (KF_EINVAL if beams does not divide the batch).  layer >= 0: that layer
+ * (KF_ESTATE before its prompt phase); layer = -1: all layers, one launch. */
+int kf_reorder_beams(kf_ctx* ctx, int32_t layer, int32_t beams, const int32_t* d_parent, void* stream);
+
 /* Frees host metadata.  The workspace stays with the caller. */
 int kf_destroy(kf_ctx* ctx);
 

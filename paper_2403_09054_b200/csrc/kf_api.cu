@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "kf_decode.cuh"
+#include "kf_ops.cuh"
 #include "kf_prefill.cuh"
 
 namespace {
@@ -567,6 +568,35 @@ int kf_compact_layer(kf_ctx* ctx, int32_t layer, void* stream) {
                          c.budget_k, c.head_dim, L.units, static_cast<cudaStream_t>(stream)) != cudaSuccess)
     return KF_ECUDA;
   ctx->launches += 2;
+  return KF_OK;
+}
+
+int kf_reorder_beams(kf_ctx* ctx, int32_t layer, int32_t beams, const int32_t* d_parent, void* stream) {
+  if (!ctx || !d_parent || (reinterpret_cast<uintptr_t>(d_parent) & 3u)) return KF_EINVAL;
+  const kf_config& c = ctx->cfg;
+  if (layer < -1 || layer >= c.n_layers || beams < 1 || beams > kf::BEAM_MAX || c.batch % beams != 0) return KF_EINVAL;
+  for (int l = layer < 0 ? 0 : layer; l < (layer < 0 ? c.n_layers : layer + 1); ++l)
+    if (ctx->n_prompt[l] < 0) return KF_ESTATE;
+  const Layout& L = ctx->lay;
+  const int64_t hkv = L.units / c.batch, slots = hkv * c.budget_k;
+  const size_t first = layer < 0 ? 0 : (size_t)layer;
+  kf::ReorderParams P{};
+  auto add = [&](size_t off, size_t stride, int64_t row_bytes) {
+    kf::ReorderBuffer& b = P.buf[P.n_buffers++];
+    b.base = ctx->ws + off + first * stride;
+    b.row_bytes = row_bytes;
+    b.outer = layer < 0 ? c.n_layers : 1;
+    b.outer_stride = (int64_t)stride;
+  };
+  add(L.K, L.kv_layer, slots * c.head_dim * 2);
+  add(L.V, L.kv_layer, slots * c.head_dim * 2);
+  add(L.acc, L.sc_layer, slots * 4);
+  add(L.pos, L.sc_layer, slots * 4);
+  add(L.len, L.len_layer, hkv * 4);
+  if (c.pos_mode == KF_POS_NEW) add(L.place, L.sc_layer, slots * 4);
+  P.parent = d_parent; P.batch = c.batch / beams; P.beams = beams;
+  if (kf::launch_reorder(P, static_cast<cudaStream_t>(stream)) != cudaSuccess) return KF_ECUDA;
+  ctx->launches += 1;
   return KF_OK;
 }
 

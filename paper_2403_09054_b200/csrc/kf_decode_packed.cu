@@ -1,0 +1,440 @@
+// One generation step over a 4-bit cache (slot format: kf_packed.cuh); the arithmetic of Algorithm 1 is that of
+// kf_decode.cu, only the rows are read from 4 bits.  Two launches: packed_stream_kernel reads every slot once and
+// leaves one partial per split, packed_close_kernel (the closing stage of kf_close.cuh with a 4-bit row store) merges,
+// scores, evicts and writes the new token's slot.
+//
+// Per slot 1.25 d bytes come from HBM, a quarter of the binary16 form less the group parameters, so the arithmetic that the
+// binary16 kernel hides behind its loads would bound this one: 2 d multiply-adds per slot and head and as many
+// conversions.  Both products therefore run on the tensor pipe as m16n8k16 instructions whose 4-bit operand is
+// converted in registers (it never passes through shared memory, which is why mma.sync and not tcgen05, whose
+// operands have to lie there): S = K q^T with slots as rows, O^T = V^T p^T with features as rows, the query heads of a
+// cache (1, 2, 4 or 8) in the eight columns.  A contraction may take its terms in any order, so every lane contracts
+// the features (for S) or the slots (for O) that its own 16-byte loads brought, and the other operand is laid out to match.
+//
+// Every warp walks 32-slot tiles of its CTA's range by itself.  The registers of the K tile are reloaded for the next tile
+// as soon as the logits exist, those of the V tile as soon as the output is updated: a tile is always in flight.
+#include "kf_close.cuh"
+#include "kf_packed.cuh"
+
+#include <algorithm>
+
+namespace kf {
+
+namespace {
+
+constexpr int TILE = 32;   // slots per tile, one per lane in the per-logit work
+constexpr int NW = 4;      // warps per CTA
+
+// ---- noise.  ln x for normal x > 0: x = 2^e (1 + f), f in [sqrt(1/2) - 1, sqrt(2) - 1], t = f / (2 + f),
+// ln(1 + f) = 2 atanh(t) = 2 t (1 + t^2/3 + t^4/5 + ...) with 2 t = f - t f; the terms up to t^9 leave 1e-9.  Relative
+// error below 3e-7 right up to x = 1, where the largest Gumbel variates come from.
+__device__ __forceinline__ float ln_atanh(float x) {
+  const int bits = __float_as_int(x);
+  const int e = (bits - 0x3f3504f3) >> 23;                    // 0x3f3504f3: sqrt(1/2)
+  const float f = __int_as_float(bits - (e << 23)) - 1.0f;
+  const float t = __fdividef(f, 2.0f + f), z = t * t;
+  const float r = 2.0f * z * fmaf(z, fmaf(z, fmaf(z, 1.0f / 9.0f, 1.0f / 7.0f), 0.2f), 1.0f / 3.0f);
+  return fmaf((float)e, LN2, f - t * (f - r));
+}
+__device__ __forceinline__ float packed_noise(const PackedParams& P, uint32_t b, uint32_t lh, uint32_t i, uint32_t j) {
+  if (P.noise_mode == 0) return -ln_atanh(-ln_atanh(uniform_from_word(noise_word(P.pk, b, lh, i, j))));
+  return noise_for(P, b, lh, i, j);
+}
+
+// ---- the new token's row, quantised by the closing CTA.  Warps hold 32 consecutive features at a time: one group.
+template <int D, int NT, int CPT>
+struct CloseRow<PackedParams, D, NT, CPT> {
+  __half kn[CPT], vn[CPT];
+  __half2 kg[CPT], vg[CPT];     // the groups of the thread's columns
+  uint32_t code[CPT];           // K code | V code << 4
+
+  static __device__ __forceinline__ float noise(const PackedParams& P, uint32_t b, uint32_t lh, uint32_t i, uint32_t j) {
+    return packed_noise(P, b, lh, i, j);
+  }
+  static __device__ __forceinline__ __half2 group_of(__half x) {
+    __half low = x, high = x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      low = __hmin_nan(low, __shfl_xor_sync(0xffffffffu, low, o));
+      high = __hmax_nan(high, __shfl_xor_sync(0xffffffffu, high, o));
+    }
+    return packed_group(__half2float(low), __half2float(high));
+  }
+  static __device__ __forceinline__ __half value(uint32_t code, __half2 g) {
+    return __hfma(__float2half_rn((float)code), __low2half(g), __high2half(g));
+  }
+  __device__ __forceinline__ void prepare(const PackedParams& P, int u) {
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      kg[i] = group_of(kn[i]);
+      vg[i] = group_of(vn[i]);
+      const uint32_t kc = packed_code(__half2float(kn[i]), __high2float(kg[i]), packed_inverse(__low2half(kg[i])));
+      const uint32_t vc = packed_code(__half2float(vn[i]), __high2float(vg[i]), packed_inverse(__low2half(vg[i])));
+      code[i] = kc | vc << 4;
+      const int c = threadIdx.x + i * NT;
+      if (P.row_opt && c < D) {
+        P.row_opt[(size_t)u * 2 * D + c] = value(kc, kg[i]);
+        P.row_opt[(size_t)u * 2 * D + D + c] = value(vc, vg[i]);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(const PackedParams& P, int u, int slot) const {
+    if (P.slot_opt && threadIdx.x == 0) P.slot_opt[u] = slot;
+    if (slot < 0) return;
+    unsigned char* at = P.cache + ((size_t)u * P.k + slot) * packed_slot_bytes(D);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      const int c = threadIdx.x + i * NT;
+      const uint32_t next = __shfl_down_sync(0xffffffffu, code[i], 1);   // the odd feature's codes
+      if (c < D && (c & 1) == 0) {
+        at[c / 2] = (unsigned char)((code[i] & 15u) | (next & 15u) << 4);
+        at[D / 2 + c / 2] = (unsigned char)(code[i] >> 4 | (next & 0xf0u));
+      }
+      if (c < D && (c & 31) == 0) {
+        *reinterpret_cast<uint32_t*>(at + D + c / 8) = h2_bits(kg[i]);
+        *reinterpret_cast<uint32_t*>(at + D + D / 8 + c / 8) = h2_bits(vg[i]);
+      }
+    }
+  }
+};
+
+// Loads that leave L1 alone: every byte of the cache is wanted once.
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&w)[N], const unsigned char* p) {
+  if constexpr (N == 1) {
+    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+  } else if constexpr (N == 2) {
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "l"(p + 4 * i));
+  }
+}
+
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ float redux_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// What a lane holds of a 32-slot tile.  K: rows (lane / 4) + 8 i, features [(lane % 4) D/4, + D/4) of each.
+// V: slots 16 h + 4 (lane % 4) + {0 .. 3}, features [(lane / 4) D/8, + D/8) of each.
+template <int D>
+struct KTile {
+  static constexpr int W = D / 32;                 // code words per row and lane
+  static constexpr int NG = D == 256 ? 2 : 1;      // groups those features span
+  uint32_t w[4][W], g[4][NG];
+  __device__ __forceinline__ void load(const unsigned char* base, int rows, int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = (lane >> 2) + 8 * i, t = lane & 3;
+      const unsigned char* slot = base + r * packed_slot_bytes(D);
+      if (r < rows) {
+        load_words(w[i], slot + t * (D / 8));
+        load_words(g[i], slot + D + (D == 64 ? (t >> 1) * 4 : t * NG * 4));
+      } else {
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[i][j] = 0u;
+#pragma unroll
+        for (int j = 0; j < NG; ++j) g[i][j] = 0u;
+      }
+    }
+  }
+};
+template <int D>
+struct VTile {
+  static constexpr int W = D / 64;
+  uint32_t w[8][W], g[8][1];
+  __device__ __forceinline__ void load(const unsigned char* base, int rows, int lane) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = (i >> 2) * 16 + (lane & 3) * 4 + (i & 3), f = lane >> 2;
+      const unsigned char* slot = base + r * packed_slot_bytes(D);
+      if (r < rows) {
+        load_words(w[i], slot + D / 2 + f * (D / 16));
+        load_words(g[i], slot + D + D / 8 + (f * (D / 8) / PACK_GROUP) * 4);
+      } else {   // a slot behind the last entry: zeros, whatever it holds
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[i][j] = 0u;
+        g[i][0] = 0u;
+      }
+    }
+  }
+};
+
+template <int D, int G>
+__global__ void __launch_bounds__(NW * 32) packed_stream_kernel(const __grid_constant__ PackedParams P) {
+  constexpr int PSTRIDE = 4 + D;
+  constexpr int NT = NW * 32;
+  __shared__ float sh_m[NW][G], sh_l[NW][G], sh_my[NW][G], sh_ly[NW][G];
+  __shared__ float sh_o[NW][G][D];
+  __shared__ float sh_x[NW][G][TILE];                       // logits of the warp's tile, one column per slot
+  __shared__ __align__(8) __half sh_p[NW][G][TILE];         // output weights, binary16 operands of the second product
+
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int s = blockIdx.x, u = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int r8 = lane >> 2, t4 = lane & 3;
+  const int len = P.len[u];
+  if (len < 0 || len > P.k) return;   // a damaged entry count: nothing of this unit is touched
+  const int row_begin = s * P.tiles_per_split * TILE;
+  const int row_end = min(len, row_begin + P.tiles_per_split * TILE);
+  const unsigned char* cache_u = P.cache + (size_t)u * P.k * packed_slot_bytes(D);
+  const int32_t* pos_u = P.pos + (size_t)u * P.k;
+  const int Hkv = P.H / G;
+  const uint32_t b = (uint32_t)(u / Hkv), h0 = (uint32_t)(u % Hkv) * G, lh0 = (uint32_t)P.layer * P.H + h0;
+
+  int tile = row_begin + warp * TILE;
+  KTile<D> kt;
+  VTile<D> vt;
+  kt.load(cache_u + (size_t)tile * packed_slot_bytes(D), row_end - tile, lane);
+  vt.load(cache_u + (size_t)tile * packed_slot_bytes(D), row_end - tile, lane);
+  int pos_next = tile + lane < row_end ? pos_u[tile + lane] : 0;
+
+  // queries as the second operand of S: column = head r8, the features this lane's K words bring, pairs (i, i + 4)
+  uint32_t qf[D / 32][4];
+#pragma unroll
+  for (int w = 0; w < D / 32; ++w) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r8 < G) v = *reinterpret_cast<const uint4*>(P.q + ((size_t)u * G + r8) * D + t4 * (D / 4) + 8 * w);
+    qf[w][0] = __byte_perm(v.x, v.z, 0x5410);
+    qf[w][1] = __byte_perm(v.x, v.z, 0x7632);
+    qf[w][2] = __byte_perm(v.y, v.w, 0x5410);
+    qf[w][3] = __byte_perm(v.y, v.w, 0x7632);
+  }
+
+  float m_x[G], l_x[G], m_y[G], l_y[G];   // m_*: common to the warp; l_*: this lane's slots
+#pragma unroll
+  for (int g = 0; g < G; ++g) { m_x[g] = -INFINITY; l_x[g] = 0.f; m_y[g] = -INFINITY; l_y[g] = 0.f; }
+  float o[D / 16][4];                      // out^T: features as rows, heads 2 t4 and 2 t4 + 1 as columns
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[i][c] = 0.f;
+
+  for (; tile < row_end; tile += NW * TILE) {
+    const int rows = row_end - tile;        // may exceed TILE
+    const int after = tile + NW * TILE;
+    const unsigned char* next = cache_u + (size_t)after * packed_slot_bytes(D);
+    const int pj = pos_next;
+    pos_next = after + lane < row_end ? pos_u[after + lane] : 0;
+
+    // ---- logits
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w) {
+        __half2 a[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const __half2 g = bits_h2(kt.g[2 * h + i][D == 256 ? w / 4 : 0]);
+          nibble_pairs(kt.w[2 * h + i][w], a[i]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) a[i][e] = __hfma2(a[i][e], __low2half2(g), __high2half2(g));
+        }
+        mma_16816(c, h2_bits(a[0][0]), h2_bits(a[1][0]), h2_bits(a[0][1]), h2_bits(a[1][1]), qf[w][0], qf[w][1]);
+        mma_16816(c, h2_bits(a[0][2]), h2_bits(a[1][2]), h2_bits(a[0][3]), h2_bits(a[1][3]), qf[w][2], qf[w][3]);
+      }
+      if (2 * t4 < G) { sh_x[warp][2 * t4][16 * h + r8] = c[0]; sh_x[warp][2 * t4][16 * h + 8 + r8] = c[2]; }
+      if (2 * t4 + 1 < G) { sh_x[warp][2 * t4 + 1][16 * h + r8] = c[1]; sh_x[warp][2 * t4 + 1][16 * h + 8 + r8] = c[3]; }
+    }
+    kt.load(next, row_end - after, lane);
+    __syncwarp();
+
+    // ---- per logit (a lane is a slot): bias, noise, the two running softmaxes.  The output weights are taken against a
+    //      reference that moves only when a tile exceeds it by 2^8, so that the accumulators are hardly ever rescaled
+    //      (binary16 holds weights up to 2^8, the sums are binary32).
+    const bool valid = lane < rows;
+    float scale_o[G];
+    bool moved = false;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float x = -INFINITY, y = -INFINITY;
+      if (valid) {
+        const float slope = P.slopes ? P.slopes[h0 + g] : 0.f;
+        x = fmaf(sh_x[warp][g][lane], P.scale, -slope * (float)(P.p - pj));
+        y = (x + packed_noise(P, b, lh0 + g, (uint32_t)P.p, (uint32_t)pj)) * P.inv_tau;
+        P.y_scratch[((size_t)u * G + g) * (P.k + 1) + tile + lane] = y;
+      }
+      const float tx = redux_max(x), my_new = fmaxf(m_y[g], redux_max(y));
+      scale_o[g] = 1.f;
+      if (!(tx <= m_x[g] + 5.5f)) {   // 2^8 = e^5.55; also the first tile (and a NaN, which stays one)
+        scale_o[g] = fast_exp2((m_x[g] - tx) * LOG2E);
+        m_x[g] = tx;
+        l_x[g] *= scale_o[g];
+        moved = true;
+      }
+      const float px = valid ? fast_exp2((x - m_x[g]) * LOG2E) : 0.f;
+      const float ey = valid ? fast_exp2((y - my_new) * LOG2E) : 0.f;
+      l_x[g] += px;
+      l_y[g] = fmaf(l_y[g], fast_exp2((m_y[g] - my_new) * LOG2E), ey);
+      m_y[g] = my_new;
+      sh_p[warp][g][lane] = __float2half_rn(px);
+    }
+    if (moved) {
+      float f0 = 1.f, f1 = 1.f;   // of this lane's two columns
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        if (g == 2 * t4) f0 = scale_o[g];
+        if (g == 2 * t4 + 1) f1 = scale_o[g];
+      }
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) { o[i][0] *= f0; o[i][1] *= f1; o[i][2] *= f0; o[i][3] *= f1; }
+    }
+    __syncwarp();
+
+    // ---- values
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint2 pb = make_uint2(0, 0);   // weights of slots 4 t4 .. 4 t4 + 3 for head r8
+      if (r8 < G) pb = *reinterpret_cast<const uint2*>(&sh_p[warp][r8][16 * h + 4 * t4]);
+#pragma unroll
+      for (int w = 0; w < VTile<D>::W; ++w) {
+        __half2 lo[2][4], hi[2][4];   // features 8 w + (0 .. 3) and + (4 .. 7); a pair is two neighbouring slots
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int i = 4 * h + 2 * e;
+          const __half2 sc = bits_h2(__byte_perm(vt.g[i][0], vt.g[i + 1][0], 0x5410)), mn = bits_h2(__byte_perm(vt.g[i][0], vt.g[i + 1][0], 0x7632));
+          nibble_pairs(__byte_perm(vt.w[i][w], vt.w[i + 1][w], 0x5410), lo[e]);
+          nibble_pairs(__byte_perm(vt.w[i][w], vt.w[i + 1][w], 0x7632), hi[e]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { lo[e][j] = __hfma2(lo[e][j], sc, mn); hi[e][j] = __hfma2(hi[e][j], sc, mn); }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          mma_16816(o[4 * w + j], h2_bits(lo[0][j]), h2_bits(hi[0][j]), h2_bits(lo[1][j]), h2_bits(hi[1][j]), pb.x, pb.y);
+      }
+    }
+    vt.load(next, row_end - after, lane);
+    __syncwarp();   // the next tile overwrites the warp's logits and weights
+  }
+
+  // ---- merge the lanes, then the warps of this CTA
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const int f = r8 * (D / 8) + (i >> 2) * 8 + (i & 3);
+    if (2 * t4 < G) { sh_o[warp][2 * t4][f] = o[i][0]; sh_o[warp][2 * t4][f + 4] = o[i][2]; }
+    if (2 * t4 + 1 < G) { sh_o[warp][2 * t4 + 1][f] = o[i][1]; sh_o[warp][2 * t4 + 1][f + 4] = o[i][3]; }
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    l_x[g] = warp_sum(l_x[g]);
+    l_y[g] = warp_sum(l_y[g]);
+    if (lane == 0) { sh_m[warp][g] = m_x[g]; sh_l[warp][g] = l_x[g]; sh_my[warp][g] = m_y[g]; sh_ly[warp][g] = l_y[g]; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    float* part = P.partials + (((size_t)u * P.splits + s) * G + g) * PSTRIDE;
+    float M = -INFINITY, MY = -INFINITY;
+#pragma unroll
+    for (int wi = 0; wi < NW; ++wi) { M = fmaxf(M, sh_m[wi][g]); MY = fmaxf(MY, sh_my[wi][g]); }
+    float sc[NW];
+#pragma unroll
+    for (int wi = 0; wi < NW; ++wi) sc[wi] = sh_l[wi][g] > 0.f ? fast_exp2((sh_m[wi][g] - M) * LOG2E) : 0.f;
+    for (int c = tid; c < D; c += NT) {
+      float acc_o = 0.f;
+#pragma unroll
+      for (int wi = 0; wi < NW; ++wi) acc_o = fmaf(sh_o[wi][g][c], sc[wi], acc_o);
+      part[4 + c] = acc_o;
+    }
+    if (tid == 0) {
+      float L = 0.f, LY = 0.f;
+#pragma unroll
+      for (int wi = 0; wi < NW; ++wi) {
+        L = fmaf(sh_l[wi][g], sc[wi], L);
+        if (sh_ly[wi][g] > 0.f) LY = fmaf(sh_ly[wi][g], fast_exp2((sh_my[wi][g] - MY) * LOG2E), LY);
+      }
+      part[0] = M; part[1] = L; part[2] = MY; part[3] = LY;
+    }
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(512, 1) packed_close_wide_kernel(const __grid_constant__ PackedParams P) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int u = blockIdx.x;
+  const int len = P.len[u];
+  if (len < 0 || len > P.k) return;
+  combine_and_evict_group<D, 512, 1>(P, u, len);
+}
+
+template <int D, int G>
+__global__ void __launch_bounds__(close_threads(D, G), G == 1 ? 6 : (G == 8 ? 1 : 2)) packed_close_kernel(const __grid_constant__ PackedParams P) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int u = blockIdx.x;
+  const int len = P.len[u];
+  if (len < 0 || len > P.k) return;
+  if constexpr (G == 1) combine_and_evict<D, 128, 1>(P, u, len);
+  else combine_and_evict_group<D, close_threads(D, G), G>(P, u, len);
+}
+
+template <int D, int G>
+cudaError_t launch_one(const PackedParams& P, int units, cudaStream_t stream) {
+  // Programmatic stream serialization on both launches, as for the binary16 kernels.
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)P.splits, (unsigned)units);
+  cfg.blockDim = dim3(NW * 32);
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, packed_stream_kernel<D, G>, P);
+  if (e != cudaSuccess) return e;
+  cfg.gridDim = dim3((unsigned)units);
+  cfg.blockDim = dim3(close_threads(D, G));
+  if constexpr (G == 1) {
+    if (close_is_wide(units, P.k)) {
+      cfg.blockDim = dim3(512);
+      return cudaLaunchKernelEx(&cfg, packed_close_wide_kernel<D>, P);
+    }
+  }
+  return cudaLaunchKernelEx(&cfg, packed_close_kernel<D, G>, P);
+}
+
+template <int D>
+cudaError_t launch_dim(const PackedParams& P, int units, cudaStream_t stream) {
+  switch (P.group) {
+    case 1: return launch_one<D, 1>(P, units, stream);
+    case 2: return launch_one<D, 2>(P, units, stream);
+    case 4: return launch_one<D, 4>(P, units, stream);
+    case 8: return launch_one<D, 8>(P, units, stream);
+    default: return cudaErrorInvalidValue;
+  }
+}
+
+}  // namespace
+
+void decode_packed_plan(int units, int budget_k, int head_dim, int* splits_out, int* tiles_per_split_out) {
+  const int tiles = (budget_k + TILE - 1) / TILE;
+  const int target_ctas = units >= 148 ? 148 * 16 : 148 * 4;
+  int splits = (target_ctas + units - 1) / units;
+  splits = std::max(1, std::min(splits, std::min(MAX_SPLITS, (tiles + NW - 1) / NW)));
+  int tps = (tiles + splits - 1) / splits;
+  tps = (tps + NW - 1) / NW * NW;   // whole rounds of the CTA's warps
+  *splits_out = (tiles + tps - 1) / tps;
+  *tiles_per_split_out = tps;
+}
+
+cudaError_t launch_decode_packed(const PackedParams& P, int head_dim, int units, cudaStream_t stream) {
+  if (P.splits < 1 || P.splits > MAX_SPLITS) return cudaErrorInvalidValue;
+  switch (head_dim) {
+    case 64: return launch_dim<64>(P, units, stream);
+    case 128: return launch_dim<128>(P, units, stream);
+    case 256: return launch_dim<256>(P, units, stream);
+    default: return cudaErrorInvalidValue;
+  }
+}
+
+}  // namespace kf

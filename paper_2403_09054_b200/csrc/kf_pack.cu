@@ -1,0 +1,137 @@
+// Conversion of cache rows between binary16 and the 4-bit slots of kf_packed.cuh.  Pure streaming: every row is read
+// once and every slot written once, so HBM bounds both directions (4 d + 1.25 d bytes per slot).
+//
+// A thread owns eight features (one 16-byte chunk) of the K row and of the V row of a slot, so that two loads are in
+// flight per thread and a group of 32 features is four neighbouring lanes: its extremes take two shuffles each.
+#include "kf_packed.cuh"
+
+namespace kf {
+
+namespace {
+
+constexpr int THREADS = 256;
+
+// Extremes of the eight features; a NaN wins over every number, so that a group that holds one is recognised.
+__device__ __forceinline__ void extremes8(const uint4& v, __half2& low, __half2& high) {
+  const __half2 a = bits_h2(v.x), b = bits_h2(v.y), c = bits_h2(v.z), d = bits_h2(v.w);
+  low = __hmin2_nan(__hmin2_nan(a, b), __hmin2_nan(c, d));
+  high = __hmax2_nan(__hmax2_nan(a, b), __hmax2_nan(c, d));
+}
+
+__device__ __forceinline__ uint32_t pack8(const uint4& v, float low, float inverse) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t code = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(bits_h2(w[i]));
+    code |= packed_code(f.x, low, inverse) << (8 * i);
+    code |= packed_code(f.y, low, inverse) << (8 * i + 4);
+  }
+  return code;
+}
+
+// (scale, minimum) of the group this lane's chunk belongs to; the four lanes of a group call it together.
+__device__ __forceinline__ __half2 group_of(const uint4& v) {
+  __half2 low, high;
+  extremes8(v, low, high);
+#pragma unroll
+  for (int o = 1; o <= 2; o <<= 1) {
+    low = __hmin2_nan(low, __shfl_xor_sync(0xffffffffu, low, o));
+    high = __hmax2_nan(high, __shfl_xor_sync(0xffffffffu, high, o));
+  }
+  const __half lo = __hmin_nan(__low2half(low), __high2half(low)), hi = __hmax_nan(__low2half(high), __high2half(high));
+  return packed_group(__half2float(lo), __half2float(hi));
+}
+
+template <int D>
+__global__ void __launch_bounds__(THREADS) pack_kernel(const __half* __restrict__ K, const __half* __restrict__ V,
+                                                       const int32_t* __restrict__ len, unsigned char* __restrict__ cache,
+                                                       int64_t rows, int n, int k) {
+  constexpr int CPR = D / 8;   // chunks per row
+  const int64_t idx = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+  const int64_t row = idx / CPR;
+  const int c = (int)(idx % CPR);
+  bool in = row < rows;
+  const int64_t u = in ? row / n : 0;
+  const int j = in ? (int)(row % n) : 0;
+  if (in && len) in = j < len[u];
+  uint4 kv = make_uint4(0, 0, 0, 0), vv = kv;
+  if (in) {
+    kv = __ldcs(reinterpret_cast<const uint4*>(K + row * D) + c);
+    vv = __ldcs(reinterpret_cast<const uint4*>(V + row * D) + c);
+  }
+  const __half2 kg = group_of(kv), vg = group_of(vv);   // whole warps: a group never straddles a row
+  if (!in) return;
+  unsigned char* slot = cache + ((size_t)u * k + j) * packed_slot_bytes(D);
+  *reinterpret_cast<uint32_t*>(slot + 4 * c) = pack8(kv, __high2float(kg), packed_inverse(__low2half(kg)));
+  *reinterpret_cast<uint32_t*>(slot + D / 2 + 4 * c) = pack8(vv, __high2float(vg), packed_inverse(__low2half(vg)));
+  if ((c & 3) == 0) {
+    *reinterpret_cast<uint32_t*>(slot + D + c) = h2_bits(kg);
+    *reinterpret_cast<uint32_t*>(slot + D + D / 8 + c) = h2_bits(vg);
+  }
+}
+
+__device__ __forceinline__ uint4 unpack8(uint32_t w, __half2 group) {
+  const __half2 s = __low2half2(group), m = __high2half2(group);
+  __half2 c[4];
+  nibble_pairs(w, c);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c[i] = __hfma2(c[i], s, m);   // pairs (i, i + 4)
+  uint4 out;
+  out.x = h2_bits(__lows2half2(c[0], c[1]));
+  out.y = h2_bits(__lows2half2(c[2], c[3]));
+  out.z = h2_bits(__highs2half2(c[0], c[1]));
+  out.w = h2_bits(__highs2half2(c[2], c[3]));
+  return out;
+}
+
+template <int D>
+__global__ void __launch_bounds__(THREADS) unpack_kernel(const unsigned char* __restrict__ cache, const int32_t* __restrict__ len,
+                                                         __half* __restrict__ K, __half* __restrict__ V, int64_t rows, int n, int k) {
+  constexpr int CPR = D / 8;
+  const int64_t idx = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+  const int64_t row = idx / CPR;
+  const int c = (int)(idx % CPR);
+  if (row >= rows) return;
+  const int64_t u = row / n;
+  const int j = (int)(row % n);
+  if (len && j >= len[u]) return;
+  const unsigned char* slot = cache + ((size_t)u * k + j) * packed_slot_bytes(D);
+  const uint32_t kw = *reinterpret_cast<const uint32_t*>(slot + 4 * c), vw = *reinterpret_cast<const uint32_t*>(slot + D / 2 + 4 * c);
+  const uint32_t kg = *reinterpret_cast<const uint32_t*>(slot + D + 4 * (c / 4));
+  const uint32_t vg = *reinterpret_cast<const uint32_t*>(slot + D + D / 8 + 4 * (c / 4));
+  __stcs(reinterpret_cast<uint4*>(K + row * D) + c, unpack8(kw, bits_h2(kg)));
+  __stcs(reinterpret_cast<uint4*>(V + row * D) + c, unpack8(vw, bits_h2(vg)));
+}
+
+inline unsigned blocks_for(int64_t rows, int d) { return (unsigned)((rows * (d / 8) + THREADS - 1) / THREADS); }
+
+}  // namespace
+
+cudaError_t launch_pack(const __half* K, const __half* V, const int32_t* len, unsigned char* cache, int64_t units, int n, int k,
+                        int head_dim, cudaStream_t stream) {
+  const int64_t rows = units * n;
+  const unsigned grid = blocks_for(rows, head_dim);
+  switch (head_dim) {
+    case 64: pack_kernel<64><<<grid, THREADS, 0, stream>>>(K, V, len, cache, rows, n, k); break;
+    case 128: pack_kernel<128><<<grid, THREADS, 0, stream>>>(K, V, len, cache, rows, n, k); break;
+    case 256: pack_kernel<256><<<grid, THREADS, 0, stream>>>(K, V, len, cache, rows, n, k); break;
+    default: return cudaErrorInvalidValue;
+  }
+  return cudaGetLastError();
+}
+
+cudaError_t launch_unpack(const unsigned char* cache, const int32_t* len, __half* K, __half* V, int64_t units, int n, int k,
+                          int head_dim, cudaStream_t stream) {
+  const int64_t rows = units * n;
+  const unsigned grid = blocks_for(rows, head_dim);
+  switch (head_dim) {
+    case 64: unpack_kernel<64><<<grid, THREADS, 0, stream>>>(cache, len, K, V, rows, n, k); break;
+    case 128: unpack_kernel<128><<<grid, THREADS, 0, stream>>>(cache, len, K, V, rows, n, k); break;
+    case 256: unpack_kernel<256><<<grid, THREADS, 0, stream>>>(cache, len, K, V, rows, n, k); break;
+    default: return cudaErrorInvalidValue;
+  }
+  return cudaGetLastError();
+}
+
+}  // namespace kf
