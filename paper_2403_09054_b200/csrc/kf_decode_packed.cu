@@ -11,8 +11,9 @@
 // cache (1, 2, 4 or 8) in the eight columns.  A contraction may take its terms in any order, so every lane contracts
 // the features (for S) or the slots (for O) that its own 16-byte loads brought, and the other operand is laid out to match.
 //
-// Every warp walks 32-slot tiles of its CTA's range by itself.  The registers of the K tile are reloaded for the next tile
-// as soon as the logits exist, those of the V tile as soon as the output is updated: a tile is always in flight.
+// Every warp walks 32-slot tiles of its CTA's range by itself, through a private ring of two shared-memory buffers filled by
+// one bulk copy per tile (a tile is contiguous): no register holds a row that is still on its way, so that twenty warps
+// fit an SM and hide one another's conversion chains.
 #include "kf_close.cuh"
 #include "kf_packed.cuh"
 
@@ -98,21 +99,6 @@ struct CloseRow<PackedParams, D, NT, CPT> {
   }
 };
 
-// Loads that leave L1 alone: every byte of the cache is wanted once.
-template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&w)[N], const unsigned char* p) {
-  if constexpr (N == 1) {
-    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
-  } else if constexpr (N == 2) {
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 4)
-      asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "l"(p + 4 * i));
-  }
-}
-
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -124,59 +110,38 @@ __device__ __forceinline__ float redux_max(float v) {
   return r;
 }
 
-// What a lane holds of a 32-slot tile.  K: rows (lane / 4) + 8 i, features [(lane % 4) D/4, + D/4) of each.
-// V: slots 16 h + 4 (lane % 4) + {0 .. 3}, features [(lane / 4) D/8, + D/8) of each.
-template <int D>
-struct KTile {
-  static constexpr int W = D / 32;                 // code words per row and lane
-  static constexpr int NG = D == 256 ? 2 : 1;      // groups those features span
-  uint32_t w[4][W], g[4][NG];
-  __device__ __forceinline__ void load(const unsigned char* base, int rows, int lane) {
+template <int N>
+__device__ __forceinline__ void shared_words(uint32_t (&w)[N], const unsigned char* p) {
+  if constexpr (N == 1) {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (N == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    w[0] = v.x; w[1] = v.y;
+  } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = (lane >> 2) + 8 * i, t = lane & 3;
-      const unsigned char* slot = base + r * packed_slot_bytes(D);
-      if (r < rows) {
-        load_words(w[i], slot + t * (D / 8));
-        load_words(g[i], slot + D + (D == 64 ? (t >> 1) * 4 : t * NG * 4));
-      } else {
-#pragma unroll
-        for (int j = 0; j < W; ++j) w[i][j] = 0u;
-#pragma unroll
-        for (int j = 0; j < NG; ++j) g[i][j] = 0u;
-      }
+    for (int i = 0; i < N; i += 4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p + 4 * i);
+      w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
     }
   }
-};
-template <int D>
-struct VTile {
-  static constexpr int W = D / 64;
-  uint32_t w[8][W], g[8][1];
-  __device__ __forceinline__ void load(const unsigned char* base, int rows, int lane) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = (i >> 2) * 16 + (lane & 3) * 4 + (i & 3), f = lane >> 2;
-      const unsigned char* slot = base + r * packed_slot_bytes(D);
-      if (r < rows) {
-        load_words(w[i], slot + D / 2 + f * (D / 16));
-        load_words(g[i], slot + D + D / 8 + (f * (D / 8) / PACK_GROUP) * 4);
-      } else {   // a slot behind the last entry: zeros, whatever it holds
-#pragma unroll
-        for (int j = 0; j < W; ++j) w[i][j] = 0u;
-        g[i][0] = 0u;
-      }
-    }
-  }
-};
+}
+
+// Ring buffers per warp, and the CTAs of which an SM holds that many: the register limit that goes with it.
+constexpr int NSTAGE = 2;
+template <int D, int G>
+constexpr int resident_ctas() { return D == 256 ? 2 : (G == 8 ? 3 : (G == 1 ? 5 : 4)); }
 
 template <int D, int G>
-__global__ void __launch_bounds__(NW * 32) packed_stream_kernel(const __grid_constant__ PackedParams P) {
+__global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_kernel(const __grid_constant__ PackedParams P) {
   constexpr int PSTRIDE = 4 + D;
   constexpr int NT = NW * 32;
+  constexpr int SB = packed_slot_bytes(D);
+  constexpr int TILE_BYTES = TILE * SB;
+  extern __shared__ __align__(128) unsigned char dyn_smem[];
   __shared__ float sh_m[NW][G], sh_l[NW][G], sh_my[NW][G], sh_ly[NW][G];
-  __shared__ float sh_o[NW][G][D];
   __shared__ float sh_x[NW][G][TILE];                       // logits of the warp's tile, one column per slot
   __shared__ __align__(8) __half sh_p[NW][G][TILE];         // output weights, binary16 operands of the second product
+  __shared__ uint64_t bars_all[NW][NSTAGE];
 
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -187,17 +152,32 @@ __global__ void __launch_bounds__(NW * 32) packed_stream_kernel(const __grid_con
   if (len < 0 || len > P.k) return;   // a damaged entry count: nothing of this unit is touched
   const int row_begin = s * P.tiles_per_split * TILE;
   const int row_end = min(len, row_begin + P.tiles_per_split * TILE);
-  const unsigned char* cache_u = P.cache + (size_t)u * P.k * packed_slot_bytes(D);
+  const unsigned char* cache_u = P.cache + (size_t)u * P.k * SB;
   const int32_t* pos_u = P.pos + (size_t)u * P.k;
   const int Hkv = P.H / G;
   const uint32_t b = (uint32_t)(u / Hkv), h0 = (uint32_t)(u % Hkv) * G, lh0 = (uint32_t)P.layer * P.H + h0;
 
-  int tile = row_begin + warp * TILE;
-  KTile<D> kt;
-  VTile<D> vt;
-  kt.load(cache_u + (size_t)tile * packed_slot_bytes(D), row_end - tile, lane);
-  vt.load(cache_u + (size_t)tile * packed_slot_bytes(D), row_end - tile, lane);
-  int pos_next = tile + lane < row_end ? pos_u[tile + lane] : 0;
+  // ---- the warp's ring
+  const int first_tile = row_begin + warp * TILE;
+  const int n_tiles = row_end > first_tile ? (row_end - first_tile + NW * TILE - 1) / (NW * TILE) : 0;
+  unsigned char* ring = dyn_smem + (size_t)warp * NSTAGE * TILE_BYTES;
+  uint64_t* bars = bars_all[warp];
+  auto issue = [&](int it) {
+    if (lane == 0) {
+      const int tb = first_tile + it * NW * TILE;
+      const uint32_t bytes = (uint32_t)min(TILE, row_end - tb) * SB;
+      uint64_t* bar = bars + it % NSTAGE;
+      mbar_expect_tx(bar, bytes);
+      bulk_load(ring + (size_t)(it % NSTAGE) * TILE_BYTES, cache_u + (size_t)tb * SB, bytes, bar);
+    }
+  };
+  if (lane == 0) {
+    for (int i = 0; i < NSTAGE; ++i) mbar_init(bars + i, 1);
+    mbar_fence_init();
+  }
+  __syncwarp();
+  for (int it = 0; it < NSTAGE && it < n_tiles; ++it) issue(it);
+  int pos_next = first_tile + lane < row_end ? pos_u[first_tile + lane] : 0;
 
   // queries as the second operand of S: column = head r8, the features this lane's K words bring, pairs (i, i + 4)
   uint32_t qf[D / 32][4];
@@ -220,34 +200,54 @@ __global__ void __launch_bounds__(NW * 32) packed_stream_kernel(const __grid_con
 #pragma unroll
     for (int c = 0; c < 4; ++c) o[i][c] = 0.f;
 
-  for (; tile < row_end; tile += NW * TILE) {
-    const int rows = row_end - tile;        // may exceed TILE
-    const int after = tile + NW * TILE;
-    const unsigned char* next = cache_u + (size_t)after * packed_slot_bytes(D);
-    const int pj = pos_next;
-    pos_next = after + lane < row_end ? pos_u[after + lane] : 0;
+  // Where the lane finds its share of a tile.  K: rows k_row + 8 i, features [t4 D/4, + D/4).  V: slots 16 h + t4 + 4 i,
+  // features [r8 D/8, + D/8).  Both orders keep the lanes of a shared-memory phase on distinct banks (the slots of two
+  // neighbouring lane groups lie 2 apart for K, 1 apart for V; a slot is 8 banks, mod 32, at d = 128).
+  const int k_row = (r8 & 4) | (r8 & 1) << 1 | (r8 >> 1 & 1);
+  const int k_codes = k_row * SB + t4 * (D / 8);
+  const int k_group = k_row * SB + D + (D == 64 ? (t4 >> 1) * 4 : t4 * (D / 32));
+  const int v_codes = t4 * SB + D / 2 + r8 * (D / 16);
+  const int v_group = t4 * SB + D + D / 8 + (r8 * (D / 8) / PACK_GROUP) * 4;
+  const int p_at = (lane & 16) + (lane & 3) * 4 + (lane >> 2 & 3);   // where the weight of slot `lane` is read as an operand
+  float* y_out = P.y_scratch + (size_t)u * G * (P.k + 1) + first_tile + lane;
 
-    // ---- logits
+  bool failed = false;
+  int it = 0;
+  for (; it < n_tiles; ++it, y_out += NW * TILE) {
+    const int rows = row_end - (first_tile + it * NW * TILE);        // may exceed TILE
+    const int pj = pos_next;
+    pos_next = rows - NW * TILE > lane ? pos_u[first_tile + (it + 1) * NW * TILE + lane] : 0;
+    const bool ok = mbar_wait_bounded(bars + it % NSTAGE, (uint32_t)(it / NSTAGE & 1));
+    if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+    const unsigned char* buf = ring + (size_t)(it % NSTAGE) * TILE_BYTES;
+
+    // ---- logits (rows behind the last entry give numbers that nobody reads)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float c[4] = {0.f, 0.f, 0.f, 0.f};
+      constexpr int NG = D == 256 ? 2 : 1;      // groups a lane's features span
+      uint32_t kw[2][D / 32], kg[2][NG];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        shared_words(kw[i], buf + k_codes + (16 * h + 8 * i) * SB);
+        shared_words(kg[i], buf + k_group + (16 * h + 8 * i) * SB);
+      }
 #pragma unroll
       for (int w = 0; w < D / 32; ++w) {
         __half2 a[2][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const __half2 g = bits_h2(kt.g[2 * h + i][D == 256 ? w / 4 : 0]);
-          nibble_pairs(kt.w[2 * h + i][w], a[i]);
+          const __half2 g = bits_h2(kg[i][NG == 2 ? w / 4 : 0]);
+          nibble_pairs(kw[i][w], a[i]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) a[i][e] = __hfma2(a[i][e], __low2half2(g), __high2half2(g));
         }
         mma_16816(c, h2_bits(a[0][0]), h2_bits(a[1][0]), h2_bits(a[0][1]), h2_bits(a[1][1]), qf[w][0], qf[w][1]);
         mma_16816(c, h2_bits(a[0][2]), h2_bits(a[1][2]), h2_bits(a[0][3]), h2_bits(a[1][3]), qf[w][2], qf[w][3]);
       }
-      if (2 * t4 < G) { sh_x[warp][2 * t4][16 * h + r8] = c[0]; sh_x[warp][2 * t4][16 * h + 8 + r8] = c[2]; }
-      if (2 * t4 + 1 < G) { sh_x[warp][2 * t4 + 1][16 * h + r8] = c[1]; sh_x[warp][2 * t4 + 1][16 * h + 8 + r8] = c[3]; }
+      if (2 * t4 < G) { sh_x[warp][2 * t4][16 * h + k_row] = c[0]; sh_x[warp][2 * t4][16 * h + 8 + k_row] = c[2]; }
+      if (2 * t4 + 1 < G) { sh_x[warp][2 * t4 + 1][16 * h + k_row] = c[1]; sh_x[warp][2 * t4 + 1][16 * h + 8 + k_row] = c[3]; }
     }
-    kt.load(next, row_end - after, lane);
     __syncwarp();
 
     // ---- per logit (a lane is a slot): bias, noise, the two running softmaxes.  The output weights are taken against a
@@ -260,10 +260,10 @@ __global__ void __launch_bounds__(NW * 32) packed_stream_kernel(const __grid_con
     for (int g = 0; g < G; ++g) {
       float x = -INFINITY, y = -INFINITY;
       if (valid) {
-        const float slope = P.slopes ? P.slopes[h0 + g] : 0.f;
-        x = fmaf(sh_x[warp][g][lane], P.scale, -slope * (float)(P.p - pj));
+        x = sh_x[warp][g][lane] * P.scale;
+        if (P.slopes) x = fmaf(-__ldg(P.slopes + h0 + g), (float)(P.p - pj), x);
         y = (x + packed_noise(P, b, lh0 + g, (uint32_t)P.p, (uint32_t)pj)) * P.inv_tau;
-        P.y_scratch[((size_t)u * G + g) * (P.k + 1) + tile + lane] = y;
+        y_out[(size_t)g * (P.k + 1)] = y;
       }
       const float tx = redux_max(x), my_new = fmaxf(m_y[g], redux_max(y));
       scale_o[g] = 1.f;
@@ -273,12 +273,12 @@ __global__ void __launch_bounds__(NW * 32) packed_stream_kernel(const __grid_con
         l_x[g] *= scale_o[g];
         moved = true;
       }
-      const float px = valid ? fast_exp2((x - m_x[g]) * LOG2E) : 0.f;
+      const __half px = __float2half_rn(valid ? fast_exp2((x - m_x[g]) * LOG2E) : 0.f);
       const float ey = valid ? fast_exp2((y - my_new) * LOG2E) : 0.f;
-      l_x[g] += px;
+      l_x[g] += __half2float(px);   // the weights that are used are the ones that are summed
       l_y[g] = fmaf(l_y[g], fast_exp2((m_y[g] - my_new) * LOG2E), ey);
       m_y[g] = my_new;
-      sh_p[warp][g][lane] = __float2half_rn(px);
+      sh_p[warp][g][p_at] = px;
     }
     if (moved) {
       float f0 = 1.f, f1 = 1.f;   // of this lane's two columns
@@ -292,20 +292,31 @@ __global__ void __launch_bounds__(NW * 32) packed_stream_kernel(const __grid_con
     }
     __syncwarp();
 
-    // ---- values
+    // ---- values; a slot behind the last entry counts as zeros, whatever the buffer holds
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      uint2 pb = make_uint2(0, 0);   // weights of slots 4 t4 .. 4 t4 + 3 for head r8
+      constexpr int W = D / 64;
+      uint2 pb = make_uint2(0, 0);   // weights of slots 16 h + t4 + 4 {0 .. 3} for head r8
       if (r8 < G) pb = *reinterpret_cast<const uint2*>(&sh_p[warp][r8][16 * h + 4 * t4]);
+      uint32_t vw[4][W], vg[4][1];
 #pragma unroll
-      for (int w = 0; w < VTile<D>::W; ++w) {
-        __half2 lo[2][4], hi[2][4];   // features 8 w + (0 .. 3) and + (4 .. 7); a pair is two neighbouring slots
+      for (int i = 0; i < 4; ++i) {
+        shared_words(vw[i], buf + v_codes + (16 * h + 4 * i) * SB);
+        shared_words(vg[i], buf + v_group + (16 * h + 4 * i) * SB);
+      }
+      if (rows < TILE) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * h + 4 * i + t4 >= rows) vg[i][0] = 0u;      // scale and minimum 0
+      }
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        __half2 lo[2][4], hi[2][4];   // features 8 w + (0 .. 3) and + (4 .. 7); a pair is two of the lane's slots
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int i = 4 * h + 2 * e;
-          const __half2 sc = bits_h2(__byte_perm(vt.g[i][0], vt.g[i + 1][0], 0x5410)), mn = bits_h2(__byte_perm(vt.g[i][0], vt.g[i + 1][0], 0x7632));
-          nibble_pairs(__byte_perm(vt.w[i][w], vt.w[i + 1][w], 0x5410), lo[e]);
-          nibble_pairs(__byte_perm(vt.w[i][w], vt.w[i + 1][w], 0x7632), hi[e]);
+          const __half2 sc = bits_h2(__byte_perm(vg[2 * e][0], vg[2 * e + 1][0], 0x5410)), mn = bits_h2(__byte_perm(vg[2 * e][0], vg[2 * e + 1][0], 0x7632));
+          nibble_pairs(__byte_perm(vw[2 * e][w], vw[2 * e + 1][w], 0x5410), lo[e]);
+          nibble_pairs(__byte_perm(vw[2 * e][w], vw[2 * e + 1][w], 0x7632), hi[e]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) { lo[e][j] = __hfma2(lo[e][j], sc, mn); hi[e][j] = __hfma2(hi[e][j], sc, mn); }
         }
@@ -314,16 +325,24 @@ __global__ void __launch_bounds__(NW * 32) packed_stream_kernel(const __grid_con
           mma_16816(o[4 * w + j], h2_bits(lo[0][j]), h2_bits(hi[0][j]), h2_bits(lo[1][j]), h2_bits(hi[1][j]), pb.x, pb.y);
       }
     }
-    vt.load(next, row_end - after, lane);
-    __syncwarp();   // the next tile overwrites the warp's logits and weights
+    __syncwarp();   // the buffer, the logits and the weights have been read by every lane
+    if (it + NSTAGE < n_tiles) issue(it + NSTAGE);
+  }
+  if (failed) {
+    // a copy did not land in time: flag it, then give every copy still in flight a second bounded wait
+    if (lane == 0) atomicExch(P.err, ERR_TIMEOUT);
+    const int issued = min(n_tiles, it + NSTAGE);
+    for (; it < issued; ++it) (void)mbar_wait_bounded(bars + it % NSTAGE, (uint32_t)(it / NSTAGE & 1));
   }
 
-  // ---- merge the lanes, then the warps of this CTA
+  // ---- merge the lanes, then the warps of this CTA; the sums lie in the rings, which are done with
+  static_assert(G * D * 4 <= NSTAGE * TILE_BYTES, "a warp's sums fit its ring");
+  float* sums = reinterpret_cast<float*>(ring);              // [G][D]
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     const int f = r8 * (D / 8) + (i >> 2) * 8 + (i & 3);
-    if (2 * t4 < G) { sh_o[warp][2 * t4][f] = o[i][0]; sh_o[warp][2 * t4][f + 4] = o[i][2]; }
-    if (2 * t4 + 1 < G) { sh_o[warp][2 * t4 + 1][f] = o[i][1]; sh_o[warp][2 * t4 + 1][f + 4] = o[i][3]; }
+    if (2 * t4 < G) { sums[2 * t4 * D + f] = o[i][0]; sums[2 * t4 * D + f + 4] = o[i][2]; }
+    if (2 * t4 + 1 < G) { sums[(2 * t4 + 1) * D + f] = o[i][1]; sums[(2 * t4 + 1) * D + f + 4] = o[i][3]; }
   }
 #pragma unroll
   for (int g = 0; g < G; ++g) {
@@ -344,7 +363,8 @@ __global__ void __launch_bounds__(NW * 32) packed_stream_kernel(const __grid_con
     for (int c = tid; c < D; c += NT) {
       float acc_o = 0.f;
 #pragma unroll
-      for (int wi = 0; wi < NW; ++wi) acc_o = fmaf(sh_o[wi][g][c], sc[wi], acc_o);
+      for (int wi = 0; wi < NW; ++wi)
+        acc_o = fmaf(reinterpret_cast<const float*>(dyn_smem + (size_t)wi * NSTAGE * TILE_BYTES)[g * D + c], sc[wi], acc_o);
       part[4 + c] = acc_o;
     }
     if (tid == 0) {
@@ -387,11 +407,16 @@ cudaError_t launch_one(const PackedParams& P, int units, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)P.splits, (unsigned)units);
   cfg.blockDim = dim3(NW * 32);
+  cfg.dynamicSmemBytes = NW * NSTAGE * TILE * packed_slot_bytes(D);
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, packed_stream_kernel<D, G>, P);
+  cudaError_t e = cudaSuccess;
+  if (cfg.dynamicSmemBytes > 40 * 1024)   // with the static part above what every kernel may have
+    e = cudaFuncSetAttribute(packed_stream_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, packed_stream_kernel<D, G>, P);
   if (e != cudaSuccess) return e;
+  cfg.dynamicSmemBytes = 0;
   cfg.gridDim = dim3((unsigned)units);
   cfg.blockDim = dim3(close_threads(D, G));
   if constexpr (G == 1) {
