@@ -7,11 +7,11 @@
 // one CTA per request and launched as its programmatic dependent, joins the sums in binary64 (two continuations of
 // different beams may differ by less than binary32 tells) and takes the best of the lists.
 //
-// Finding the best few of thousands of registers: the largest values of the threads are sorted within their warp and the
-// eight largest of each warp ranked against one another; the take-th of those 64 is a value that at least `take`
-// elements reach, and few more than that do.  Those are collected in shared memory and ranked by comparison.  Rows with so
-// many equal values that the collection does not fit (all tokens forbidden, constant logits) are worked off one
-// element at a time.
+// Finding the best few of thousands of registers: with c = take / 8 rounded up, each of the eight warps finds the c-th
+// largest of its threads' maxima, and the smallest of those eight values is one that at least `take` elements reach and
+// few more than that do (about three times `take` of 8192 random ones).  Those are collected in shared memory and ranked by
+// comparison.  Rows with so many equal values that the collection does not fit (all tokens forbidden, constant
+// logits) are worked off one element at a time.
 //
 // Order everywhere: larger value first, of equal values the lower beam, then the lower token.
 //
@@ -26,9 +26,7 @@ namespace kf {
 namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
-constexpr int TOP = 8;                    // maxima each warp contributes; WARPS * TOP >= BEAM_TAKE_MAX
-constexpr int CAP = 512;                  // collected elements
-static_assert(WARPS * TOP >= BEAM_TAKE_MAX, "the threshold needs `take` maxima");
+constexpr int CAP = 1024;                 // collected elements
 
 // Larger value, then lower index: larger key.  Values are never NaN.
 __device__ __forceinline__ uint32_t ordered(float v) {
@@ -40,44 +38,9 @@ __device__ __forceinline__ float unordered(uint32_t k) {
 }
 __device__ __forceinline__ uint64_t key_of(float v, uint32_t index) { return (uint64_t)ordered(v) << 32 | (0xffffffffu - index); }
 
-__device__ __forceinline__ float usable(float v) { return v < INFINITY ? v : -INFINITY; }   // NaN and +inf count as -inf
-
-template <class T>
-__device__ __forceinline__ float one_logit(const T* p);
-template <> __device__ __forceinline__ float one_logit<__half>(const __half* p) { return __half2float(*p); }
-template <> __device__ __forceinline__ float one_logit<__nv_bfloat16>(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-template <> __device__ __forceinline__ float one_logit<float>(const float* p) { return *p; }
-
-template <class T>
-__device__ __forceinline__ void widen(const uint4& v, float* x) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 4) {
-      x[i] = __uint_as_float(w[i]);
-    } else {
-      float2 f;
-      if constexpr (__is_same(T, __half)) f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      else f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
-      x[2 * i] = f.x;
-      x[2 * i + 1] = f.y;
-    }
-  }
-}
-
-// Descending sort of one value per lane (bitonic network).
-__device__ __forceinline__ float sort_lanes(float v, int lane) {
-#pragma unroll
-  for (int size = 2; size <= 32; size <<= 1) {
-#pragma unroll
-    for (int o = size >> 1; o > 0; o >>= 1) {
-      const float other = __shfl_xor_sync(0xffffffffu, v, o);
-      const bool keep_max = ((lane & o) == 0) == ((lane & size) == 0 || size == 32);
-      v = keep_max ? fmaxf(v, other) : fminf(v, other);
-    }
-  }
-  return v;
-}
+__device__ __forceinline__ float widen(__half v) { return __half2float(v); }
+__device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float widen(float v) { return v; }
 
 template <class KEY>
 __device__ __forceinline__ KEY warp_best(KEY v) {
@@ -89,90 +52,189 @@ __device__ __forceinline__ KEY warp_best(KEY v) {
   return v;
 }
 
-// The take-th largest of the values that the warps left in `tops` (WARPS x TOP, each warp's in descending order): a
-// threshold that at least `take` of the CTA's elements reach.  Every thread of the CTA calls it.
-template <class V>
-__device__ __forceinline__ V threshold_of(const V (&tops)[WARPS * TOP], V* where, int take) {
-  const int tid = threadIdx.x;
-  __syncthreads();
-  if (tid < WARPS * TOP) {
-    const V mine = tops[tid];
-    int rank = 0;
-#pragma unroll
-    for (int i = 0; i < WARPS * TOP; ++i) rank += (tops[i] > mine || (tops[i] == mine && i < tid)) ? 1 : 0;
-    if (rank == take - 1) *where = mine;
+// The c-th largest of the lanes' values (equal ones count one by one).
+__device__ __forceinline__ float warp_nth(float v, int c, int lane) {
+  float m = -INFINITY;
+  for (int i = 0; i < c; ++i) {
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    const unsigned who = __ballot_sync(0xffffffffu, v == m);
+    if (lane == __ffs(who) - 1) v = -INFINITY;
   }
-  __syncthreads();
-  return *where;
+  return m;
 }
+
+// One 16-byte vector of logits, worked on in its own type (two values at a time where they have 16 bits).  What lies outside
+// the row and what is not finite is -inf.
+template <class T>
+struct Vec {
+  static constexpr int N = 16 / (int)sizeof(T), PER = 4 / (int)sizeof(T);   // values per vector, per 32-bit word
+  static constexpr uint32_t MINUS_INF = sizeof(T) == 4 ? 0xff800000u : (__is_same(T, __half) ? 0xfc00fc00u : 0xff80ff80u);
+  uint32_t w[4];
+
+  template <class F>
+  __device__ __forceinline__ static auto pair(uint32_t bits, F&& f) {
+    if constexpr (__is_same(T, __half)) return f(*reinterpret_cast<const __half2*>(&bits));
+    else return f(*reinterpret_cast<const __nv_bfloat162*>(&bits));
+  }
+  __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = MINUS_INF; }
+  __device__ __forceinline__ void load(const T* p) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  }
+  __device__ __forceinline__ void load_within(const T* row, int at, int vocab) {   // a vector that the row's ends cut
+    T v[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = at + e >= 0 && at + e < vocab ? row[at + e] : minus_inf();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = reinterpret_cast<const uint32_t*>(v)[i];
+  }
+  __device__ __forceinline__ void only_finite() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {     // NaN and +inf are not below +inf
+      if constexpr (sizeof(T) == 4) {
+        w[i] = __uint_as_float(w[i]) < INFINITY ? w[i] : MINUS_INF;
+      } else {
+        const uint32_t ok = less(w[i], MINUS_INF & 0x7fff7fffu);
+        w[i] = (w[i] & ok) | (MINUS_INF & ~ok);
+      }
+    }
+  }
+  __device__ __forceinline__ static T minus_inf() {
+    if constexpr (sizeof(T) == 4) return -INFINITY;
+    else if constexpr (__is_same(T, __half)) return __ushort_as_half((unsigned short)0xfc00u);
+    else return __ushort_as_bfloat16((unsigned short)0xff80u);
+  }
+  // 16-bit types: masks of the halves where a < b, a >= b
+  __device__ __forceinline__ static uint32_t less(uint32_t a, uint32_t b) {
+    return pair(a, [&](auto x) { return pair(b, [&](auto y) { return __hlt2_mask(x, y); }); });
+  }
+  __device__ __forceinline__ static uint32_t reaches(uint32_t a, uint32_t b) {
+    return pair(a, [&](auto x) { return pair(b, [&](auto y) { return __hge2_mask(x, y); }); });
+  }
+  __device__ __forceinline__ static float value(uint32_t bits, int e) {   // value e of a word
+    if constexpr (sizeof(T) == 4) return __uint_as_float(bits);
+    else if constexpr (__is_same(T, __half)) return __half2float(__ushort_as_half((unsigned short)(bits >> 16 * e)));
+    else return __uint_as_float(e ? bits & 0xffff0000u : bits << 16);
+  }
+  __device__ __forceinline__ static uint32_t larger(uint32_t a, uint32_t b) {
+    if constexpr (sizeof(T) == 4) {
+      return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    } else {
+      return pair(a, [&](auto x) { return pair(b, [&](auto y) { const auto m = __hmax2(x, y); return *reinterpret_cast<const uint32_t*>(&m); }); });
+    }
+  }
+  // the word with `v`, which the type holds exactly, in every place
+  __device__ __forceinline__ static uint32_t splat(float v) {
+    if constexpr (sizeof(T) == 4) return __float_as_uint(v);
+    else if constexpr (__is_same(T, __half)) return (uint32_t)__half_as_ushort(__float2half_rn(v)) * 0x10001u;
+    else return (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v)) * 0x10001u;
+  }
+};
 
 // VPT 16-byte vectors per thread.
 template <class T, int VPT>
-__global__ void __launch_bounds__(THREADS) beam_chunk_kernel(const __grid_constant__ BeamParams P) {
-  constexpr int EPV = 16 / (int)sizeof(T), E = EPV * VPT;
-  __shared__ float tops[WARPS * TOP];
-  __shared__ float sh_thr, sh_sum[WARPS];
+__global__ void __launch_bounds__(THREADS, 4) beam_chunk_kernel(const __grid_constant__ BeamParams P) {
+  using V = Vec<T>;
+  constexpr int EPV = V::N, PER = V::PER;
+  __shared__ float sh_nth[WARPS], sh_top[WARPS], sh_sum[WARPS];
   __shared__ uint64_t list[CAP];
   __shared__ int count;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int row = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (P.finished && P.finished[row]) return;              // goes on with the padding token; nothing is read
   const T* logits = static_cast<const T*>(P.logits) + (int64_t)row * P.row_stride;
-  // vectors start on 16-byte boundaries; the first one may begin before the row, the last one end behind it
+  // vectors start on 16-byte boundaries; the row's first one may begin before it, its last one end behind it
   const int lead = (int)((reinterpret_cast<uintptr_t>(logits) & 15u) / sizeof(T));
-  const int first = chunk * (THREADS * E) - lead;         // element at which the chunk's first vector starts
+  const int vectors = (P.vocab + lead + EPV - 1) / EPV, per_chunk = (vectors + P.chunks - 1) / P.chunks;   // at most THREADS * VPT
+  const int first = chunk * per_chunk, last = min(vectors, first + per_chunk);
+  auto place = [&](int v) { return (first + v * THREADS + tid) * EPV - lead; };   // element at which the vector starts
 
-  float x[E];
-  float top = -INFINITY;
+  V vec[VPT];
 #pragma unroll
-  for (int v = 0; v < VPT; ++v) {
-    const int at = first + (v * THREADS + tid) * EPV;
-    if (at >= 0 && at + EPV <= P.vocab) {
-      widen<T>(__ldg(reinterpret_cast<const uint4*>(logits + at)), x + v * EPV);
-    } else {
+  for (int v = 0; v < VPT; ++v) vec[v].clear();
+  if (first * EPV - lead >= 0 && last * EPV - lead <= P.vocab) {   // the same for the whole CTA: nothing is cut
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) x[v * EPV + e] = at + e >= 0 && at + e < P.vocab ? one_logit<T>(logits + at + e) : -INFINITY;
+    for (int v = 0; v < VPT; ++v)
+      if (first + v * THREADS + tid < last) vec[v].load(logits + place(v));
+  } else {
+#pragma unroll 1
+    for (int v = 0; v < VPT; ++v) {
+      const int at = place(v);
+      V one;
+      one.clear();
+      if (first + v * THREADS + tid < last) {
+        if (at >= 0 && at + EPV <= P.vocab) one.load(logits + at);
+        else one.load_within(logits, at, P.vocab);
+      }
+#pragma unroll
+      for (int k = 0; k < VPT; ++k)
+        if (k == v) vec[k] = one;
     }
   }
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    x[e] = usable(x[e]);
-    top = fmaxf(top, x[e]);
-  }
-  const float sorted = sort_lanes(top, lane);
-  if (lane < TOP) tops[warp * TOP + lane] = sorted;
+  for (int v = 0; v < VPT; ++v) vec[v].only_finite();
   if (tid == 0) count = 0;
-  const float thr = threshold_of(tops, &sh_thr, P.take);
-  float best = tops[0];
+  uint32_t top_word = V::MINUS_INF;
 #pragma unroll
-  for (int i = 1; i < WARPS; ++i) best = fmaxf(best, tops[i * TOP]);
+  for (int v = 0; v < VPT; ++v)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top_word = V::larger(top_word, vec[v].w[i]);
+  const float top = fmaxf(V::value(top_word, 0), V::value(top_word, PER - 1));
+  const float nth = warp_nth(top, (P.take + WARPS - 1) / WARPS, lane), most = warp_nth(top, 1, lane);
+  if (lane == 0) { sh_nth[warp] = nth; sh_top[warp] = most; }
+  __syncthreads();
+  float thr = sh_nth[0], best = sh_top[0];
+#pragma unroll
+  for (int i = 1; i < WARPS; ++i) { thr = fminf(thr, sh_nth[i]); best = fmaxf(best, sh_top[i]); }
 
+  // collect what reaches the threshold; the order of arrival does not matter, keys are ranked below.  The few words that hold
+  // such a value are noted and read again.
+  uint32_t hits = 0;
+  if (top >= thr) {
+    const uint32_t thr_word = V::splat(thr);
+#pragma unroll
+    for (int k = 0; k < 4 * VPT; ++k) {
+      const uint32_t word = vec[k / 4].w[k % 4];
+      bool hit;
+      if constexpr (PER == 1) hit = __uint_as_float(word) >= thr;
+      else hit = V::reaches(word, thr_word) != 0u;
+      hits |= hit ? 1u << k : 0u;
+    }
+  }
+  while (hits) {
+    const int k = __ffs(hits) - 1, at = place(k >> 2) + (k & 3) * PER;
+    hits &= hits - 1;
+    if (first + (k >> 2) * THREADS + tid < last) {
+#pragma unroll
+      for (int e = 0; e < PER; ++e)
+        if (at + e >= 0 && at + e < P.vocab) {
+          float x = widen(logits[at + e]);
+          x = x < INFINITY ? x : -INFINITY;
+          if (x >= thr) {
+            const int slot = atomicAdd(&count, 1);
+            if (slot < CAP) list[slot] = key_of(x, (uint32_t)(at + e));
+          }
+        }
+    }
+  }
   // sum of exponentials against the chunk's maximum
   float sum = 0.f;
   if (best > -INFINITY) {
     const float off = best * LOG2E;
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum += fast_exp2(fmaf(x[e], LOG2E, -off));
+    for (int v = 0; v < VPT; ++v)
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) sum += fast_exp2(fmaf(V::value(vec[v].w[e / PER], e % PER), LOG2E, -off));
   }
   sum = warp_sum(sum);
   if (lane == 0) sh_sum[warp] = sum;
-
-  // collect what reaches the threshold
-  auto index_of = [&](int e) { return first + ((e / EPV) * THREADS + tid) * EPV + e % EPV; };
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int idx = index_of(e);
-    if (x[e] >= thr && idx >= 0 && idx < P.vocab) {
-      const int slot = atomicAdd(&count, 1);              // the order of arrival does not matter: keys are ranked below
-      if (slot < CAP) list[slot] = key_of(x[e], (uint32_t)idx);
-    }
-  }
   __syncthreads();
+
   const int64_t entry = (int64_t)row * P.chunks + chunk;
   uint2* out = P.lists + entry * P.take;
   auto put = [&](int rank, uint64_t key) { out[rank] = make_uint2(__float_as_uint(unordered((uint32_t)(key >> 32))), 0xffffffffu - (uint32_t)key); };
   const int n = count;
-  if (tid == 0) {
+  if (tid == THREADS - 1) {
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < WARPS; ++i) s += sh_sum[i];
@@ -182,6 +244,7 @@ __global__ void __launch_bounds__(THREADS) beam_chunk_kernel(const __grid_consta
     for (int i = tid; i < n; i += THREADS) {
       const uint64_t mine = list[i];
       int rank = 0;
+#pragma unroll 4
       for (int j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
       if (rank < P.take) put(rank, mine);
     }
@@ -190,24 +253,26 @@ __global__ void __launch_bounds__(THREADS) beam_chunk_kernel(const __grid_consta
   }
   // many equal values: one element per round, the best key below the last one
   __shared__ uint64_t sh_key[WARPS];
-  uint64_t last = ~0ull;
+  uint64_t prev = ~0ull;
   for (int r = 0; r < P.take; ++r) {
     uint64_t mine = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int idx = index_of(e);
-      if (idx >= 0 && idx < P.vocab) {
-        const uint64_t key = key_of(x[e], (uint32_t)idx);
-        if (key < last && key > mine) mine = key;
+    for (int v = 0; v < VPT; ++v)
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) {
+        const int idx = place(v) + e;
+        if (first + v * THREADS + tid < last && idx >= 0 && idx < P.vocab) {
+          const uint64_t key = key_of(V::value(vec[v].w[e / PER], e % PER), (uint32_t)idx);
+          if (key < prev && key > mine) mine = key;
+        }
       }
-    }
     mine = warp_best(mine);
     if (lane == 0) sh_key[warp] = mine;
     __syncthreads();
-    last = sh_key[0];
+    prev = sh_key[0];
 #pragma unroll
-    for (int i = 1; i < WARPS; ++i) last = sh_key[i] > last ? sh_key[i] : last;
-    if (tid == 0) put(r, last);          // n > CAP >= take: there is one in every round
+    for (int i = 1; i < WARPS; ++i) prev = sh_key[i] > prev ? sh_key[i] : prev;
+    if (tid == 0) put(r, prev);          // n > CAP >= take: there is one in every round
     __syncthreads();
   }
 }
@@ -215,108 +280,152 @@ __global__ void __launch_bounds__(THREADS) beam_chunk_kernel(const __grid_consta
 // A continuation as it is ranked: value, then the place beam * vocab + token.
 struct Candidate {
   double value;
-  int64_t place;
+  int place;        // below 2^31: at most 32 beams of 2^26 tokens
 };
 __device__ __forceinline__ bool better(const Candidate& a, const Candidate& b) {
   return a.value > b.value || (a.value == b.value && a.place < b.place);
 }
 
+// The entries of the lists are dealt to the threads; those a thread can hold in registers (all of them, in ordinary searches) are
+// requested before anything else and read once.
 __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_constant__ BeamParams P) {
-  constexpr int MCAP = 1024;
+  constexpr int MCAP = 1024, HELD = 8;
   __shared__ double base[BEAM_MAX];          // score - log of the sum of exponentials; -inf: no continuation counts
-  __shared__ double tops[WARPS * TOP];
-  __shared__ double sh_thr;
+  __shared__ int kind[BEAM_MAX];             // 0: lists of the chunks, 1: at its end, 2: nothing left
+  constexpr int GROUPS = THREADS / 4;
+  static_assert(GROUPS >= BEAM_TAKE_MAX, "the threshold needs `take` maxima");
+  __shared__ __align__(16) float sh_max[GROUPS];
+  __shared__ unsigned int least;
   __shared__ Candidate cand[MCAP];
   __shared__ int count;
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int n_lists = P.beams * P.chunks, entries = n_lists * P.take;
+  const uint2* lists = P.lists + (int64_t)b * entries;
+  // entry e: number i = e / n_lists of list l = e % n_lists, so that the best entries of all lists lie in different threads
+  auto locate = [&](int e, int& l, int& i) {
+    i = n_lists == 1 ? e : (e < HELD * THREADS ? (int)__umulhi((uint32_t)e, P.by_lists) : e / n_lists);   // exact: e n_lists < 2^32
+    l = e - i * n_lists;
+  };
   if (tid == 0) count = 0;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  uint2 held[HELD];
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    held[i] = make_uint2(0u, 0xffffffffu);
+    if (tid + i * THREADS < entries) {
+      int l, k;
+      locate(tid + i * THREADS, l, k);
+      held[i] = __ldcg(lists + l * P.take + k);
+    }
+  }
 
   // ---- the beams' normalisers: one warp per beam
   for (int w = warp; w < P.beams; w += WARPS) {
     const int64_t row = (int64_t)b * P.beams + w;
-    double s = (double)P.scores[row], lse = 0.0;
-    bool live = isfinite(s);
-    if (!(P.finished && P.finished[row])) {
-      float m = -INFINITY;
-      for (int c = lane; c < P.chunks; c += 32) m = fmaxf(m, __ldcg(&P.stats[row * P.chunks + c]).x);
-      m = warp_max(m);
-      double sum = 0.0;
-      if (m > -INFINITY)
-        for (int c = lane; c < P.chunks; c += 32) {
-          const float2 st = __ldcg(&P.stats[row * P.chunks + c]);
-          if (st.x > -INFINITY) sum += (double)st.y * exp((double)st.x - (double)m);
+    const float score = P.scores[row];
+    const bool done = P.finished && P.finished[row];
+    float m = -INFINITY, sum = 0.f;
+    if (!done) {
+      for (int c = lane; c < P.chunks; c += 32) {
+        const float2 st = __ldcg(&P.stats[row * P.chunks + c]);
+        if (st.x > m) {
+          sum = fmaf(sum, fast_exp2((m - st.x) * LOG2E), st.y);
+          m = st.x;
+        } else if (st.x > -INFINITY) {
+          sum = fmaf(st.y, fast_exp2((st.x - m) * LOG2E), sum);
         }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      live = live && m > -INFINITY;
-      lse = live ? (double)m + log(sum) : 0.0;
+      }
+      const float all = warp_max(m);
+      sum = warp_sum(m > -INFINITY ? sum * fast_exp2((m - all) * LOG2E) : 0.f);
+      m = all;
     }
-    if (lane == 0) base[w] = live ? s - lse : -INFINITY;
+    if (lane == 0) {
+      const bool live = isfinite(score) && (done || m > -INFINITY);
+      kind[w] = live ? (done ? 1 : 0) : 2;
+      base[w] = live ? (done ? (double)score : (double)score - ((double)m + (double)logf(sum))) : -INFINITY;
+    }
   }
   __syncthreads();
 
-  // ---- entry i of list l.  A beam without a live continuation offers its first tokens, all at -inf; a finished one the
-  //      padding token at its score, then the other tokens at -inf.  Lists end where entry() says so.
-  const int lists = P.beams * P.chunks;
-  auto entry = [&](int l, int i, Candidate& c) -> bool {
-    const int w = l / P.chunks, ch = l % P.chunks;
-    const int64_t row = (int64_t)b * P.beams + w;
-    const bool dead = base[w] == -INFINITY, done = P.finished && P.finished[row];
-    int token;
-    double value;
-    if (dead || done) {
-      if (ch > 0 || i >= P.vocab) return false;
-      token = dead ? i : (i == 0 ? P.pad : (i - 1 < P.pad ? i - 1 : i));
-      value = dead || i > 0 ? -INFINITY : base[w];
-    } else {
-      const uint2 e = __ldcg(&P.lists[(row * P.chunks + ch) * P.take + i]);
-      if (e.y == 0xffffffffu) return false;
-      token = (int)e.y;
-      value = base[w] + (double)__uint_as_float(e.x);
+  // ---- entries as continuations.  A beam without a live continuation offers its first tokens, all at -inf, in place of its first
+  //      list; one at its end the padding token at its score, then the other tokens at -inf.  A place of -1: the list has ended.
+  auto candidate = [&](int e, const uint2& raw) {
+    int l, i;
+    locate(e, l, i);
+    const int w = P.chunks == 1 ? l : (int)__umulhi((uint32_t)l, P.by_chunks);      // l / chunks, exact: l chunks < 2^32
+    Candidate c;
+    int token = (int)raw.y;
+    c.value = base[w] + (double)__uint_as_float(raw.x);
+    if (kind[w] != 0) {
+      const bool done = kind[w] == 1;
+      token = l != w * P.chunks || i >= P.vocab ? -1 : (!done ? i : (i == 0 ? P.pad : (i - 1 < P.pad ? i - 1 : i)));
+      c.value = done && i == 0 ? base[w] : -INFINITY;
     }
-    c.value = value;
-    c.place = (int64_t)w * P.vocab + token;
-    return true;
+    c.place = token < 0 ? -1 : w * P.vocab + token;
+    return c;
+  };
+  Candidate mine[HELD];
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    mine[i].value = -INFINITY;
+    mine[i].place = -1;
+    if (tid + i * THREADS < entries) mine[i] = candidate(tid + i * THREADS, held[i]);
+  }
+  auto each = [&](auto&& use) {     // use(continuation) for every one of this thread
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (mine[i].place >= 0) use(mine[i]);
+    for (int e = tid + HELD * THREADS; e < entries; e += THREADS) {
+      int l, i;
+      locate(e, l, i);
+      const Candidate c = candidate(e, __ldcg(lists + l * P.take + i));
+      if (c.place >= 0) use(c);
+    }
   };
 
-  // ---- a value that at least `take` continuations reach, found as in the chunks: every thread takes its share of the
-  //      entries, neighbouring entries of a list in different threads
-  const int entries = lists * P.take;
-  double left = -INFINITY;
-  for (int i = tid; i < entries; i += THREADS) {
-    Candidate c;
-    if (entry(i / P.take, i % P.take, c) && c.value > left) left = c.value;
+  // ---- a value that at least `take` continuations reach: the take-th of the maxima of groups of four threads, in binary32; what
+  //      rounding may have taken off it is granted.  With fewer entries than threads all of them are ranked.
+  double thr = -INFINITY;
+  if (entries > THREADS) {
+    float top = -INFINITY;
+    each([&](const Candidate& c) { top = fmaxf(top, (float)c.value); });
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    if ((tid & 3) == 0) sh_max[tid / 4] = top;
+    if (tid == 0) least = ~0u;
+    __syncthreads();
+    int above = 0;
+#pragma unroll
+    for (int i = 0; i < GROUPS; i += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(sh_max + i);
+      above += (v.x > top) + (v.y > top) + (v.z > top) + (v.w > top);
+    }
+    if ((tid & 3) == 0 && above < P.take) atomicMin(&least, ordered(top));   // the smallest value with fewer than `take` above it
+    __syncthreads();
+    const double t = (double)unordered(least);
+    thr = t - 1e-6 * fabs(t);      // -inf stays -inf
   }
-  for (int i = 0; i < TOP; ++i) {
-    const double m = warp_best(left);
-    if (lane == 0) tops[warp * TOP + i] = m;
-    const unsigned who = __ballot_sync(0xffffffffu, left == m);
-    if (lane == __ffs(who) - 1) left = -INFINITY;
-  }
-  const double thr = threshold_of(tops, &sh_thr, P.take);
-
-  for (int i = tid; i < entries; i += THREADS) {
-    Candidate c;
-    if (entry(i / P.take, i % P.take, c) && c.value >= thr) {
+  each([&](const Candidate& c) {
+    if (!(c.value < thr)) {          // a threshold of -inf lets everything through
       const int slot = atomicAdd(&count, 1);
       if (slot < MCAP) cand[slot] = c;
     }
-  }
+  });
   __syncthreads();
   const int n = count;
   auto put = [&](int rank, const Candidate& c) {
     const int64_t at = (int64_t)b * P.take + rank;
     P.out_scores[at] = (float)c.value;
-    P.out_parent[at] = (int)(c.place / P.vocab);
-    P.out_token[at] = (int)(c.place % P.vocab);
+    P.out_parent[at] = c.place / P.vocab;
+    P.out_token[at] = c.place % P.vocab;
   };
   if (n <= MCAP) {
     for (int i = tid; i < n; i += THREADS) {
-      const Candidate mine = cand[i];
+      const Candidate one = cand[i];
       int rank = 0;
-      for (int j = 0; j < n; ++j) rank += better(cand[j], mine) ? 1 : 0;
-      if (rank < P.take) put(rank, mine);
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) rank += better(cand[j], one) ? 1 : 0;
+      if (rank < P.take) put(rank, one);
     }
     return;
   }
@@ -326,21 +435,20 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
   last.value = INFINITY;
   last.place = -1;
   for (int r = 0; r < P.take; ++r) {
-    Candidate mine;
-    mine.value = -INFINITY;
-    mine.place = (int64_t)1 << 62;
-    for (int i = tid; i < entries; i += THREADS) {
-      Candidate c;
-      if (entry(i / P.take, i % P.take, c) && better(last, c) && better(c, mine)) mine = c;
-    }
+    Candidate next;
+    next.value = -INFINITY;
+    next.place = INT32_MAX;
+    each([&](const Candidate& c) {
+      if (better(last, c) && better(c, next)) next = c;
+    });
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       Candidate other;
-      other.value = __shfl_xor_sync(0xffffffffu, mine.value, o);
-      other.place = __shfl_xor_sync(0xffffffffu, mine.place, o);
-      if (better(other, mine)) mine = other;
+      other.value = __shfl_xor_sync(0xffffffffu, next.value, o);
+      other.place = __shfl_xor_sync(0xffffffffu, next.place, o);
+      if (better(other, next)) next = other;
     }
-    if (lane == 0) sh_best[warp] = mine;
+    if (lane == 0) sh_best[warp] = next;
     __syncthreads();
     last = sh_best[0];
 #pragma unroll
@@ -352,7 +460,10 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
 }
 
 template <class T>
-cudaError_t launch_type(const BeamParams& P, bool wide, cudaStream_t stream) {
+cudaError_t launch_type(BeamParams P, bool wide, cudaStream_t stream) {
+  // floor(2^32 / n) + 1: the high word of its product with e is e / n while e n < 2^32 (n = 1 does without)
+  P.by_lists = (uint32_t)(((uint64_t)1 << 32) / (uint64_t)(P.beams * P.chunks)) + 1;
+  P.by_chunks = (uint32_t)(((uint64_t)1 << 32) / (uint64_t)P.chunks) + 1;
   constexpr int NARROW = (int)sizeof(T) / 2, WIDE = 4 * NARROW;   // 8 or 32 values per thread
   const dim3 grid((unsigned)P.chunks, (unsigned)(P.batch * P.beams));
   if (wide) beam_chunk_kernel<T, WIDE><<<grid, THREADS, 0, stream>>>(P);

@@ -100,7 +100,7 @@ struct CloseRow<PackedParams, D, NT, CPT> {
 };
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
@@ -129,7 +129,7 @@ __device__ __forceinline__ void shared_words(uint32_t (&w)[N], const unsigned ch
 // Ring buffers per warp, and the CTAs of which an SM holds that many: the register limit that goes with it.
 constexpr int NSTAGE = 2;
 template <int D, int G>
-constexpr int resident_ctas() { return D == 256 ? 2 : (G == 8 ? 3 : (G == 1 ? 5 : 4)); }
+constexpr int resident_ctas() { return D == 256 ? 2 : (G == 8 ? 3 : 4); }
 
 template <int D, int G>
 __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_kernel(const __grid_constant__ PackedParams P) {
@@ -142,6 +142,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
   __shared__ float sh_x[NW][G][TILE];                       // logits of the warp's tile, one column per slot
   __shared__ __align__(8) __half sh_p[NW][G][TILE];         // output weights, binary16 operands of the second product
   __shared__ uint64_t bars_all[NW][NSTAGE];
+  __shared__ float sh_slope[G];
 
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -175,7 +176,8 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     for (int i = 0; i < NSTAGE; ++i) mbar_init(bars + i, 1);
     mbar_fence_init();
   }
-  __syncwarp();
+  if (tid < G) sh_slope[tid] = P.slopes ? P.slopes[h0 + tid] : 0.f;
+  __syncthreads();
   for (int it = 0; it < NSTAGE && it < n_tiles; ++it) issue(it);
   int pos_next = first_tile + lane < row_end ? pos_u[first_tile + lane] : 0;
 
@@ -217,6 +219,10 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     const int rows = row_end - (first_tile + it * NW * TILE);        // may exceed TILE
     const int pj = pos_next;
     pos_next = rows - NW * TILE > lane ? pos_u[first_tile + (it + 1) * NW * TILE + lane] : 0;
+    // the noise needs positions only: its long dependent chains fill the gaps of the conversions below
+    float zeta[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) zeta[g] = packed_noise(P, b, lh0 + g, (uint32_t)P.p, (uint32_t)pj);
     const bool ok = mbar_wait_bounded(bars + it % NSTAGE, (uint32_t)(it / NSTAGE & 1));
     if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
     const unsigned char* buf = ring + (size_t)(it % NSTAGE) * TILE_BYTES;
@@ -258,13 +264,12 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     bool moved = false;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      float x = -INFINITY, y = -INFINITY;
-      if (valid) {
-        x = sh_x[warp][g][lane] * P.scale;
-        if (P.slopes) x = fmaf(-__ldg(P.slopes + h0 + g), (float)(P.p - pj), x);
-        y = (x + packed_noise(P, b, lh0 + g, (uint32_t)P.p, (uint32_t)pj)) * P.inv_tau;
-        y_out[(size_t)g * (P.k + 1)] = y;
-      }
+      // every lane computes, so that the warp stays together; what has no entry becomes -inf at the end
+      float x = fmaf(-sh_slope[g], (float)(P.p - pj), sh_x[warp][g][lane] * P.scale);
+      float y = (x + zeta[g]) * P.inv_tau;
+      if (valid) y_out[(size_t)g * (P.k + 1)] = y;
+      x = valid ? x : -INFINITY;
+      y = valid ? y : -INFINITY;
       const float tx = redux_max(x), my_new = fmaxf(m_y[g], redux_max(y));
       scale_o[g] = 1.f;
       if (!(tx <= m_x[g] + 5.5f)) {   // 2^8 = e^5.55; also the first tile (and a NaN, which stays one)
@@ -443,7 +448,7 @@ cudaError_t launch_dim(const PackedParams& P, int units, cudaStream_t stream) {
 
 void decode_packed_plan(int units, int budget_k, int head_dim, int* splits_out, int* tiles_per_split_out) {
   const int tiles = (budget_k + TILE - 1) / TILE;
-  const int target_ctas = units >= 148 ? 148 * 16 : 148 * 4;
+  const int target_ctas = units >= 148 ? 148 * 13 : 148 * 8;
   int splits = (target_ctas + units - 1) / units;
   splits = std::max(1, std::min(splits, std::min(MAX_SPLITS, (tiles + NW - 1) / NW)));
   int tps = (tiles + splits - 1) / splits;

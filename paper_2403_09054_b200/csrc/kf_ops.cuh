@@ -37,6 +37,7 @@ struct BeamParams {
   float2* stats;                // scratch: [row][chunk] (maximum, sum of exponentials)
   int64_t row_stride;
   int32_t batch, beams, vocab, take, pad, chunks;
+  uint32_t by_lists, by_chunks; // reciprocals for the merge, filled in by launch_beam_select
 };
 // Chunks a row of logits is cut into; `wide` is the form with 32 values per thread.
 void beam_plan(int64_t rows, int vocab, int* chunks, bool* wide);

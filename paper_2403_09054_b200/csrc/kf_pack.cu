@@ -18,29 +18,51 @@ __device__ __forceinline__ void extremes8(const uint4& v, __half2& low, __half2&
   high = __hmax2_nan(__hmax2_nan(a, b), __hmax2_nan(c, d));
 }
 
+// Eight codes.  Adding 1.5 * 2^23 rounds to whole numbers (to even, as rintf does) and leaves the code in the low bits.
 __device__ __forceinline__ uint32_t pack8(const uint4& v, float low, float inverse) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   uint32_t code = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 3; i >= 0; --i) {
     const float2 f = __half22float2(bits_h2(w[i]));
-    code |= packed_code(f.x, low, inverse) << (8 * i);
-    code |= packed_code(f.y, low, inverse) << (8 * i + 4);
+    const float a = __fadd_rn(fminf(__fmul_rn(__fsub_rn(f.x, low), inverse), 15.f), 12582912.f);
+    const float c = __fadd_rn(fminf(__fmul_rn(__fsub_rn(f.y, low), inverse), 15.f), 12582912.f);
+    code = code << 4 | (__float_as_uint(c) & 15u);
+    code = code << 4 | (__float_as_uint(a) & 15u);
   }
-  return code;
+  return low == low ? code : 0u;   // not finite: every code 0
 }
 
-// (scale, minimum) of the group this lane's chunk belongs to; the four lanes of a group call it together.
-__device__ __forceinline__ __half2 group_of(const uint4& v) {
-  __half2 low, high;
-  extremes8(v, low, high);
+struct Group {
+  __half2 params;   // (scale, minimum)
+  float inverse;
+};
+
+// The groups that this lane's two chunks belong to; the four lanes of a group call it together.  The even lanes work out the
+// K group, the odd ones the V group, and neighbours exchange: one division and one reciprocal per lane.
+__device__ __forceinline__ void groups_of(const uint4& kv, const uint4& vv, Group& kg, Group& vg) {
+  __half2 klo, khi, vlo, vhi;
+  extremes8(kv, klo, khi);
+  extremes8(vv, vlo, vhi);
+  klo = __hmin2_nan(klo, __lowhigh2highlow(klo));
+  khi = __hmax2_nan(khi, __lowhigh2highlow(khi));
+  vlo = __hmin2_nan(vlo, __lowhigh2highlow(vlo));
+  vhi = __hmax2_nan(vhi, __lowhigh2highlow(vhi));
+  __half2 lo = __lows2half2(klo, vlo), hi = __lows2half2(khi, vhi);   // (K, V)
 #pragma unroll
   for (int o = 1; o <= 2; o <<= 1) {
-    low = __hmin2_nan(low, __shfl_xor_sync(0xffffffffu, low, o));
-    high = __hmax2_nan(high, __shfl_xor_sync(0xffffffffu, high, o));
+    lo = __hmin2_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = __hmax2_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
   }
-  const __half lo = __hmin_nan(__low2half(low), __high2half(low)), hi = __hmax_nan(__low2half(high), __high2half(high));
-  return packed_group(__half2float(lo), __half2float(hi));
+  const bool odd = threadIdx.x & 1;
+  Group mine;
+  mine.params = packed_group(__half2float(odd ? __high2half(lo) : __low2half(lo)), __half2float(odd ? __high2half(hi) : __low2half(hi)));
+  mine.inverse = packed_inverse(__low2half(mine.params));
+  Group other;
+  other.params = __shfl_xor_sync(0xffffffffu, mine.params, 1);
+  other.inverse = __shfl_xor_sync(0xffffffffu, mine.inverse, 1);
+  kg = odd ? other : mine;
+  vg = odd ? mine : other;
 }
 
 template <int D>
@@ -60,14 +82,15 @@ __global__ void __launch_bounds__(THREADS) pack_kernel(const __half* __restrict_
     kv = __ldcs(reinterpret_cast<const uint4*>(K + row * D) + c);
     vv = __ldcs(reinterpret_cast<const uint4*>(V + row * D) + c);
   }
-  const __half2 kg = group_of(kv), vg = group_of(vv);   // whole warps: a group never straddles a row
+  Group kg, vg;
+  groups_of(kv, vv, kg, vg);   // whole warps: a group never straddles a row
   if (!in) return;
   unsigned char* slot = cache + ((size_t)u * k + j) * packed_slot_bytes(D);
-  *reinterpret_cast<uint32_t*>(slot + 4 * c) = pack8(kv, __high2float(kg), packed_inverse(__low2half(kg)));
-  *reinterpret_cast<uint32_t*>(slot + D / 2 + 4 * c) = pack8(vv, __high2float(vg), packed_inverse(__low2half(vg)));
+  *reinterpret_cast<uint32_t*>(slot + 4 * c) = pack8(kv, __high2float(kg.params), kg.inverse);
+  *reinterpret_cast<uint32_t*>(slot + D / 2 + 4 * c) = pack8(vv, __high2float(vg.params), vg.inverse);
   if ((c & 3) == 0) {
-    *reinterpret_cast<uint32_t*>(slot + D + c) = h2_bits(kg);
-    *reinterpret_cast<uint32_t*>(slot + D + D / 8 + c) = h2_bits(vg);
+    *reinterpret_cast<uint32_t*>(slot + D + c) = h2_bits(kg.params);
+    *reinterpret_cast<uint32_t*>(slot + D + D / 8 + c) = h2_bits(vg.params);
   }
 }
 

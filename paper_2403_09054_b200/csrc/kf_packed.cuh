@@ -56,16 +56,22 @@ __device__ __forceinline__ uint32_t packed_code(float x, float low, float invers
 __device__ __forceinline__ uint32_t h2_bits(__half2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
 __device__ __forceinline__ __half2 bits_h2(uint32_t v) { return *reinterpret_cast<const __half2*>(&v); }
 
+// (w & mask) | bits in one instruction: both constants in registers, which the compiler does not do by itself.
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+  return r;
+}
 // Eight nibbles -> four pairs (nibble i, nibble i + 4) of binary16 integers 0..15, exact.  1024 + c has the bits
 // 0x6400 | c, and 1024 + 16 c the bits 0x6400 | 16 c: one logic instruction per pair, and one arithmetic instruction
 // that takes the offset off again.
 __device__ __forceinline__ void nibble_pairs(uint32_t w, __half2 (&c)[4]) {
   const uint32_t w8 = w >> 8;
   const __half2 sixteenth = __floats2half2_rn(0.0625f, 0.0625f);
-  c[0] = __hadd2(bits_h2((w & 0x000f000fu) | 0x64006400u), bits_h2(0xe400e400u));                  // - 1024
-  c[1] = __hfma2(bits_h2((w & 0x00f000f0u) | 0x64006400u), sixteenth, bits_h2(0xd400d400u));       // / 16 - 64
-  c[2] = __hadd2(bits_h2((w8 & 0x000f000fu) | 0x64006400u), bits_h2(0xe400e400u));
-  c[3] = __hfma2(bits_h2((w8 & 0x00f000f0u) | 0x64006400u), sixteenth, bits_h2(0xd400d400u));
+  c[0] = __hadd2(bits_h2(and_or(w, 0x000f000fu, 0x64006400u)), bits_h2(0xe400e400u));                  // - 1024
+  c[1] = __hfma2(bits_h2(and_or(w, 0x00f000f0u, 0x64006400u)), sixteenth, bits_h2(0xd400d400u));       // / 16 - 64
+  c[2] = __hadd2(bits_h2(and_or(w8, 0x000f000fu, 0x64006400u)), bits_h2(0xe400e400u));
+  c[3] = __hfma2(bits_h2(and_or(w8, 0x00f000f0u, 0x64006400u)), sixteenth, bits_h2(0xd400d400u));
 }
 
 #endif  // __CUDACC__
