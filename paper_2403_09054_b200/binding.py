@@ -1,7 +1,7 @@
 """Thin ctypes binding of the C ABI declared in ``include/keyformer.h``.
 
-Argument marshalling only: every step of the path runs in the CUDA kernels of
-``libkeyformer_b200.so``.  PyTorch supplies device memory and streams.  There is
+Argument marshalling only (for the operators that need no context in the compiled ``_kf_torch``): every step of the path runs
+in the CUDA kernels of ``libkeyformer_b200.so``.  PyTorch supplies device memory and streams.  There is
 no fallback: if the library cannot be loaded, importing this module fails.
 """
 from __future__ import annotations
@@ -159,6 +159,9 @@ def _load() -> C.CDLL:
 
 LIB = _load()
 LIB_PATH = _build.LIB
+if not os.path.exists(_build.TORCH_LIB):
+    _build.build_torch()
+from . import _kf_torch  # noqa: E402  (links against the library loaded above)
 
 
 class KeyformerError(RuntimeError):
@@ -244,90 +247,25 @@ def kf_decode_step_static(*, batch, n_heads, head_dim, budget_k, recent_w, layer
 
 
 # ---- operators that need no context.  Tensors of a call live on one CUDA device, which need not be the current one; work goes
-# to `stream`, or to that device's current stream.
-_TYPES = {torch.float16: KF_TYPE_FP16, torch.bfloat16: KF_TYPE_BF16, torch.float32: KF_TYPE_FP32}
-
-
-def _on(t, name, dtype, numel, device):
-    """Pointer of a contiguous CUDA tensor of this type and size on the call's device; None stays None."""
-    if t is None:
-        return None
-    if t.dtype != dtype or t.numel() != numel or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor with {numel} elements on {device}, "
-                         f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-    return t.data_ptr()
-
-
-def _device_of(t, name):
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise ValueError(f"{name}: expected a CUDA tensor")
-    return t.device
-
-
-def _call(device, stream, where, fn, *args):
-    """fn(*args, stream pointer) with `device` current."""
-    if torch.cuda.current_device() != device.index:
-        with torch.cuda.device(device):
-            return _call(device, stream, where, fn, *args)
-    code = fn(*args, _stream_ptr(stream))
-    if code != KF_OK:
-        raise KeyformerError(code, where)
-
-
-def _scratch(given, nbytes, device, stream, where):
-    """(pointer, bytes, tensor) of a call's scratch: the caller's, or one from torch's allocator."""
-    if nbytes == 0:
-        raise KeyformerError(KF_EINVAL, where)
-    if given is None:
-        if stream is None:
-            given = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        else:
-            with torch.cuda.stream(stream):
-                given = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return _on(given, "scratch", torch.uint8, given.numel(), device), given.numel(), given
-
-
+# to `stream`, or to that device's current stream.  The calls' tensors are checked in the compiled _kf_torch (ValueError).
 def kf_packed_slot_bytes(head_dim) -> int:
     return int(LIB.kf_packed_slot_bytes(head_dim))
-
-
-def _packed_shape(K, V, cache):
-    d, n, k = K.shape[-1], K.shape[-2], cache.shape[-2]
-    units = K.numel() // max(1, n * d)
-    if V.shape != K.shape or tuple(K.shape[:-2]) != tuple(cache.shape[:-2]) or cache.shape[-1] != kf_packed_slot_bytes(d):
-        raise ValueError(f"K {tuple(K.shape)}, V {tuple(V.shape)} and cache {tuple(cache.shape)}: expected [..., n, d] twice and [..., k, 5d/4] "
-                         "with d 64, 128 or 256")
-    return units, n, k, d
 
 
 def kf_pack_cache(*, K, V, cache, length=None, stream=None):
     """Rows K, V (fp16 [..., n, d]) to slots 0 .. n-1 of the 4-bit cache (uint8 [..., k, 5d/4]); with `length` (int32 [...])
     only the rows below it."""
-    dev = _device_of(K, "K")
-    units, n, k, d = _packed_shape(K, V, cache)
-    _call(dev, stream, "kf_pack_cache", LIB.kf_pack_cache, units, n, k, d, _on(K, "K", torch.float16, units * n * d, dev),
-          _on(V, "V", torch.float16, units * n * d, dev), _on(length, "length", torch.int32, units, dev),
-          _on(cache, "cache", torch.uint8, units * k * (5 * d // 4), dev))
+    _check(_kf_torch.pack_cache(K, V, cache, length, stream), "kf_pack_cache")
 
 
 def kf_unpack_cache(*, cache, K, V, length=None, stream=None):
     """Slots 0 .. n-1 of a 4-bit cache back to rows K, V (fp16 [..., n, d]): the values that the codes stand for."""
-    dev = _device_of(cache, "cache")
-    units, n, k, d = _packed_shape(K, V, cache)
-    _call(dev, stream, "kf_unpack_cache", LIB.kf_unpack_cache, units, n, k, d, _on(cache, "cache", torch.uint8, units * k * (5 * d // 4), dev),
-          _on(length, "length", torch.int32, units, dev), _on(K, "K", torch.float16, units * n * d, dev),
-          _on(V, "V", torch.float16, units * n * d, dev))
-
-
-def _packed_args(batch, n_heads, n_kv_heads, head_dim, budget_k, recent_w, layer, position, tau, noise_seed, noise_mode, noise_const,
-                 noise_mu, noise_sigma, bias_mode, slopes, logit_scale):
-    return kf_packed_step(batch, n_heads, n_kv_heads, head_dim, budget_k, recent_w, layer, position, noise_mode, bias_mode, tau,
-                          noise_seed & 0xFFFFFFFFFFFFFFFF, logit_scale, noise_const, noise_mu, noise_sigma, slopes)
+    _check(_kf_torch.unpack_cache(K, V, cache, length, stream), "kf_unpack_cache")
 
 
 def kf_packed_scratch_bytes(*, batch, n_heads, head_dim, budget_k, n_kv_heads=0) -> int:
     """Bytes of scratch a kf_decode_step_packed of this shape needs; 0 if the shape is not supported."""
-    a = _packed_args(batch, n_heads, n_kv_heads, head_dim, budget_k, 0, 0, 0, 1.0, 0, KF_NOISE_NONE, 0.0, 0.0, 0.0, KF_BIAS_NONE, None, 0.0)
+    a = kf_packed_step(batch=batch, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, budget_k=budget_k, noise_mode=KF_NOISE_NONE, tau=1.0)
     return int(LIB.kf_packed_scratch_bytes(C.byref(a)))
 
 
@@ -337,74 +275,29 @@ def kf_decode_step_packed(*, batch, n_heads, head_dim, budget_k, recent_w, layer
                           bias_mode=KF_BIAS_NONE, alibi_slopes_dev=None, logit_scale=0.0, scratch=None, stream=None):
     """One generation step over a cache in 4 bits (kf_pack_cache), all state in the caller's tensors.  `scratch`: a uint8 CUDA tensor of
     kf_packed_scratch_bytes(...) bytes; without one torch's allocator provides it for the call."""
-    dev = _device_of(cache, "cache")
-    U, d, k = batch * (n_kv_heads or n_heads), head_dim, budget_k
-    a = _packed_args(batch, n_heads, n_kv_heads, d, k, recent_w, layer, position, tau, noise_seed, noise_mode, noise_const, noise_mu, noise_sigma,
-                     bias_mode, _on(alibi_slopes_dev, "alibi_slopes_dev", torch.float32, n_heads, dev), logit_scale)
-    ref = C.byref(a)
-    ptr, nbytes, scratch = _scratch(scratch, LIB.kf_packed_scratch_bytes(ref), dev, stream, "kf_decode_step_packed")
-    f16, i32 = torch.float16, torch.int32
-    _call(dev, stream, "kf_decode_step_packed", LIB.kf_decode_step_packed, ref,
-          _on(cache, "cache", torch.uint8, U * k * (5 * d // 4), dev), _on(pos, "pos", i32, U * k, dev), _on(acc, "acc", torch.float32, U * k, dev),
-          _on(length, "length", i32, U, dev), _on(q, "q", f16, batch * n_heads * d, dev), _on(knew, "knew", f16, U * d, dev),
-          _on(vnew, "vnew", f16, U * d, dev), _on(out, "out", f16, batch * n_heads * d, dev), _on(score_out, "score_out", torch.float32, U * (k + 1), dev),
-          _on(slot_out, "slot_out", i32, U, dev), _on(row_out, "row_out", f16, U * 2 * d, dev), ptr, nbytes)
+    _check(_kf_torch.decode_step_packed(batch, n_heads, n_kv_heads, head_dim, budget_k, recent_w, layer, position, noise_mode, bias_mode, tau, noise_seed,
+                                        logit_scale, noise_const, noise_mu, noise_sigma, alibi_slopes_dev, cache, pos, acc, length, q, knew, vnew, out,
+                                        score_out, slot_out, row_out, scratch, stream), "kf_decode_step_packed")
 
 
 def kf_qk_norm_rotate(*, qkv, n_heads, n_kv_heads, head_dim, q, k, v=None, positions=None, position0=0, norm_mode=KF_NORM_NONE,
                       q_weight=None, k_weight=None, eps=1e-6, rotary_dims=0, rotary_base=10000.0, rotary_style=KF_ROTARY_PAIRS, stream=None):
     """Projection rows (fp16 or bf16 [B, n, (H + 2 Hkv) d], any batch and token stride) to normed and rotated head-major q, k and to v
     (fp16 [B, H, n, d], [B, Hkv, n, d]; for n = 1 also without that dimension)."""
-    dev = _device_of(qkv, "qkv")
-    H, Hkv, d = n_heads, n_kv_heads, head_dim
-    if qkv.dim() != 3 or qkv.shape[2] != (H + 2 * Hkv) * d or qkv.stride(2) != 1 or qkv.dtype not in (torch.float16, torch.bfloat16):
-        raise ValueError(f"qkv: expected fp16 or bf16 [batch, tokens, {(H + 2 * Hkv) * d}] with contiguous rows, got {qkv.dtype} {tuple(qkv.shape)} "
-                         f"with strides {qkv.stride()}")
-    B, n, width = qkv.shape
-    # the stride of a dimension with one element is never used
-    a = kf_qk_norm_args(B, n, H, Hkv, d, _TYPES[qkv.dtype], qkv.stride(0) if B > 1 else 0, qkv.stride(1) if n > 1 else width, norm_mode, eps,
-                        rotary_dims, rotary_style, rotary_base, position0)
-    _call(dev, stream, "kf_qk_norm_rotate", LIB.kf_qk_norm_rotate, C.byref(a), qkv.data_ptr(), _on(q_weight, "q_weight", qkv.dtype, d, dev),
-          _on(k_weight, "k_weight", qkv.dtype, d, dev), _on(positions, "positions", torch.int32, B * n, dev), _on(q, "q", torch.float16, B * H * n * d, dev),
-          _on(k, "k", torch.float16, B * Hkv * n * d, dev), _on(v, "v", torch.float16, B * Hkv * n * d, dev))
+    _check(_kf_torch.qk_norm_rotate(qkv, n_heads, n_kv_heads, head_dim, q, k, v, positions, position0, norm_mode, q_weight, k_weight, eps, rotary_dims,
+                                    rotary_base, rotary_style, stream), "kf_qk_norm_rotate")
 
 
 def kf_beam_select(*, logits, scores, out_scores, out_parent, out_token, finished=None, pad_token=0, scratch=None, stream=None):
     """The best continuations over beams and vocabulary: logits (fp16, bf16 or fp32 [B, beams, V], rows evenly spaced), scores
     (fp32 [B, beams]); out_* [B, take], best first.  `finished`: uint8 or bool [B, beams], beams that go on with pad_token alone."""
-    dev = _device_of(logits, "logits")
-    if logits.dim() != 3 or logits.dtype not in _TYPES or out_scores.dim() != 2:
-        raise ValueError(f"logits: expected fp16, bf16 or fp32 [batch, beams, vocab], got {logits.dtype} {tuple(logits.shape)}; out_scores: [batch, take]")
-    B, W, V = logits.shape
-    stride = logits.stride(1) if W > 1 else (logits.stride(0) if B > 1 else V)
-    if (V > 1 and logits.stride(2) != 1) or (W > 1 and B > 1 and logits.stride(0) != W * stride):
-        raise ValueError(f"logits: rows have to be contiguous and evenly spaced, got strides {logits.stride()}")
-    take = out_scores.shape[1]
-    a = kf_beam_args(B, W, V, take, _TYPES[logits.dtype], pad_token, stride)
-    ref = C.byref(a)
-    ptr, nbytes, scratch = _scratch(scratch, LIB.kf_beam_scratch_bytes(ref), dev, stream, "kf_beam_select")
-    if finished is not None and finished.dtype == torch.bool:
-        finished = finished.view(torch.uint8)
-    _call(dev, stream, "kf_beam_select", LIB.kf_beam_select, ref, logits.data_ptr(), _on(scores, "scores", torch.float32, B * W, dev),
-          _on(finished, "finished", torch.uint8, B * W, dev), _on(out_scores, "out_scores", torch.float32, B * take, dev),
-          _on(out_parent, "out_parent", torch.int32, B * take, dev), _on(out_token, "out_token", torch.int32, B * take, dev), ptr, nbytes)
+    _check(_kf_torch.beam_select(logits, scores, out_scores, out_parent, out_token, finished, pad_token, scratch, stream), "kf_beam_select")
 
 
 def kf_reorder_rows(*, buffers, parent, n_layers=1, stream=None):
     """In every tensor of `buffers` (contiguous [batch * beams, ...], or [n_layers, batch * beams, ...]) row (b, i) becomes what row
     (b, parent[b, i]) was, in place; parent: int32 [batch, beams]."""
-    dev = _device_of(parent, "parent")
-    if parent.dim() != 2:
-        raise ValueError(f"parent: expected [batch, beams], got {tuple(parent.shape)}")
-    B, W = parent.shape
-    descs = (kf_row_buffer * len(buffers))()
-    for i, t in enumerate(buffers):
-        rows = n_layers * B * W
-        if t.numel() == 0 or t.numel() % rows != 0 or (t.shape[0] if n_layers == 1 else t.shape[0] * t.shape[1]) != rows:
-            raise ValueError(f"buffers[{i}]: expected {'' if n_layers == 1 else f'{n_layers} x '}{B * W} rows, got {tuple(t.shape)}")
-        nbytes = t.numel() // rows * t.element_size()
-        descs[i] = kf_row_buffer(_on(t, f"buffers[{i}]", t.dtype, t.numel(), dev), nbytes, nbytes * B * W, n_layers)
-    _call(dev, stream, "kf_reorder_rows", LIB.kf_reorder_rows, descs, len(buffers), B, W, _on(parent, "parent", torch.int32, B * W, dev))
+    _check(_kf_torch.reorder_rows(buffers, parent, n_layers, stream), "kf_reorder_rows")
 
 
 class Keyformer:

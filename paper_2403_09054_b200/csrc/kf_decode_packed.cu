@@ -18,6 +18,7 @@
 #include "kf_packed.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 namespace kf {
 
@@ -417,8 +418,15 @@ cudaError_t launch_one(const PackedParams& P, int units, cudaStream_t stream) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   cudaError_t e = cudaSuccess;
-  if (cfg.dynamicSmemBytes > 40 * 1024)   // with the static part above what every kernel may have
-    e = cudaFuncSetAttribute(packed_stream_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+  if (cfg.dynamicSmemBytes > 40 * 1024) {   // with the static part above what every kernel may have; asked for once per device
+    static std::atomic<uint64_t> asked{0};
+    int dev = 0;
+    e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (dev >= 64 || !(asked.load(std::memory_order_relaxed) >> dev & 1))) {
+      e = cudaFuncSetAttribute(packed_stream_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+      if (e == cudaSuccess && dev < 64) asked.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
+    }
+  }
   if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, packed_stream_kernel<D, G>, P);
   if (e != cudaSuccess) return e;
   cfg.dynamicSmemBytes = 0;
