@@ -11,9 +11,10 @@
 // cache (1, 2, 4 or 8) in the eight columns.  A contraction may take its terms in any order, so every lane contracts
 // the features (for S) or the slots (for O) that its own 16-byte loads brought, and the other operand is laid out to match.
 //
-// Every warp walks 32-slot tiles of its CTA's range by itself, through a private ring of two shared-memory buffers filled by
-// one bulk copy per tile (a tile is contiguous): no register holds a row that is still on its way, so that twenty warps
-// fit an SM and hide one another's conversion chains.
+// Every warp walks its CTA's range by itself, 64 slots at a time: two tiles of 32 slots, each in a private shared-memory
+// buffer that one bulk copy fills (a tile is contiguous), so that no register holds a row that is still on its way.  A
+// lane owns two slots in the per-logit work, whose chains (generator, logarithms, exponentials) then overlap, and the
+// bookkeeping of the running softmaxes is paid once for 64 slots.  A buffer is refilled as soon as its values have been used.
 #include "kf_close.cuh"
 #include "kf_packed.cuh"
 
@@ -24,7 +25,8 @@ namespace kf {
 
 namespace {
 
-constexpr int TILE = 32;   // slots per tile, one per lane in the per-logit work
+constexpr int TILE = 32;   // slots per buffer
+constexpr int SPAN = 64;   // slots per warp and round: two buffers, two slots per lane in the per-logit work
 constexpr int NW = 4;      // warps per CTA
 
 // ---- noise.  ln x for normal x > 0: x = 2^e (1 + f), f in [sqrt(1/2) - 1, sqrt(2) - 1], t = f / (2 + f),
@@ -38,9 +40,8 @@ __device__ __forceinline__ float ln_atanh(float x) {
   const float r = 2.0f * z * fmaf(z, fmaf(z, fmaf(z, 1.0f / 9.0f, 1.0f / 7.0f), 0.2f), 1.0f / 3.0f);
   return fmaf((float)e, LN2, f - t * (f - r));
 }
-__device__ __forceinline__ float packed_noise(const PackedParams& P, uint32_t b, uint32_t lh, uint32_t i, uint32_t j) {
-  if (P.noise_mode == 0) return -ln_atanh(-ln_atanh(uniform_from_word(noise_word(P.pk, b, lh, i, j))));
-  return noise_for(P, b, lh, i, j);
+__device__ __forceinline__ float packed_gumbel(const PackedParams& P, uint32_t b, uint32_t lh, uint32_t i, uint32_t j) {
+  return -ln_atanh(-ln_atanh(uniform_from_word(noise_word(P.pk, b, lh, i, j))));
 }
 
 // ---- the new token's row, quantised by the closing CTA.  Warps hold 32 consecutive features at a time: one group.
@@ -51,7 +52,7 @@ struct CloseRow<PackedParams, D, NT, CPT> {
   uint32_t code[CPT];           // K code | V code << 4
 
   static __device__ __forceinline__ float noise(const PackedParams& P, uint32_t b, uint32_t lh, uint32_t i, uint32_t j) {
-    return packed_noise(P, b, lh, i, j);
+    return P.noise_mode == 0 ? packed_gumbel(P, b, lh, i, j) : noise_for(P, b, lh, i, j);
   }
   static __device__ __forceinline__ __half2 group_of(__half x) {
     __half low = x, high = x;
@@ -127,22 +128,23 @@ __device__ __forceinline__ void shared_words(uint32_t (&w)[N], const unsigned ch
   }
 }
 
-// Ring buffers per warp, and the CTAs of which an SM holds that many: the register limit that goes with it.
-constexpr int NSTAGE = 2;
+// CTAs an SM holds: the register limit that goes with them.
 template <int D, int G>
-constexpr int resident_ctas() { return D == 256 ? 2 : (G == 8 ? 3 : 4); }
+constexpr int resident_ctas() { return D == 256 ? 2 : (G == 8 ? 3 : (G == 1 ? 4 : 4)); }
 
-template <int D, int G>
+// GUMBEL: the method's own adjustment, alone in its kernel (up to sixteen places draw noise, and the instructions of all the
+// alternatives together would not stay in the instruction cache).
+template <int D, int G, bool GUMBEL>
 __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_kernel(const __grid_constant__ PackedParams P) {
   constexpr int PSTRIDE = 4 + D;
   constexpr int NT = NW * 32;
   constexpr int SB = packed_slot_bytes(D);
   constexpr int TILE_BYTES = TILE * SB;
   extern __shared__ __align__(128) unsigned char dyn_smem[];
-  __shared__ float sh_m[NW][G], sh_l[NW][G], sh_my[NW][G], sh_ly[NW][G];
-  __shared__ float sh_x[NW][G][TILE];                       // logits of the warp's tile, one column per slot
-  __shared__ __align__(8) __half sh_p[NW][G][TILE];         // output weights, binary16 operands of the second product
-  __shared__ uint64_t bars_all[NW][NSTAGE];
+  __shared__ float sh_m[NW][G], sh_l[NW][G], sh_my[NW][G], sh_ly[NW][G], sh_f[NW][G];
+  __shared__ float sh_x[NW][G][SPAN];                       // logits of the warp's slots
+  __shared__ __align__(8) __half sh_p[NW][G][SPAN];         // output weights, binary16 operands of the second product
+  __shared__ uint64_t bars_all[NW][2];
   __shared__ float sh_slope[G];
 
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -159,28 +161,31 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
   const int Hkv = P.H / G;
   const uint32_t b = (uint32_t)(u / Hkv), h0 = (uint32_t)(u % Hkv) * G, lh0 = (uint32_t)P.layer * P.H + h0;
 
-  // ---- the warp's ring
-  const int first_tile = row_begin + warp * TILE;
-  const int n_tiles = row_end > first_tile ? (row_end - first_tile + NW * TILE - 1) / (NW * TILE) : 0;
-  unsigned char* ring = dyn_smem + (size_t)warp * NSTAGE * TILE_BYTES;
+  // ---- the warp's two buffers
+  const int first = row_begin + warp * SPAN;                 // first slot of the warp's first round
+  const int rounds = row_end > first ? (row_end - first + NW * SPAN - 1) / (NW * SPAN) : 0;
+  unsigned char* ring = dyn_smem + (size_t)warp * 2 * TILE_BYTES;
   uint64_t* bars = bars_all[warp];
-  auto issue = [&](int it) {
-    if (lane == 0) {
-      const int tb = first_tile + it * NW * TILE;
+  auto issue = [&](int it, int sub) {                        // fetches tile `sub` of round `it`, if it has a slot
+    const int tb = first + it * NW * SPAN + sub * TILE;
+    if (lane == 0 && tb < row_end) {
       const uint32_t bytes = (uint32_t)min(TILE, row_end - tb) * SB;
-      uint64_t* bar = bars + it % NSTAGE;
-      mbar_expect_tx(bar, bytes);
-      bulk_load(ring + (size_t)(it % NSTAGE) * TILE_BYTES, cache_u + (size_t)tb * SB, bytes, bar);
+      mbar_expect_tx(bars + sub, bytes);
+      bulk_load(ring + sub * TILE_BYTES, cache_u + (size_t)tb * SB, bytes, bars + sub);
     }
   };
   if (lane == 0) {
-    for (int i = 0; i < NSTAGE; ++i) mbar_init(bars + i, 1);
+    mbar_init(bars, 1);
+    mbar_init(bars + 1, 1);
     mbar_fence_init();
   }
   if (tid < G) sh_slope[tid] = P.slopes ? P.slopes[h0 + tid] : 0.f;
   __syncthreads();
-  for (int it = 0; it < NSTAGE && it < n_tiles; ++it) issue(it);
-  int pos_next = first_tile + lane < row_end ? pos_u[first_tile + lane] : 0;
+  issue(0, 0);
+  issue(0, 1);
+  int pos_next[2];
+#pragma unroll
+  for (int sub = 0; sub < 2; ++sub) pos_next[sub] = first + sub * TILE + lane < row_end ? pos_u[first + sub * TILE + lane] : 0;
 
   // queries as the second operand of S: column = head r8, the features this lane's K words bring, pairs (i, i + 4)
   uint32_t qf[D / 32][4];
@@ -194,9 +199,10 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     qf[w][3] = __byte_perm(v.y, v.w, 0x7632);
   }
 
-  float m_x[G], l_x[G], m_y[G], l_y[G];   // m_*: common to the warp; l_*: this lane's slots
+  float m_x[G], m_y[G], l_y[G];            // m_*: common to the warp; l_y: this lane's slots
 #pragma unroll
-  for (int g = 0; g < G; ++g) { m_x[g] = -INFINITY; l_x[g] = 0.f; m_y[g] = -INFINITY; l_y[g] = 0.f; }
+  for (int g = 0; g < G; ++g) { m_x[g] = -INFINITY; m_y[g] = -INFINITY; l_y[g] = 0.f; }
+  float l_x[4] = {0.f, 0.f, 0.f, 0.f};     // sums of the output weights, as the product of a row of ones: the columns of o
   float o[D / 16][4];                      // out^T: features as rows, heads 2 t4 and 2 t4 + 1 as columns
 #pragma unroll
   for (int i = 0; i < D / 16; ++i)
@@ -212,79 +218,98 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
   const int v_codes = t4 * SB + D / 2 + r8 * (D / 16);
   const int v_group = t4 * SB + D + D / 8 + (r8 * (D / 8) / PACK_GROUP) * 4;
   const int p_at = (lane & 16) + (lane & 3) * 4 + (lane >> 2 & 3);   // where the weight of slot `lane` is read as an operand
-  float* y_out = P.y_scratch + (size_t)u * G * (P.k + 1) + first_tile + lane;
+  float* y_out = P.y_scratch + (size_t)u * G * (P.k + 1) + first + lane;
 
   bool failed = false;
   int it = 0;
-  for (; it < n_tiles; ++it, y_out += NW * TILE) {
-    const int rows = row_end - (first_tile + it * NW * TILE);        // may exceed TILE
-    const int pj = pos_next;
-    pos_next = rows - NW * TILE > lane ? pos_u[first_tile + (it + 1) * NW * TILE + lane] : 0;
+  for (; it < rounds; ++it, y_out += NW * SPAN) {
+    const int rows = row_end - (first + it * NW * SPAN);             // may exceed SPAN
+    int pj[2];
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      pj[sub] = pos_next[sub];
+      pos_next[sub] = rows - NW * SPAN > sub * TILE + lane ? pos_u[first + (it + 1) * NW * SPAN + sub * TILE + lane] : 0;
+    }
     // the noise needs positions only: its long dependent chains fill the gaps of the conversions below
-    float zeta[G];
+    float zeta[2][G];
 #pragma unroll
-    for (int g = 0; g < G; ++g) zeta[g] = packed_noise(P, b, lh0 + g, (uint32_t)P.p, (uint32_t)pj);
-    const bool ok = mbar_wait_bounded(bars + it % NSTAGE, (uint32_t)(it / NSTAGE & 1));
-    if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-    const unsigned char* buf = ring + (size_t)(it % NSTAGE) * TILE_BYTES;
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int g = 0; g < G; ++g) zeta[sub][g] = GUMBEL ? packed_gumbel(P, b, lh0 + g, (uint32_t)P.p, (uint32_t)pj[sub])
+                              : noise_for(P, b, lh0 + g, (uint32_t)P.p, (uint32_t)pj[sub]);
 
-    // ---- logits (rows behind the last entry give numbers that nobody reads)
+    // ---- logits (slots behind the last entry give numbers that nobody reads)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float c[4] = {0.f, 0.f, 0.f, 0.f};
-      constexpr int NG = D == 256 ? 2 : 1;      // groups a lane's features span
-      uint32_t kw[2][D / 32], kg[2][NG];
+    for (int sub = 0; sub < 2; ++sub) {
+      if (sub * TILE >= rows) break;
+      const bool ok = mbar_wait_bounded(bars + sub, (uint32_t)(it & 1));
+      if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+      const unsigned char* buf = ring + sub * TILE_BYTES;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        shared_words(kw[i], buf + k_codes + (16 * h + 8 * i) * SB);
-        shared_words(kg[i], buf + k_group + (16 * h + 8 * i) * SB);
-      }
-#pragma unroll
-      for (int w = 0; w < D / 32; ++w) {
-        __half2 a[2][4];
+      for (int h = 0; h < 2; ++h) {
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
+        constexpr int NG = D == 256 ? 2 : 1;      // groups a lane's features span
+        uint32_t kw[2][D / 32], kg[2][NG];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const __half2 g = bits_h2(kg[i][NG == 2 ? w / 4 : 0]);
-          nibble_pairs(kw[i][w], a[i]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) a[i][e] = __hfma2(a[i][e], __low2half2(g), __high2half2(g));
+          shared_words(kw[i], buf + k_codes + (16 * h + 8 * i) * SB);
+          shared_words(kg[i], buf + k_group + (16 * h + 8 * i) * SB);
         }
-        mma_16816(c, h2_bits(a[0][0]), h2_bits(a[1][0]), h2_bits(a[0][1]), h2_bits(a[1][1]), qf[w][0], qf[w][1]);
-        mma_16816(c, h2_bits(a[0][2]), h2_bits(a[1][2]), h2_bits(a[0][3]), h2_bits(a[1][3]), qf[w][2], qf[w][3]);
+#pragma unroll
+        for (int w = 0; w < D / 32; ++w) {
+          __half2 a[2][4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const __half2 g = bits_h2(kg[i][NG == 2 ? w / 4 : 0]);
+            nibble_pairs(kw[i][w], a[i]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[i][e] = __hfma2(a[i][e], __low2half2(g), __high2half2(g));
+          }
+          mma_16816(c, h2_bits(a[0][0]), h2_bits(a[1][0]), h2_bits(a[0][1]), h2_bits(a[1][1]), qf[w][0], qf[w][1]);
+          mma_16816(c, h2_bits(a[0][2]), h2_bits(a[1][2]), h2_bits(a[0][3]), h2_bits(a[1][3]), qf[w][2], qf[w][3]);
+        }
+        const int at = sub * TILE + 16 * h + k_row;
+        if (2 * t4 < G) { sh_x[warp][2 * t4][at] = c[0]; sh_x[warp][2 * t4][at + 8] = c[2]; }
+        if (2 * t4 + 1 < G) { sh_x[warp][2 * t4 + 1][at] = c[1]; sh_x[warp][2 * t4 + 1][at + 8] = c[3]; }
       }
-      if (2 * t4 < G) { sh_x[warp][2 * t4][16 * h + k_row] = c[0]; sh_x[warp][2 * t4][16 * h + 8 + k_row] = c[2]; }
-      if (2 * t4 + 1 < G) { sh_x[warp][2 * t4 + 1][16 * h + k_row] = c[1]; sh_x[warp][2 * t4 + 1][16 * h + 8 + k_row] = c[3]; }
     }
+    if (failed) break;
     __syncwarp();
 
-    // ---- per logit (a lane is a slot): bias, noise, the two running softmaxes.  The output weights are taken against a
-    //      reference that moves only when a tile exceeds it by 2^8, so that the accumulators are hardly ever rescaled
-    //      (binary16 holds weights up to 2^8, the sums are binary32).
-    const bool valid = lane < rows;
+    // ---- per logit (a lane owns slots `lane` and `lane` + 32): bias, noise, the two running softmaxes.  The output weights are taken
+    //      against a reference that moves only when a round exceeds it by 2^8, so that the accumulators are hardly ever
+    //      rescaled (binary16 holds weights up to 2^8, the sums are binary32).
     float scale_o[G];
     bool moved = false;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       // every lane computes, so that the warp stays together; what has no entry becomes -inf at the end
-      float x = fmaf(-sh_slope[g], (float)(P.p - pj), sh_x[warp][g][lane] * P.scale);
-      float y = (x + zeta[g]) * P.inv_tau;
-      if (valid) y_out[(size_t)g * (P.k + 1)] = y;
-      x = valid ? x : -INFINITY;
-      y = valid ? y : -INFINITY;
-      const float tx = redux_max(x), my_new = fmaxf(m_y[g], redux_max(y));
+      float x[2], y[2];
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const bool valid = sub * TILE + lane < rows;
+        x[sub] = fmaf(-sh_slope[g], (float)(P.p - pj[sub]), sh_x[warp][g][sub * TILE + lane] * P.scale);
+        y[sub] = (x[sub] + zeta[sub][g]) * P.inv_tau;
+        if (valid) y_out[(size_t)g * (P.k + 1) + sub * TILE] = y[sub];
+        x[sub] = valid ? x[sub] : -INFINITY;
+        y[sub] = valid ? y[sub] : -INFINITY;
+      }
+      const float tx = redux_max(fmaxf(x[0], x[1])), my_new = fmaxf(m_y[g], redux_max(fmaxf(y[0], y[1])));
       scale_o[g] = 1.f;
-      if (!(tx <= m_x[g] + 5.5f)) {   // 2^8 = e^5.55; also the first tile (and a NaN, which stays one)
+      if (!(tx <= m_x[g] + 5.5f)) {   // 2^8 = e^5.55; also the first round (and a NaN, which stays one)
         scale_o[g] = fast_exp2((m_x[g] - tx) * LOG2E);
         m_x[g] = tx;
-        l_x[g] *= scale_o[g];
         moved = true;
       }
-      const __half px = __float2half_rn(valid ? fast_exp2((x - m_x[g]) * LOG2E) : 0.f);
-      const float ey = valid ? fast_exp2((y - my_new) * LOG2E) : 0.f;
-      l_x[g] += __half2float(px);   // the weights that are used are the ones that are summed
+      float ey = 0.f;
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const bool valid = sub * TILE + lane < rows;
+        ey += valid ? fast_exp2((y[sub] - my_new) * LOG2E) : 0.f;
+        sh_p[warp][g][sub * TILE + p_at] = __float2half_rn(valid ? fast_exp2((x[sub] - m_x[g]) * LOG2E) : 0.f);
+      }
       l_y[g] = fmaf(l_y[g], fast_exp2((m_y[g] - my_new) * LOG2E), ey);
       m_y[g] = my_new;
-      sh_p[warp][g][p_at] = px;
     }
     if (moved) {
       float f0 = 1.f, f1 = 1.f;   // of this lane's two columns
@@ -295,54 +320,63 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
       }
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) { o[i][0] *= f0; o[i][1] *= f1; o[i][2] *= f0; o[i][3] *= f1; }
+      l_x[0] *= f0;
+      l_x[1] *= f1;
     }
     __syncwarp();
 
     // ---- values; a slot behind the last entry counts as zeros, whatever the buffer holds
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      constexpr int W = D / 64;
-      uint2 pb = make_uint2(0, 0);   // weights of slots 16 h + t4 + 4 {0 .. 3} for head r8
-      if (r8 < G) pb = *reinterpret_cast<const uint2*>(&sh_p[warp][r8][16 * h + 4 * t4]);
-      uint32_t vw[4][W], vg[4][1];
+    for (int sub = 0; sub < 2; ++sub) {
+      if (sub * TILE >= rows) break;
+      const unsigned char* buf = ring + sub * TILE_BYTES;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        shared_words(vw[i], buf + v_codes + (16 * h + 4 * i) * SB);
-        shared_words(vg[i], buf + v_group + (16 * h + 4 * i) * SB);
-      }
-      if (rows < TILE) {
+      for (int h = 0; h < 2; ++h) {
+        constexpr int W = D / 64;
+        uint2 pb = make_uint2(0, 0);   // weights of slots 16 h + t4 + 4 {0 .. 3} for head r8
+        if (r8 < G) pb = *reinterpret_cast<const uint2*>(&sh_p[warp][r8][sub * TILE + 16 * h + 4 * t4]);
+        // the weights that are used, rounded as they are, are the ones that are summed
+        mma_16816(l_x, 0x3c003c00u, 0u, 0x3c003c00u, 0u, pb.x, pb.y);
+        uint32_t vw[4][W], vg[4][1];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (16 * h + 4 * i + t4 >= rows) vg[i][0] = 0u;      // scale and minimum 0
-      }
+        for (int i = 0; i < 4; ++i) {
+          shared_words(vw[i], buf + v_codes + (16 * h + 4 * i) * SB);
+          shared_words(vg[i], buf + v_group + (16 * h + 4 * i) * SB);
+        }
+        if (rows < SPAN) {
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
-        __half2 lo[2][4], hi[2][4];   // features 8 w + (0 .. 3) and + (4 .. 7); a pair is two of the lane's slots
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const __half2 sc = bits_h2(__byte_perm(vg[2 * e][0], vg[2 * e + 1][0], 0x5410)), mn = bits_h2(__byte_perm(vg[2 * e][0], vg[2 * e + 1][0], 0x7632));
-          nibble_pairs(__byte_perm(vw[2 * e][w], vw[2 * e + 1][w], 0x5410), lo[e]);
-          nibble_pairs(__byte_perm(vw[2 * e][w], vw[2 * e + 1][w], 0x7632), hi[e]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) { lo[e][j] = __hfma2(lo[e][j], sc, mn); hi[e][j] = __hfma2(hi[e][j], sc, mn); }
+          for (int i = 0; i < 4; ++i)
+            if (sub * TILE + 16 * h + 4 * i + t4 >= rows) vg[i][0] = 0u;      // scale and minimum 0
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          mma_16816(o[4 * w + j], h2_bits(lo[0][j]), h2_bits(hi[0][j]), h2_bits(lo[1][j]), h2_bits(hi[1][j]), pb.x, pb.y);
+        for (int w = 0; w < W; ++w) {
+          __half2 lo[2][4], hi[2][4];   // features 8 w + (0 .. 3) and + (4 .. 7); a pair is two of the lane's slots
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const __half2 sc = bits_h2(__byte_perm(vg[2 * e][0], vg[2 * e + 1][0], 0x5410)), mn = bits_h2(__byte_perm(vg[2 * e][0], vg[2 * e + 1][0], 0x7632));
+            nibble_pairs(__byte_perm(vw[2 * e][w], vw[2 * e + 1][w], 0x5410), lo[e]);
+            nibble_pairs(__byte_perm(vw[2 * e][w], vw[2 * e + 1][w], 0x7632), hi[e]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { lo[e][j] = __hfma2(lo[e][j], sc, mn); hi[e][j] = __hfma2(hi[e][j], sc, mn); }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            mma_16816(o[4 * w + j], h2_bits(lo[0][j]), h2_bits(hi[0][j]), h2_bits(lo[1][j]), h2_bits(hi[1][j]), pb.x, pb.y);
+        }
       }
+      __syncwarp();   // the buffer has been read by every lane
+      if (it + 1 < rounds) issue(it + 1, sub);
     }
-    __syncwarp();   // the buffer, the logits and the weights have been read by every lane
-    if (it + NSTAGE < n_tiles) issue(it + NSTAGE);
   }
   if (failed) {
-    // a copy did not land in time: flag it, then give every copy still in flight a second bounded wait
+    // a copy did not land in time: flag it, then give the copies still in flight a second bounded wait
     if (lane == 0) atomicExch(P.err, ERR_TIMEOUT);
-    const int issued = min(n_tiles, it + NSTAGE);
-    for (; it < issued; ++it) (void)mbar_wait_bounded(bars + it % NSTAGE, (uint32_t)(it / NSTAGE & 1));
+    for (int sub = 0; sub < 2; ++sub)
+      if (first + it * NW * SPAN + sub * TILE < row_end) (void)mbar_wait_bounded(bars + sub, (uint32_t)(it & 1));
   }
 
-  // ---- merge the lanes, then the warps of this CTA; the sums lie in the rings, which are done with
-  static_assert(G * D * 4 <= NSTAGE * TILE_BYTES, "a warp's sums fit its ring");
+  // ---- merge the lanes, then the warps of this CTA; the sums lie in the buffers, which are done with
+  static_assert(G * D * 4 <= 2 * TILE_BYTES, "a warp's sums fit its buffers");
   float* sums = reinterpret_cast<float*>(ring);              // [G][D]
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
@@ -350,38 +384,38 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     if (2 * t4 < G) { sums[2 * t4 * D + f] = o[i][0]; sums[2 * t4 * D + f + 4] = o[i][2]; }
     if (2 * t4 + 1 < G) { sums[(2 * t4 + 1) * D + f] = o[i][1]; sums[(2 * t4 + 1) * D + f + 4] = o[i][3]; }
   }
+  if (r8 == 0) {
+    if (2 * t4 < G) sh_l[warp][2 * t4] = l_x[0];
+    if (2 * t4 + 1 < G) sh_l[warp][2 * t4 + 1] = l_x[1];
+  }
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    l_x[g] = warp_sum(l_x[g]);
     l_y[g] = warp_sum(l_y[g]);
-    if (lane == 0) { sh_m[warp][g] = m_x[g]; sh_l[warp][g] = l_x[g]; sh_my[warp][g] = m_y[g]; sh_ly[warp][g] = l_y[g]; }
+    if (lane == 0) { sh_m[warp][g] = m_x[g]; sh_my[warp][g] = m_y[g]; sh_ly[warp][g] = l_y[g]; }
   }
   __syncthreads();
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    float* part = P.partials + (((size_t)u * P.splits + s) * G + g) * PSTRIDE;
-    float M = -INFINITY, MY = -INFINITY;
+  float* part = P.partials + ((size_t)u * P.splits + s) * G * PSTRIDE;      // [head][4 + D]
+  if (tid < G) {                                                            // one thread per head joins the statistics
+    const int g = tid;
+    float M = -INFINITY, MY = -INFINITY, L = 0.f, LY = 0.f;
 #pragma unroll
     for (int wi = 0; wi < NW; ++wi) { M = fmaxf(M, sh_m[wi][g]); MY = fmaxf(MY, sh_my[wi][g]); }
-    float sc[NW];
 #pragma unroll
-    for (int wi = 0; wi < NW; ++wi) sc[wi] = sh_l[wi][g] > 0.f ? fast_exp2((sh_m[wi][g] - M) * LOG2E) : 0.f;
-    for (int c = tid; c < D; c += NT) {
-      float acc_o = 0.f;
-#pragma unroll
-      for (int wi = 0; wi < NW; ++wi)
-        acc_o = fmaf(reinterpret_cast<const float*>(dyn_smem + (size_t)wi * NSTAGE * TILE_BYTES)[g * D + c], sc[wi], acc_o);
-      part[4 + c] = acc_o;
+    for (int wi = 0; wi < NW; ++wi) {
+      const float f = sh_l[wi][g] > 0.f ? fast_exp2((sh_m[wi][g] - M) * LOG2E) : 0.f;
+      L = fmaf(sh_l[wi][g], f, L);
+      if (sh_ly[wi][g] > 0.f) LY = fmaf(sh_ly[wi][g], fast_exp2((sh_my[wi][g] - MY) * LOG2E), LY);
+      sh_f[wi][g] = f;
     }
-    if (tid == 0) {
-      float L = 0.f, LY = 0.f;
+    *reinterpret_cast<float4*>(part + g * PSTRIDE) = make_float4(M, L, MY, LY);
+  }
+  __syncthreads();
+  for (int idx = tid; idx < G * D; idx += NT) {
+    const int g = idx / D, c = idx % D;
+    float sum = 0.f;
 #pragma unroll
-      for (int wi = 0; wi < NW; ++wi) {
-        L = fmaf(sh_l[wi][g], sc[wi], L);
-        if (sh_ly[wi][g] > 0.f) LY = fmaf(sh_ly[wi][g], fast_exp2((sh_my[wi][g] - MY) * LOG2E), LY);
-      }
-      part[0] = M; part[1] = L; part[2] = MY; part[3] = LY;
-    }
+    for (int wi = 0; wi < NW; ++wi) sum = fmaf(reinterpret_cast<const float*>(dyn_smem + (size_t)wi * 2 * TILE_BYTES)[idx], sh_f[wi][g], sum);
+    part[g * PSTRIDE + 4 + c] = sum;
   }
 }
 
@@ -413,21 +447,24 @@ cudaError_t launch_one(const PackedParams& P, int units, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)P.splits, (unsigned)units);
   cfg.blockDim = dim3(NW * 32);
-  cfg.dynamicSmemBytes = NW * NSTAGE * TILE * packed_slot_bytes(D);
+  cfg.dynamicSmemBytes = NW * 2 * TILE * packed_slot_bytes(D);
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
+  auto kern = P.noise_mode == 0 ? packed_stream_kernel<D, G, true> : packed_stream_kernel<D, G, false>;
   cudaError_t e = cudaSuccess;
-  if (cfg.dynamicSmemBytes > 40 * 1024) {   // with the static part above what every kernel may have; asked for once per device
+  if (cfg.dynamicSmemBytes > 32 * 1024) {   // with the static part (up to 13 KB) above what every kernel may have; asked for once per device
     static std::atomic<uint64_t> asked{0};
     int dev = 0;
     e = cudaGetDevice(&dev);
     if (e == cudaSuccess && (dev >= 64 || !(asked.load(std::memory_order_relaxed) >> dev & 1))) {
-      e = cudaFuncSetAttribute(packed_stream_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+      e = cudaFuncSetAttribute(packed_stream_kernel<D, G, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+      if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(packed_stream_kernel<D, G, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
       if (e == cudaSuccess && dev < 64) asked.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
     }
   }
-  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, packed_stream_kernel<D, G>, P);
+  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kern, P);
   if (e != cudaSuccess) return e;
   cfg.dynamicSmemBytes = 0;
   cfg.gridDim = dim3((unsigned)units);
@@ -456,11 +493,12 @@ cudaError_t launch_dim(const PackedParams& P, int units, cudaStream_t stream) {
 
 void decode_packed_plan(int units, int budget_k, int head_dim, int* splits_out, int* tiles_per_split_out) {
   const int tiles = (budget_k + TILE - 1) / TILE;
+  constexpr int ROUND = NW * SPAN / TILE;   // tiles of a round of the CTA's warps
   const int target_ctas = units >= 148 ? 148 * 13 : 148 * 8;
   int splits = (target_ctas + units - 1) / units;
-  splits = std::max(1, std::min(splits, std::min(MAX_SPLITS, (tiles + NW - 1) / NW)));
+  splits = std::max(1, std::min(splits, std::min(MAX_SPLITS, (tiles + ROUND - 1) / ROUND)));
   int tps = (tiles + splits - 1) / splits;
-  tps = (tps + NW - 1) / NW * NW;   // whole rounds of the CTA's warps
+  tps = (tps + ROUND - 1) / ROUND * ROUND;
   *splits_out = (tiles + tps - 1) / tps;
   *tiles_per_split_out = tps;
 }
