@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
 
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int s = blockIdx.x, u = blockIdx.y;
+  const int s = blockIdx.x, u = blockIdx.z * gridDim.y + blockIdx.y;   // grid: splits, key/value heads, batch rows
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r8 = lane >> 2, t4 = lane & 3;
   const int len = P.len[u];
@@ -158,8 +158,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
   const int row_end = min(len, row_begin + P.tiles_per_split * TILE);
   const unsigned char* cache_u = P.cache + (size_t)u * P.k * SB;
   const int32_t* pos_u = P.pos + (size_t)u * P.k;
-  const int Hkv = P.H / G;
-  const uint32_t b = (uint32_t)(u / Hkv), h0 = (uint32_t)(u % Hkv) * G, lh0 = (uint32_t)P.layer * P.H + h0;
+  const uint32_t b = blockIdx.z, h0 = blockIdx.y * G, lh0 = (uint32_t)P.layer * P.H + h0;
 
   // ---- the warp's two buffers
   const int first = row_begin + warp * SPAN;                 // first slot of the warp's first round
@@ -445,7 +444,7 @@ cudaError_t launch_one(const PackedParams& P, int units, cudaStream_t stream) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)P.splits, (unsigned)units);
+  cfg.gridDim = dim3((unsigned)P.splits, (unsigned)(P.H / G), (unsigned)(units / (P.H / G)));
   cfg.blockDim = dim3(NW * 32);
   cfg.dynamicSmemBytes = NW * 2 * TILE * packed_slot_bytes(D);
   cfg.stream = stream;
