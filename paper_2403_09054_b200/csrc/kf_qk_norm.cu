@@ -2,11 +2,12 @@
 // norm of queries and keys (x r w, r = 1 / sqrt(mean(x^2) + eps)) and the rotary embedding, then head-major binary16
 // rows; the values are only laid out.  Every value is read once and written once: HBM bounds it.
 //
-// A head's row is d / 8 neighbouring lanes with eight features (16 bytes) each, so that the sum of squares takes
-// log2(d / 8) shuffles and a pair of features that turn together lies in one lane (pairs 2i, 2i + 1) or in two lanes
-// R / 16 apart (pairs i, i + R / 2).  The angles of a token are shared by all of its heads: a CTA computes them once
-// into shared memory.  Positions reach far, so angle / 2 pi is formed and reduced in binary64; what is left, at most
-// half a turn, goes through binary32.
+// A head's row is d / 8 neighbouring lanes with eight features each, two runs of four that are chosen so that the features
+// of a pair lie in one lane: [4 l, 4 l + 4) and [R/2 + 4 l, ...) of the rotary features for pairs (i, i + R/2), eight
+// neighbours for pairs (2i, 2i + 1) and for what does not turn.  The sum of squares takes log2(d / 8) shuffles, the rotation
+// none.  The angles of a token are shared by all of its heads: a CTA takes up to four tokens and computes their angles
+// first, one per thread, into shared memory.  Positions reach far, so angle / 2 pi is formed and reduced in binary64; what
+// is left, at most half a turn, goes through binary32.
 #include <cuda_bf16.h>
 
 #include "kf_ops.cuh"
@@ -16,137 +17,137 @@ namespace kf {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int MAX_TOKENS = 8;     // tokens per CTA (few heads: several, so that all threads have a row)
-constexpr int UNROLL = 2;         // rows in flight per lane, and as many being worked on
+constexpr int MAX_TOKENS = 8;     // tokens per CTA
+constexpr int AHEAD = 6;          // rows a lane requests before it works on the first
 
+// Four values of a run.
 template <class T>
-__device__ __forceinline__ void widen(const uint4& v, float (&x)[8]) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ void widen(const uint2& v, float* x) {
+  const uint32_t w[2] = {v.x, v.y};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 2; ++i) {
     float2 f;
-    if constexpr (sizeof(T) == 2 && __is_same(T, __half)) f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+    if constexpr (__is_same(T, __half)) f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
     else f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
     x[2 * i] = f.x;
     x[2 * i + 1] = f.y;
   }
 }
+__device__ __forceinline__ uint2 narrow(const float* x) {
+  const __half2 a = __floats2half2_rn(x[0], x[1]), b = __floats2half2_rn(x[2], x[3]);
+  return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
 
-// A CTA works on one token, or, where a token has fewer rows than the CTA has places, on several with one row per
-// place; either way a thread's token never changes, and its share of the token's angles and of the weights stays in registers.
+// A round of the CTA is one row for every place (d / 8 lanes): PLACES rows of one token, or, where a token has fewer rows than
+// that, one row each of several tokens.
 template <int D, class T, bool HALVES>
-__global__ void __launch_bounds__(THREADS, 4) qk_norm_kernel(const __grid_constant__ QkNormParams P, int tokens_per_cta) {
+__global__ void __launch_bounds__(THREADS, 3) qk_norm_kernel(const __grid_constant__ QkNormParams P, int tokens_per_cta) {
   constexpr int LPR = D / 8;                    // lanes per row
-  constexpr int PLACES = THREADS / LPR;         // rows the CTA works on at a time
-  constexpr int NCS = HALVES ? 8 : 4;           // pairs that this lane's features take part in
-  __shared__ float2 turn[MAX_TOKENS][D / 2];    // (cos, sin)
-  const int tid = threadIdx.x, lane = tid & 31, sub = lane % LPR, place = tid / LPR;
+  constexpr int PLACES = THREADS / LPR;
+  __shared__ __align__(16) float2 turn[MAX_TOKENS][D / 2];    // (cos, sin)
+  const int tid = threadIdx.x, sub = tid % LPR, place = tid / LPR;
   const int64_t tokens = (int64_t)P.batch * P.n, first = (int64_t)blockIdx.x * tokens_per_cta;
   const int here = (int)(tokens - first < tokens_per_cta ? tokens - first : tokens_per_cta);
   const int half = P.rotary_dims / 2;
-  const int rows_per_token = P.H + (P.v ? 2 : 1) * P.Hkv;
-  const int tk = tokens_per_cta > 1 ? place / rows_per_token : 0;
-  const int row0 = tokens_per_cta > 1 ? place % rows_per_token : place;
-  const int rows = tk < here ? rows_per_token : 0;          // a place without a token takes part in the shuffles only
-  const int64_t tok = first + (tk < here ? tk : 0), b = tok / P.n, t = tok % P.n;
-  const T* src = static_cast<const T*>(P.qkv) + b * P.batch_stride + t * P.token_stride + sub * 8;
-
-  uint4 raw[UNROLL];
-  auto load = [&](int row) {
-#pragma unroll
-    for (int i = 0; i < UNROLL; ++i)
-      raw[i] = row + i * PLACES < rows ? __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)(row + i * PLACES) * D)) : make_uint4(0, 0, 0, 0);
-  };
-  load(row0);   // in flight while the angles are computed
+  const int rows = P.H + (P.v ? 2 : 1) * P.Hkv;
+  const int side = rows < PLACES ? PLACES / rows : 1;            // tokens side by side in a round
+  const int my_token = rows < PLACES ? place / rows : 0, row0 = rows < PLACES ? place % rows : place;
+  const bool idle = my_token >= side;                            // places left over; they take part in the shuffles
+  // the lane's two runs of four features
+  const bool turns = 8 * sub < P.rotary_dims;
+  const int run0 = HALVES && turns ? 4 * sub : 8 * sub, run1 = HALVES && turns ? half + 4 * sub : 8 * sub + 4;
 
   for (int idx = tid; idx < here * half; idx += THREADS) {
-    const int tk2 = idx / half, i = idx % half;
-    const int64_t tok2 = first + tk2;
-    const int pos = P.positions ? P.positions[tok2] : P.position0 + (int)(tok2 % P.n);
-    const double turns = (double)pos * (exp2(-P.log2_base * (double)i / (double)half) * 0.15915494309189535);
+    const int tk = idx / half, i = idx % half;
+    const int64_t tok = first + tk;
+    const int pos = P.positions ? P.positions[tok] : P.position0 + (int)(tok % P.n);
+    const double turned = (double)pos * (exp2(-P.log2_base * (double)i / (double)half) * 0.15915494309189535);
     float s, c;
-    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-    turn[tk2][i] = make_float2(c, s);
+    sincospif(2.0f * (float)(turned - rint(turned)), &s, &c);
+    turn[tk][i] = make_float2(c, s);
   }
   constexpr uint32_t ONES = __is_same(T, __half) ? 0x3c003c00u : 0x3f803f80u;
-  uint4 wq = make_uint4(ONES, ONES, ONES, ONES), wk = wq;      // weights, as they came
-  if (P.norm && P.q_weight) wq = __ldg(static_cast<const uint4*>(P.q_weight) + sub);
-  if (P.norm && P.k_weight) wk = __ldg(static_cast<const uint4*>(P.k_weight) + sub);
-  __syncthreads();
-  // features that stay as they are turn by nothing
-  const bool turns_here = 8 * sub < 2 * half;
-  const bool low = 8 * sub < half;               // HALVES: this lane holds the first features of its pairs
-  float cs[NCS], sn[NCS];
-#pragma unroll
-  for (int e = 0; e < NCS; ++e) {
-    float2 v = make_float2(1.f, 0.f);
-    if (turns_here) {
-      if constexpr (!HALVES) v = turn[tk < here ? tk : 0][4 * sub + e];
-      else v = turn[tk < here ? tk : 0][half == 4 ? e & 3 : (low ? 8 * sub : 8 * sub - half) + e];
-    }
-    cs[e] = v.x;
-    // what the other feature of the pair is multiplied by: a c - b s for the first one, b c + a s for the second
-    sn[e] = HALVES && (half == 4 ? e < 4 : low) ? -v.y : v.y;
+  uint2 wq[2] = {make_uint2(ONES, ONES), make_uint2(ONES, ONES)}, wk[2] = {wq[0], wq[0]};      // weights, as they came
+  if (P.q_weight) {
+    wq[0] = __ldg(reinterpret_cast<const uint2*>(static_cast<const T*>(P.q_weight) + run0));
+    wq[1] = __ldg(reinterpret_cast<const uint2*>(static_cast<const T*>(P.q_weight) + run1));
   }
+  if (P.k_weight) {
+    wk[0] = __ldg(reinterpret_cast<const uint2*>(static_cast<const T*>(P.k_weight) + run0));
+    wk[1] = __ldg(reinterpret_cast<const uint2*>(static_cast<const T*>(P.k_weight) + run1));
+  }
+  __syncthreads();
 
-  const int rounds = (rows_per_token + PLACES - 1) / PLACES;
-  for (int r0 = 0; r0 < rounds; r0 += UNROLL) {
-    uint4 now[UNROLL];
+  for (int group = 0; group < here; group += side) {
+    const int tk = group + my_token;
+    const bool there = !idle && tk < here;
+    const int64_t tok = first + (there ? tk : 0), b = tok / P.n, t = tok % P.n;
+    const T* src = static_cast<const T*>(P.qkv) + b * P.batch_stride + t * P.token_stride;
+    const int mine = there ? rows : 0;
+    const int64_t step = (int64_t)P.n * D;              // from a head's row to the next head's
+    // row r of the token goes to one of these plus r steps
+    __half* to_q = P.q + (b * P.H * P.n + t) * D;
+    __half* to_k = P.k + (b * P.Hkv * P.n + t) * D - P.H * step;
+    __half* to_v = P.v + (b * P.Hkv * P.n + t) * D - (P.H + P.Hkv) * step;
+    float cs[4] = {}, sn[4] = {};                       // of the lane's four pairs
+    if (turns) {
+      const float4* at = reinterpret_cast<const float4*>(&turn[there ? tk : 0][4 * sub]);
+      const float4 u = at[0], v = at[1];
+      cs[0] = u.x; sn[0] = u.y; cs[1] = u.z; sn[1] = u.w;
+      cs[2] = v.x; sn[2] = v.y; cs[3] = v.z; sn[3] = v.w;
+    }
+    for (int r0 = 0; r0 < rows; r0 += AHEAD * PLACES) {     // AHEAD rounds at a time, their rows requested first
+      uint2 raw[AHEAD][2];
 #pragma unroll
-    for (int i = 0; i < UNROLL; ++i) now[i] = raw[i];
-    if (r0 + UNROLL < rounds) load(row0 + (r0 + UNROLL) * PLACES);
-#pragma unroll
-    for (int i = 0; i < UNROLL; ++i) {
-      if (r0 + i >= rounds) break;                // the same for the whole CTA
-      const int head = row0 + (r0 + i) * PLACES;
-      const bool is_q = head < P.H, is_v = head >= P.H + P.Hkv;
-      float x[8];
-      widen<T>(now[i], x);
-      if (P.norm) {
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        const float r = rsqrtf(fmaf(ss, 1.0f / (float)D, P.eps));
-        if (!is_v) {
-          float w[8];
-          widen<T>(is_q ? wq : wk, w);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= r * w[e];
+      for (int i = 0; i < AHEAD; ++i) {
+        const int row = r0 + i * PLACES + row0;
+        raw[i][0] = raw[i][1] = make_uint2(0, 0);
+        if (row < mine) {
+          raw[i][0] = __ldcs(reinterpret_cast<const uint2*>(src + (int64_t)row * D + run0));
+          raw[i][1] = __ldcs(reinterpret_cast<const uint2*>(src + (int64_t)row * D + run1));
         }
       }
-      if (half > 0) {
-        if constexpr (!HALVES) {
-          if (!is_v) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float a = x[2 * e], c = x[2 * e + 1];
-              x[2 * e] = a * cs[e] - c * sn[e];
-              x[2 * e + 1] = fmaf(a, sn[e], c * cs[e]);
+      for (int i = 0; i < AHEAD; ++i) {
+        if (r0 + i * PLACES >= rows) break;             // the same for the whole CTA
+        const int row = r0 + i * PLACES + row0;
+        const bool is_q = row < P.H, is_v = row >= P.H + P.Hkv;
+        float x[8];
+        widen<T>(raw[i][0], x);
+        widen<T>(raw[i][1], x + 4);
+        if (!__all_sync(0xffffffffu, is_v)) {           // a warp of value rows only lays them out
+          float r = 1.f;
+          if (P.norm) {
+            float ss = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+#pragma unroll
+            for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            r = rsqrtf(fmaf(ss, 1.0f / (float)D, P.eps));
+          }
+          if (!is_v) {
+            float w[8];
+            widen<T>(is_q ? wq[0] : wk[0], w);
+            widen<T>(is_q ? wq[1] : wk[1], w + 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= r * w[e];
+            if (turns) {      // what does not turn keeps its value (the other feature may be infinite)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float& a = HALVES ? x[e] : x[2 * e];
+                float& c = HALVES ? x[e + 4] : x[2 * e + 1];
+                const float a1 = a * cs[e] - c * sn[e];
+                c = fmaf(a, sn[e], c * cs[e]);
+                a = a1;
+              }
             }
           }
-        } else {
-          float other[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) other[e] = half == 4 ? x[e ^ 4] : __shfl_xor_sync(0xffffffffu, x[e], half / 8);
-          if (!is_v) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = fmaf(other[e], sn[e], x[e] * cs[e]);
-          }
         }
-      }
-      if (head < rows) {
-        __half* base = is_q ? P.q : (is_v ? P.v : P.k);
-        const int64_t slab = is_q ? b * P.H + head : b * P.Hkv + head - P.H - (is_v ? P.Hkv : 0);
-        __half* dst = base + (slab * P.n + t) * D;
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const __half2 h = __floats2half2_rn(x[2 * e], x[2 * e + 1]);
-          w[e] = *reinterpret_cast<const uint32_t*>(&h);
+        if (row < mine) {
+          __half* dst = (is_q ? to_q : (is_v ? to_v : to_k)) + row * step;
+          __stcs(reinterpret_cast<uint2*>(dst + run0), narrow(x));
+          __stcs(reinterpret_cast<uint2*>(dst + run1), narrow(x + 4));
         }
-        reinterpret_cast<uint4*>(dst)[sub] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
   }
@@ -154,10 +155,12 @@ __global__ void __launch_bounds__(THREADS, 4) qk_norm_kernel(const __grid_consta
 
 template <int D>
 cudaError_t launch_dim(const QkNormParams& P, bool bf16, cudaStream_t stream) {
-  const int rows = P.H + (P.v ? 2 : 1) * P.Hkv;
-  int per_cta = THREADS / (D / 8) / rows;
-  per_cta = per_cta < 1 ? 1 : (per_cta > MAX_TOKENS ? MAX_TOKENS : per_cta);
+  const int rows = P.H + (P.v ? 2 : 1) * P.Hkv, places = THREADS / (D / 8);
   const int64_t tokens = (int64_t)P.batch * P.n;
+  // as many tokens side by side as fit; several one after the other only where that leaves every SM several CTAs
+  int per_cta = rows < places ? places / rows : 1;
+  per_cta = per_cta > MAX_TOKENS ? MAX_TOKENS : per_cta;
+  while (per_cta * 2 <= 4 && tokens >= (int64_t)per_cta * 2 * 148 * 8) per_cta *= 2;
   const unsigned grid = (unsigned)((tokens + per_cta - 1) / per_cta);
   if (bf16 && P.halves) qk_norm_kernel<D, __nv_bfloat16, true><<<grid, THREADS, 0, stream>>>(P, per_cta);
   else if (bf16) qk_norm_kernel<D, __nv_bfloat16, false><<<grid, THREADS, 0, stream>>>(P, per_cta);
