@@ -18,17 +18,19 @@ __device__ __forceinline__ void extremes8(const uint4& v, __half2& low, __half2&
   high = __hmax2_nan(__hmax2_nan(a, b), __hmax2_nan(c, d));
 }
 
-// Eight codes.  Adding 1.5 * 2^23 rounds to whole numbers (to even, as rintf does) and leaves the code in the low bits.
+// Eight codes.  Adding M = 1.5 * 2^23 rounds to whole numbers (to even, as rintf does) and leaves the code in the low bits of
+// M's own; the eight words are shifted and added up as they are, and the M's taken off together (modulo 2^32).
 __device__ __forceinline__ uint32_t pack8(const uint4& v, float low, float inverse) {
+  constexpr float M = 12582912.f;
+  constexpr uint32_t M_BITS = 0x4b400000u;
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t code = 0;
+  uint32_t code = 0u - M_BITS * 0x11111111u;
 #pragma unroll
-  for (int i = 3; i >= 0; --i) {
+  for (int i = 0; i < 4; ++i) {
     const float2 f = __half22float2(bits_h2(w[i]));
-    const float a = __fadd_rn(fminf(__fmul_rn(__fsub_rn(f.x, low), inverse), 15.f), 12582912.f);
-    const float c = __fadd_rn(fminf(__fmul_rn(__fsub_rn(f.y, low), inverse), 15.f), 12582912.f);
-    code = code << 4 | (__float_as_uint(c) & 15u);
-    code = code << 4 | (__float_as_uint(a) & 15u);
+    const float a = __fadd_rn(fminf(__fmul_rn(__fsub_rn(f.x, low), inverse), 15.f), M);
+    const float c = __fadd_rn(fminf(__fmul_rn(__fsub_rn(f.y, low), inverse), 15.f), M);
+    code += (__float_as_uint(a) << 8 * i) + (__float_as_uint(c) << (8 * i + 4));
   }
   return low == low ? code : 0u;   // not finite: every code 0
 }
@@ -65,32 +67,34 @@ __device__ __forceinline__ void groups_of(const uint4& kv, const uint4& vv, Grou
   vg = odd ? mine : other;
 }
 
+// grid: chunks of a unit's rows, units (the rest of them in further rounds)
 template <int D>
 __global__ void __launch_bounds__(THREADS) pack_kernel(const __half* __restrict__ K, const __half* __restrict__ V,
                                                        const int32_t* __restrict__ len, unsigned char* __restrict__ cache,
-                                                       int64_t rows, int n, int k) {
+                                                       int64_t units, int n, int k) {
   constexpr int CPR = D / 8;   // chunks per row
-  const int64_t idx = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-  const int64_t row = idx / CPR;
-  const int c = (int)(idx % CPR);
-  bool in = row < rows;
-  const int64_t u = in ? row / n : 0;
-  const int j = in ? (int)(row % n) : 0;
-  if (in && len) in = j < len[u];
-  uint4 kv = make_uint4(0, 0, 0, 0), vv = kv;
-  if (in) {
-    kv = __ldcs(reinterpret_cast<const uint4*>(K + row * D) + c);
-    vv = __ldcs(reinterpret_cast<const uint4*>(V + row * D) + c);
-  }
-  Group kg, vg;
-  groups_of(kv, vv, kg, vg);   // whole warps: a group never straddles a row
-  if (!in) return;
-  unsigned char* slot = cache + ((size_t)u * k + j) * packed_slot_bytes(D);
-  *reinterpret_cast<uint32_t*>(slot + 4 * c) = pack8(kv, __high2float(kg.params), kg.inverse);
-  *reinterpret_cast<uint32_t*>(slot + D / 2 + 4 * c) = pack8(vv, __high2float(vg.params), vg.inverse);
-  if ((c & 3) == 0) {
-    *reinterpret_cast<uint32_t*>(slot + D + c) = h2_bits(kg.params);
-    *reinterpret_cast<uint32_t*>(slot + D + D / 8 + c) = h2_bits(vg.params);
+  const int64_t at = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+  const int64_t j = at / CPR;
+  const int c = (int)(at % CPR);
+  for (int64_t u = blockIdx.y; u < units; u += gridDim.y) {
+    const bool in = j < n && (!len || j < len[u]);
+    const int64_t row = u * n + j;
+    uint4 kv = make_uint4(0, 0, 0, 0), vv = kv;
+    if (in) {
+      kv = __ldcs(reinterpret_cast<const uint4*>(K + row * D) + c);
+      vv = __ldcs(reinterpret_cast<const uint4*>(V + row * D) + c);
+    }
+    Group kg, vg;
+    groups_of(kv, vv, kg, vg);   // whole warps: a group never straddles a row
+    if (in) {
+      unsigned char* slot = cache + ((size_t)u * k + j) * packed_slot_bytes(D);
+      *reinterpret_cast<uint32_t*>(slot + 4 * c) = pack8(kv, __high2float(kg.params), kg.inverse);
+      *reinterpret_cast<uint32_t*>(slot + D / 2 + 4 * c) = pack8(vv, __high2float(vg.params), vg.inverse);
+      if ((c & 3) == 0) {
+        *reinterpret_cast<uint32_t*>(slot + D + c) = h2_bits(kg.params);
+        *reinterpret_cast<uint32_t*>(slot + D + D / 8 + c) = h2_bits(vg.params);
+      }
+    }
   }
 }
 
@@ -110,35 +114,37 @@ __device__ __forceinline__ uint4 unpack8(uint32_t w, __half2 group) {
 
 template <int D>
 __global__ void __launch_bounds__(THREADS) unpack_kernel(const unsigned char* __restrict__ cache, const int32_t* __restrict__ len,
-                                                         __half* __restrict__ K, __half* __restrict__ V, int64_t rows, int n, int k) {
+                                                         __half* __restrict__ K, __half* __restrict__ V, int64_t units, int n, int k) {
   constexpr int CPR = D / 8;
-  const int64_t idx = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-  const int64_t row = idx / CPR;
-  const int c = (int)(idx % CPR);
-  if (row >= rows) return;
-  const int64_t u = row / n;
-  const int j = (int)(row % n);
-  if (len && j >= len[u]) return;
-  const unsigned char* slot = cache + ((size_t)u * k + j) * packed_slot_bytes(D);
-  const uint32_t kw = *reinterpret_cast<const uint32_t*>(slot + 4 * c), vw = *reinterpret_cast<const uint32_t*>(slot + D / 2 + 4 * c);
-  const uint32_t kg = *reinterpret_cast<const uint32_t*>(slot + D + 4 * (c / 4));
-  const uint32_t vg = *reinterpret_cast<const uint32_t*>(slot + D + D / 8 + 4 * (c / 4));
-  __stcs(reinterpret_cast<uint4*>(K + row * D) + c, unpack8(kw, bits_h2(kg)));
-  __stcs(reinterpret_cast<uint4*>(V + row * D) + c, unpack8(vw, bits_h2(vg)));
+  const int64_t at = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+  const int64_t j = at / CPR;
+  const int c = (int)(at % CPR);
+  if (j >= n) return;
+  for (int64_t u = blockIdx.y; u < units; u += gridDim.y) {
+    if (len && j >= len[u]) continue;
+    const int64_t row = u * n + j;
+    const unsigned char* slot = cache + ((size_t)u * k + j) * packed_slot_bytes(D);
+    const uint32_t kw = *reinterpret_cast<const uint32_t*>(slot + 4 * c), vw = *reinterpret_cast<const uint32_t*>(slot + D / 2 + 4 * c);
+    const uint32_t kg = *reinterpret_cast<const uint32_t*>(slot + D + 4 * (c / 4));
+    const uint32_t vg = *reinterpret_cast<const uint32_t*>(slot + D + D / 8 + 4 * (c / 4));
+    __stcs(reinterpret_cast<uint4*>(K + row * D) + c, unpack8(kw, bits_h2(kg)));
+    __stcs(reinterpret_cast<uint4*>(V + row * D) + c, unpack8(vw, bits_h2(vg)));
+  }
 }
 
-inline unsigned blocks_for(int64_t rows, int d) { return (unsigned)((rows * (d / 8) + THREADS - 1) / THREADS); }
+inline dim3 grid_for(int64_t units, int n, int d) {
+  return dim3((unsigned)(((int64_t)n * (d / 8) + THREADS - 1) / THREADS), (unsigned)(units < 65535 ? units : 65535));
+}
 
 }  // namespace
 
 cudaError_t launch_pack(const __half* K, const __half* V, const int32_t* len, unsigned char* cache, int64_t units, int n, int k,
                         int head_dim, cudaStream_t stream) {
-  const int64_t rows = units * n;
-  const unsigned grid = blocks_for(rows, head_dim);
+  const dim3 grid = grid_for(units, n, head_dim);
   switch (head_dim) {
-    case 64: pack_kernel<64><<<grid, THREADS, 0, stream>>>(K, V, len, cache, rows, n, k); break;
-    case 128: pack_kernel<128><<<grid, THREADS, 0, stream>>>(K, V, len, cache, rows, n, k); break;
-    case 256: pack_kernel<256><<<grid, THREADS, 0, stream>>>(K, V, len, cache, rows, n, k); break;
+    case 64: pack_kernel<64><<<grid, THREADS, 0, stream>>>(K, V, len, cache, units, n, k); break;
+    case 128: pack_kernel<128><<<grid, THREADS, 0, stream>>>(K, V, len, cache, units, n, k); break;
+    case 256: pack_kernel<256><<<grid, THREADS, 0, stream>>>(K, V, len, cache, units, n, k); break;
     default: return cudaErrorInvalidValue;
   }
   return cudaGetLastError();
@@ -146,12 +152,11 @@ cudaError_t launch_pack(const __half* K, const __half* V, const int32_t* len, un
 
 cudaError_t launch_unpack(const unsigned char* cache, const int32_t* len, __half* K, __half* V, int64_t units, int n, int k,
                           int head_dim, cudaStream_t stream) {
-  const int64_t rows = units * n;
-  const unsigned grid = blocks_for(rows, head_dim);
+  const dim3 grid = grid_for(units, n, head_dim);
   switch (head_dim) {
-    case 64: unpack_kernel<64><<<grid, THREADS, 0, stream>>>(cache, len, K, V, rows, n, k); break;
-    case 128: unpack_kernel<128><<<grid, THREADS, 0, stream>>>(cache, len, K, V, rows, n, k); break;
-    case 256: unpack_kernel<256><<<grid, THREADS, 0, stream>>>(cache, len, K, V, rows, n, k); break;
+    case 64: unpack_kernel<64><<<grid, THREADS, 0, stream>>>(cache, len, K, V, units, n, k); break;
+    case 128: unpack_kernel<128><<<grid, THREADS, 0, stream>>>(cache, len, K, V, units, n, k); break;
+    case 256: unpack_kernel<256><<<grid, THREADS, 0, stream>>>(cache, len, K, V, units, n, k); break;
     default: return cudaErrorInvalidValue;
   }
   return cudaGetLastError();
