@@ -20,17 +20,21 @@ __device__ __forceinline__ void extremes8(const uint4& v, __half2& low, __half2&
 
 // Eight codes.  Adding M = 1.5 * 2^23 rounds to whole numbers (to even, as rintf does) and leaves the code in the low bits of
 // M's own; the eight words are shifted and added up as they are, and the M's taken off together (modulo 2^32).
+constexpr float M = 12582912.f;
+constexpr uint32_t M_BITS = 0x4b400000u;
+template <bool CLAMP>
 __device__ __forceinline__ uint32_t pack8(const uint4& v, float low, float inverse) {
-  constexpr float M = 12582912.f;
-  constexpr uint32_t M_BITS = 0x4b400000u;
+  auto place = [&](float x) {
+    float p = __fmul_rn(__fsub_rn(x, low), inverse);
+    if (CLAMP) p = fminf(p, 15.f);
+    return __float_as_uint(__fadd_rn(p, M));
+  };
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   uint32_t code = 0u - M_BITS * 0x11111111u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 f = __half22float2(bits_h2(w[i]));
-    const float a = __fadd_rn(fminf(__fmul_rn(__fsub_rn(f.x, low), inverse), 15.f), M);
-    const float c = __fadd_rn(fminf(__fmul_rn(__fsub_rn(f.y, low), inverse), 15.f), M);
-    code += (__float_as_uint(a) << 8 * i) + (__float_as_uint(c) << (8 * i + 4));
+    code += (place(f.x) << 8 * i) + (place(f.y) << (8 * i + 4));
   }
   return low == low ? code : 0u;   // not finite: every code 0
 }
@@ -38,6 +42,7 @@ __device__ __forceinline__ uint32_t pack8(const uint4& v, float low, float inver
 struct Group {
   __half2 params;   // (scale, minimum)
   float inverse;
+  bool clamp;       // whether a code could pass 15 (scales of few bits, near the smallest binary16 numbers), of either group
 };
 
 // The groups that this lane's two chunks belong to; the four lanes of a group call it together.  The even lanes work out the
@@ -58,11 +63,14 @@ __device__ __forceinline__ void groups_of(const uint4& kv, const uint4& vv, Grou
   }
   const bool odd = threadIdx.x & 1;
   Group mine;
-  mine.params = packed_group(__half2float(odd ? __high2half(lo) : __low2half(lo)), __half2float(odd ? __high2half(hi) : __low2half(hi)));
+  const float low = __half2float(odd ? __high2half(lo) : __low2half(lo)), high = __half2float(odd ? __high2half(hi) : __low2half(hi));
+  mine.params = packed_group(low, high);
   mine.inverse = packed_inverse(__low2half(mine.params));
+  mine.clamp = !(__fmul_rn(__fsub_rn(high, low), mine.inverse) < 15.5f);   // the largest quotient of the group
   Group other;
   other.params = __shfl_xor_sync(0xffffffffu, mine.params, 1);
   other.inverse = __shfl_xor_sync(0xffffffffu, mine.inverse, 1);
+  other.clamp = mine.clamp = __any_sync(0xffffffffu, mine.clamp);
   kg = odd ? other : mine;
   vg = odd ? mine : other;
 }
@@ -88,8 +96,16 @@ __global__ void __launch_bounds__(THREADS) pack_kernel(const __half* __restrict_
     groups_of(kv, vv, kg, vg);   // whole warps: a group never straddles a row
     if (in) {
       unsigned char* slot = cache + ((size_t)u * k + j) * packed_slot_bytes(D);
-      *reinterpret_cast<uint32_t*>(slot + 4 * c) = pack8(kv, __high2float(kg.params), kg.inverse);
-      *reinterpret_cast<uint32_t*>(slot + D / 2 + 4 * c) = pack8(vv, __high2float(vg.params), vg.inverse);
+      uint32_t kc, vc;
+      if (kg.clamp) {            // the same for the whole warp
+        kc = pack8<true>(kv, __high2float(kg.params), kg.inverse);
+        vc = pack8<true>(vv, __high2float(vg.params), vg.inverse);
+      } else {
+        kc = pack8<false>(kv, __high2float(kg.params), kg.inverse);
+        vc = pack8<false>(vv, __high2float(vg.params), vg.inverse);
+      }
+      *reinterpret_cast<uint32_t*>(slot + 4 * c) = kc;
+      *reinterpret_cast<uint32_t*>(slot + D / 2 + 4 * c) = vc;
       if ((c & 3) == 0) {
         *reinterpret_cast<uint32_t*>(slot + D + c) = h2_bits(kg.params);
         *reinterpret_cast<uint32_t*>(slot + D + D / 8 + c) = h2_bits(vg.params);

@@ -42,12 +42,19 @@ __device__ __forceinline__ __half2 packed_group(float low, float high) {
   const float range = __fsub_rn(high, low);
   const bool finite = range <= 131008.0f;   // the span of finite binary16 numbers; false for NaN too
   const __half nan = __ushort_as_half((unsigned short)0x7fffu);
-  return finite ? __halves2half2(__float2half_rd(__fdiv_rn(range, 15.0f)), __float2half_rn(low)) : __halves2half2(nan, nan);
+  // range / 15, correctly rounded: a quotient by the rounded reciprocal and one correction by the remainder, which the
+  // fused multiply-add gives exactly (Markstein 1990)
+  const float q = __fmul_rn(range, 1.0f / 15.0f);
+  const float span = fmaf(fmaf(-15.0f, q, range), 1.0f / 15.0f, q);
+  return finite ? __halves2half2(__float2half_rd(span), __float2half_rn(low)) : __halves2half2(nan, nan);
 }
 // 1 / scale, or 0 where every code of the group is 0.
 __device__ __forceinline__ float packed_inverse(__half scale) {
   const float s = __half2float(scale);
-  return s > 0.f ? __frcp_rn(s) : 0.f;   // false for NaN
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(s));   // to the last place; one Newton step with exact residual rounds it
+  y = fmaf(y, fmaf(-s, y, 1.0f), y);
+  return s > 0.f ? y : 0.f;              // false for NaN
 }
 __device__ __forceinline__ uint32_t packed_code(float x, float low, float inverse) {
   const float c = rintf(__fmul_rn(__fsub_rn(x, low), inverse));

@@ -60,6 +60,27 @@ def test_pack_and_unpack(units, n, k, d):
         assert np.array_equal(back.cpu().numpy(), expect, equal_nan=True)
 
 
+def test_pack_with_every_scale():
+    """Groups whose span is just below, at and just above fifteen times each binary16 number: every scale there is, with its reciprocal, bit for bit."""
+    scale = torch.arange(1, 0x7c00, dtype=torch.int16).view(torch.float16).double()
+    top = (15 * scale).half()
+    top = top[top.isfinite()]
+    bits = top.view(torch.int16)
+    top = torch.cat([(bits - 1).clamp(min=0).view(torch.float16), top, (bits + 1).clamp(max=0x7bff).view(torch.float16)])
+    n = top.numel() // 8
+    g = torch.rand(n * 8, 32, generator=torch.Generator().manual_seed(1)) * top[:n * 8, None].float()
+    g[:, 3], g[:, 17] = 0.0, top[:n * 8].float()
+    x = g.half().view(2, 1, n, 128)
+    sign = torch.tensor([1.0, -1.0], dtype=torch.float16).repeat(n // 2 + 1)[:n, None]
+    K, V = (x[0] * sign).contiguous().to(DEV), x[1].contiguous().to(DEV)
+    cache = torch.zeros(1, n, 160, dtype=torch.uint8, device=DEV)
+    kf.kf_pack_cache(K=K, V=V, cache=cache)
+    want = ref.slots_of(K.cpu().numpy(), V.cpu().numpy())
+    got = cache.cpu().numpy()
+    assert np.array_equal(got[..., :128], want[..., :128])
+    assert np.array_equal(got[..., 128:].view(np.float16), want[..., 128:].view(np.float16))
+
+
 def test_pack_leaves_rows_behind_the_entry_count():
     K, V = _randn(1, 2, 3, 9, 64).half(), _randn(2, 2, 3, 9, 64).half()
     length = torch.tensor([[0, 1, 9], [5, 12, -3]], dtype=torch.int32, device=DEV)      # counts outside 0..n: all rows, none
