@@ -9,9 +9,10 @@
 //
 // Finding the best few of thousands of registers: with c = take / 8 rounded up, each of the eight warps finds the c-th
 // largest of its threads' maxima, and the smallest of those eight values is one that at least `take` elements reach and
-// few more than that do (about three times `take` of 8192 random ones).  Those are collected in shared memory and ranked by
-// comparison.  Rows with so many equal values that the collection does not fit (all tokens forbidden, constant
-// logits) are worked off one element at a time.
+// few more than that do (about three times `take` of 8192 random ones).  (Of a chunk that fills fewer warps, those count;
+// where a warp has too few tokens that are not forbidden, a single warp's take-th largest serves.)  They are collected in shared
+// memory and ranked by comparison.  Chunks with so many equal values that the collection does not fit (all tokens
+// forbidden, constant logits) are worked off one element at a time.
 //
 // Order everywhere: larger value first, of equal values the lower beam, then the lower token.
 //
@@ -26,7 +27,7 @@ namespace kf {
 namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
-constexpr int CAP = 1024;                 // collected elements
+constexpr int CAP = THREADS;              // collected elements, one per thread when they are ranked
 
 // Larger value, then lower index: larger key.  Values are never NaN.
 __device__ __forceinline__ uint32_t ordered(float v) {
@@ -152,23 +153,20 @@ __global__ void __launch_bounds__(THREADS, 4) beam_chunk_kernel(const __grid_con
   V vec[VPT];
 #pragma unroll
   for (int v = 0; v < VPT; ++v) vec[v].clear();
-  if (first * EPV - lead >= 0 && last * EPV - lead <= P.vocab) {   // the same for the whole CTA: nothing is cut
 #pragma unroll
-    for (int v = 0; v < VPT; ++v)
-      if (first + v * THREADS + tid < last) vec[v].load(logits + place(v));
-  } else {
+  for (int v = 0; v < VPT; ++v)
+    if (first + v * THREADS + tid < last && place(v) >= 0 && place(v) + EPV <= P.vocab) vec[v].load(logits + place(v));
+  if (first * EPV < lead || last * EPV - lead > P.vocab) {   // the same for the whole CTA: one of its vectors is cut
 #pragma unroll 1
     for (int v = 0; v < VPT; ++v) {
       const int at = place(v);
-      V one;
-      one.clear();
-      if (first + v * THREADS + tid < last) {
-        if (at >= 0 && at + EPV <= P.vocab) one.load(logits + at);
-        else one.load_within(logits, at, P.vocab);
-      }
+      if (first + v * THREADS + tid < last && (at < 0 || at + EPV > P.vocab)) {
+        V one;
+        one.load_within(logits, at, P.vocab);
 #pragma unroll
-      for (int k = 0; k < VPT; ++k)
-        if (k == v) vec[k] = one;
+        for (int k = 0; k < VPT; ++k)
+          if (k == v) vec[k] = one;
+      }
     }
   }
 #pragma unroll
@@ -180,12 +178,25 @@ __global__ void __launch_bounds__(THREADS, 4) beam_chunk_kernel(const __grid_con
 #pragma unroll
     for (int i = 0; i < 4; ++i) top_word = V::larger(top_word, vec[v].w[i]);
   const float top = fmaxf(V::value(top_word, 0), V::value(top_word, PER - 1));
-  const float nth = warp_nth(top, (P.take + WARPS - 1) / WARPS, lane), most = warp_nth(top, 1, lane);
+  // warps of which every lane has a vector; a chunk that does not fill one is small enough to be collected whole
+  const int full = min(WARPS, (last - first) / 32), each = full > 0 ? (P.take + full - 1) / full : 33;
+  const float most = warp_nth(top, 1, lane), nth = each <= 32 ? warp_nth(top, each, lane) : -INFINITY;
   if (lane == 0) { sh_nth[warp] = nth; sh_top[warp] = most; }
   __syncthreads();
   float thr = sh_nth[0], best = sh_top[0];
 #pragma unroll
-  for (int i = 1; i < WARPS; ++i) { thr = fminf(thr, sh_nth[i]); best = fmaxf(best, sh_top[i]); }
+  for (int i = 1; i < WARPS; ++i) {
+    if (i < full) thr = fminf(thr, sh_nth[i]);
+    best = fmaxf(best, sh_top[i]);
+  }
+  if (thr == -INFINITY && best > -INFINITY && P.take <= 32) {   // the same for the whole CTA
+    const float one = warp_nth(top, P.take, lane);
+    __syncthreads();
+    if (lane == 0) sh_nth[warp] = one;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) thr = fmaxf(thr, sh_nth[i]);
+  }
 
   // collect what reaches the threshold; the order of arrival does not matter, keys are ranked below.  The few words that hold
   // such a value are noted and read again.
@@ -204,11 +215,16 @@ __global__ void __launch_bounds__(THREADS, 4) beam_chunk_kernel(const __grid_con
   while (hits) {
     const int k = __ffs(hits) - 1, at = place(k >> 2) + (k & 3) * PER;
     hits &= hits - 1;
+    uint32_t word = 0;
+    if constexpr (VPT <= 2) {        // the others are read again: choosing among 16 registers costs more
+#pragma unroll
+      for (int i = 0; i < 4 * VPT; ++i) word = i == k ? vec[i / 4].w[i % 4] : word;
+    }
     if (first + (k >> 2) * THREADS + tid < last) {
 #pragma unroll
       for (int e = 0; e < PER; ++e)
         if (at + e >= 0 && at + e < P.vocab) {
-          float x = widen(logits[at + e]);
+          float x = VPT <= 2 ? V::value(word, e) : widen(logits[at + e]);
           x = x < INFINITY ? x : -INFINITY;
           if (x >= thr) {
             const int slot = atomicAdd(&count, 1);
@@ -241,8 +257,8 @@ __global__ void __launch_bounds__(THREADS, 4) beam_chunk_kernel(const __grid_con
     P.stats[entry] = make_float2(best, s);
   }
   if (n <= CAP) {
-    for (int i = tid; i < n; i += THREADS) {
-      const uint64_t mine = list[i];
+    if (tid < n) {
+      const uint64_t mine = list[tid];
       int rank = 0;
 #pragma unroll 4
       for (int j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
@@ -277,42 +293,52 @@ __global__ void __launch_bounds__(THREADS, 4) beam_chunk_kernel(const __grid_con
   }
 }
 
-// A continuation as it is ranked: value, then the place beam * vocab + token.
+// A continuation as it is ranked: value (larger key: larger value; whole numbers compare faster than binary64 ones), then the
+// place beam * vocab + token.
 struct Candidate {
-  double value;
+  uint64_t key;
   int place;        // below 2^31: at most 32 beams of 2^26 tokens
 };
 __device__ __forceinline__ bool better(const Candidate& a, const Candidate& b) {
-  return a.value > b.value || (a.value == b.value && a.place < b.place);
+  return (a.key > b.key) | ((a.key == b.key) & (a.place < b.place));   // no branches: this is the inner loop of a ranking
+}
+__device__ __forceinline__ uint64_t ordered(double v) {
+  const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);
+  return b >> 63 ? ~b : b | 0x8000000000000000ull;
+}
+__device__ __forceinline__ double unordered(uint64_t k) {
+  return __longlong_as_double((long long)(k >> 63 ? k & 0x7fffffffffffffffull : ~k));
 }
 
-// The entries of the lists are dealt to the threads; those a thread can hold in registers (all of them, in ordinary searches) are
-// requested before anything else and read once.
+// The first entries of all lists, as many as the threads hold in registers, are requested before anything else.  They are dealt
+// to the threads position by position and beam by beam in turn, so that the best ones lie in different threads.  What lies
+// further down a list is read only where the list is still above the threshold there.
 __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_constant__ BeamParams P) {
-  constexpr int MCAP = 1024, HELD = 8;
+  constexpr int MCAP = 1024, HELD = 8, RANKED = 384, FEW = 96;
   __shared__ double base[BEAM_MAX];          // score - log of the sum of exponentials; -inf: no continuation counts
   __shared__ int kind[BEAM_MAX];             // 0: lists of the chunks, 1: at its end, 2: nothing left
-  constexpr int GROUPS = THREADS / 4;
-  static_assert(GROUPS >= BEAM_TAKE_MAX, "the threshold needs `take` maxima");
-  __shared__ __align__(16) float sh_max[GROUPS];
+  __shared__ __align__(16) float sh_max[THREADS];
   __shared__ unsigned int least;
   __shared__ Candidate cand[MCAP];
   __shared__ int count;
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int n_lists = P.beams * P.chunks, entries = n_lists * P.take;
-  const uint2* lists = P.lists + (int64_t)b * entries;
-  // entry e: number i = e / n_lists of list l = e % n_lists, so that the best entries of all lists lie in different threads
+  const int n_lists = P.beams * P.chunks;
+  const int depth = min(P.take, HELD * THREADS / n_lists);        // entries of a list that are held
+  const uint2* lists = P.lists + (int64_t)b * n_lists * P.take;
+  // held entry e: number i = e / n_lists of a list, the lists shifted by i beams
   auto locate = [&](int e, int& l, int& i) {
-    i = n_lists == 1 ? e : (e < HELD * THREADS ? (int)__umulhi((uint32_t)e, P.by_lists) : e / n_lists);   // exact: e n_lists < 2^32
-    l = e - i * n_lists;
+    i = n_lists == 1 ? e : (int)__umulhi((uint32_t)e, P.by_lists);            // exact: e n_lists < 2^32
+    const int shift = i * P.chunks;                                           // below e: chunks <= n_lists
+    l = e - i * n_lists + shift - (n_lists == 1 ? shift : (int)__umulhi((uint32_t)shift, P.by_lists) * n_lists);
+    if (l >= n_lists) l -= n_lists;
   };
-  if (tid == 0) count = 0;
+  if (tid == 0) { count = 0; least = ~0u; }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   uint2 held[HELD];
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     held[i] = make_uint2(0u, 0xffffffffu);
-    if (tid + i * THREADS < entries) {
+    if (tid + i * THREADS < depth * n_lists) {
       int l, k;
       locate(tid + i * THREADS, l, k);
       held[i] = __ldcg(lists + l * P.take + k);
@@ -347,79 +373,93 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
   }
   __syncthreads();
 
-  // ---- entries as continuations.  A beam without a live continuation offers its first tokens, all at -inf, in place of its first
-  //      list; one at its end the padding token at its score, then the other tokens at -inf.  A place of -1: the list has ended.
-  auto candidate = [&](int e, const uint2& raw) {
-    int l, i;
-    locate(e, l, i);
+  // ---- entry i of list l as a continuation.  A beam without a live continuation offers its first tokens, all at -inf, in place of its
+  //      first list; one at its end the padding token at its score, then the other tokens at -inf.  A place of -1: the list has ended.
+  auto candidate = [&](int l, int i, const uint2& raw) {
     const int w = P.chunks == 1 ? l : (int)__umulhi((uint32_t)l, P.by_chunks);      // l / chunks, exact: l chunks < 2^32
     Candidate c;
     int token = (int)raw.y;
-    c.value = base[w] + (double)__uint_as_float(raw.x);
+    double value = base[w] + (double)__uint_as_float(raw.x);
     if (kind[w] != 0) {
       const bool done = kind[w] == 1;
       token = l != w * P.chunks || i >= P.vocab ? -1 : (!done ? i : (i == 0 ? P.pad : (i - 1 < P.pad ? i - 1 : i)));
-      c.value = done && i == 0 ? base[w] : -INFINITY;
+      value = done && i == 0 ? base[w] : -INFINITY;
     }
+    c.key = token < 0 ? 0 : ordered(value);             // below every real one
     c.place = token < 0 ? -1 : w * P.vocab + token;
     return c;
   };
   Candidate mine[HELD];
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
-    mine[i].value = -INFINITY;
+    mine[i].key = 0;
     mine[i].place = -1;
-    if (tid + i * THREADS < entries) mine[i] = candidate(tid + i * THREADS, held[i]);
+    if (tid + i * THREADS < depth * n_lists) {
+      int l, k;
+      locate(tid + i * THREADS, l, k);
+      mine[i] = candidate(l, k, held[i]);
+    }
   }
-  auto each = [&](auto&& use) {     // use(continuation) for every one of this thread
+  // use(continuation) for every one of this thread whose key reaches `from`
+  auto each = [&](uint64_t from, auto&& use) {
 #pragma unroll
     for (int i = 0; i < HELD; ++i)
-      if (mine[i].place >= 0) use(mine[i]);
-    for (int e = tid + HELD * THREADS; e < entries; e += THREADS) {
-      int l, i;
-      locate(e, l, i);
-      const Candidate c = candidate(e, __ldcg(lists + l * P.take + i));
-      if (c.place >= 0) use(c);
-    }
+      if (mine[i].place >= 0 && mine[i].key >= from) use(mine[i]);
+    if (depth < P.take)
+      for (int l = tid; l < n_lists; l += THREADS)
+        for (int i = depth; i < P.take; ++i) {          // lists descend
+          const Candidate c = candidate(l, i, __ldcg(lists + (int64_t)l * P.take + i));
+          if (c.place < 0 || c.key < from) break;
+          use(c);
+        }
   };
 
-  // ---- a value that at least `take` continuations reach: the take-th of the maxima of groups of four threads, in binary32; what
-  //      rounding may have taken off it is granted.  With fewer entries than threads all of them are ranked.
-  double thr = -INFINITY;
-  if (entries > THREADS) {
-    float top = -INFINITY;
-    each([&](const Candidate& c) { top = fmaxf(top, (float)c.value); });
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    if ((tid & 3) == 0) sh_max[tid / 4] = top;
-    if (tid == 0) least = ~0u;
+  // ---- a value that at least `take` continuations reach: the take-th of the threads' maxima, in binary32; what rounding may
+  //      have taken off it is granted.  With few entries all of them are ranked.
+  uint64_t thr = 0;
+  if (n_lists * P.take > FEW) {
+    uint64_t most = ordered((double)-INFINITY);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) most = mine[i].key > most ? mine[i].key : most;
+    if (depth == 0)                                     // more lists than can be held: their heads
+      for (int l = tid; l < n_lists; l += THREADS) {
+        const Candidate c = candidate(l, 0, __ldcg(lists + (int64_t)l * P.take));
+        if (c.place >= 0 && c.key > most) most = c.key;
+      }
+    float top = (float)unordered(most);
+    // a sixteenth of the maxima is asked for at most: those of four threads together will do
+    const int group = P.take <= 16 ? 4 : 1;
+    if (group == 4) {
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    }
+    const bool mark = (tid & (group - 1)) == 0;
+    if (mark) sh_max[group == 4 ? tid >> 2 : tid] = top;
     __syncthreads();
     int above = 0;
-#pragma unroll
-    for (int i = 0; i < GROUPS; i += 4) {
+#pragma unroll 16
+    for (int i = 0; i < THREADS / group; i += 4) {
       const float4 v = *reinterpret_cast<const float4*>(sh_max + i);
       above += (v.x > top) + (v.y > top) + (v.z > top) + (v.w > top);
     }
-    if ((tid & 3) == 0 && above < P.take) atomicMin(&least, ordered(top));   // the smallest value with fewer than `take` above it
+    if (mark && above < P.take) atomicMin(&least, ordered(top));   // the smallest value with fewer than `take` above it
     __syncthreads();
     const double t = (double)unordered(least);
-    thr = t - 1e-6 * fabs(t);      // -inf stays -inf
+    thr = ordered(t - 1e-6 * fabs(t));      // -inf stays -inf
   }
-  each([&](const Candidate& c) {
-    if (!(c.value < thr)) {          // a threshold of -inf lets everything through
-      const int slot = atomicAdd(&count, 1);
-      if (slot < MCAP) cand[slot] = c;
-    }
+  each(thr, [&](const Candidate& c) {
+    const int slot = atomicAdd(&count, 1);
+    if (slot < MCAP) cand[slot] = c;
   });
   __syncthreads();
   const int n = count;
   auto put = [&](int rank, const Candidate& c) {
     const int64_t at = (int64_t)b * P.take + rank;
-    P.out_scores[at] = (float)c.value;
+    P.out_scores[at] = (float)unordered(c.key);
     P.out_parent[at] = c.place / P.vocab;
     P.out_token[at] = c.place % P.vocab;
   };
-  if (n <= MCAP) {
+  if (n <= RANKED) {
     for (int i = tid; i < n; i += THREADS) {
       const Candidate one = cand[i];
       int rank = 0;
@@ -429,22 +469,26 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
     }
     return;
   }
-  // many equal values: one continuation per round, the best one behind the last
+  // many equal values: one continuation per round, the best one behind the last, of those collected if they all were
   __shared__ Candidate sh_best[WARPS];
   Candidate last;
-  last.value = INFINITY;
+  last.key = ~0ull;
   last.place = -1;
   for (int r = 0; r < P.take; ++r) {
     Candidate next;
-    next.value = -INFINITY;
+    next.key = 0;
     next.place = INT32_MAX;
-    each([&](const Candidate& c) {
+    auto look = [&](const Candidate& c) {
       if (better(last, c) && better(c, next)) next = c;
-    });
+    };
+    if (n <= MCAP)
+      for (int i = tid; i < n; i += THREADS) look(cand[i]);
+    else
+      each(0, look);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       Candidate other;
-      other.value = __shfl_xor_sync(0xffffffffu, next.value, o);
+      other.key = __shfl_xor_sync(0xffffffffu, next.key, o);
       other.place = __shfl_xor_sync(0xffffffffu, next.place, o);
       if (better(other, next)) next = other;
     }
@@ -525,7 +569,7 @@ void beam_plan(int64_t rows, int vocab, int* chunks, bool* wide) {
   // first vector may begin before it
   const int64_t span = (int64_t)vocab + 7;
   const int64_t big = (span + THREADS * 32 - 1) / (THREADS * 32);
-  *wide = rows * big >= 148;
+  *wide = rows * big >= 148 && span > THREADS * 8;
   *chunks = (int)(*wide ? big : (span + THREADS * 8 - 1) / (THREADS * 8));
 }
 

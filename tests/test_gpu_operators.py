@@ -484,6 +484,11 @@ def test_beam_select_finished_beams(as_bool):
     scores[2, 2] = -float("inf")
     for take, pad in ((8, 0), (8, 7000), (20, 3)):
         _check_beams(logits, scores, take, finished=finished.bool() if as_bool else finished, pad=pad)
+    # most beams at their end, a few continuations left: nothing but them and the padding counts
+    many = torch.ones(6, 16, device=DEV, dtype=torch.uint8)
+    many[:, 3], many[0, 11] = 0, 0
+    for V, take in ((6213, 32), (6213, 9), (90, 64), (20000, 17)):
+        _check_beams(_randn(V, 6, 16, V).half(), -3 * torch.rand(6, 16, device=DEV, generator=_gen(V)), take, finished=many, pad=V - 1)
     short = _randn(10, 1, 2, 3)
     for pad in range(3):
         _check_beams(short, torch.zeros(1, 2, device=DEV), 6, finished=torch.tensor([[1, 0]], dtype=torch.uint8, device=DEV), pad=pad)
