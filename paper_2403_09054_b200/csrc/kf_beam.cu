@@ -134,7 +134,7 @@ struct Vec {
 
 // VPT 16-byte vectors per thread.
 template <class T, int VPT>
-__global__ void __launch_bounds__(THREADS, 4) beam_chunk_kernel(const __grid_constant__ BeamParams P) {
+__global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 4 : 5) beam_chunk_kernel(const __grid_constant__ BeamParams P) {
   using V = Vec<T>;
   constexpr int EPV = V::N, PER = V::PER;
   __shared__ float sh_nth[WARPS], sh_top[WARPS], sh_sum[WARPS];
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(THREADS, 4) beam_chunk_kernel(const __grid_con
   }
 
   // collect what reaches the threshold; the order of arrival does not matter, keys are ranked below.  The few words that hold
-  // such a value are noted and read again.
+  // such a value are noted first.
   uint32_t hits = 0;
   if (top >= thr) {
     const uint32_t thr_word = V::splat(thr);
@@ -216,16 +216,13 @@ __global__ void __launch_bounds__(THREADS, 4) beam_chunk_kernel(const __grid_con
     const int k = __ffs(hits) - 1, at = place(k >> 2) + (k & 3) * PER;
     hits &= hits - 1;
     uint32_t word = 0;
-    if constexpr (VPT <= 2) {        // the others are read again: choosing among 16 registers costs more
 #pragma unroll
-      for (int i = 0; i < 4 * VPT; ++i) word = i == k ? vec[i / 4].w[i % 4] : word;
-    }
+    for (int i = 0; i < 4 * VPT; ++i) word = i == k ? vec[i / 4].w[i % 4] : word;
     if (first + (k >> 2) * THREADS + tid < last) {
 #pragma unroll
       for (int e = 0; e < PER; ++e)
         if (at + e >= 0 && at + e < P.vocab) {
-          float x = VPT <= 2 ? V::value(word, e) : widen(logits[at + e]);
-          x = x < INFINITY ? x : -INFINITY;
+          const float x = V::value(word, e);
           if (x >= thr) {
             const int slot = atomicAdd(&count, 1);
             if (slot < CAP) list[slot] = key_of(x, (uint32_t)(at + e));
@@ -267,21 +264,19 @@ __global__ void __launch_bounds__(THREADS, 4) beam_chunk_kernel(const __grid_con
     for (int i = n + tid; i < P.take; i += THREADS) out[i] = make_uint2(0u, 0xffffffffu);   // fewer elements than asked for
     return;
   }
-  // many equal values: one element per round, the best key below the last one
+  // many equal values: one element per round, the best key below the last one (read from memory again: this is rare, and what it
+  // would hold costs the common path registers)
   __shared__ uint64_t sh_key[WARPS];
   uint64_t prev = ~0ull;
+  const int from = max(0, first * EPV - lead), to = min(P.vocab, last * EPV - lead);
   for (int r = 0; r < P.take; ++r) {
     uint64_t mine = 0;
-#pragma unroll
-    for (int v = 0; v < VPT; ++v)
-#pragma unroll
-      for (int e = 0; e < EPV; ++e) {
-        const int idx = place(v) + e;
-        if (first + v * THREADS + tid < last && idx >= 0 && idx < P.vocab) {
-          const uint64_t key = key_of(V::value(vec[v].w[e / PER], e % PER), (uint32_t)idx);
-          if (key < prev && key > mine) mine = key;
-        }
-      }
+    for (int idx = from + tid; idx < to; idx += THREADS) {
+      float x = widen(logits[idx]);
+      x = x < INFINITY ? x : -INFINITY;
+      const uint64_t key = key_of(x, (uint32_t)idx);
+      if (key < prev && key > mine) mine = key;
+    }
     mine = warp_best(mine);
     if (lane == 0) sh_key[warp] = mine;
     __syncthreads();
@@ -333,7 +328,18 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
     if (l >= n_lists) l -= n_lists;
   };
   if (tid == 0) { count = 0; least = ~0u; }
+  // the caller's tensors do not depend on the chunks
+  float score = 0.f;
+  bool done = false;
+  auto ask = [&](int w) {
+    const int64_t row = (int64_t)b * P.beams + w;
+    score = P.scores[row];
+    done = P.finished && P.finished[row];
+  };
+  if (warp < P.beams) ask(warp);
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  float2 first_stat = make_float2(-INFINITY, 0.f);
+  if (warp < P.beams && lane < P.chunks && !done) first_stat = __ldcg(&P.stats[((int64_t)b * P.beams + warp) * P.chunks + lane]);
   uint2 held[HELD];
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
@@ -348,12 +354,11 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
   // ---- the beams' normalisers: one warp per beam
   for (int w = warp; w < P.beams; w += WARPS) {
     const int64_t row = (int64_t)b * P.beams + w;
-    const float score = P.scores[row];
-    const bool done = P.finished && P.finished[row];
+    if (w != warp) ask(w);
     float m = -INFINITY, sum = 0.f;
     if (!done) {
       for (int c = lane; c < P.chunks; c += 32) {
-        const float2 st = __ldcg(&P.stats[row * P.chunks + c]);
+        const float2 st = w == warp && c == lane ? first_stat : __ldcg(&P.stats[row * P.chunks + c]);
         if (st.x > m) {
           sum = fmaf(sum, fast_exp2((m - st.x) * LOG2E), st.y);
           m = st.x;
