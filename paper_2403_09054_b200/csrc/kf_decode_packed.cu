@@ -130,7 +130,7 @@ __device__ __forceinline__ void shared_words(uint32_t (&w)[N], const unsigned ch
 
 // CTAs an SM holds: the register limit that goes with them.
 template <int D, int G>
-constexpr int resident_ctas() { return D == 256 ? 2 : (G == 8 ? 3 : (G == 1 ? 4 : 4)); }
+constexpr int resident_ctas() { return D == 256 ? 2 : (G == 8 ? 3 : 4); }
 
 // GUMBEL: the method's own adjustment, alone in its kernel (up to sixteen places draw noise, and the instructions of all the
 // alternatives together would not stay in the instruction cache).
@@ -146,6 +146,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
   __shared__ __align__(8) __half sh_p[NW][G][SPAN];         // output weights, binary16 operands of the second product
   __shared__ uint64_t bars_all[NW][2];
   __shared__ float sh_slope[G];
+  __shared__ uint4 sh_q[D / 32][32];                        // queries, as every lane of a warp wants them
 
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -178,6 +179,12 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     mbar_init(bars + 1, 1);
     mbar_fence_init();
   }
+  // queries as the second operand of S: column = head r8, the features this lane's K words bring, pairs (i, i + 4)
+  for (int w = warp; w < D / 32; w += NW) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r8 < G) v = *reinterpret_cast<const uint4*>(P.q + ((size_t)u * G + r8) * D + t4 * (D / 4) + 8 * w);
+    sh_q[w][lane] = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+  }
   if (tid < G) sh_slope[tid] = P.slopes ? P.slopes[h0 + tid] : 0.f;
   __syncthreads();
   issue(0, 0);
@@ -185,18 +192,6 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
   int pos_next[2];
 #pragma unroll
   for (int sub = 0; sub < 2; ++sub) pos_next[sub] = first + sub * TILE + lane < row_end ? pos_u[first + sub * TILE + lane] : 0;
-
-  // queries as the second operand of S: column = head r8, the features this lane's K words bring, pairs (i, i + 4)
-  uint32_t qf[D / 32][4];
-#pragma unroll
-  for (int w = 0; w < D / 32; ++w) {
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (r8 < G) v = *reinterpret_cast<const uint4*>(P.q + ((size_t)u * G + r8) * D + t4 * (D / 4) + 8 * w);
-    qf[w][0] = __byte_perm(v.x, v.z, 0x5410);
-    qf[w][1] = __byte_perm(v.x, v.z, 0x7632);
-    qf[w][2] = __byte_perm(v.y, v.w, 0x5410);
-    qf[w][3] = __byte_perm(v.y, v.w, 0x7632);
-  }
 
   float m_x[G], m_y[G], l_y[G];            // m_*: common to the warp; l_y: this lane's slots
 #pragma unroll
@@ -264,8 +259,9 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
 #pragma unroll
             for (int e = 0; e < 4; ++e) a[i][e] = __hfma2(a[i][e], __low2half2(g), __high2half2(g));
           }
-          mma_16816(c, h2_bits(a[0][0]), h2_bits(a[1][0]), h2_bits(a[0][1]), h2_bits(a[1][1]), qf[w][0], qf[w][1]);
-          mma_16816(c, h2_bits(a[0][2]), h2_bits(a[1][2]), h2_bits(a[0][3]), h2_bits(a[1][3]), qf[w][2], qf[w][3]);
+          const uint4 qf = sh_q[w][lane];
+          mma_16816(c, h2_bits(a[0][0]), h2_bits(a[1][0]), h2_bits(a[0][1]), h2_bits(a[1][1]), qf.x, qf.y);
+          mma_16816(c, h2_bits(a[0][2]), h2_bits(a[1][2]), h2_bits(a[0][3]), h2_bits(a[1][3]), qf.z, qf.w);
         }
         const int at = sub * TILE + 16 * h + k_row;
         if (2 * t4 < G) { sh_x[warp][2 * t4][at] = c[0]; sh_x[warp][2 * t4][at + 8] = c[2]; }
