@@ -363,7 +363,8 @@ typedef struct kf_packed_step {
  *   d_row_opt   : DEVICE fp16 [B][Hkv][2][d] or NULL; the new K and V row as the values their codes stand for
  *   d_scratch   : DEVICE, kf_packed_scratch_bytes(args) bytes, 256-byte aligned (KF_ENOSPC if `scratch_bytes` is less)
  * d_cache, d_q, d_knew, d_vnew, d_out must be 16-byte aligned.  A unit whose d_len entry is outside 0..k is skipped:
- * nothing of it is read or written.  A non-finite value in a cached row makes the output of its unit NaN. */
+ * nothing of it is read or written.  Scores in d_acc are not negative (sums of softmax values).  A non-finite value in a
+ * cached row makes the output of its unit NaN. */
 size_t kf_packed_scratch_bytes(const kf_packed_step* args);   /* 0 if the arguments are invalid */
 int kf_decode_step_packed(const kf_packed_step* args, void* d_cache, int32_t* d_pos, float* d_acc, int32_t* d_len,
                           const void* d_q, const void* d_knew, const void* d_vnew, void* d_out, float* d_score_opt,

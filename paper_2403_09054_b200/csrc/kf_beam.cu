@@ -233,11 +233,11 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 4 : 5) beam_chunk_ke
   // sum of exponentials against the chunk's maximum
   float sum = 0.f;
   if (best > -INFINITY) {
-    const float off = best * LOG2E;
+    // the difference first: masks of the type's lowest value times log2(e) would overflow
 #pragma unroll
     for (int v = 0; v < VPT; ++v)
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) sum += fast_exp2(fmaf(V::value(vec[v].w[e / PER], e % PER), LOG2E, -off));
+      for (int e = 0; e < EPV; ++e) sum += fast_exp2((V::value(vec[v].w[e / PER], e % PER) - best) * LOG2E);
   }
   sum = warp_sum(sum);
   if (lane == 0) sh_sum[warp] = sum;
@@ -310,7 +310,8 @@ __device__ __forceinline__ double unordered(uint64_t k) {
 // further down a list is read only where the list is still above the threshold there.
 __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_constant__ BeamParams P) {
   constexpr int MCAP = 1024, HELD = 8, RANKED = 384, FEW = 96;
-  __shared__ double base[BEAM_MAX];          // score - log of the sum of exponentials; -inf: no continuation counts
+  __shared__ double base[BEAM_MAX];          // score - log of the sum of exponentials against the largest logit
+  __shared__ float largest[BEAM_MAX];        // that logit, taken off each logit by itself: it may be the type's lowest value
   __shared__ int kind[BEAM_MAX];             // 0: lists of the chunks, 1: at its end, 2: nothing left
   __shared__ __align__(16) float sh_max[THREADS];
   __shared__ unsigned int least;
@@ -373,7 +374,8 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
     if (lane == 0) {
       const bool live = isfinite(score) && (done || m > -INFINITY);
       kind[w] = live ? (done ? 1 : 0) : 2;
-      base[w] = live ? (done ? (double)score : (double)score - ((double)m + (double)logf(sum))) : -INFINITY;
+      base[w] = live ? (done ? (double)score : (double)score - (double)logf(sum)) : -INFINITY;
+      largest[w] = m;
     }
   }
   __syncthreads();
@@ -384,7 +386,7 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
     const int w = P.chunks == 1 ? l : (int)__umulhi((uint32_t)l, P.by_chunks);      // l / chunks, exact: l chunks < 2^32
     Candidate c;
     int token = (int)raw.y;
-    double value = base[w] + (double)__uint_as_float(raw.x);
+    double value = base[w] + ((double)__uint_as_float(raw.x) - (double)largest[w]);
     if (kind[w] != 0) {
       const bool done = kind[w] == 1;
       token = l != w * P.chunks || i >= P.vocab ? -1 : (!done ? i : (i == 0 ? P.pad : (i - 1 < P.pad ? i - 1 : i)));

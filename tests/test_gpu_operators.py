@@ -81,6 +81,17 @@ def test_pack_with_every_scale():
     assert np.array_equal(got[..., 128:].view(np.float16), want[..., 128:].view(np.float16))
 
 
+def test_pack_many_units_of_one_row():
+    """More units than a grid dimension holds."""
+    K, V = _randn(1, 70001, 1, 64).half(), _randn(2, 70001, 1, 64).half()
+    cache = torch.zeros(70001, 1, 80, dtype=torch.uint8, device=DEV)
+    kf.kf_pack_cache(K=K, V=V, cache=cache)
+    assert np.array_equal(cache.cpu().numpy()[..., :64], ref.slots_of(K.cpu().numpy(), V.cpu().numpy())[..., :64])
+    Kb, Vb = torch.zeros_like(K), torch.zeros_like(V)
+    kf.kf_unpack_cache(cache=cache, K=Kb, V=Vb)
+    assert np.array_equal(Kb.cpu().numpy(), ref.rows_of(cache.cpu().numpy(), 64)[0])
+
+
 def test_pack_leaves_rows_behind_the_entry_count():
     K, V = _randn(1, 2, 3, 9, 64).half(), _randn(2, 2, 3, 9, 64).half()
     length = torch.tensor([[0, 1, 9], [5, 12, -3]], dtype=torch.int32, device=DEV)      # counts outside 0..n: all rows, none
@@ -273,6 +284,36 @@ def test_packed_step_skips_units_with_damaged_counts():
         for now, old in zip((s.cache, s.pos, s.acc, s.length), before):
             assert torch.equal(now[u], old[u]) or (torch.isnan(old[u].float()).any())
     assert (out[0, 1] != 9.0).any() and slot[1] >= 0
+
+
+def test_packed_step_without_the_optional_outputs():
+    """What is returned beside it does not change the state: bit for bit the same with and without."""
+    a, b = (Packed(2, 4, 2, 128, 90, 20, lengths=[90, 40], seed=8) for _ in range(2))
+    q, kn, vn = a.inputs(1)
+    out = a.call(1, q, kn, vn)[0]
+    mine = torch.empty_like(q)
+    kf.kf_decode_step_packed(batch=2, n_heads=4, n_kv_heads=2, head_dim=128, budget_k=90, recent_w=20, layer=0, position=b.n, tau=ko.tau(b.P, 1), cache=b.cache,
+                             pos=b.pos, acc=b.acc, length=b.length, q=q, knew=kn, vnew=vn, out=mine, noise_seed=b.seed)
+    assert torch.equal(out, mine) and torch.equal(a.cache, b.cache) and torch.equal(a.pos, b.pos) and torch.equal(a.length, b.length)
+    assert torch.equal(torch.nan_to_num(a.acc), torch.nan_to_num(b.acc))
+
+
+def test_packed_steps_of_two_streams_at_once():
+    """Two layers' steps in flight on two streams, each with scratch of its own from torch's allocator."""
+    states = [Packed(4, 8, 8, 128, 700, 100, seed=40 + i) for i in range(2)]
+    want = [Packed(4, 8, 8, 128, 700, 100, seed=40 + i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    inputs = [[s.inputs(step) for step in range(1, 9)] for s in states]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for step in range(8):
+        for i in range(2):
+            outs[i].append(states[i].call(step + 1, *inputs[i][step], stream=streams[i])[0])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for step in range(8):
+            assert torch.equal(outs[i][step], want[i].call(step + 1, *inputs[i][step])[0])
+        assert torch.equal(states[i].cache, want[i].cache) and torch.equal(states[i].acc, want[i].acc)
 
 
 def test_packed_step_is_reproducible_and_holds_nothing_between_calls():
@@ -473,6 +514,25 @@ def test_beam_select_forbidden_tokens_and_dead_beams():
     first[:, 0] = 0
     _check_beams(_randn(6, 4, 4, 20000), first, 8)
     _check_beams(torch.full((1, 2, 30), float("nan"), device=DEV), torch.zeros(1, 2, device=DEV), 60)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+def test_beam_select_masks_of_the_lowest_value(dtype):
+    """Tokens masked with the type's lowest finite value are tokens all the same: a row of nothing else is uniform."""
+    low = torch.finfo(dtype).min
+    logits = (2 * _randn(11, 3, 4, 9001)).to(dtype)
+    logits[0, :, 100:] = low
+    logits[1, 2] = low
+    logits[2] = low
+    scores = torch.tensor([-1.0, -2.0, -0.5, -3.0], device=DEV).expand(3, 4).contiguous()
+    for take in (4, 20):
+        got, parent, token = _check_beams(logits, scores, take)
+        assert (parent[2] == 2).all() and (token[2] == np.arange(take)).all() and abs(got[2, 0] - (-0.5 - math.log(9001))) < 1e-5
+
+
+def test_beam_select_more_lists_than_are_held():
+    _check_beams((3 * _randn(13, 1, 32, 600011)).half(), -torch.rand(1, 32, device=DEV, generator=_gen(5)), 4)
+    _check_beams(torch.zeros(1, 32, 600011, device=DEV, dtype=torch.float16), torch.zeros(1, 32, device=DEV), 64)
 
 
 @pytest.mark.parametrize("as_bool", [True, False])
