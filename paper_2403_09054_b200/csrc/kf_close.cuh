@@ -274,7 +274,9 @@ __device__ void combine_and_evict(const PARAMS& P, int u, int len) {
 // worked on side by side instead of one after the other; 512 for a single head with a long cache and few units): warp n merges the split statistics of head n and leaves them in shared
 // memory; then every thread owns one (head, column) of the outputs and a few entries of the score update, all of whose
 // loads are issued together.
-template <int D, int NT, int G, class PARAMS>
+// BATCH: entries per thread and round.  EARLY: the adjusted logits of the first round are requested together with the
+// split statistics instead of after them (G * BATCH more registers).
+template <int D, int NT, int G, int BATCH = 4, bool EARLY = false, class PARAMS>
 __device__ void combine_and_evict_group(const PARAMS& P, int u, int len) {
   static_assert(NT >= 32 * G && NT >= D, "one warp per head for the statistics, one thread per column of the new row");
   __shared__ float sh_mx[G], sh_inv_lx[G], sh_my[G], sh_inv_ly[G], sh_xnew[G], sh_ynew[G];
@@ -293,7 +295,6 @@ __device__ void combine_and_evict_group(const PARAMS& P, int u, int len) {
   const float* __restrict__ ys = P.y_scratch + (size_t)u * G * (P.k + 1);   // [head][k + 1]
 
   // ---- independent of the streaming kernel
-  constexpr int BATCH = 4;
   float av[BATCH];
   int pv[BATCH];
 #pragma unroll
@@ -322,6 +323,17 @@ __device__ void combine_and_evict_group(const PARAMS& P, int u, int len) {
 
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the streaming kernel has finished; its writes are visible
 
+  float yv[G][BATCH];
+  auto load_y = [&](int j0) {
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) {
+        const int j = j0 + i * NT;
+        yv[g][i] = j < len ? __ldcg(ys + (size_t)g * (P.k + 1) + j) : 0.f;
+      }
+  };
+  if (EARLY) load_y(tid);
   if (warp < G) {
     const int g = warp;
     float4 ps0 = make_float4(-INFINITY, 0.f, -INFINITY, 0.f), ps1 = ps0;
@@ -369,14 +381,7 @@ __device__ void combine_and_evict_group(const PARAMS& P, int u, int len) {
         pv[i] = in ? pos[j] : 0x7fffffff;
       }
     }
-    float yv[G][BATCH];
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const int j = j0 + i * NT;
-        yv[g][i] = j < len ? __ldcg(ys + (size_t)g * (P.k + 1) + j) : 0.f;
-      }
+    if (!EARLY || j0 != tid) load_y(j0);
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
       const int j = j0 + i * NT;

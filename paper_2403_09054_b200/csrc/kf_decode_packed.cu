@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(512, 1) packed_close_wide_kernel(const __grid_
   const int u = blockIdx.x;
   const int len = P.len[u];
   if (len < 0 || len > P.k) return;
-  combine_and_evict_group<D, 512, 1>(P, u, len);
+  combine_and_evict_group<D, 512, 1, 8, true>(P, u, len);   // 4096 entries in one round
 }
 
 template <int D, int G>
@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(close_threads(D, G), G == 1 ? 6 : (G == 8 ? 1 
   const int len = P.len[u];
   if (len < 0 || len > P.k) return;
   if constexpr (G == 1) combine_and_evict<D, 128, 1>(P, u, len);
-  else combine_and_evict_group<D, close_threads(D, G), G>(P, u, len);
+  else combine_and_evict_group<D, close_threads(D, G), G, 4, true>(P, u, len);
 }
 
 template <int D, int G>
