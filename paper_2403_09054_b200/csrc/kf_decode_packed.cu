@@ -141,9 +141,13 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
   constexpr int SB = packed_slot_bytes(D);
   constexpr int TILE_BYTES = TILE * SB;
   extern __shared__ __align__(128) unsigned char dyn_smem[];
-  __shared__ float sh_m[NW][G], sh_l[NW][G], sh_my[NW][G], sh_ly[NW][G], sh_f[NW][G];
+  // An output weight goes into the second product as two binary16 numbers, itself rounded and what the rounding left out,
+  // so that only the output is rounded.  With up to four heads the two are columns of one instruction (col and col + G),
+  // with eight they follow one another into the same accumulators.
+  constexpr int COLS = G <= 4 ? 2 * G : G;
+  __shared__ float sh_m[NW][G], sh_l[NW][COLS], sh_my[NW][G], sh_ly[NW][G], sh_f[NW][G];
   __shared__ float sh_x[NW][G][SPAN];                       // logits of the warp's slots
-  __shared__ __align__(8) __half sh_p[NW][G][SPAN];         // output weights, binary16 operands of the second product
+  __shared__ __align__(8) __half sh_p[NW][2 * G][SPAN];     // output weights of the heads, then the remainders
   __shared__ uint64_t bars_all[NW][2];
   __shared__ float sh_slope[G];
   __shared__ uint4 sh_q[D / 32][32];                        // queries, as every lane of a warp wants them
@@ -197,7 +201,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
 #pragma unroll
   for (int g = 0; g < G; ++g) { m_x[g] = -INFINITY; m_y[g] = -INFINITY; l_y[g] = 0.f; }
   float l_x[4] = {0.f, 0.f, 0.f, 0.f};     // sums of the output weights, as the product of a row of ones: the columns of o
-  float o[D / 16][4];                      // out^T: features as rows, heads 2 t4 and 2 t4 + 1 as columns
+  float o[D / 16][4];                      // out^T: features as rows, columns 2 t4 and 2 t4 + 1
 #pragma unroll
   for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -301,7 +305,10 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
       for (int sub = 0; sub < 2; ++sub) {
         const bool valid = sub * TILE + lane < rows;
         ey += valid ? fast_exp2((y[sub] - my_new) * LOG2E) : 0.f;
-        sh_p[warp][g][sub * TILE + p_at] = __float2half_rn(valid ? fast_exp2((x[sub] - m_x[g]) * LOG2E) : 0.f);
+        const float px = valid ? fast_exp2((x[sub] - m_x[g]) * LOG2E) : 0.f;
+        const __half hi = __float2half_rn(px);
+        sh_p[warp][g][sub * TILE + p_at] = hi;
+        sh_p[warp][G + g][sub * TILE + p_at] = __float2half_rn(px - __half2float(hi));
       }
       l_y[g] = fmaf(l_y[g], fast_exp2((m_y[g] - my_new) * LOG2E), ey);
       m_y[g] = my_new;
@@ -310,8 +317,8 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
       float f0 = 1.f, f1 = 1.f;   // of this lane's two columns
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        if (g == 2 * t4) f0 = scale_o[g];
-        if (g == 2 * t4 + 1) f1 = scale_o[g];
+        if (2 * t4 < COLS && g == 2 * t4 % G) f0 = scale_o[g];
+        if (2 * t4 + 1 < COLS && g == (2 * t4 + 1) % G) f1 = scale_o[g];
       }
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) { o[i][0] *= f0; o[i][1] *= f1; o[i][2] *= f0; o[i][3] *= f1; }
@@ -328,10 +335,11 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         constexpr int W = D / 64;
-        uint2 pb = make_uint2(0, 0);   // weights of slots 16 h + t4 + 4 {0 .. 3} for head r8
-        if (r8 < G) pb = *reinterpret_cast<const uint2*>(&sh_p[warp][r8][sub * TILE + 16 * h + 4 * t4]);
-        // the weights that are used, rounded as they are, are the ones that are summed
+        uint2 pb = make_uint2(0, 0), rest = pb;   // weights of slots 16 h + t4 + 4 {0 .. 3} for column r8
+        if (r8 < COLS) pb = *reinterpret_cast<const uint2*>(&sh_p[warp][r8][sub * TILE + 16 * h + 4 * t4]);
+        if (G == 8) rest = *reinterpret_cast<const uint2*>(&sh_p[warp][G + r8 % G][sub * TILE + 16 * h + 4 * t4]);
         mma_16816(l_x, 0x3c003c00u, 0u, 0x3c003c00u, 0u, pb.x, pb.y);
+        if (G == 8) mma_16816(l_x, 0x3c003c00u, 0u, 0x3c003c00u, 0u, rest.x, rest.y);
         uint32_t vw[4][W], vg[4][1];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -355,8 +363,10 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
             for (int j = 0; j < 4; ++j) { lo[e][j] = __hfma2(lo[e][j], sc, mn); hi[e][j] = __hfma2(hi[e][j], sc, mn); }
           }
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 4; ++j) {
             mma_16816(o[4 * w + j], h2_bits(lo[0][j]), h2_bits(hi[0][j]), h2_bits(lo[1][j]), h2_bits(hi[1][j]), pb.x, pb.y);
+            if (G == 8) mma_16816(o[4 * w + j], h2_bits(lo[0][j]), h2_bits(hi[0][j]), h2_bits(lo[1][j]), h2_bits(hi[1][j]), rest.x, rest.y);
+          }
         }
       }
       __syncwarp();   // the buffer has been read by every lane
@@ -371,17 +381,17 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
   }
 
   // ---- merge the lanes, then the warps of this CTA; the sums lie in the buffers, which are done with
-  static_assert(G * D * 4 <= 2 * TILE_BYTES, "a warp's sums fit its buffers");
-  float* sums = reinterpret_cast<float*>(ring);              // [G][D]
+  static_assert(COLS * D * 4 <= 2 * TILE_BYTES, "a warp's sums fit its buffers");
+  float* sums = reinterpret_cast<float*>(ring);              // [COLS][D]
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     const int f = r8 * (D / 8) + (i >> 2) * 8 + (i & 3);
-    if (2 * t4 < G) { sums[2 * t4 * D + f] = o[i][0]; sums[2 * t4 * D + f + 4] = o[i][2]; }
-    if (2 * t4 + 1 < G) { sums[(2 * t4 + 1) * D + f] = o[i][1]; sums[(2 * t4 + 1) * D + f + 4] = o[i][3]; }
+    if (2 * t4 < COLS) { sums[2 * t4 * D + f] = o[i][0]; sums[2 * t4 * D + f + 4] = o[i][2]; }
+    if (2 * t4 + 1 < COLS) { sums[(2 * t4 + 1) * D + f] = o[i][1]; sums[(2 * t4 + 1) * D + f + 4] = o[i][3]; }
   }
   if (r8 == 0) {
-    if (2 * t4 < G) sh_l[warp][2 * t4] = l_x[0];
-    if (2 * t4 + 1 < G) sh_l[warp][2 * t4 + 1] = l_x[1];
+    if (2 * t4 < COLS) sh_l[warp][2 * t4] = l_x[0];
+    if (2 * t4 + 1 < COLS) sh_l[warp][2 * t4 + 1] = l_x[1];
   }
 #pragma unroll
   for (int g = 0; g < G; ++g) {
@@ -397,8 +407,9 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     for (int wi = 0; wi < NW; ++wi) { M = fmaxf(M, sh_m[wi][g]); MY = fmaxf(MY, sh_my[wi][g]); }
 #pragma unroll
     for (int wi = 0; wi < NW; ++wi) {
-      const float f = sh_l[wi][g] > 0.f ? fast_exp2((sh_m[wi][g] - M) * LOG2E) : 0.f;
-      L = fmaf(sh_l[wi][g], f, L);
+      const float l = sh_l[wi][g] + (COLS > G ? sh_l[wi][COLS - G + g] : 0.f);
+      const float f = l > 0.f ? fast_exp2((sh_m[wi][g] - M) * LOG2E) : 0.f;
+      L = fmaf(l, f, L);
       if (sh_ly[wi][g] > 0.f) LY = fmaf(sh_ly[wi][g], fast_exp2((sh_my[wi][g] - MY) * LOG2E), LY);
       sh_f[wi][g] = f;
     }
@@ -409,7 +420,10 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     const int g = idx / D, c = idx % D;
     float sum = 0.f;
 #pragma unroll
-    for (int wi = 0; wi < NW; ++wi) sum = fmaf(reinterpret_cast<const float*>(dyn_smem + (size_t)wi * 2 * TILE_BYTES)[idx], sh_f[wi][g], sum);
+    for (int wi = 0; wi < NW; ++wi) {
+      const float* of = reinterpret_cast<const float*>(dyn_smem + (size_t)wi * 2 * TILE_BYTES);
+      sum = fmaf(of[idx] + (COLS > G ? of[(COLS - G) * D + idx] : 0.f), sh_f[wi][g], sum);
+    }
     part[g * PSTRIDE + 4 + c] = sum;
   }
 }
@@ -448,7 +462,7 @@ cudaError_t launch_one(const PackedParams& P, int units, cudaStream_t stream) {
   cfg.numAttrs = 1;
   auto kern = P.noise_mode == 0 ? packed_stream_kernel<D, G, true> : packed_stream_kernel<D, G, false>;
   cudaError_t e = cudaSuccess;
-  if (cfg.dynamicSmemBytes > 32 * 1024) {   // with the static part (up to 13 KB) above what every kernel may have; asked for once per device
+  if (cfg.dynamicSmemBytes > 32 * 1024) {   // with the static part (up to 22 KB) above what every kernel may have; asked for once per device
     static std::atomic<uint64_t> asked{0};
     int dev = 0;
     e = cudaGetDevice(&dev);
