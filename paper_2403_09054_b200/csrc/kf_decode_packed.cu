@@ -41,7 +41,8 @@ __device__ __forceinline__ float ln_atanh(float x) {
   return fmaf((float)e, LN2, f - t * (f - r));
 }
 __device__ __forceinline__ float packed_gumbel(const PackedParams& P, uint32_t b, uint32_t lh, uint32_t i, uint32_t j) {
-  return -ln_atanh(-ln_atanh(uniform_from_word(noise_word(P.pk, b, lh, i, j))));
+  // the outer logarithm may be the fast one: its error is absolute, below 1e-6 even for the largest variates
+  return -LN2 * __log2f(-ln_atanh(uniform_from_word(noise_word(P.pk, b, lh, i, j))));
 }
 
 // ---- the new token's row, quantised by the closing CTA.  Warps hold 32 consecutive features at a time: one group.
