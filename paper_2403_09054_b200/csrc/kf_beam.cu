@@ -374,7 +374,11 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
     if (lane == 0) {
       const bool live = isfinite(score) && (done || m > -INFINITY);
       kind[w] = live ? (done ? 1 : 0) : 2;
-      base[w] = live ? (done ? (double)score : (double)score - (double)logf(sum)) : -INFINITY;
+      // log(sum) from its exponent, exactly, and the logarithm of a number near 1: binary32 alone would round a sum of thousands
+      // to half a millionth
+      const int e = (__float_as_int(sum) - 0x3f3504f3) >> 23;       // 0x3f3504f3: sqrt(1/2)
+      const double log_sum = (double)e * 0.69314718055994531 + (double)logf(__int_as_float(__float_as_int(sum) - (e << 23)));
+      base[w] = live ? (done ? (double)score : (double)score - log_sum) : -INFINITY;
       largest[w] = m;
     }
   }
