@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
       const unsigned char* buf = ring + sub * TILE_BYTES;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float c[4] = {0.f, 0.f, 0.f, 0.f};
+        float c[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};   // two chains: half the latency, and half the roundings
         constexpr int NG = D == 256 ? 2 : 1;      // groups a lane's features span
         uint32_t kw[2][D / 32], kg[2][NG];
 #pragma unroll
@@ -266,8 +266,10 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
           }
           const uint4 qf = sh_q[w][lane];
           mma_16816(c, h2_bits(a[0][0]), h2_bits(a[1][0]), h2_bits(a[0][1]), h2_bits(a[1][1]), qf.x, qf.y);
-          mma_16816(c, h2_bits(a[0][2]), h2_bits(a[1][2]), h2_bits(a[0][3]), h2_bits(a[1][3]), qf.z, qf.w);
+          mma_16816(c2, h2_bits(a[0][2]), h2_bits(a[1][2]), h2_bits(a[0][3]), h2_bits(a[1][3]), qf.z, qf.w);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] += c2[i];
         const int at = sub * TILE + 16 * h + k_row;
         if (2 * t4 < G) { sh_x[warp][2 * t4][at] = c[0]; sh_x[warp][2 * t4][at + 8] = c[2]; }
         if (2 * t4 + 1 < G) { sh_x[warp][2 * t4 + 1][at] = c[1]; sh_x[warp][2 * t4 + 1][at + 8] = c[3]; }
