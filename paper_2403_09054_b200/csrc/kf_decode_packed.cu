@@ -15,6 +15,12 @@
 // buffer that one bulk copy fills (a tile is contiguous), so that no register holds a row that is still on its way.  A
 // lane owns two slots in the per-logit work, whose chains (generator, logarithms, exponentials) then overlap, and the
 // bookkeeping of the running softmaxes is paid once for 64 slots.  A buffer is refilled as soon as its values have been used.
+//
+// What bounds it: issue.  1024 caches of 2048 slots (d 128, one head each; 361 MB): 85 us a call, of which 76 are the streaming kernel
+// (4.7 TB/s; 846 warp instructions per 32 slots, 480 of them conversions; issue slots 63 %) and 9 the closing one; the bytes alone
+// would take 56.  32 caches of 4096: 13 us.  256 caches of 2000 slots on average half full, four heads each: 37 us, each further
+// head adding its noise (90 instructions per 32 slots) and softmaxes.  Measured and not taken: tiles staged in registers (106), the
+// closing stage inside the streaming CTA with one CTA per cache (101), the heads as a loop (37.4, and 42 instead of 40 at d 256).
 #include "kf_close.cuh"
 #include "kf_packed.cuh"
 
@@ -129,7 +135,8 @@ __device__ __forceinline__ void shared_words(uint32_t (&w)[N], const unsigned ch
   }
 }
 
-// CTAs an SM holds: the register limit that goes with them.
+// CTAs an SM holds: the register limit that goes with them.  At d 128 and one head: 4 (111 registers) 85 us, 3 90, 5 (96 registers,
+// spilling) 102.  d 256 needs 80 KB of buffers a CTA, eight heads 150 registers.
 template <int D, int G>
 constexpr int resident_ctas() { return D == 256 ? 2 : (G == 8 ? 3 : 4); }
 
@@ -506,6 +513,8 @@ cudaError_t launch_dim(const PackedParams& P, int units, cudaStream_t stream) {
 void decode_packed_plan(int units, int budget_k, int head_dim, int* splits_out, int* tiles_per_split_out) {
   const int tiles = (budget_k + TILE - 1) / TILE;
   constexpr int ROUND = NW * SPAN / TILE;   // tiles of a round of the CTA's warps
+  // Many caches: about three waves of CTAs (two CTAs for each of 1024 caches; one each 86.7 us, two 86.6, three 90.3).  Few: as many
+  // CTAs as give every warp at least one round (32 caches of 4096: 16 CTAs each 13.7 us, 10 15.0, 8 17.3).
   const int target_ctas = units >= 148 ? 148 * 13 : 148 * 8;
   int splits = (target_ctas + units - 1) / units;
   splits = std::max(1, std::min(splits, std::min(MAX_SPLITS, (tiles + ROUND - 1) / ROUND)));

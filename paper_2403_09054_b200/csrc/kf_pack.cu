@@ -3,6 +3,10 @@
 //
 // A thread owns eight features (one 16-byte chunk) of the K row and of the V row of a slot, so that two loads are in
 // flight per thread and a group of 32 features is four neighbouring lanes: its extremes take two shuffles each.
+//
+// 1024 units of 2048 rows, d 128: unpack 210 us (6.7 TB/s, as fast as a copy), pack 325 us (4.3 TB/s): rounding 16 features to codes
+// takes about 250 instructions a thread (issue slots 87 %); 415 us with a division and a reciprocal per chunk and codes shifted into
+// place one by one.
 #include "kf_packed.cuh"
 
 namespace kf {

@@ -8,6 +8,10 @@
 // none.  The angles of a token are shared by all of its heads: a CTA takes up to four tokens and computes their angles
 // first, one per thread, into shared memory.  Positions reach far, so angle / 2 pi is formed and reduced in binary64; what
 // is left, at most half a turn, goes through binary32.
+//
+// 8 x 4096 tokens of 32 + 32 heads, d 128, whole heads turned (1.6 GB): 302 us = 5.3 TB/s, 0.83 of a copy; 32 tokens of 32 + 8 heads
+// 3.3 us.  What it took: angles in registers instead of shared memory for every row 908 -> 382, pairs within a lane (no
+// shuffles) 342, six rows requested ahead and streaming stores 302 (three 324, twelve 367: registers).
 #include <cuda_bf16.h>
 
 #include "kf_ops.cuh"
