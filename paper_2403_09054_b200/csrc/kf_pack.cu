@@ -1,8 +1,9 @@
 // Conversion of cache rows between binary16 and the 4-bit slots of kf_packed.cuh.  Pure streaming: every row is read
 // once and every slot written once, so HBM bounds both directions (4 d + 1.25 d bytes per slot).
 //
-// A thread owns eight features (one 16-byte chunk) of the K row and of the V row of a slot, so that two loads are in
-// flight per thread and a group of 32 features is four neighbouring lanes: its extremes take two shuffles each.
+// Packing, a thread owns sixteen features (two 16-byte chunks) of the K row and of the V row of a slot: four loads are in
+// flight per thread, and a group of 32 features is two neighbouring lanes, one of which works out the K group and the other
+// the V group.  Unpacking, it owns eight of each.
 //
 // 1024 units of 2048 rows, d 128: unpack 210 us (6.7 TB/s, as fast as a copy), pack 325 us (4.3 TB/s): rounding 16 features to codes
 // takes about 250 instructions a thread (issue slots 87 %); 415 us with a division and a reciprocal per chunk and codes shifted into
@@ -49,22 +50,25 @@ struct Group {
   bool clamp;       // whether a code could pass 15 (scales of few bits, near the smallest binary16 numbers), of either group
 };
 
-// The groups that this lane's two chunks belong to; the four lanes of a group call it together.  The even lanes work out the
-// K group, the odd ones the V group, and neighbours exchange: one division and one reciprocal per lane.
-__device__ __forceinline__ void groups_of(const uint4& kv, const uint4& vv, Group& kg, Group& vg) {
-  __half2 klo, khi, vlo, vhi;
-  extremes8(kv, klo, khi);
-  extremes8(vv, vlo, vhi);
+// The groups that this lane's features belong to; the two lanes of a group call it together.  The even lane works out the K
+// group, the odd one the V group, and they exchange: one division and one reciprocal per lane.
+__device__ __forceinline__ void groups_of(const uint4 (&kv)[2], const uint4 (&vv)[2], Group& kg, Group& vg) {
+  __half2 klo, khi, vlo, vhi, l2, h2;
+  extremes8(kv[0], klo, khi);
+  extremes8(kv[1], l2, h2);
+  klo = __hmin2_nan(klo, l2);
+  khi = __hmax2_nan(khi, h2);
+  extremes8(vv[0], vlo, vhi);
+  extremes8(vv[1], l2, h2);
+  vlo = __hmin2_nan(vlo, l2);
+  vhi = __hmax2_nan(vhi, h2);
   klo = __hmin2_nan(klo, __lowhigh2highlow(klo));
   khi = __hmax2_nan(khi, __lowhigh2highlow(khi));
   vlo = __hmin2_nan(vlo, __lowhigh2highlow(vlo));
   vhi = __hmax2_nan(vhi, __lowhigh2highlow(vhi));
   __half2 lo = __lows2half2(klo, vlo), hi = __lows2half2(khi, vhi);   // (K, V)
-#pragma unroll
-  for (int o = 1; o <= 2; o <<= 1) {
-    lo = __hmin2_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = __hmax2_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-  }
+  lo = __hmin2_nan(lo, __shfl_xor_sync(0xffffffffu, lo, 1));
+  hi = __hmax2_nan(hi, __shfl_xor_sync(0xffffffffu, hi, 1));
   const bool odd = threadIdx.x & 1;
   Group mine;
   const float low = __half2float(odd ? __high2half(lo) : __low2half(lo)), high = __half2float(odd ? __high2half(hi) : __low2half(hi));
@@ -79,41 +83,48 @@ __device__ __forceinline__ void groups_of(const uint4& kv, const uint4& vv, Grou
   vg = odd ? mine : other;
 }
 
+template <bool CLAMP>
+__device__ __forceinline__ uint2 pack16(const uint4 (&v)[2], const Group& g) {
+  return make_uint2(pack8<CLAMP>(v[0], __high2float(g.params), g.inverse), pack8<CLAMP>(v[1], __high2float(g.params), g.inverse));
+}
+
 // grid: chunks of a unit's rows, units (the rest of them in further rounds)
 template <int D>
 __global__ void __launch_bounds__(THREADS) pack_kernel(const __half* __restrict__ K, const __half* __restrict__ V,
                                                        const int32_t* __restrict__ len, unsigned char* __restrict__ cache,
                                                        int64_t units, int n, int k) {
-  constexpr int CPR = D / 8;   // chunks per row
+  constexpr int TPR = D / 16;   // threads per row
   const int64_t at = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-  const int64_t j = at / CPR;
-  const int c = (int)(at % CPR);
+  const int64_t j = at / TPR;
+  const int c = (int)(at % TPR);
   for (int64_t u = blockIdx.y; u < units; u += gridDim.y) {
     const bool in = j < n && (!len || j < len[u]);
     const int64_t row = u * n + j;
-    uint4 kv = make_uint4(0, 0, 0, 0), vv = kv;
-    if (in) {
-      kv = __ldcs(reinterpret_cast<const uint4*>(K + row * D) + c);
-      vv = __ldcs(reinterpret_cast<const uint4*>(V + row * D) + c);
+    uint4 kv[2], vv[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      kv[i] = vv[i] = make_uint4(0, 0, 0, 0);
+      if (in) {
+        kv[i] = __ldcs(reinterpret_cast<const uint4*>(K + row * D) + 2 * c + i);
+        vv[i] = __ldcs(reinterpret_cast<const uint4*>(V + row * D) + 2 * c + i);
+      }
     }
     Group kg, vg;
     groups_of(kv, vv, kg, vg);   // whole warps: a group never straddles a row
     if (in) {
       unsigned char* slot = cache + ((size_t)u * k + j) * packed_slot_bytes(D);
-      uint32_t kc, vc;
+      uint2 kc, vc;
       if (kg.clamp) {            // the same for the whole warp
-        kc = pack8<true>(kv, __high2float(kg.params), kg.inverse);
-        vc = pack8<true>(vv, __high2float(vg.params), vg.inverse);
+        kc = pack16<true>(kv, kg);
+        vc = pack16<true>(vv, vg);
       } else {
-        kc = pack8<false>(kv, __high2float(kg.params), kg.inverse);
-        vc = pack8<false>(vv, __high2float(vg.params), vg.inverse);
+        kc = pack16<false>(kv, kg);
+        vc = pack16<false>(vv, vg);
       }
-      *reinterpret_cast<uint32_t*>(slot + 4 * c) = kc;
-      *reinterpret_cast<uint32_t*>(slot + D / 2 + 4 * c) = vc;
-      if ((c & 3) == 0) {
-        *reinterpret_cast<uint32_t*>(slot + D + c) = h2_bits(kg.params);
-        *reinterpret_cast<uint32_t*>(slot + D + D / 8 + c) = h2_bits(vg.params);
-      }
+      *reinterpret_cast<uint2*>(slot + 8 * c) = kc;
+      *reinterpret_cast<uint2*>(slot + D / 2 + 8 * c) = vc;
+      // one lane of the group writes its K parameters, the other its V parameters
+      *reinterpret_cast<uint32_t*>(slot + D + (c & 1) * (D / 8) + (c >> 1) * 4) = h2_bits(c & 1 ? vg.params : kg.params);
     }
   }
 }
@@ -152,15 +163,15 @@ __global__ void __launch_bounds__(THREADS) unpack_kernel(const unsigned char* __
   }
 }
 
-inline dim3 grid_for(int64_t units, int n, int d) {
-  return dim3((unsigned)(((int64_t)n * (d / 8) + THREADS - 1) / THREADS), (unsigned)(units < 65535 ? units : 65535));
+inline dim3 grid_for(int64_t units, int n, int threads_per_row) {
+  return dim3((unsigned)(((int64_t)n * threads_per_row + THREADS - 1) / THREADS), (unsigned)(units < 65535 ? units : 65535));
 }
 
 }  // namespace
 
 cudaError_t launch_pack(const __half* K, const __half* V, const int32_t* len, unsigned char* cache, int64_t units, int n, int k,
                         int head_dim, cudaStream_t stream) {
-  const dim3 grid = grid_for(units, n, head_dim);
+  const dim3 grid = grid_for(units, n, head_dim / 16);
   switch (head_dim) {
     case 64: pack_kernel<64><<<grid, THREADS, 0, stream>>>(K, V, len, cache, units, n, k); break;
     case 128: pack_kernel<128><<<grid, THREADS, 0, stream>>>(K, V, len, cache, units, n, k); break;
@@ -172,7 +183,7 @@ cudaError_t launch_pack(const __half* K, const __half* V, const int32_t* len, un
 
 cudaError_t launch_unpack(const unsigned char* cache, const int32_t* len, __half* K, __half* V, int64_t units, int n, int k,
                           int head_dim, cudaStream_t stream) {
-  const dim3 grid = grid_for(units, n, head_dim);
+  const dim3 grid = grid_for(units, n, head_dim / 8);
   switch (head_dim) {
     case 64: unpack_kernel<64><<<grid, THREADS, 0, stream>>>(cache, len, K, V, units, n, k); break;
     case 128: unpack_kernel<128><<<grid, THREADS, 0, stream>>>(cache, len, K, V, units, n, k); break;

@@ -373,6 +373,40 @@ def test_packed_step_after_the_prompt_phase():
     gpu.kf_destroy()
 
 
+def test_a_cache_whose_offsets_pass_32_bits():
+    """4.3 GB of slots in one unit: one entry near the end outweighs 54 million indifferent ones; among those, all with the same score, the
+    one with the highest position outside the window leaves."""
+    d, k, w = 64, 54_000_000, 10
+    cache = torch.zeros(1, k, 80, dtype=torch.uint8, device=DEV)           # scale and minimum 0: rows of zeros
+    kn, vn, q = _randn(1, 1, 1, d).half(), _randn(2, 1, 1, d).half(), torch.ones(1, 1, d, dtype=torch.float16, device=DEV)
+    K, V = torch.full((1, 1, d), 4.0, dtype=torch.float16, device=DEV), _randn(3, 1, 1, d).half()
+    one = torch.zeros(1, 1, 80, dtype=torch.uint8, device=DEV)
+    kf.kf_pack_cache(K=K, V=V, cache=one)
+    at = k - 5
+    cache[0, at] = one[0, 0]
+    pos = torch.arange(k, dtype=torch.int32, device=DEV).view(1, k)
+    acc, length = torch.zeros(1, k, device=DEV), torch.full((1,), k, dtype=torch.int32, device=DEV)
+    out, slot, score = torch.zeros_like(q), torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(1, k + 1, device=DEV)
+    kf.kf_decode_step_packed(batch=1, n_heads=1, head_dim=d, budget_k=k, recent_w=w, layer=0, position=k, tau=1.0, cache=cache, pos=pos, acc=acc, length=length,
+                             q=q, knew=kn, vnew=vn, out=out, slot_out=slot, score_out=score, noise_mode=kf.KF_NOISE_NONE)
+    x_new = float(kn.double().sum()) / 8                                   # q is all ones; the heavy entry's logit is 64 * 4 / 8 = 32
+    total = math.exp(32.0) + (k - 1) + math.exp(x_new)
+    rows = ref.rows_of(one.cpu().numpy(), d)[1][0, 0].astype(np.float64)
+    want = (math.exp(32.0) * rows + math.exp(x_new) * vn.double().cpu().numpy()[0, 0]) / total
+    assert (np.abs(out.double().cpu().numpy()[0, 0] - want) <= U16 * np.abs(want) + 2.0 ** -25 + 1e-5).all()
+    assert abs(float(score[0, at]) - math.exp(32.0) / total) < 1e-5 and int(slot) == k - w and int(pos[0, k - w]) == k
+    Kb = torch.zeros(1, k, d, dtype=torch.float16, device=DEV)
+    Vb = torch.zeros_like(Kb)
+    kf.kf_unpack_cache(cache=cache, K=Kb, V=Vb)
+    assert np.array_equal(Vb[0, at].cpu().numpy(), rows.astype(np.float16)) and (Kb[0, at] == 4).all() and (Kb[0, at - 1] == 0).all()
+    again = torch.zeros_like(cache)
+    kf.kf_pack_cache(K=Kb, V=Vb, cache=again)
+    back = torch.zeros(1, 1, d, dtype=torch.float16, device=DEV)
+    kf.kf_unpack_cache(cache=again[:, at:at + 1].contiguous(), K=torch.zeros_like(back), V=back)
+    again_rows = ref.rows_of(ref.slots_of(rows.astype(np.float16)[None], rows.astype(np.float16)[None]), d)[1][0]
+    assert np.array_equal(back[0, 0].cpu().numpy(), again_rows)
+
+
 # ------------------------------------------------------------------------------------------------ norm and rotation
 
 def _check_norm(B, n, H, kv, d, dtype, R, halves, norm, base=10000.0, positions=None, position0=0, pad=0, weights=True, with_v=True, eps=1e-6, seed=0):
@@ -421,6 +455,19 @@ def test_norm_rotate_far_positions():
         _check_norm(1, 6, 2, 1, 128, torch.float16, 128, halves, True, positions=at, seed=8)
         _check_norm(1, 6, 2, 1, 64, torch.bfloat16, 16, halves, False, positions=at, base=500000.0, seed=9)
     _check_norm(1, 4, 2, 1, 64, torch.float16, 64, False, False, position0=2 ** 31 - 4, seed=10)
+
+
+def test_norm_rotate_of_more_than_two_to_the_31_values():
+    B, n, H, d = 3, 5600, 1022, 128
+    x = torch.randint(-3000, 3000, (B, n, (H + 2) * d), dtype=torch.int16, device=DEV, generator=_gen(4)).half().div_(1000)
+    q, k, v = (torch.empty(B, h, n, d, dtype=torch.float16, device=DEV) for h in (H, 1, 1))
+    kf.kf_qk_norm_rotate(qkv=x, n_heads=H, n_kv_heads=1, head_dim=d, q=q, k=k, v=v, norm_mode=kf.KF_NORM_RMS, rotary_dims=128, rotary_style=kf.KF_ROTARY_HALVES)
+    for b, t in ((0, 0), (2, n - 1), (1, 4000)):
+        row = x[b, t].double().cpu().numpy()[None, None]
+        want = ref.norm_rotate(row, H, 1, d, np.array([[t]]), None, None, True, np.float64(np.float32(1e-6)), 128, 10000.0, True)
+        for got, w in zip((q[b, :, t], k[b, :, t], v[b, :, t]), want):
+            w = w[0, :, 0]
+            assert (np.abs(got.double().cpu().numpy() - w) <= U16 * np.abs(w) + 2.0 ** -20 * np.abs(w).max(-1, keepdims=True)).all()
 
 
 def test_norm_rotate_small_and_zero_rows():
