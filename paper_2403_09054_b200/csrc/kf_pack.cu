@@ -5,9 +5,9 @@
 // flight per thread, and a group of 32 features is two neighbouring lanes, one of which works out the K group and the other
 // the V group.  Unpacking, it owns eight of each.
 //
-// 1024 units of 2048 rows, d 128: unpack 210 us (6.7 TB/s, as fast as a copy), pack 325 us (4.3 TB/s): rounding 16 features to codes
-// takes about 250 instructions a thread (issue slots 87 %); 415 us with a division and a reciprocal per chunk and codes shifted into
-// place one by one.
+// 1024 units of 2048 rows, d 128: pack 218 us, unpack 231 us, each 1.41 GB at the rate of a copy.  With eight features a thread
+// packing took 325 us (four lanes worked out the same group, 250 instructions per 16 features); with a division and a reciprocal
+// each and codes shifted into place one by one 415.  Unpacking sixteen features a thread takes 286 (stores in halves of 32 bytes).
 #include "kf_packed.cuh"
 
 namespace kf {
