@@ -306,8 +306,8 @@ int64_t kf_launch_count(const kf_ctx* ctx);
  * Operators around the generation step that need no context.  As above: device buffers and scratch belong to the
  * caller, work is enqueued on `stream` of the current device, arguments are checked on the host before anything is
  * enqueued, and nothing is allocated.  Scratch holds nothing between calls and need not be cleared; two calls that may run at
- * the same time (other streams, other captured graphs) need scratch of their own.  Tensors of one call must not overlap
- * unless they are the same argument.
+ * the same time (other streams, other captured graphs) need scratch of their own.  No output of a call may overlap another of its
+ * tensors (KF_EINVAL where a call could otherwise read what it has written).
  * ------------------------------------------------------------------------------------------------------------------ */
 
 #define KF_TYPE_FP16 0
@@ -421,7 +421,8 @@ int kf_beam_select(const kf_beam_args* args, const void* d_logits, const float* 
 
 /* State rows that follow their beam: in every buffer [outer][batch * beams][row_bytes], row (b, i) becomes what row
  * (b, d_parent[b][i]) was before the call, in place.  A parent outside 0..beams-1 leaves its row as it is.
- *   d_parent : DEVICE int32 [batch][beams].  At most 8 buffers; any row_bytes (multiples of 16 move fastest). */
+ *   d_parent : DEVICE int32 [batch][beams].  At most 8 buffers, which may not overlap (nor interleave);
+ *   any row_bytes (multiples of 16 move fastest). */
 typedef struct kf_row_buffer {
   void*   d_base;
   int64_t row_bytes;

@@ -13,6 +13,11 @@ namespace {
 constexpr size_t ALIGN = 256;
 inline size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 inline bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+// Whether [a, a + n) and [b, b + m) share a byte.
+inline bool overlap(const void* a, uint64_t n, const void* b, uint64_t m) {
+  const uint64_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + m && y < x + n;
+}
 inline bool head_dim_ok(int d) { return d == 64 || d == 128 || d == 256; }
 
 bool rows_ok(int64_t units, int32_t n, int32_t k, int32_t d) {
@@ -68,6 +73,8 @@ int kf_pack_cache(int64_t units, int32_t n, int32_t budget_k, int32_t head_dim, 
                   const int32_t* d_len, void* d_cache, void* stream) {
   if (!rows_ok(units, n, budget_k, head_dim) || !d_K || !d_V || !d_cache) return KF_EINVAL;
   if (misaligned(d_K, 16) || misaligned(d_V, 16) || misaligned(d_cache, 16) || misaligned(d_len, 4)) return KF_EINVAL;
+  const uint64_t rows = (uint64_t)units * n * head_dim * 2, slots = (uint64_t)units * budget_k * kf::packed_slot_bytes(head_dim);
+  if (overlap(d_K, rows, d_cache, slots) || overlap(d_V, rows, d_cache, slots)) return KF_EINVAL;
   return kf::launch_pack(static_cast<const __half*>(d_K), static_cast<const __half*>(d_V), d_len, static_cast<unsigned char*>(d_cache), units, n,
                          budget_k, head_dim, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KF_OK : KF_ECUDA;
 }
@@ -76,6 +83,8 @@ int kf_unpack_cache(int64_t units, int32_t n, int32_t budget_k, int32_t head_dim
                     void* d_K, void* d_V, void* stream) {
   if (!rows_ok(units, n, budget_k, head_dim) || !d_K || !d_V || !d_cache) return KF_EINVAL;
   if (misaligned(d_K, 16) || misaligned(d_V, 16) || misaligned(d_cache, 16) || misaligned(d_len, 4)) return KF_EINVAL;
+  const uint64_t rows = (uint64_t)units * n * head_dim * 2, slots = (uint64_t)units * budget_k * kf::packed_slot_bytes(head_dim);
+  if (overlap(d_K, rows, d_V, rows) || overlap(d_K, rows, d_cache, slots) || overlap(d_V, rows, d_cache, slots)) return KF_EINVAL;
   return kf::launch_unpack(static_cast<const unsigned char*>(d_cache), d_len, static_cast<__half*>(d_K), static_cast<__half*>(d_V), units, n,
                            budget_k, head_dim, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KF_OK : KF_ECUDA;
 }
@@ -93,6 +102,8 @@ int kf_decode_step_packed(const kf_packed_step* a, void* d_cache, int32_t* d_pos
       misaligned(a->d_alibi_slopes, 4))
     return KF_EINVAL;
   const PackedLayout L = packed_layout(a);
+  const uint64_t heads = (uint64_t)L.units * L.group * a->head_dim * 2, rows = (uint64_t)L.units * a->head_dim * 2;
+  if (overlap(d_out, heads, d_q, heads) || overlap(d_out, heads, d_knew, rows) || overlap(d_out, heads, d_vnew, rows)) return KF_EINVAL;
   if (scratch_bytes < L.total) return KF_ENOSPC;
   unsigned char* scratch = static_cast<unsigned char*>(d_scratch);
   kf::PackedParams P{};
@@ -138,6 +149,11 @@ int kf_qk_norm_rotate(const kf_qk_norm_args* a, const void* d_qkv, const void* d
   for (const void* p : {d_qkv, d_q_weight, d_k_weight, static_cast<const void*>(d_q), static_cast<const void*>(d_k), static_cast<const void*>(d_v_opt)})
     if (misaligned(p, 16)) return KF_EINVAL;
   if (misaligned(d_positions, 4)) return KF_EINVAL;
+  const uint64_t tokens = (uint64_t)a->batch * a->n_tokens * a->head_dim * 2, out_q = tokens * a->n_heads, out_kv = tokens * a->n_kv_heads;
+  const uint64_t in = ((uint64_t)(a->batch - 1) * a->batch_stride + (uint64_t)(a->n_tokens - 1) * a->token_stride + row) * 2;
+  if (overlap(d_q, out_q, d_k, out_kv) || overlap(d_q, out_q, d_v_opt, out_kv) || overlap(d_k, out_kv, d_v_opt, out_kv) || overlap(d_qkv, in, d_q, out_q) ||
+      overlap(d_qkv, in, d_k, out_kv) || overlap(d_qkv, in, d_v_opt, out_kv))
+    return KF_EINVAL;
   kf::QkNormParams P{};
   P.qkv = d_qkv; P.q_weight = d_q_weight; P.k_weight = d_k_weight; P.positions = d_positions;
   P.q = static_cast<__half*>(d_q); P.k = static_cast<__half*>(d_k); P.v = static_cast<__half*>(d_v_opt);
@@ -164,6 +180,10 @@ int kf_beam_select(const kf_beam_args* a, const void* d_logits, const float* d_s
   if (misaligned(d_logits, a->logits_type == KF_TYPE_FP32 ? 4 : 2) || misaligned(d_scores, 4) || misaligned(d_out_scores, 4) ||
       misaligned(d_out_parent, 4) || misaligned(d_out_token, 4) || misaligned(d_scratch, 256))
     return KF_EINVAL;
+  const uint64_t in = (uint64_t)a->batch * a->beams * 4, out = (uint64_t)a->batch * a->take * 4;
+  if (overlap(d_scores, in, d_out_scores, out) || overlap(d_out_scores, out, d_out_parent, out) || overlap(d_out_scores, out, d_out_token, out) ||
+      overlap(d_out_parent, out, d_out_token, out))
+    return KF_EINVAL;
   if (scratch_bytes < kf_beam_scratch_bytes(a)) return KF_ENOSPC;
   kf::BeamParams P{};
   bool wide = false;
@@ -186,6 +206,11 @@ int kf_reorder_rows(const kf_row_buffer* buffers, int32_t n_buffers, int32_t bat
     const kf_row_buffer& b = buffers[i];
     if (!b.d_base || b.row_bytes < 1 || b.row_bytes > ((int64_t)1 << 40) || b.outer < 1) return KF_EINVAL;
     if (b.outer > 1 && b.outer_stride < b.row_bytes * batch * beams) return KF_EINVAL;
+    // a row that two descriptions move would be read while it is written
+    auto extent = [&](const kf_row_buffer& x) { return (uint64_t)(x.outer - 1) * (x.outer > 1 ? x.outer_stride : 0) + (uint64_t)x.row_bytes * batch * beams; };
+    for (int j = 0; j < i; ++j)
+      if (overlap(b.d_base, extent(b), buffers[j].d_base, extent(buffers[j]))) return KF_EINVAL;
+    if (overlap(b.d_base, extent(b), d_parent, (uint64_t)batch * beams * 4)) return KF_EINVAL;
     P.buf[i].base = static_cast<unsigned char*>(b.d_base);
     P.buf[i].row_bytes = b.row_bytes;
     P.buf[i].outer = b.outer;

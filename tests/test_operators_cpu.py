@@ -10,6 +10,7 @@ import paper_2403_09054_b200 as kf
 from tests import operators_reference as ref
 
 OK = 4096      # an aligned address that is never dereferenced
+FAR = [OK + (i << 32) for i in range(16)]      # such addresses, far apart
 
 
 def test_slot_sizes():
@@ -18,13 +19,15 @@ def test_slot_sizes():
 
 @pytest.mark.parametrize("call", ["pack", "unpack"])
 def test_row_conversion_refusals(call):
-    def rc(units=2, n=3, k=4, d=64, a=OK, b=OK, length=None, c=OK):
+    def rc(units=2, n=3, k=4, d=64, a=FAR[0], b=FAR[1], length=None, c=FAR[2]):
         if call == "pack":
             return kf.LIB.kf_pack_cache(units, n, k, d, a, b, length, c, None)
         return kf.LIB.kf_unpack_cache(units, n, k, d, c, length, a, b, None)
     for bad in (dict(units=0), dict(n=0), dict(n=5), dict(d=96), dict(a=None), dict(b=None), dict(c=None), dict(a=OK + 2), dict(b=OK + 8), dict(c=OK + 4),
-                dict(length=OK + 2), dict(units=1 << 40), dict(units=-1)):
+                dict(length=OK + 2), dict(units=1 << 40), dict(units=-1), dict(c=FAR[0]), dict(c=FAR[1] + 128)):
         assert rc(**bad) == kf.KF_EINVAL, bad
+    if call == "unpack":
+        assert rc(a=FAR[1] + 128) == kf.KF_EINVAL
 
 
 def _step(**kw):
@@ -52,7 +55,7 @@ def test_packed_step_pointers_are_checked():
     assert need == kf.kf_packed_scratch_bytes(batch=2, n_heads=4, head_dim=64, budget_k=32) and need % 256 == 0
 
     def rc(index=None, value=None, nbytes=need):
-        p = [OK] * 12
+        p = FAR[:12]
         if index is not None:
             p[index] = value
         return kf.LIB.kf_decode_step_packed(C.byref(a), *p, nbytes, None)
@@ -64,6 +67,8 @@ def test_packed_step_pointers_are_checked():
     for i in (1, 2, 3, 8, 9):                            # positions, scores, counts, score_opt, slot_opt
         assert rc(i, OK + 2) == kf.KF_EINVAL
     assert rc(10, OK + 1) == kf.KF_EINVAL and rc(11, OK + 128) == kf.KF_EINVAL
+    for i in (4, 5, 6):                                  # the output in place of q, k_new, v_new
+        assert rc(7, FAR[i] + 16) == kf.KF_EINVAL
     assert rc(nbytes=need - 1) == kf.KF_ENOSPC
     assert kf.LIB.kf_decode_step_packed(None, *[OK] * 12, need, None) == kf.KF_EINVAL
 
@@ -94,8 +99,12 @@ def test_norm_rotate_pointers_are_checked():
         p[i] = None
         assert kf.LIB.kf_qk_norm_rotate(C.byref(a), *p, None) == kf.KF_EINVAL
     for i, off in ((0, 8), (1, 8), (2, 2), (3, 2), (4, 8), (5, 4), (6, 8)):
-        p = [OK] * 7
-        p[i] = OK + off
+        p = FAR[:7]
+        p[i] += off
+        assert kf.LIB.kf_qk_norm_rotate(C.byref(a), *p, None) == kf.KF_EINVAL
+    for i, j in ((4, 0), (5, 0), (6, 0), (5, 4), (6, 4), (6, 5)):      # outputs that overlap
+        p = FAR[:7]
+        p[i] = p[j] + 512
         assert kf.LIB.kf_qk_norm_rotate(C.byref(a), *p, None) == kf.KF_EINVAL
     a = _norm(position0=2 ** 31 - 2)                      # positions would pass 2^31 - 1
     assert kf.LIB.kf_qk_norm_rotate(C.byref(a), OK, OK, OK, None, OK, OK, OK, None) == kf.KF_EINVAL
@@ -126,21 +135,28 @@ def test_beam_select_pointers_are_checked():
         p[i] = None
         assert kf.LIB.kf_beam_select(C.byref(a), *p, need, None) == kf.KF_EINVAL
     for i, off in ((0, 1), (1, 2), (3, 2), (4, 2), (5, 2), (6, 64)):
-        p = [OK] * 7
-        p[i] = OK + off
+        p = FAR[:7]
+        p[i] += off
         assert kf.LIB.kf_beam_select(C.byref(a), *p, need, None) == kf.KF_EINVAL
-    assert kf.LIB.kf_beam_select(C.byref(a), *[OK] * 7, need - 1, None) == kf.KF_ENOSPC
+    for i, j in ((3, 1), (4, 3), (5, 3), (5, 4)):                      # new scores over the old ones, outputs over one another
+        p = FAR[:7]
+        p[i] = p[j] + 8
+        assert kf.LIB.kf_beam_select(C.byref(a), *p, need, None) == kf.KF_EINVAL
+    assert kf.LIB.kf_beam_select(C.byref(a), *FAR[:7], need - 1, None) == kf.KF_ENOSPC
 
 
 def test_reorder_arguments_are_checked():
     def rc(n=1, batch=2, beams=4, parent=OK, **kw):
-        b = kf.kf_row_buffer(OK, 64, 0, 1)
+        b = kf.kf_row_buffer(FAR[1], 64, 0, 1)
         for name, value in kw.items():
             setattr(b, name, value)
         return kf.LIB.kf_reorder_rows(C.byref(b), n, batch, beams, parent, None)
     for bad in (dict(n=0), dict(n=9), dict(batch=0), dict(batch=65536), dict(beams=0), dict(beams=33), dict(parent=None), dict(parent=OK + 2), dict(d_base=None),
                 dict(row_bytes=0), dict(row_bytes=-16), dict(outer=0), dict(outer=2, outer_stride=64 * 8 - 1)):
         assert rc(**bad) == kf.KF_EINVAL, bad
+    two = (kf.kf_row_buffer * 2)(kf.kf_row_buffer(FAR[0], 64, 0, 1), kf.kf_row_buffer(FAR[0] + 256, 64, 0, 1))      # 512 bytes each
+    assert kf.LIB.kf_reorder_rows(two, 2, 2, 4, FAR[3], None) == kf.KF_EINVAL
+    assert kf.LIB.kf_reorder_rows(two, 1, 2, 4, FAR[0] + 64, None) == kf.KF_EINVAL                             # the parents inside a buffer
     assert kf.LIB.kf_reorder_rows(None, 1, 1, 1, OK, None) == kf.KF_EINVAL
     assert kf.LIB.kf_reorder_beams(None, 0, 1, OK, None) == kf.KF_EINVAL
 
