@@ -18,7 +18,7 @@
 //
 // What bounds it: issue.  1024 caches of 2048 slots (d 128, one head each; 361 MB): 85 us a call, of which 76 are the streaming kernel
 // (4.7 TB/s; 846 warp instructions per 32 slots, 480 of them conversions; issue slots 63 %) and 9 the closing one; the bytes alone
-// would take 56.  32 caches of 4096: 13 us.  256 caches of 2000 slots on average half full, four heads each: 37 us, each further
+// would take 56.  32 caches of 4096: 13 us.  256 caches of 2000 slots on average half full, four heads each: 36 us, each further
 // head adding its noise (90 instructions per 32 slots) and softmaxes.  Measured and not taken: tiles staged in registers (106), the
 // closing stage inside the streaming CTA with one CTA per cache (101), the heads as a loop (37.4, and 42 instead of 40 at d 256).
 #include "kf_close.cuh"
@@ -226,6 +226,9 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
   const int p_at = (lane & 16) + (lane & 3) * 4 + (lane >> 2 & 3);   // where the weight of slot `lane` is read as an operand
   float* y_out = P.y_scratch + (size_t)u * G * (P.k + 1) + first + lane;
 
+  // With several heads their noise and softmaxes fill the instruction cache: the two tiles share their instructions (37.6 -> 35.9 us
+  // for 256 caches with four heads; with one head unrolled tiles overlap better, 85 against 88 us for 1024 caches).
+  constexpr int TILES_UNROLLED = G == 1 ? 2 : 1;
   bool failed = false;
   int it = 0;
   for (; it < rounds; ++it, y_out += NW * SPAN) {
@@ -245,7 +248,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
                               : noise_for(P, b, lh0 + g, (uint32_t)P.p, (uint32_t)pj[sub]);
 
     // ---- logits (slots behind the last entry give numbers that nobody reads)
-#pragma unroll
+#pragma unroll(TILES_UNROLLED)
     for (int sub = 0; sub < 2; ++sub) {
       if (sub * TILE >= rows) break;
       const bool ok = mbar_wait_bounded(bars + sub, (uint32_t)(it & 1));
@@ -338,7 +341,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     __syncwarp();
 
     // ---- values; a slot behind the last entry counts as zeros, whatever the buffer holds
-#pragma unroll
+#pragma unroll(TILES_UNROLLED)
     for (int sub = 0; sub < 2; ++sub) {
       if (sub * TILE >= rows) break;
       const unsigned char* buf = ring + sub * TILE_BYTES;
