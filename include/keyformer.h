@@ -349,6 +349,8 @@ typedef struct kf_packed_step {
   float   noise_const;                /* c of KF_NOISE_CONST                                                      */
   float   noise_mu, noise_sigma;      /* KF_NOISE_GAUSS                                                           */
   const float* d_alibi_slopes;        /* DEVICE [H] when bias_mode == KF_BIAS_ALIBI, else ignored                 */
+  int32_t debug_fail_first_wait;      /* self-test of the error path, see kf_config: 1 makes every warp give up its first wait
+                                         for cache rows at once.  0 in normal use                                  */
 } kf_packed_step;
 
 /* One generation step of Algorithm 1 (as kf_decode_step, original positions, keys stored as they are to be multiplied)
@@ -363,7 +365,8 @@ typedef struct kf_packed_step {
  *   d_row_opt   : DEVICE fp16 [B][Hkv][2][d] or NULL; the new K and V row as the values their codes stand for
  *   d_scratch   : DEVICE, kf_packed_scratch_bytes(args) bytes, 256-byte aligned (KF_ENOSPC if `scratch_bytes` is less)
  * d_cache, d_q, d_knew, d_vnew, d_out must be 16-byte aligned.  A unit whose d_len entry is outside 0..k is skipped:
- * nothing of it is read or written.  Scores in d_acc are not negative (sums of softmax values).  A non-finite value in a
+ * nothing of it is read or written.  A unit whose rows did not arrive within the kernel's bounded wait keeps its state (cache, positions, scores, count):
+ * its rows of d_out and its z are NaN, and its d_slot_opt entry is KF_ETIMEOUT.  Scores in d_acc are not negative (sums of softmax values).  A non-finite value in a
  * cached row makes the output of its unit NaN. */
 size_t kf_packed_scratch_bytes(const kf_packed_step* args);   /* 0 if the arguments are invalid */
 int kf_decode_step_packed(const kf_packed_step* args, void* d_cache, int32_t* d_pos, float* d_acc, int32_t* d_len,

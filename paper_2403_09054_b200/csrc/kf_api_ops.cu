@@ -32,6 +32,7 @@ bool packed_ok(const kf_packed_step* a) {
   if (a->n_heads % hkv != 0 || !kf::decode_group_supported(a->n_heads / hkv) || !head_dim_ok(a->head_dim)) return false;
   if (a->budget_k < 1 || a->budget_k > (1 << 26) || a->recent_w < 0 || a->recent_w > a->budget_k) return false;
   if (a->layer < 0 || a->position < 0 || !(a->tau > 0.0) || !std::isfinite(a->tau) || !(a->logit_scale >= 0.f)) return false;
+  if (a->debug_fail_first_wait < 0 || a->debug_fail_first_wait > 1) return false;
   if (a->noise_mode < KF_NOISE_GUMBEL || a->noise_mode > KF_NOISE_GAUSS) return false;
   if (a->noise_mode == KF_NOISE_GAUSS && !(a->noise_sigma >= 0.f)) return false;
   if (a->bias_mode != KF_BIAS_NONE && a->bias_mode != KF_BIAS_ALIBI) return false;
@@ -124,6 +125,7 @@ int kf_decode_step_packed(const kf_packed_step* a, void* d_cache, int32_t* d_pos
   P.group = L.group;
   P.scale = a->logit_scale > 0.f ? a->logit_scale : (float)(1.0 / std::sqrt((double)a->head_dim));
   P.inv_tau = (float)(1.0 / a->tau);
+  P.first_wait_limit = a->debug_fail_first_wait ? 0u : kf::DECODE_WAIT_LIMIT;
   P.noise_const = a->noise_const; P.noise_mu = a->noise_mu; P.noise_sigma = a->noise_sigma;
   P.pk = kf::philox_expand_key(a->noise_seed);
   return kf::launch_decode_packed(P, a->head_dim, L.units, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KF_OK : KF_ECUDA;

@@ -26,6 +26,9 @@ struct CloseRow {
   }
   // Called by every thread with the columns loaded, before the streaming kernel's results are waited for.
   __device__ __forceinline__ void prepare(const PARAMS&, int) {}
+  // Whether the streaming kernel marks the statistics of a split that it could not finish (sums of -1); the context's
+  // kernels report through its error word instead.
+  static constexpr bool MARKS_FAILURES = false;
   // Called once by every thread: the row goes to `slot`, or nowhere if slot is -1.
   __device__ __forceinline__ void store(const PARAMS& P, int u, int slot) const {
     if (slot < 0) return;
@@ -42,6 +45,16 @@ struct CloseRow {
 __device__ __forceinline__ unsigned long long evict_key(float a, int pos) {
   // smallest key = smallest accumulated score; equal scores: the higher position leaves
   return ((unsigned long long)__float_as_uint(a) << 32) | (unsigned long long)(0xFFFFFFFFu - (uint32_t)pos);
+}
+
+// A unit whose rows did not all arrive: its outputs and scores say so, its state stays as it was.
+template <int D, int NT, int G, class PARAMS>
+__device__ __forceinline__ void report_failure(const PARAMS& P, int u, int len) {
+  const float nan = __int_as_float(0x7fc00000);
+  for (int c = threadIdx.x; c < G * D; c += NT) P.out[(size_t)u * G * D + c] = __float2half_rn(nan);
+  if (P.score_opt)
+    for (int j = threadIdx.x; j <= len; j += NT) P.score_opt[(size_t)u * (P.k + 1) + j] = nan;
+  if (P.slot_opt && threadIdx.x == 0) P.slot_opt[u] = ERR_TIMEOUT;
 }
 
 // The eviction decision and the replacement, common to every form of the closing stage: `best` / `best_j` are the
@@ -182,6 +195,12 @@ __device__ void combine_and_evict(const PARAMS& P, int u, int len) {
     float4 ps0 = make_float4(-INFINITY, 0.f, -INFINITY, 0.f), ps1 = ps0;
     if (lane < P.splits) ps0 = __ldcg(reinterpret_cast<const float4*>(part + ((size_t)lane * G + g) * PSTRIDE));
     if (lane + 32 < P.splits) ps1 = __ldcg(reinterpret_cast<const float4*>(part + ((size_t)(lane + 32) * G + g) * PSTRIDE));
+    if constexpr (CloseRow<PARAMS, D, NT, CPT>::MARKS_FAILURES) {
+      if (__any_sync(0xffffffffu, ps0.y < 0.f || ps1.y < 0.f)) {   // every warp looks at the same statistics
+        report_failure<D, NT, G>(P, u, len);
+        return;
+      }
+    }
     const float mx = warp_max(fmaxf(x_new[g], fmaxf(ps0.y > 0.f ? ps0.x : -INFINITY, ps1.y > 0.f ? ps1.x : -INFINITY)));
     my[g] = warp_max(fmaxf(y_new[g], fmaxf(ps0.w > 0.f ? ps0.z : -INFINITY, ps1.w > 0.f ? ps1.z : -INFINITY)));
     const float w0 = ps0.y > 0.f ? fast_exp2((ps0.x - mx) * LOG2E) : 0.f;   // weight of split `lane` in the output
@@ -334,11 +353,13 @@ __device__ void combine_and_evict_group(const PARAMS& P, int u, int len) {
       }
   };
   if (EARLY) load_y(tid);
+  bool lost = false;
   if (warp < G) {
     const int g = warp;
     float4 ps0 = make_float4(-INFINITY, 0.f, -INFINITY, 0.f), ps1 = ps0;
     if (lane < P.splits) ps0 = __ldcg(reinterpret_cast<const float4*>(part + ((size_t)lane * G + g) * PSTRIDE));
     if (lane + 32 < P.splits) ps1 = __ldcg(reinterpret_cast<const float4*>(part + ((size_t)(lane + 32) * G + g) * PSTRIDE));
+    if constexpr (CloseRow<PARAMS, D, NT, 1>::MARKS_FAILURES) lost = __any_sync(0xffffffffu, ps0.y < 0.f || ps1.y < 0.f);
     const float mx = warp_max(fmaxf(x_new, fmaxf(ps0.y > 0.f ? ps0.x : -INFINITY, ps1.y > 0.f ? ps1.x : -INFINITY)));
     const float my = warp_max(fmaxf(y_new, fmaxf(ps0.w > 0.f ? ps0.z : -INFINITY, ps1.w > 0.f ? ps1.z : -INFINITY)));
     const float w0 = ps0.y > 0.f ? fast_exp2((ps0.x - mx) * LOG2E) : 0.f;
@@ -351,7 +372,14 @@ __device__ void combine_and_evict_group(const PARAMS& P, int u, int len) {
     sh_w[g][lane + 32] = w1;
     if (lane == 0) { sh_mx[g] = mx; sh_inv_lx[g] = inv_lx; sh_my[g] = my; sh_inv_ly[g] = inv_ly; sh_xnew[g] = x_new; sh_ynew[g] = y_new; }
   }
-  __syncthreads();
+  if constexpr (CloseRow<PARAMS, D, NT, 1>::MARKS_FAILURES) {
+    if (__syncthreads_or(lost)) {
+      report_failure<D, NT, G>(P, u, len);
+      return;
+    }
+  } else {
+    __syncthreads();
+  }
 
   // ---- attention outputs (Eq. 1): one (head, column) per thread and round
   for (int idx = tid; idx < G * D; idx += NT) {

@@ -57,6 +57,7 @@ struct CloseRow<PackedParams, D, NT, CPT> {
   __half kn[CPT], vn[CPT];
   __half2 kg[CPT], vg[CPT];     // the groups of the thread's columns
   uint32_t code[CPT];           // K code | V code << 4
+  static constexpr bool MARKS_FAILURES = true;
 
   static __device__ __forceinline__ float noise(const PackedParams& P, uint32_t b, uint32_t lh, uint32_t i, uint32_t j) {
     return P.noise_mode == 0 ? packed_gumbel(P, b, lh, i, j) : noise_for(P, b, lh, i, j);
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
 #pragma unroll(TILES_UNROLLED)
     for (int sub = 0; sub < 2; ++sub) {
       if (sub * TILE >= rows) break;
-      const bool ok = mbar_wait_bounded(bars + sub, (uint32_t)(it & 1));
+      const bool ok = mbar_wait_bounded(bars + sub, (uint32_t)(it & 1), it == 0 ? P.first_wait_limit : DECODE_WAIT_LIMIT);
       if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
       const unsigned char* buf = ring + sub * TILE_BYTES;
 #pragma unroll
@@ -387,8 +388,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     }
   }
   if (failed) {
-    // a copy did not land in time: flag it, then give the copies still in flight a second bounded wait
-    if (lane == 0) atomicExch(P.err, ERR_TIMEOUT);
+    // a copy did not land in time: the unit is marked below; the copies still in flight get a second bounded wait
     for (int sub = 0; sub < 2; ++sub)
       if (first + it * NW * SPAN + sub * TILE < row_end) (void)mbar_wait_bounded(bars + sub, (uint32_t)(it & 1));
   }
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
     l_y[g] = warp_sum(l_y[g]);
     if (lane == 0) { sh_m[warp][g] = m_x[g]; sh_my[warp][g] = m_y[g]; sh_ly[warp][g] = l_y[g]; }
   }
-  __syncthreads();
+  const bool lost = __syncthreads_or(failed);
   float* part = P.partials + ((size_t)u * P.splits + s) * G * PSTRIDE;      // [head][4 + D]
   if (tid < G) {                                                            // one thread per head joins the statistics
     const int g = tid;
@@ -426,7 +426,8 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
       if (sh_ly[wi][g] > 0.f) LY = fmaf(sh_ly[wi][g], fast_exp2((sh_my[wi][g] - MY) * LOG2E), LY);
       sh_f[wi][g] = f;
     }
-    *reinterpret_cast<float4*>(part + g * PSTRIDE) = make_float4(M, L, MY, LY);
+    // sums of -1, which no softmax has, tell the closing kernel that rows are missing
+    *reinterpret_cast<float4*>(part + g * PSTRIDE) = lost ? make_float4(-INFINITY, -1.f, -INFINITY, -1.f) : make_float4(M, L, MY, LY);
   }
   __syncthreads();
   for (int idx = tid; idx < G * D; idx += NT) {
