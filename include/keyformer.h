@@ -361,13 +361,15 @@ typedef struct kf_packed_step {
  *   d_q, d_out : DEVICE fp16 [B][H][d];  d_knew, d_vnew : DEVICE fp16 [B][Hkv][d]
  *   d_score_opt : DEVICE fp32 [B][Hkv][k+1] or NULL; z of the slots [0, len), the new token's at index len
  *   d_slot_opt  : DEVICE int32 [B][Hkv] or NULL; the slot the new row went to, -1 if it was not stored (w = 0 and its own
- *                 score was the smallest)
+ *                 score was the smallest), KF_EBOUNDS or KF_ETIMEOUT where the step could not be taken (below)
  *   d_row_opt   : DEVICE fp16 [B][Hkv][2][d] or NULL; the new K and V row as the values their codes stand for
  *   d_scratch   : DEVICE, kf_packed_scratch_bytes(args) bytes, 256-byte aligned (KF_ENOSPC if `scratch_bytes` is less)
  * d_cache, d_q, d_knew, d_vnew, d_out must be 16-byte aligned.  A unit whose d_len entry is outside 0..k is skipped:
- * nothing of it is read or written.  A unit whose rows did not arrive within the kernel's bounded wait keeps its state (cache, positions, scores, count):
- * its rows of d_out and its z are NaN, and its d_slot_opt entry is KF_ETIMEOUT.  Scores in d_acc are not negative (sums of softmax values).  A non-finite value in a
- * cached row makes the output of its unit NaN. */
+ * nothing of it is read or written.  The positions of a unit's entries are distinct and lie before args->position; where they are not
+ * and every entry of a full unit is inside the recent window, outputs and scores are as ever, but the new row is not stored and
+ * the unit's d_slot_opt entry is KF_EBOUNDS.  A unit whose rows did not arrive within the kernel's bounded wait keeps its state
+ * (cache, positions, scores, count): its rows of d_out and its z are NaN, and its d_slot_opt entry is KF_ETIMEOUT.  Scores in d_acc
+ * are not negative (sums of softmax values).  A non-finite value in a cached row makes the output of its unit NaN. */
 size_t kf_packed_scratch_bytes(const kf_packed_step* args);   /* 0 if the arguments are invalid */
 int kf_decode_step_packed(const kf_packed_step* args, void* d_cache, int32_t* d_pos, float* d_acc, int32_t* d_len,
                           const void* d_q, const void* d_knew, const void* d_vnew, void* d_out, float* d_score_opt,

@@ -41,7 +41,7 @@ bool packed_ok(const kf_packed_step* a) {
 
 struct PackedLayout {
   int units, group, splits, tiles_per_split;
-  size_t partials, err, total;   // offsets; the adjusted logits come first
+  size_t partials, total;   // offsets; the adjusted logits come first
 };
 PackedLayout packed_layout(const kf_packed_step* a) {
   PackedLayout L{};
@@ -51,8 +51,7 @@ PackedLayout packed_layout(const kf_packed_step* a) {
   kf::decode_packed_plan(L.units, a->budget_k, a->head_dim, &L.splits, &L.tiles_per_split);
   const size_t units_q = (size_t)L.units * L.group;
   L.partials = align_up(units_q * ((size_t)a->budget_k + 1) * 4);
-  L.err = L.partials + align_up(units_q * L.splits * (4 + (size_t)a->head_dim) * 4);
-  L.total = L.err + ALIGN;
+  L.total = L.partials + align_up(units_q * L.splits * (4 + (size_t)a->head_dim) * 4);
   return L;
 }
 
@@ -117,7 +116,6 @@ int kf_decode_step_packed(const kf_packed_step* a, void* d_cache, int32_t* d_pos
   P.score_opt = d_score_opt; P.slot_opt = d_slot_opt; P.row_opt = static_cast<__half*>(d_row_opt);
   P.y_scratch = reinterpret_cast<float*>(scratch);
   P.partials = reinterpret_cast<float*>(scratch + L.partials);
-  P.err = reinterpret_cast<int*>(scratch + L.err);   // the closing kernel's self-check; nothing reads it
   P.slopes = a->bias_mode == KF_BIAS_ALIBI ? a->d_alibi_slopes : nullptr;
   P.k = a->budget_k; P.w = a->recent_w; P.p = a->position;
   P.splits = L.splits; P.tiles_per_split = L.tiles_per_split;

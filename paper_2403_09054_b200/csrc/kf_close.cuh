@@ -29,6 +29,10 @@ struct CloseRow {
   // Whether the streaming kernel marks the statistics of a split that it could not finish (sums of -1); the context's
   // kernels report through its error word instead.
   static constexpr bool MARKS_FAILURES = false;
+  // Called by every thread of a full unit that has no entry to evict.
+  static __device__ __forceinline__ void nothing_to_evict(const PARAMS& P, int) {
+    if (threadIdx.x == 0) atomicExch(P.err, ERR_BOUNDS);
+  }
   // Called once by every thread: the row goes to `slot`, or nowhere if slot is -1.
   __device__ __forceinline__ void store(const PARAMS& P, int u, int slot) const {
     if (slot < 0) return;
@@ -90,8 +94,8 @@ __device__ __forceinline__ void evict_and_replace(const PARAMS& P, int u, int le
     for (int wi = 1; wi < NT / 32; ++wi)
       if (sh_key[wi] < best) { best = sh_key[wi]; slot = sh_j[wi]; }
     if (P.w == 0 && key_new < best) { row.store(P, u, -1); return; }  // the new token itself has the lowest score: it is not stored
-    if (best == ~0ull || slot < 0 || slot >= len) {  // cannot happen for 0 <= w <= k; flag it instead of guessing
-      if (tid == 0) atomicExch(P.err, ERR_BOUNDS);
+    if (best == ~0ull || slot < 0 || slot >= len) {  // not with 0 <= w <= k and distinct positions before the new one: report it instead of guessing
+      row.nothing_to_evict(P, u);
       return;
     }
   }

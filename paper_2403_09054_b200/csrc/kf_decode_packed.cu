@@ -58,6 +58,9 @@ struct CloseRow<PackedParams, D, NT, CPT> {
   __half2 kg[CPT], vg[CPT];     // the groups of the thread's columns
   uint32_t code[CPT];           // K code | V code << 4
   static constexpr bool MARKS_FAILURES = true;
+  static __device__ __forceinline__ void nothing_to_evict(const PackedParams& P, int u) {
+    if (P.slot_opt && threadIdx.x == 0) P.slot_opt[u] = ERR_BOUNDS;
+  }
 
   static __device__ __forceinline__ float noise(const PackedParams& P, uint32_t b, uint32_t lh, uint32_t i, uint32_t j) {
     return P.noise_mode == 0 ? packed_gumbel(P, b, lh, i, j) : noise_for(P, b, lh, i, j);

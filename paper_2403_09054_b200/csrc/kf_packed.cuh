@@ -19,9 +19,9 @@ namespace kf {
 constexpr int PACK_GROUP = 32;
 __host__ __device__ constexpr int packed_slot_bytes(int d) { return d + d / 4; }
 
-struct PackedParams : DecodeParams {   // K, V, rope and place fields unused
+struct PackedParams : DecodeParams {   // K, V, err, rope and place fields unused
   unsigned char* cache;   // [units][k][5d/4]
-  int32_t* slot_opt;      // [units] or null: slot the new row went to, -1 if it was not stored
+  int32_t* slot_opt;      // [units] or null: slot the new row went to, -1 if it was not stored, ERR_* where the step could not be taken
   __half* row_opt;        // [units][2][d] or null: the new K and V row as the values their codes stand for
 };
 

@@ -43,3 +43,23 @@ def test_packed_step_checks_the_self_test_argument():
     s = Packed(1, 2, 2, 64, 8, 2)
     with pytest.raises(kf.KeyformerError):
         s.call(1, *s.inputs(1), debug_fail_first_wait=2)
+
+
+@pytest.mark.parametrize("batch,heads,kv,d,k", [(40, 4, 4, 64, 60), (1, 2, 2, 128, 2300), (2, 8, 2, 128, 90)])
+def test_packed_step_without_an_entry_to_evict(batch, heads, kv, d, k):
+    """A position passed twice with w = k: every entry of the full cache lies inside the window.  The step says so in slot_out; outputs and scores are those
+    of a step that stores its row."""
+    s = Packed(batch, heads, kv, d, k, k, noise=kf.KF_NOISE_NONE, seed=71)        # noise would depend on the position
+    s.step(1)
+    state = [t.clone() for t in (s.cache, s.pos, s.acc, s.length)]
+    inputs = s.inputs(2)
+    want, want_score, slot, _ = s.call(2, *inputs)                        # the next position: the oldest leaves
+    assert (slot >= 0).all()
+    for t, old in zip((s.cache, s.pos, s.acc, s.length), state):
+        t.copy_(old)
+    s.n -= 1                                                              # step 2 at the position of step 1
+    out, score, slot, _ = s.call(2, *inputs)
+    assert (slot == kf.KF_EBOUNDS).all()
+    assert torch.equal(out, want) and torch.equal(score, want_score)
+    assert torch.equal(s.cache, state[0]) and torch.equal(s.pos, state[1]) and torch.equal(s.length, state[3])
+    assert torch.equal(s.acc, state[2] + score[:, :k])
