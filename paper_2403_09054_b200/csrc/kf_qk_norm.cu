@@ -14,6 +14,8 @@
 // shuffles) 342, six rows requested ahead and streaming stores 302 (three 324, twelve 367: registers).
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "kf_ops.cuh"
 
 namespace kf {
@@ -49,6 +51,10 @@ __global__ void __launch_bounds__(THREADS, 3) qk_norm_kernel(const __grid_consta
   constexpr int LPR = D / 8;                    // lanes per row
   constexpr int PLACES = THREADS / LPR;
   __shared__ __align__(16) float2 turn[MAX_TOKENS][D / 2];    // (cos, sin)
+  // bfloat16 reaches as far as binary32, so the squares of a row may leave it.  Where a mean square was not inside [2^-96, 2^96] (as words:
+  // LOW + [0, SPAN]), the warp works on its rows of the token once more and scales such rows.
+  constexpr bool FAR_ROWS = !__is_same(T, __half);
+  constexpr uint32_t LOW = 0x0f800000u, SPAN = 0x60000000u;
   const int tid = threadIdx.x, sub = tid % LPR, place = tid / LPR;
   const int64_t tokens = (int64_t)P.batch * P.n, first = (int64_t)blockIdx.x * tokens_per_cta;
   const int here = (int)(tokens - first < tokens_per_cta ? tokens - first : tokens_per_cta);
@@ -82,52 +88,65 @@ __global__ void __launch_bounds__(THREADS, 3) qk_norm_kernel(const __grid_consta
   }
   __syncthreads();
 
-  for (int group = 0; group < here; group += side) {
-    const int tk = group + my_token;
-    const bool there = !idle && tk < here;
-    const int64_t tok = first + (there ? tk : 0), b = tok / P.n, t = tok % P.n;
-    const T* src = static_cast<const T*>(P.qkv) + b * P.batch_stride + t * P.token_stride;
-    const int mine = there ? rows : 0;
-    const int64_t step = (int64_t)P.n * D;              // from a head's row to the next head's
-    // row r of the token goes to one of these plus r steps
-    __half* to_q = P.q + (b * P.H * P.n + t) * D;
-    __half* to_k = P.k + (b * P.Hkv * P.n + t) * D - P.H * step;
-    __half* to_v = P.v + (b * P.Hkv * P.n + t) * D - (P.H + P.Hkv) * step;
-    float cs[4] = {}, sn[4] = {};                       // of the lane's four pairs
-    if (turns) {
-      const float4* at = reinterpret_cast<const float4*>(&turn[there ? tk : 0][4 * sub]);
-      const float4 u = at[0], v = at[1];
-      cs[0] = u.x; sn[0] = u.y; cs[1] = u.z; sn[1] = u.w;
-      cs[2] = v.x; sn[2] = v.y; cs[3] = v.z; sn[3] = v.w;
-    }
-    for (int r0 = 0; r0 < rows; r0 += AHEAD * PLACES) {     // AHEAD rounds at a time, their rows requested first
-      uint2 raw[AHEAD][2];
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const int row = r0 + i * PLACES + row0;
-        raw[i][0] = raw[i][1] = make_uint2(0, 0);
-        if (row < mine) {
-          raw[i][0] = __ldcs(reinterpret_cast<const uint2*>(src + (int64_t)row * D + run0));
-          raw[i][1] = __ldcs(reinterpret_cast<const uint2*>(src + (int64_t)row * D + run1));
-        }
+  uint32_t farthest = 0;
+  auto walk = [&](auto again) {
+    for (int group = 0; group < here; group += side) {
+      const int tk = group + my_token;
+      const bool there = !idle && tk < here;
+      const int64_t tok = first + (there ? tk : 0), b = tok / P.n, t = tok % P.n;
+      const T* src = static_cast<const T*>(P.qkv) + b * P.batch_stride + t * P.token_stride;
+      const int mine = there ? rows : 0;
+      const int64_t step = (int64_t)P.n * D;              // from a head's row to the next head's
+      // row r of the token goes to one of these plus r steps
+      __half* to_q = P.q + (b * P.H * P.n + t) * D;
+      __half* to_k = P.k + (b * P.Hkv * P.n + t) * D - P.H * step;
+      __half* to_v = P.v + (b * P.Hkv * P.n + t) * D - (P.H + P.Hkv) * step;
+      float cs[4] = {}, sn[4] = {};                       // of the lane's four pairs
+      if (turns) {
+        const float4* at = reinterpret_cast<const float4*>(&turn[there ? tk : 0][4 * sub]);
+        const float4 u = at[0], v = at[1];
+        cs[0] = u.x; sn[0] = u.y; cs[1] = u.z; sn[1] = u.w;
+        cs[2] = v.x; sn[2] = v.y; cs[3] = v.z; sn[3] = v.w;
       }
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        if (r0 + i * PLACES >= rows) break;             // the same for the whole CTA
-        const int row = r0 + i * PLACES + row0;
+      auto request = [&](int row, uint2 (&raw)[2]) {
+        raw[0] = raw[1] = make_uint2(ONES, ONES);
+        if (row < mine) {
+          raw[0] = __ldcs(reinterpret_cast<const uint2*>(src + (int64_t)row * D + run0));
+          raw[1] = __ldcs(reinterpret_cast<const uint2*>(src + (int64_t)row * D + run1));
+        }
+      };
+      auto work_on = [&](int row, const uint2 (&raw)[2]) {
         const bool is_q = row < P.H, is_v = row >= P.H + P.Hkv;
         float x[8];
-        widen<T>(raw[i][0], x);
-        widen<T>(raw[i][1], x + 4);
+        widen<T>(raw[0], x);
+        widen<T>(raw[1], x + 4);
         if (!__all_sync(0xffffffffu, is_v)) {           // a warp of value rows only lays them out
           float r = 1.f;
           if (P.norm) {
-            float ss = 0.f;
+            auto mean_square = [&](float eps) {
+              float ss = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+              for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
 #pragma unroll
-            for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            r = rsqrtf(fmaf(ss, 1.0f / (float)D, P.eps));
+              for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+              return fmaf(ss, 1.0f / (float)D, eps);
+            };
+            float mean = mean_square(P.eps);
+            if constexpr (decltype(again)::value) {     // a far row near 1 by a power of two, and eps with it; one with an infinity stays as it is
+              float big = sqrtf(P.eps);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[e]));
+#pragma unroll
+              for (int o = 1; o < LPR; o <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+              const int exponent = __float_as_int(big) >> 23;
+              const float by = !is_v && __float_as_uint(mean) - LOW > SPAN && exponent < 255 ? __int_as_float((254 - min(max(exponent, 1), 253)) << 23) : 1.f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] *= by;
+              mean = mean_square(P.eps * by * by);
+            } else if constexpr (FAR_ROWS) {
+              farthest = __viaddmax_u32(__float_as_uint(mean), 0u - LOW, farthest);
+            }
+            r = rsqrtf(mean);
           }
           if (!is_v) {
             float w[8];
@@ -152,9 +171,23 @@ __global__ void __launch_bounds__(THREADS, 3) qk_norm_kernel(const __grid_consta
           __stcs(reinterpret_cast<uint2*>(dst + run0), narrow(x));
           __stcs(reinterpret_cast<uint2*>(dst + run1), narrow(x + 4));
         }
+      };
+      constexpr int ROUNDS = decltype(again)::value ? 1 : AHEAD;
+      for (int r0 = 0; r0 < rows; r0 += ROUNDS * PLACES) {    // ROUNDS at a time, their rows requested first
+        uint2 raw[ROUNDS][2];
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) request(r0 + i * PLACES + row0, raw[i]);
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+          if (r0 + i * PLACES >= rows) break;             // the same for the whole CTA
+          work_on(r0 + i * PLACES + row0, raw[i]);
+        }
       }
     }
-  }
+  };
+  walk(std::false_type{});
+  if constexpr (FAR_ROWS)
+    if (__any_sync(0xffffffffu, farthest > SPAN)) walk(std::true_type{});
 }
 
 template <int D>

@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import paper_2403_09054_b200 as kf
-from tests.test_gpu_operators import DEV, Packed
+from tests import operators_reference as ref
+from tests.test_gpu_operators import DEV, U16, Packed
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +64,49 @@ def test_packed_step_without_an_entry_to_evict(batch, heads, kv, d, k):
     assert torch.equal(out, want) and torch.equal(score, want_score)
     assert torch.equal(s.cache, state[0]) and torch.equal(s.pos, state[1]) and torch.equal(s.length, state[3])
     assert torch.equal(s.acc, state[2] + score[:, :k])
+
+
+# ------------------------------------------------------------------------------------------------ norm and rotation
+
+@pytest.mark.parametrize("d,halves", [(64, True), (128, False), (256, True)])
+@pytest.mark.parametrize("eps", [0.0, 1e-6, 1e-30, 1e30])
+def test_norm_of_rows_whose_squares_leave_binary32(d, halves, eps):
+    """bfloat16 rows from 2^-132 to 2^125, ordinary ones among them; tolerances as for ordinary rows (test_gpu_operators._check_norm)."""
+    H, kv = 3, 2
+    power = torch.tensor([0, 125, 100, 65, 63, 48, 30, -30, -48, -62, -64, -100, -126, -130, -132], device=DEV)
+    n = len(power) * 2
+    x = torch.randn(1, n, H + 2 * kv, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(d))
+    x = x.clamp(-3.9, 3.9) * torch.exp2(power.double()).repeat(2)[:, None, None].float()
+    x[:, n // 2:, ::2] = torch.randn(1, n // 2, (H + 2 * kv + 1) // 2, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(d + 1))
+    x = x.bfloat16()                                     # in the second half extreme and ordinary heads alternate within a token
+    x[0, 3, 1, 0] = 0.0
+    qw, kw = ((1 + 0.3 * torch.randn(d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(i))).bfloat16() for i in (1, 2))
+    q, k, v = (torch.empty(1, h, n, d, dtype=torch.float16, device=DEV) for h in (H, kv, kv))
+    rows = x.view(1, n, -1)
+    kf.kf_qk_norm_rotate(qkv=rows, n_heads=H, n_kv_heads=kv, head_dim=d, q=q, k=k, v=v, norm_mode=kf.KF_NORM_RMS, q_weight=qw, k_weight=kw, eps=eps,
+                         rotary_dims=d, rotary_style=kf.KF_ROTARY_HALVES if halves else kf.KF_ROTARY_PAIRS)
+    wide = lambda t: t.double().cpu().numpy()                                              # noqa: E731
+    want = ref.norm_rotate(wide(rows), H, kv, d, np.arange(n)[None], wide(qw), wide(kw), True, np.float64(np.float32(eps)), d, 10000.0, halves)
+    for got, w in zip((q, k), want):
+        big = np.abs(w).max(-1, keepdims=True)
+        assert big.max() > 1.0
+        err = np.abs(wide(got) - w)
+        assert (err <= U16 * np.abs(w) + 2.0 ** -25 + 2.0 ** -20 * big).all(), (err / big).max()
+    assert torch.equal(v, x.view(1, n, H + 2 * kv, d)[:, :, H + kv:].transpose(1, 2).half())
+
+
+def test_norm_of_rows_that_are_not_finite():
+    """A NaN makes its row NaN; an infinity makes its own feature NaN and the others 0, as the formula has it; neighbouring rows do not notice."""
+    d = 128
+    for dtype in (torch.float16, torch.bfloat16):
+        x = torch.randn(1, 2, 4, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1)).to(dtype)
+        clean = x.clone()
+        x[0, 0, 0, 5], x[0, 1, 2, 7] = float("nan"), float("inf")
+        outs = []
+        for rows in (clean, x):
+            q, k = torch.empty(1, 2, 2, d, dtype=torch.float16, device=DEV), torch.empty(1, 1, 2, d, dtype=torch.float16, device=DEV)
+            kf.kf_qk_norm_rotate(qkv=rows.view(1, 2, -1), n_heads=2, n_kv_heads=1, head_dim=d, q=q, k=k, norm_mode=kf.KF_NORM_RMS, eps=0.0)
+            outs.append((q, k))
+        (q0, k0), (q, k) = outs
+        assert torch.isnan(q[0, 0, 0]).all() and torch.equal(q[0, 1], q0[0, 1]) and torch.equal(q[0, 0, 1], q0[0, 0, 1]) and torch.equal(k[0, 0, 0], k0[0, 0, 0])
+        assert torch.isnan(k[0, 0, 1, 7]) and (torch.cat([k[0, 0, 1, :7], k[0, 0, 1, 8:]]) == 0).all()
