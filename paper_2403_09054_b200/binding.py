@@ -272,12 +272,12 @@ def kf_packed_scratch_bytes(*, batch, n_heads, head_dim, budget_k, n_kv_heads=0)
 def kf_decode_step_packed(*, batch, n_heads, head_dim, budget_k, recent_w, layer, position, tau, cache, pos, acc, length,
                           q, knew, vnew, out, n_kv_heads=0, score_out=None, slot_out=None, row_out=None, noise_seed=0,
                           noise_mode=KF_NOISE_GUMBEL, noise_const=0.5772, noise_mu=0.5772, noise_sigma=1.2825,
-                          bias_mode=KF_BIAS_NONE, alibi_slopes_dev=None, logit_scale=0.0, scratch=None, stream=None, debug_fail_first_wait=0):
+                          bias_mode=KF_BIAS_NONE, alibi_slopes_dev=None, logit_scale=0.0, scratch=None, stream=None):
     """One generation step over a cache in 4 bits (kf_pack_cache), all state in the caller's tensors.  `scratch`: a uint8 CUDA tensor of
     kf_packed_scratch_bytes(...) bytes; without one torch's allocator provides it for the call."""
     _check(_kf_torch.decode_step_packed(batch, n_heads, n_kv_heads, head_dim, budget_k, recent_w, layer, position, noise_mode, bias_mode, tau, noise_seed,
                                         logit_scale, noise_const, noise_mu, noise_sigma, alibi_slopes_dev, cache, pos, acc, length, q, knew, vnew, out,
-                                        score_out, slot_out, row_out, scratch, stream, debug_fail_first_wait), "kf_decode_step_packed")
+                                        score_out, slot_out, row_out, scratch, stream), "kf_decode_step_packed")
 
 
 def kf_qk_norm_rotate(*, qkv, n_heads, n_kv_heads, head_dim, q, k, v=None, positions=None, position0=0, norm_mode=KF_NORM_NONE,

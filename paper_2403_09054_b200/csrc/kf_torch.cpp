@@ -157,7 +157,7 @@ PyObject* unpack_cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 // ---- kf_decode_step_packed
 PyObject* decode_step_packed(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  return guarded(args, n, 31, [](PyObject* const* a) -> int {
+  return guarded(args, n, 30, [](PyObject* const* a) -> int {
     kf_packed_step s{};
     s.batch = integer32(a[0]); s.n_heads = integer32(a[1]); s.n_kv_heads = integer32(a[2]); s.head_dim = integer32(a[3]);
     s.budget_k = integer32(a[4]); s.recent_w = integer32(a[5]); s.layer = integer32(a[6]); s.position = integer32(a[7]);
@@ -182,7 +182,6 @@ PyObject* decode_step_packed(PyObject*, PyObject* const* args, Py_ssize_t n) {
     void* row = address(a[27], "row_out", at::kHalf, U * 2 * d, device, true);
     const Where at_(device, a[29]);
     const Scratch scratch(a[28], need, device, at_);
-    s.debug_fail_first_wait = integer32(a[30]);
     return kf_decode_step_packed(&s, cache, pos, acc, len, q, kn, vn, out, score, slot, row, scratch.p, scratch.bytes, at_.stream.stream());
   });
 }

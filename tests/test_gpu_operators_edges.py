@@ -1,4 +1,6 @@
 """The context-free operators where a call goes wrong or its inputs are at the edge of what is allowed."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -23,7 +25,12 @@ def test_packed_step_whose_rows_do_not_arrive(batch, heads, kv, d, k):
     inputs = s.inputs(1)
     scratch = torch.zeros(kf.kf_packed_scratch_bytes(batch=batch, n_heads=heads, n_kv_heads=kv, head_dim=d, budget_k=k), dtype=torch.uint8, device=DEV)
     before = _state(s)
-    out, score, slot, _ = s.call(1, *inputs, scratch=scratch, debug_fail_first_wait=1)
+    out, score = torch.full_like(inputs[0], 9.0), torch.full((s.U, k + 1), -5.0, device=DEV)
+    slot, row = torch.full((s.U,), -7, dtype=torch.int32, device=DEV), torch.zeros(s.U, 2, d, dtype=torch.float16, device=DEV)
+    args = kf.kf_packed_step(batch=batch, n_heads=heads, n_kv_heads=kv, head_dim=d, budget_k=k, recent_w=20, layer=0, position=s.n, noise_mode=s.noise, tau=1.0,
+                             noise_seed=s.seed, debug_fail_first_wait=1)
+    tensors = (s.cache, s.pos, s.acc, s.length, *inputs, out, score, slot, row, scratch)
+    assert kf.LIB.kf_decode_step_packed(C.byref(args), *(t.data_ptr() for t in tensors), scratch.numel(), torch.cuda.current_stream().cuda_stream) == kf.KF_OK
     torch.cuda.synchronize()
     length = before[3].tolist()
     out, after = out.view(s.U, -1), _state(s)
@@ -38,12 +45,6 @@ def test_packed_step_whose_rows_do_not_arrive(batch, heads, kv, d, k):
     again, want = s.call(1, *inputs, scratch=scratch), plain.call(1, *inputs)
     assert all(torch.equal(a, b) for a, b in zip(again, want)) and torch.isfinite(again[0]).all()
     assert all(torch.equal(a, b) for a, b in zip(_state(s), _state(plain)))
-
-
-def test_packed_step_checks_the_self_test_argument():
-    s = Packed(1, 2, 2, 64, 8, 2)
-    with pytest.raises(kf.KeyformerError):
-        s.call(1, *s.inputs(1), debug_fail_first_wait=2)
 
 
 @pytest.mark.parametrize("batch,heads,kv,d,k", [(40, 4, 4, 64, 60), (1, 2, 2, 128, 2300), (2, 8, 2, 128, 90)])
