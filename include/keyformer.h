@@ -306,8 +306,8 @@ int64_t kf_launch_count(const kf_ctx* ctx);
  * Operators around the generation step that need no context.  As above: device buffers and scratch belong to the
  * caller, work is enqueued on `stream` of the current device, arguments are checked on the host before anything is
  * enqueued, and nothing is allocated.  Scratch holds nothing between calls and need not be cleared; two calls that may run at
- * the same time (other streams, other captured graphs) need scratch of their own.  No output of a call may overlap another of its
- * tensors (KF_EINVAL where a call could otherwise read what it has written).
+ * the same time (other streams, other captured graphs) need scratch of their own.  Nothing that a call
+ * writes, its scratch included, may share memory with another of its tensors (KF_EINVAL).
  * ------------------------------------------------------------------------------------------------------------------ */
 
 #define KF_TYPE_FP16 0
@@ -418,7 +418,7 @@ typedef struct kf_beam_args {
   int64_t row_stride;                 /* elements between the rows of two beams, >= vocab                         */
 } kf_beam_args;
 /*   d_logits : DEVICE [B * beams] rows;  d_scores : DEVICE fp32 [B][beams];  d_finished_opt : DEVICE uint8 [B][beams] or NULL
- *   d_out_scores fp32, d_out_parent, d_out_token int32 : DEVICE [B][take]; d_out_scores may not be d_scores
+ *   d_out_scores fp32, d_out_parent, d_out_token int32 : DEVICE [B][take]
  *   d_scratch : DEVICE, kf_beam_scratch_bytes(args) bytes, 256-byte aligned */
 size_t kf_beam_scratch_bytes(const kf_beam_args* args);
 int kf_beam_select(const kf_beam_args* args, const void* d_logits, const float* d_scores, const uint8_t* d_finished_opt,
@@ -438,7 +438,7 @@ int kf_reorder_rows(const kf_row_buffer* buffers, int32_t n_buffers, int32_t bat
 
 /* The same for the caches of a context (K, V, positions, scores, entry counts, places): its batch rows are
  * batch / beams requests of `beams` beams each (KF_EINVAL if beams does not divide the batch).  layer >= 0: that layer
- * (KF_ESTATE before its prompt phase); layer = -1: all layers, one launch. */
+ * (KF_ESTATE before its prompt phase); layer = -1: all layers, one launch.  d_parent lies outside the workspace (KF_EINVAL). */
 int kf_reorder_beams(kf_ctx* ctx, int32_t layer, int32_t beams, const int32_t* d_parent, void* stream);
 
 /* Frees host metadata.  The workspace stays with the caller. */

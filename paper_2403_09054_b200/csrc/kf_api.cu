@@ -578,6 +578,8 @@ int kf_reorder_beams(kf_ctx* ctx, int32_t layer, int32_t beams, const int32_t* d
   for (int l = layer < 0 ? 0 : layer; l < (layer < 0 ? c.n_layers : layer + 1); ++l)
     if (ctx->n_prompt[l] < 0) return KF_ESTATE;
   const Layout& L = ctx->lay;
+  const uintptr_t parents = reinterpret_cast<uintptr_t>(d_parent), ws = reinterpret_cast<uintptr_t>(ctx->ws);
+  if (parents < ws + L.total && ws < parents + (size_t)c.batch * 4) return KF_EINVAL;   // its rows would move while they are read
   const int64_t hkv = L.units / c.batch, slots = hkv * c.budget_k;
   const size_t first = layer < 0 ? 0 : (size_t)layer;
   kf::ReorderParams P{};

@@ -4,6 +4,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "kf_ops.cuh"
 #include "kf_packed.cuh"
@@ -17,6 +18,43 @@ inline bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<u
 inline bool overlap(const void* a, uint64_t n, const void* b, uint64_t m) {
   const uint64_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return a && b && x < y + m && y < x + n;
+}
+// A tensor of a call.  `rows` > 1: that many rows of `bytes`, `stride` bytes apart; what lies between them is not the call's.
+struct Range {
+  const void* at;
+  uint64_t bytes, rows = 1, stride = 0;
+  uint64_t extent() const { return (rows - 1) * stride + bytes; }
+};
+// Whether one of the rows of `a` shares a byte with the extent of `b`, given that the two extents do.
+bool touches(const Range& a, const Range& b) {
+  if (a.rows == 1 || a.stride <= a.bytes) return true;
+  const uint64_t base = reinterpret_cast<uintptr_t>(a.at), x = reinterpret_cast<uintptr_t>(b.at);
+  const uint64_t begin = x > base ? x - base : 0, end = x + b.extent() - base;     // of b, from the first row on
+  return begin % a.stride < a.bytes || end > (begin / a.stride + 1) * a.stride;
+}
+// Whether something that the call writes shares memory with another of its tensors.  Every pair of extents without a branch
+// (this runs for every token and layer): two meet where both differences are negative; one that is absent ends before everything.
+bool conflict(std::initializer_list<Range> writes, std::initializer_list<Range> reads) {
+  constexpr int MOST = 16;
+  uint64_t from[MOST], to[MOST];
+  int n = 0;
+  auto add = [&](const Range& r) {
+    from[n] = reinterpret_cast<uintptr_t>(r.at);
+    to[n] = r.at ? from[n] + r.extent() : 0;
+    ++n;
+  };
+  for (const Range& r : writes) add(r);
+  const int written = n;
+  for (const Range& r : reads) add(r);
+  uint64_t meet = 0;
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < n; ++j) meet |= (from[j] - to[i]) & (from[i] - to[j]);
+  if (meet >> 63 == 0) return false;
+  auto range = [&](int i) { return i < written ? writes.begin()[i] : reads.begin()[i - written]; };
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < n; ++j)
+      if (from[j] < to[i] && from[i] < to[j] && touches(range(j), range(i))) return true;    // only what is read may have rows
+  return false;
 }
 inline bool head_dim_ok(int d) { return d == 64 || d == 128 || d == 256; }
 
@@ -74,7 +112,8 @@ int kf_pack_cache(int64_t units, int32_t n, int32_t budget_k, int32_t head_dim, 
   if (!rows_ok(units, n, budget_k, head_dim) || !d_K || !d_V || !d_cache) return KF_EINVAL;
   if (misaligned(d_K, 16) || misaligned(d_V, 16) || misaligned(d_cache, 16) || misaligned(d_len, 4)) return KF_EINVAL;
   const uint64_t rows = (uint64_t)units * n * head_dim * 2, slots = (uint64_t)units * budget_k * kf::packed_slot_bytes(head_dim);
-  if (overlap(d_K, rows, d_cache, slots) || overlap(d_V, rows, d_cache, slots)) return KF_EINVAL;
+  if (conflict({{d_cache, slots}},
+               {{d_K, rows}, {d_V, rows}, {d_len, (uint64_t)units * 4}})) return KF_EINVAL;
   return kf::launch_pack(static_cast<const __half*>(d_K), static_cast<const __half*>(d_V), d_len, static_cast<unsigned char*>(d_cache), units, n,
                          budget_k, head_dim, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KF_OK : KF_ECUDA;
 }
@@ -84,7 +123,8 @@ int kf_unpack_cache(int64_t units, int32_t n, int32_t budget_k, int32_t head_dim
   if (!rows_ok(units, n, budget_k, head_dim) || !d_K || !d_V || !d_cache) return KF_EINVAL;
   if (misaligned(d_K, 16) || misaligned(d_V, 16) || misaligned(d_cache, 16) || misaligned(d_len, 4)) return KF_EINVAL;
   const uint64_t rows = (uint64_t)units * n * head_dim * 2, slots = (uint64_t)units * budget_k * kf::packed_slot_bytes(head_dim);
-  if (overlap(d_K, rows, d_V, rows) || overlap(d_K, rows, d_cache, slots) || overlap(d_V, rows, d_cache, slots)) return KF_EINVAL;
+  if (conflict({{d_K, rows}, {d_V, rows}},
+               {{d_len, (uint64_t)units * 4}, {d_cache, slots}})) return KF_EINVAL;
   return kf::launch_unpack(static_cast<const unsigned char*>(d_cache), d_len, static_cast<__half*>(d_K), static_cast<__half*>(d_V), units, n,
                            budget_k, head_dim, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KF_OK : KF_ECUDA;
 }
@@ -102,9 +142,12 @@ int kf_decode_step_packed(const kf_packed_step* a, void* d_cache, int32_t* d_pos
       misaligned(a->d_alibi_slopes, 4))
     return KF_EINVAL;
   const PackedLayout L = packed_layout(a);
-  const uint64_t heads = (uint64_t)L.units * L.group * a->head_dim * 2, rows = (uint64_t)L.units * a->head_dim * 2;
-  if (overlap(d_out, heads, d_q, heads) || overlap(d_out, heads, d_knew, rows) || overlap(d_out, heads, d_vnew, rows)) return KF_EINVAL;
   if (scratch_bytes < L.total) return KF_ENOSPC;
+  const uint64_t units = (uint64_t)L.units, heads = units * L.group * a->head_dim * 2, rows = units * a->head_dim * 2, slots = units * a->budget_k;
+  if (conflict({{d_cache, slots * kf::packed_slot_bytes(a->head_dim)}, {d_pos, slots * 4}, {d_acc, slots * 4}, {d_len, units * 4}, {d_out, heads},
+                {d_score_opt, (slots + units) * 4}, {d_slot_opt, units * 4}, {d_row_opt, rows * 2}, {d_scratch, L.total}},
+               {{d_q, heads}, {d_knew, rows}, {d_vnew, rows}, {a->bias_mode == KF_BIAS_ALIBI ? a->d_alibi_slopes : nullptr, (uint64_t)a->n_heads * 4}}))
+    return KF_EINVAL;
   unsigned char* scratch = static_cast<unsigned char*>(d_scratch);
   kf::PackedParams P{};
   P.cache = static_cast<unsigned char*>(d_cache);
@@ -151,8 +194,9 @@ int kf_qk_norm_rotate(const kf_qk_norm_args* a, const void* d_qkv, const void* d
   if (misaligned(d_positions, 4)) return KF_EINVAL;
   const uint64_t tokens = (uint64_t)a->batch * a->n_tokens * a->head_dim * 2, out_q = tokens * a->n_heads, out_kv = tokens * a->n_kv_heads;
   const uint64_t in = ((uint64_t)(a->batch - 1) * a->batch_stride + (uint64_t)(a->n_tokens - 1) * a->token_stride + row) * 2;
-  if (overlap(d_q, out_q, d_k, out_kv) || overlap(d_q, out_q, d_v_opt, out_kv) || overlap(d_k, out_kv, d_v_opt, out_kv) || overlap(d_qkv, in, d_q, out_q) ||
-      overlap(d_qkv, in, d_k, out_kv) || overlap(d_qkv, in, d_v_opt, out_kv))
+  const uint64_t weight = (uint64_t)a->head_dim * 2;
+  if (conflict({{d_q, out_q}, {d_k, out_kv}, {d_v_opt, out_kv}},
+               {{d_qkv, in}, {d_q_weight, weight}, {d_k_weight, weight}, {d_positions, (uint64_t)a->batch * a->n_tokens * 4}}))
     return KF_EINVAL;
   kf::QkNormParams P{};
   P.qkv = d_qkv; P.q_weight = d_q_weight; P.k_weight = d_k_weight; P.positions = d_positions;
@@ -180,11 +224,12 @@ int kf_beam_select(const kf_beam_args* a, const void* d_logits, const float* d_s
   if (misaligned(d_logits, a->logits_type == KF_TYPE_FP32 ? 4 : 2) || misaligned(d_scores, 4) || misaligned(d_out_scores, 4) ||
       misaligned(d_out_parent, 4) || misaligned(d_out_token, 4) || misaligned(d_scratch, 256))
     return KF_EINVAL;
-  const uint64_t in = (uint64_t)a->batch * a->beams * 4, out = (uint64_t)a->batch * a->take * 4;
-  if (overlap(d_scores, in, d_out_scores, out) || overlap(d_out_scores, out, d_out_parent, out) || overlap(d_out_scores, out, d_out_token, out) ||
-      overlap(d_out_parent, out, d_out_token, out))
+  const size_t need = kf_beam_scratch_bytes(a);
+  if (scratch_bytes < need) return KF_ENOSPC;
+  const uint64_t beams = (uint64_t)a->batch * a->beams, out = (uint64_t)a->batch * a->take * 4, size = a->logits_type == KF_TYPE_FP32 ? 4 : 2;
+  if (conflict({{d_out_scores, out}, {d_out_parent, out}, {d_out_token, out}, {d_scratch, need}},
+               {{d_logits, a->vocab * size, beams, a->row_stride * size}, {d_scores, beams * 4}, {d_finished_opt, beams}}))
     return KF_EINVAL;
-  if (scratch_bytes < kf_beam_scratch_bytes(a)) return KF_ENOSPC;
   kf::BeamParams P{};
   bool wide = false;
   const int64_t rows = (int64_t)a->batch * a->beams;

@@ -6,6 +6,8 @@ import pytest
 import torch
 
 import paper_2403_09054_b200 as kf
+import workloads as W
+from tests import lockstep
 from tests import operators_reference as ref
 from tests.test_gpu_operators import DEV, U16, Packed
 
@@ -111,3 +113,45 @@ def test_norm_of_rows_that_are_not_finite():
         (q0, k0), (q, k) = outs
         assert torch.isnan(q[0, 0, 0]).all() and torch.equal(q[0, 1], q0[0, 1]) and torch.equal(q[0, 0, 1], q0[0, 0, 1]) and torch.equal(k[0, 0, 0], k0[0, 0, 0])
         assert torch.isnan(k[0, 0, 1, 7]) and (torch.cat([k[0, 0, 1, :7], k[0, 0, 1, 8:]]) == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------ shared memory between a call's tensors
+
+def test_inputs_may_share_memory_and_outputs_may_lie_between_rows():
+    """What the refusals leave open: one row as query, key and value, and outputs in the unused columns of strided logits."""
+    a, b = (Packed(1, 2, 2, 64, 30, 5, seed=15) for _ in range(2))
+    row = a.inputs(1)[0]
+    got = a.call(1, row, row, row)
+    assert all(torch.equal(x, y) for x, y in zip(got, b.call(1, row, row.clone(), row.clone())))
+    wide = torch.randn(2, 3, 600, device=DEV, generator=torch.Generator(device=DEV).manual_seed(4))
+    scores = torch.zeros(2, 3, device=DEV)
+    make = lambda: [torch.zeros(2, 5, dtype=t, device=DEV) for t in (torch.float32, torch.int32, torch.int32)]        # noqa: E731
+    want = make()
+    kf.kf_beam_select(logits=wide[..., :500], scores=scores, out_scores=want[0], out_parent=want[1], out_token=want[2])
+    spare = wide[0, 1, 500:]                                              # 100 words behind a row
+    inside = [spare[:10].view(2, 5), spare[20:30].view(torch.int32).view(2, 5), spare[90:].view(torch.int32).view(2, 5)]
+    kf.kf_beam_select(logits=wide[..., :500], scores=scores, out_scores=inside[0], out_parent=inside[1], out_token=inside[2])
+    assert all(torch.equal(x, y) for x, y in zip(inside, want))
+
+
+def test_calls_refuse_tensors_that_share_memory():
+    s = Packed(1, 1, 1, 64, 8, 2)
+    q, _, _ = s.inputs(1)
+    row = torch.zeros(1, 2, 64, dtype=torch.float16, device=DEV)
+    with pytest.raises(kf.KeyformerError):                                # the quantised row in place of the row
+        kf.kf_decode_step_packed(batch=1, n_heads=1, head_dim=64, budget_k=8, recent_w=2, layer=0, position=s.n, tau=1.0, cache=s.cache, pos=s.pos, acc=s.acc,
+                                 length=s.length, q=q, knew=row[:, 0], vnew=row[:, 1], out=torch.empty_like(q), row_out=row)
+    logits, scores = torch.zeros(2, 3, 50, device=DEV), torch.zeros(2, 3, device=DEV)
+    with pytest.raises(kf.KeyformerError):
+        kf.kf_beam_select(logits=logits, scores=scores, out_scores=torch.empty_like(scores), out_parent=scores.view(torch.int32),
+                          out_token=torch.empty_like(scores, dtype=torch.int32))
+    with pytest.raises(kf.KeyformerError):
+        x = torch.zeros(1, 4, 192, dtype=torch.float16, device=DEV)
+        k = torch.zeros(1, 1, 4, 64, dtype=torch.float16, device=DEV)
+        kf.kf_qk_norm_rotate(qkv=x, n_heads=1, n_kv_heads=1, head_dim=64, q=torch.empty_like(k), k=k, positions=k.view(-1)[:8].view(torch.int32).view(1, 4))
+    wl = W.Workload("beams", 1, 4, 2, 64, 70, 40, 8, 8, data_seed=2, noise_seed=5)
+    ctx = lockstep.make_gpu(wl)
+    ctx.kf_prefill_score_prune(0, *W.make_prompt(wl, 0, DEV))
+    with pytest.raises(kf.KeyformerError):                                # the parents inside the context's own state
+        ctx.kf_reorder_beams(0, ctx.kf_view_state(0)[4].view(-1)[:4].view(2, 2))
+    ctx.kf_destroy()

@@ -4,7 +4,7 @@ import ctypes as C
 import pytest
 
 import paper_2403_09054_b200 as kf
-from tests.test_operators_cpu import FAR, _step
+from tests.test_operators_cpu import FAR, _beam, _norm, _step
 
 
 @pytest.mark.parametrize("value", [-1, 2])
@@ -12,3 +12,56 @@ def test_packed_step_self_test_argument(value):
     a = _step(debug_fail_first_wait=value)
     assert kf.LIB.kf_packed_scratch_bytes(C.byref(a)) == 0
     assert kf.LIB.kf_decode_step_packed(C.byref(a), *FAR[:8], None, None, None, FAR[11], 1 << 30, None) == kf.KF_EINVAL
+
+
+def _overlaps(call, sizes, written, base=FAR[1:]):
+    """For every pair of which one is written: the second placed on the first's last byte's 256 bytes, or over its start, is refused."""
+    for i, a in enumerate(sizes):
+        for j, b in enumerate(sizes):
+            if i == j or not (i in written or j in written):
+                continue
+            for at in (base[i] + max(0, a - 1) // 256 * 256, base[i] - max(0, b - 1) // 256 * 256):      # the last 256 bytes of a, or the last of b on a
+                p = list(base[:len(sizes)])
+                p[j] = at
+                assert call(p) == kf.KF_EINVAL, (i, j, hex(at))
+
+
+def test_packed_step_refuses_what_it_would_write_into_another_tensor():
+    slopes = FAR[13]
+    a = _step(batch=2, n_heads=8, n_kv_heads=4, head_dim=64, budget_k=32, bias_mode=1, d_alibi_slopes=slopes)
+    need = kf.LIB.kf_packed_scratch_bytes(C.byref(a))
+    U, d, k = 8, 64, 32
+    sizes = [U * k * 80, U * k * 4, U * k * 4, U * 4, 2 * U * d * 2, U * d * 2, U * d * 2, 2 * U * d * 2, U * (k + 1) * 4, U * 4, U * 2 * d * 2, need]
+    written = {0, 1, 2, 3, 7, 8, 9, 10, 11}
+    _overlaps(lambda p: kf.LIB.kf_decode_step_packed(C.byref(a), *p, need, None), sizes, written)
+    for i in written:                                    # the slopes under an output
+        p = FAR[:12]
+        p[i] = slopes
+        assert kf.LIB.kf_decode_step_packed(C.byref(a), *p, need, None) == kf.KF_EINVAL
+
+
+def test_norm_rotate_refuses_outputs_over_its_inputs():
+    a = _norm()                                          # 2 x 3 tokens, 4 + 2 heads of 64
+    sizes = [2 * 3 * 512 * 2, 128, 128, 24, 6 * 4 * 64 * 2, 6 * 2 * 64 * 2, 6 * 2 * 64 * 2]
+    _overlaps(lambda p: kf.LIB.kf_qk_norm_rotate(C.byref(a), *p, None), sizes, {4, 5, 6})
+
+
+def test_beam_select_refuses_outputs_over_its_inputs():
+    a = _beam(batch=40, beams=3, vocab=1000, row_stride=1000, take=6)
+    need = kf.LIB.kf_beam_scratch_bytes(C.byref(a))
+    _overlaps(lambda p: kf.LIB.kf_beam_select(C.byref(a), *p, need, None), [120 * 2000, 480, 120, 960, 960, 960, need], {3, 4, 5, 6})
+    # between rows that lie apart there is room: only what touches a row is refused
+    a = _beam(batch=40, beams=3, vocab=1000, row_stride=4000, take=6)
+    need = kf.LIB.kf_beam_scratch_bytes(C.byref(a))
+    for off in (0, 1996, 7044, 119 * 8000 + 1996):       # a row's first and last words, the next row's first, the last row's last
+        p = FAR[:7]
+        p[3] = FAR[0] + off
+        assert kf.LIB.kf_beam_select(C.byref(a), *p, need, None) == kf.KF_EINVAL, off
+
+
+def test_row_conversions_refuse_a_count_that_they_would_overwrite():
+    K, V, cache, length = FAR[:4]
+    for at in (cache, cache + 2 * 4 * 80 - 4):
+        assert kf.LIB.kf_pack_cache(2, 3, 4, 64, K, V, at, cache, None) == kf.KF_EINVAL
+    for at in (K, K + 2 * 3 * 128 - 4, V):
+        assert kf.LIB.kf_unpack_cache(2, 3, 4, 64, cache, at, K, V, None) == kf.KF_EINVAL
