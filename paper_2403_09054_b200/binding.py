@@ -7,6 +7,7 @@ no fallback: if the library cannot be loaded, importing this module fails.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
 
 import numpy as np
@@ -159,9 +160,24 @@ def _load() -> C.CDLL:
 
 LIB = _load()
 LIB_PATH = _build.LIB
-if not os.path.exists(_build.TORCH_LIB):
-    _build.build_torch()
-from . import _kf_torch  # noqa: E402  (links against the library loaded above)
+
+
+class _TorchSide:
+    """Stands for the compiled extension until a call first needs it: the context's calls go through ctypes alone and do not depend on it."""
+
+    def __getattr__(self, name):
+        global _kf_torch
+        path = _build.torch_lib()
+        if not os.path.exists(path):
+            _build.build_torch()
+        spec = importlib.util.spec_from_file_location("_kf_torch", path)      # links against the library loaded above
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _kf_torch = module
+        return getattr(module, name)
+
+
+_kf_torch = _TorchSide()
 
 
 class KeyformerError(RuntimeError):

@@ -4,6 +4,7 @@ from __future__ import annotations
 import glob
 import importlib.util
 import os
+import re
 import subprocess
 import sysconfig
 from concurrent.futures import ThreadPoolExecutor
@@ -13,7 +14,6 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libkeyformer_b200.so")
 TORCH_SRC = os.path.join(CSRC, "kf_torch.cpp")      # torch side of the context-free operators, a CPython extension over the library
-TORCH_LIB = os.path.join(PKG, "_kf_torch.so")
 OBJ_DIR = os.path.join(ROOT, "_build")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -35,24 +35,36 @@ def _stale() -> bool:
     return any(os.path.getmtime(f) > t for f in sources() + _headers())
 
 
-def build_torch(force: bool = False) -> str:
-    """Build the extension that hands torch tensors to the library, if it is missing or older than its sources."""
-    newest = max(os.path.getmtime(f) for f in (TORCH_SRC, os.path.join(ROOT, "include", "keyformer.h")))
-    if not force and os.path.exists(TORCH_LIB) and os.path.getmtime(TORCH_LIB) >= newest:
-        return TORCH_LIB
+def _torch_dir() -> str:
     spec = importlib.util.find_spec("torch")
     if spec is None or not spec.submodule_search_locations:
         raise RuntimeError("torch is needed to build the extension")
-    torch_dir = list(spec.submodule_search_locations)[0]
+    return list(spec.submodule_search_locations)[0]
+
+
+def torch_lib() -> str:
+    """Path of the extension for the installed torch and Python: one built for others is never loaded."""
+    with open(os.path.join(_torch_dir(), "version.py")) as f:
+        version = re.search(r"__version__ = '([^']+)'", f.read()).group(1)
+    return os.path.join(PKG, f"_kf_torch.torch-{version}.{sysconfig.get_config_var('SOABI')}.so")
+
+
+def build_torch(force: bool = False) -> str:
+    """Build the extension that hands torch tensors to the library, if it is missing or older than its sources."""
+    path = torch_lib()
+    newest = max(os.path.getmtime(f) for f in (TORCH_SRC, os.path.join(ROOT, "include", "keyformer.h")))
+    if not force and os.path.exists(path) and os.path.getmtime(path) >= newest:
+        return path
+    torch_dir = _torch_dir()
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
     inc = [os.path.join(ROOT, "include"), os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
            os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
-    tmp = TORCH_LIB + f".tmp{os.getpid()}"
+    tmp = path + f".tmp{os.getpid()}"
     subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=1"] + [f"-I{d}" for d in inc] +
                           [TORCH_SRC, "-o", tmp, "-L" + PKG, "-l:" + os.path.basename(LIB), "-L" + os.path.join(torch_dir, "lib"), "-lc10", "-lc10_cuda",
                            "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"])
-    os.replace(tmp, TORCH_LIB)
-    return TORCH_LIB
+    os.replace(tmp, path)
+    return path
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -1,10 +1,16 @@
 """Refusals of the context-free operators that need no device, beyond tests/test_operators_cpu.py."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
+import torch
 
 import paper_2403_09054_b200 as kf
 from tests.test_operators_cpu import FAR, _beam, _norm, _step
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.mark.parametrize("value", [-1, 2])
@@ -65,3 +71,37 @@ def test_row_conversions_refuse_a_count_that_they_would_overwrite():
         assert kf.LIB.kf_pack_cache(2, 3, 4, 64, K, V, at, cache, None) == kf.KF_EINVAL
     for at in (K, K + 2 * 3 * 128 - 4, V):
         assert kf.LIB.kf_unpack_cache(2, 3, 4, 64, cache, at, K, V, None) == kf.KF_EINVAL
+
+
+def _python(code):
+    return subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+
+
+def test_the_extension_is_loaded_by_the_first_operator_call_only():
+    """Importing the package and the context's calls need neither the extension nor a compiler for it; an operator call without it fails loudly."""
+    r = _python("""
+import sys, os
+import paper_2403_09054_b200 as kf
+from paper_2403_09054_b200 import binding
+assert "_kf_torch" not in sys.modules and type(binding._kf_torch) is binding._TorchSide
+cfg, keep = kf.make_config(n_layers=1, batch=1, n_heads=1, head_dim=64, budget_k=4, recent_w=1, max_prompt_len=8, gen_len_T=1)
+assert kf.kf_workspace_bytes(cfg) > 0 and kf.kf_packed_slot_bytes(64) == 80
+os.environ["CXX"] = "false"
+here = binding._build.torch_lib
+binding._build.torch_lib = lambda: here() + ".none"
+try:
+    kf.kf_pack_cache(K=None, V=None, cache=None)
+except Exception as e:
+    print(type(e).__name__)
+binding._build.torch_lib = here
+try:
+    kf.kf_pack_cache(K=None, V=None, cache=None)
+except ValueError:
+    print("refused by", type(binding._kf_torch).__name__)
+""")
+    assert r.returncode == 0, r.stderr
+    assert r.stdout.split("\n")[:2] == ["CalledProcessError", "refused by module"], r.stdout
+
+
+def test_the_extension_is_one_of_the_installed_torch():
+    assert f"torch-{torch.__version__}." in kf.binding._build.torch_lib()
