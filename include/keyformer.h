@@ -369,7 +369,8 @@ typedef struct kf_packed_step {
  * and every entry of a full unit is inside the recent window, outputs and scores are as ever, but the new row is not stored and
  * the unit's d_slot_opt entry is KF_EBOUNDS.  A unit whose rows did not arrive within the kernel's bounded wait keeps its state
  * (cache, positions, scores, count): its rows of d_out and its z are NaN, and its d_slot_opt entry is KF_ETIMEOUT.  Scores in d_acc
- * are not negative (sums of softmax values).  A non-finite value in a cached row makes the output of its unit NaN. */
+ * are not negative (sums of softmax values).  A group of a cached K row that is not finite makes the unit's rows of d_out NaN, and what
+ * becomes of its scores is not specified; a group of a V row makes its own 32 features of them NaN and nothing else. */
 size_t kf_packed_scratch_bytes(const kf_packed_step* args);   /* 0 if the arguments are invalid */
 int kf_decode_step_packed(const kf_packed_step* args, void* d_cache, int32_t* d_pos, float* d_acc, int32_t* d_len,
                           const void* d_q, const void* d_knew, const void* d_vnew, void* d_out, float* d_score_opt,

@@ -69,6 +69,37 @@ def test_packed_step_without_an_entry_to_evict(batch, heads, kv, d, k):
     assert torch.equal(s.acc, state[2] + score[:, :k])
 
 
+@pytest.mark.parametrize("d,group", [(64, 1), (128, 4), (256, 8), (128, 2)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_packed_step_with_cached_rows_that_are_not_finite(d, group, bad):
+    """A K row makes its unit's outputs NaN, a V row its own 32 features of them; nothing else changes by a bit."""
+    k, at = 700, 389
+    make = lambda: Packed(1, 3 * group, 3, d, k, 100, seed=33)             # noqa: E731
+    s, clean = make(), make()
+    K, V = (torch.zeros(3, 1, d, dtype=torch.float16, device=DEV) for _ in range(2))
+    kf.kf_unpack_cache(cache=s.cache[:, at:at + 1].contiguous(), K=K, V=V)
+    K[0, 0, 5], V[1, 0, 40] = bad, bad
+    one = torch.zeros(3, 1, 5 * d // 4, dtype=torch.uint8, device=DEV)
+    kf.kf_pack_cache(K=K, V=V, cache=one)
+    clean.cache[2, at] = one[2, 0]                                         # unit 2: the same row, packed once more
+    s.cache[:, at] = one[:, 0]
+    clean.cache[1, at, :d // 2], clean.cache[1, at, d:9 * d // 8] = one[1, 0, :d // 2], one[1, 0, d:9 * d // 8]      # unit 1: its K row too
+    keep = [f for f in range(d // 32) if f != 1]
+    v_codes, v_groups = clean.cache[1, at, d // 2:d].view(-1, 16), clean.cache[1, at, 9 * d // 8:].view(-1, 4)
+    v_codes[keep], v_groups[keep] = one[1, 0, d // 2:d].view(-1, 16)[keep], one[1, 0, 9 * d // 8:].view(-1, 4)[keep]
+    inputs = s.inputs(1)
+    got, want = s.call(1, *inputs), clean.call(1, *inputs)
+    out, ref_out = (t[0].view(3, group, d) for t in (got, want))
+    assert torch.isnan(out[0]).all()
+    assert torch.isnan(out[1, :, 32:64]).all()
+    rest = torch.ones(d, dtype=torch.bool, device=DEV)
+    rest[32:64] = False
+    assert torch.equal(out[1][:, rest], ref_out[1][:, rest]) and torch.equal(out[2], ref_out[2]) and torch.isfinite(ref_out).all()
+    for u in (1, 2):
+        assert torch.equal(got[1][u], want[1][u]) and got[2][u] == want[2][u]
+        assert torch.equal(s.acc[u], clean.acc[u]) and torch.equal(s.pos[u], clean.pos[u])
+
+
 # ------------------------------------------------------------------------------------------------ norm and rotation
 
 @pytest.mark.parametrize("d,halves", [(64, True), (128, False), (256, True)])
