@@ -294,7 +294,8 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
 
     // ---- per logit (a lane owns slots `lane` and `lane` + 32): bias, noise, the two running softmaxes.  The output weights are taken
     //      against a reference that moves only when a round exceeds it by 2^8, so that the accumulators are hardly ever
-    //      rescaled (binary16 holds weights up to 2^8, the sums are binary32).
+    //      rescaled, and times 2^7: binary16 holds them up to 2^15, and down to 2^-32 of the reference (a warp may walk 2^18 slots, whose
+    //      small weights count together).  The sums are binary32.
     float scale_o[G];
     bool moved = false;
 #pragma unroll
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
       for (int sub = 0; sub < 2; ++sub) {
         const bool valid = sub * TILE + lane < rows;
         ey += valid ? fast_exp2((y[sub] - my_new) * LOG2E) : 0.f;
-        const float px = valid ? fast_exp2((x[sub] - m_x[g]) * LOG2E) : 0.f;
+        const float px = valid ? fast_exp2(fmaf(x[sub] - m_x[g], LOG2E, 7.f)) : 0.f;
         const __half hi = __float2half_rn(px);
         sh_p[warp][g][sub * TILE + p_at] = hi;
         sh_p[warp][G + g][sub * TILE + p_at] = __float2half_rn(px - __half2float(hi));
@@ -424,7 +425,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
 #pragma unroll
     for (int wi = 0; wi < NW; ++wi) {
       const float l = sh_l[wi][g] + (COLS > G ? sh_l[wi][COLS - G + g] : 0.f);
-      const float f = l > 0.f ? fast_exp2((sh_m[wi][g] - M) * LOG2E) : 0.f;
+      const float f = l > 0.f ? fast_exp2((sh_m[wi][g] - M) * LOG2E) * 0x1p-7f : 0.f;   // and the weights' 2^7 off again
       L = fmaf(l, f, L);
       if (sh_ly[wi][g] > 0.f) LY = fmaf(sh_ly[wi][g], fast_exp2((sh_my[wi][g] - MY) * LOG2E), LY);
       sh_f[wi][g] = f;

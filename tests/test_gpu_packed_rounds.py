@@ -85,3 +85,29 @@ def test_output_references_move_in_later_rounds(d, group):
     assert (moved > 40).all(), moved
     assert (before.sum((0, 1)) > 3e-3 * total.sum((0, 1, 2))).all()
     s.step(1)
+
+
+def test_many_small_weights_count_together():
+    """33 million entries, one in each warp 2^25.5 times as heavy as the others: those are 0.3 % of the output's weight, and all of its value."""
+    d, k = 64, 1 << 25
+    per = slots_per_split(1, 1, 1, d, k)
+    warps = k // per * WARPS
+    assert k % per == 0 and per // WARPS == 1 << 17
+    row = lambda kv: torch.full((1, 1, d), kv, dtype=torch.float16, device=DEV)            # noqa: E731
+    slots = [torch.zeros(1, 1, 80, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    kf.kf_pack_cache(K=row(0.0), V=row(8.0), cache=slots[0])               # constant groups are exact
+    kf.kf_pack_cache(K=row(2.21), V=row(0.0), cache=slots[1])
+    cache = slots[0].repeat(1, k, 1)
+    cache.view(k // per, per // SPAN, SPAN, 80)[:, :WARPS, 5] = slots[1][0, 0]
+    logit = float(row(2.21)[0, 0, 0]) * d / 8.0
+    pos = torch.arange(k, dtype=torch.int32, device=DEV).view(1, k)
+    acc, length = torch.zeros(1, k, device=DEV), torch.full((1,), k, dtype=torch.int32, device=DEV)
+    out, q = torch.zeros(1, 1, d, dtype=torch.float16, device=DEV), torch.ones(1, 1, d, dtype=torch.float16, device=DEV)
+    kf.kf_decode_step_packed(batch=1, n_heads=1, head_dim=d, budget_k=k, recent_w=10, layer=0, position=k, tau=1.0, cache=cache, pos=pos, acc=acc, length=length,
+                             q=q, knew=row(0.0), vnew=row(8.0), out=out, noise_mode=kf.KF_NOISE_NONE)
+    light = (k - warps + 1) * math.exp(-logit)
+    want = 8.0 * light / (warps + light)
+    # a weight is off by 2^-32 of its warp's largest (half a step of the smallest binary16 numbers, times 2^-7), by 2^-22 of the exponent's 26 and in its
+    # logit by 72 2^-23 of 18; the sums by less, the output by a rounding
+    off = 8.0 * per / WARPS * 2.0 ** -32 + want * (26 * 2.0 ** -22 + 72 * 2.0 ** -23 * 18 + 2.0 ** -20 + 2.0 ** -11)
+    assert want > 0.02 and (out.double() - want).abs().max() <= off, (out.double() - want).abs().max()
