@@ -233,9 +233,10 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
   // With several heads their noise and softmaxes fill the instruction cache: the two tiles share their instructions (37.6 -> 35.9 us
   // for 256 caches with four heads; with one head unrolled tiles overlap better, 85 against 88 us for 1024 caches).
   constexpr int TILES_UNROLLED = G == 1 ? 2 : 1;
-  bool failed = false;
+  bool failed = P.first_wait_limit == 0 && rounds > 0;       // the self-test: as if the first wait had run out
+  const int last = failed ? 0 : rounds;
   int it = 0;
-  for (; it < rounds; ++it, y_out += NW * SPAN) {
+  for (; it < last; ++it, y_out += NW * SPAN) {
     const int rows = row_end - (first + it * NW * SPAN);             // may exceed SPAN
     int pj[2];
 #pragma unroll
@@ -255,7 +256,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
 #pragma unroll(TILES_UNROLLED)
     for (int sub = 0; sub < 2; ++sub) {
       if (sub * TILE >= rows) break;
-      const bool ok = mbar_wait_bounded(bars + sub, (uint32_t)(it & 1), it == 0 ? P.first_wait_limit : DECODE_WAIT_LIMIT);
+      const bool ok = mbar_wait_bounded(bars + sub, (uint32_t)(it & 1));
       if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
       const unsigned char* buf = ring + sub * TILE_BYTES;
 #pragma unroll
@@ -388,7 +389,7 @@ __global__ void __launch_bounds__(NW * 32, resident_ctas<D, G>()) packed_stream_
         }
       }
       __syncwarp();   // the buffer has been read by every lane
-      if (it + 1 < rounds) issue(it + 1, sub);
+      if (it + 1 < last) issue(it + 1, sub);
     }
   }
   if (failed) {
