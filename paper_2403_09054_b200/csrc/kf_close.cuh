@@ -1,7 +1,7 @@
 // The closing stage of a generation step, shared by the kernels that follow a streaming kernel: merge the split
 // partials, normalise the scores, add them into f_theta, pick the entry to evict and write the new token's row into
 // the freed slot.  PARAMS is DecodeParams (binary16 rows) or a type derived from it that brings a row format of its
-// own: the functions named close_* below are what differs between the two.
+// own: the struct CloseRow is what differs between the two.
 #pragma once
 
 #include "kf_decode.cuh"

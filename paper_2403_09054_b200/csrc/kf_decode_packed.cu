@@ -16,9 +16,12 @@
 // lane owns two slots in the per-logit work, whose chains (generator, logarithms, exponentials) then overlap, and the
 // bookkeeping of the running softmaxes is paid once for 64 slots.  A buffer is refilled as soon as its values have been used.
 //
-// What bounds it: issue.  1024 caches of 2048 slots (d 128, one head each; 361 MB): 85 us a call, of which 76 are the streaming kernel
-// (4.7 TB/s; 846 warp instructions per 32 slots, 480 of them conversions; issue slots 63 %) and 9 the closing one; the bytes alone
-// would take 56.  32 caches of 4096: 13 us.  256 caches of 2000 slots on average half full, four heads each: 36 us, each further
+// What bounds it: latency, with nothing saturated.  1024 caches of 2048 slots (d 128, one head each; 361 MB): 86 us a call, of which 77 are
+// the streaming kernel (4.7 TB/s) and 9 the closing one; the bytes alone would take 56, and its 846 warp instructions per 32 slots (480 of
+// them conversions) about 49 if every issue slot were used.  By counters (half that size): issue slots 63 %, ALU 46 %, FMA pipes 47 %, DRAM
+// 45 %, tensor pipe 20 %; a scheduler has 3.7 warps, and of the 5.9 cycles between two instructions of a warp 1.1 are the fixed latency
+// of the one before, 1.0 other warps' turns, 0.7 memory, 0.7 a busy pipe, 0.5 dispatch.  32 caches of 4096: 13 us, one round per warp, a chain
+// of dependent latencies.  256 caches of up to 1999 slots, four heads each: 36 us half full, 48 full (issue slots 58 %, DRAM 24 %), each further
 // head adding its noise (90 instructions per 32 slots) and softmaxes.  Measured and not taken: tiles staged in registers (106), the
 // closing stage inside the streaming CTA with one CTA per cache (101), the heads as a loop (37.4, and 42 instead of 40 at d 256).
 #include "kf_close.cuh"
@@ -47,7 +50,8 @@ __device__ __forceinline__ float ln_atanh(float x) {
   return fmaf((float)e, LN2, f - t * (f - r));
 }
 __device__ __forceinline__ float packed_gumbel(const PackedParams& P, uint32_t b, uint32_t lh, uint32_t i, uint32_t j) {
-  // the outer logarithm may be the fast one: its error is absolute, below 1e-6 even for the largest variates
+  // the outer logarithm may be the fast one.  Over all 2^23 uniforms the variate is off by at most 1.8e-6 (the largest, 16.6; the spacing of
+  // binary32 there is 1.9e-6) and by 2.4e-7 where it lies within 1 of zero.
   return -LN2 * __log2f(-ln_atanh(uniform_from_word(noise_word(P.pk, b, lh, i, j))));
 }
 
@@ -139,8 +143,9 @@ __device__ __forceinline__ void shared_words(uint32_t (&w)[N], const unsigned ch
   }
 }
 
-// CTAs an SM holds: the register limit that goes with them.  At d 128 and one head: 4 (111 registers) 85 us, 3 90, 5 (96 registers,
-// spilling) 102.  d 256 needs 80 KB of buffers a CTA, eight heads 150 registers.
+// CTAs an SM holds: the register limit that goes with them.  At d 128 and one head: 4 (117 registers) 86 us, 3 90, 5 (96 registers,
+// spilling) 102.  d 256 needs 80 KB of buffers a CTA (187 to 245 registers), eight heads 159 to 168 registers.  Four heads at d 128 meet the
+// limit of 128 and spill two or three registers.
 template <int D, int G>
 constexpr int resident_ctas() { return D == 256 ? 2 : (G == 8 ? 3 : 4); }
 
@@ -524,6 +529,10 @@ void decode_packed_plan(int units, int budget_k, int head_dim, int* splits_out, 
   constexpr int ROUND = NW * SPAN / TILE;   // tiles of a round of the CTA's warps
   // Many caches: about three waves of CTAs (two CTAs for each of 1024 caches; one each 86.7 us, two 86.6, three 90.3).  Few: as many
   // CTAs as give every warp at least one round (32 caches of 4096: 16 CTAs each 13.7 us, 10 15.0, 8 17.3).
+  // The rule does not look at the heads per cache nor at d.  256 full caches of 1999 slots in 1, 2, 4 and 8 (the rule's) CTAs: four heads, d 64 60, 37, 38,
+  // 39 us, d 128 76, 47, 47, 48; eight heads, d 128 97, 87, 79, 77: it is within 5 % of the best (one head, d 64 28, 25, 24, 27: 11 %).  At d 256, where
+  // an SM holds two CTAs, fewer would do better: one head 50, 53, 57, 64, four 69, 73, 82, 92, eight 105, 111, 122, 130.  32 caches of
+  // 4096, 16 CTAs each (the rule's) against 8: d 128 13.0 and 16.4, four heads 18.7 and 24.9; d 256 22.7 and 20.1.
   const int target_ctas = units >= 148 ? 148 * 13 : 148 * 8;
   int splits = (target_ctas + units - 1) / units;
   splits = std::max(1, std::min(splits, std::min(MAX_SPLITS, (tiles + ROUND - 1) / ROUND)));

@@ -5,7 +5,7 @@
 // flight per thread, and a group of 32 features is two neighbouring lanes, one of which works out the K group and the other
 // the V group.  Unpacking, it owns eight of each.
 //
-// 1024 units of 2048 rows, d 128: pack 218 us, unpack 231 us, each 1.41 GB at the rate of a copy.  With eight features a thread
+// 1024 units of 2048 rows, d 128: pack 218 us, 1.41 GB at the rate of a copy, unpack 231 us, 0.94 of it.  With eight features a thread
 // packing took 325 us (four lanes worked out the same group, 250 instructions per 16 features); with a division and a reciprocal
 // each and codes shifted into place one by one 415.  Unpacking sixteen features a thread takes 286 (stores in halves of 32 bytes).
 #include "kf_packed.cuh"

@@ -5,13 +5,14 @@
 // A head's row is d / 8 neighbouring lanes with eight features each, two runs of four that are chosen so that the features
 // of a pair lie in one lane: [4 l, 4 l + 4) and [R/2 + 4 l, ...) of the rotary features for pairs (i, i + R/2), eight
 // neighbours for pairs (2i, 2i + 1) and for what does not turn.  The sum of squares takes log2(d / 8) shuffles, the rotation
-// none.  The angles of a token are shared by all of its heads: a CTA takes up to four tokens and computes their angles
+// none.  The angles of a token are shared by all of its heads: a CTA takes up to eight tokens and computes their angles
 // first, one per thread, into shared memory.  Positions reach far, so angle / 2 pi is formed and reduced in binary64; what
 // is left, at most half a turn, goes through binary32.
 //
 // 8 x 4096 tokens of 32 + 32 heads, d 128, whole heads turned (1.6 GB): 302 us = 5.3 TB/s, 0.83 of a copy; 32 tokens of 32 + 8 heads
 // 3.3 us.  What it took: angles in registers instead of shared memory for every row 908 -> 382, pairs within a lane (no
-// shuffles) 342, six rows requested ahead and streaming stores 302 (three 324, twelve 367: registers).
+// shuffles) 342, six rows requested ahead and streaming stores 302 (three 324, twelve 367: registers).  In bfloat16 the same prompt takes 341 us (halves; 325 in pairs) through the Python call, binary16 320; rows
+// whose squares leave binary32 cost a second pass of their warp, looking for them 1 % (judged row by row where they are met: 8 %).
 #include <cuda_bf16.h>
 
 #include <type_traits>
