@@ -186,3 +186,104 @@ def test_calls_refuse_tensors_that_share_memory():
     with pytest.raises(kf.KeyformerError):                                # the parents inside the context's own state
         ctx.kf_reorder_beams(0, ctx.kf_view_state(0)[4].view(-1)[:4].view(2, 2))
     ctx.kf_destroy()
+
+
+# ------------------------------------------------------------------------------------------------ streams, graphs, the largest sizes
+
+def _simple_calls():
+    """(call(stream), outputs) of every operator that needs no scratch, on inputs of its own."""
+    g = torch.Generator(device=DEV).manual_seed(8)
+    K, V = (torch.randn(3, 50, 64, device=DEV, generator=g).half() for _ in range(2))
+    cache = torch.zeros(3, 50, 80, dtype=torch.uint8, device=DEV)
+    packed = torch.zeros_like(cache)
+    kf.kf_pack_cache(K=K, V=V, cache=packed)
+    Kb, Vb = torch.zeros_like(K), torch.zeros_like(V)
+    x = torch.randn(2, 9, 4 * 64, device=DEV, generator=g).bfloat16()
+    q, k = torch.zeros(2, 2, 9, 64, dtype=torch.float16, device=DEV), torch.zeros(2, 1, 9, 64, dtype=torch.float16, device=DEV)
+    rows, parent = torch.randn(6, 4001, device=DEV, generator=g), torch.tensor([[1, 1, 0], [2, 0, 0]], dtype=torch.int32, device=DEV)
+    return [(lambda st: kf.kf_pack_cache(K=K, V=V, cache=cache, stream=st), [cache]),
+            (lambda st: kf.kf_unpack_cache(cache=packed, K=Kb, V=Vb, stream=st), [Kb, Vb]),
+            (lambda st: kf.kf_qk_norm_rotate(qkv=x, n_heads=2, n_kv_heads=1, head_dim=64, q=q, k=k, norm_mode=kf.KF_NORM_RMS, rotary_dims=32, stream=st), [q, k]),
+            (lambda st: kf.kf_reorder_rows(buffers=[rows], parent=parent, stream=st), [rows])]
+
+
+@pytest.mark.parametrize("which", [0, 1, 2, 3])
+def test_calls_without_scratch_on_another_stream_and_replayed(which):
+    call, outs = _simple_calls()[which]
+    start = [t.clone() for t in outs]
+
+    def reset():
+        for t, old in zip(outs, start):
+            t.copy_(old)
+    call(None)
+    want = [t.clone() for t in outs]
+    assert any(not torch.equal(a, b) for a, b in zip(want, start))
+    reset()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    call(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    reset()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(None)
+    for _ in range(2):
+        reset()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    del graph
+
+
+@pytest.mark.parametrize("batch,heads", [(65535, 1), (1, 65535), (255, 257)])
+def test_packed_step_of_the_most_units(batch, heads):
+    """Units are independent: the largest grid gives what slices of it give.  Without noise, whose coordinates hold the batch row and the head."""
+    units, k, d = batch * heads, 3, 64
+    g = torch.Generator(device=DEV).manual_seed(6)
+    K, V = (torch.randn(units, k, d, device=DEV, generator=g).half() for _ in range(2))
+    cache = torch.zeros(units, k, 80, dtype=torch.uint8, device=DEV)
+    kf.kf_pack_cache(K=K, V=V, cache=cache)
+    pos = torch.tensor([4, 9, 7], dtype=torch.int32, device=DEV).repeat(units, 1)
+    acc = torch.rand(units, k, device=DEV, generator=g)
+    length = (torch.arange(units, device=DEV, dtype=torch.int32) % 4)
+    q, kn, vn = (torch.randn(units, d, device=DEV, generator=g).half() for _ in range(3))
+
+    def step(at, n, b, h):
+        state = [t[at:at + n].clone() for t in (cache, pos, acc, length)]
+        out, slot = torch.zeros(n, d, dtype=torch.float16, device=DEV), torch.full((n,), -9, dtype=torch.int32, device=DEV)
+        kf.kf_decode_step_packed(batch=b, n_heads=h, head_dim=d, budget_k=k, recent_w=1, layer=0, position=10, tau=1.5, cache=state[0], pos=state[1], acc=state[2],
+                                 length=state[3], q=q[at:at + n], knew=kn[at:at + n], vnew=vn[at:at + n], out=out, slot_out=slot, noise_mode=kf.KF_NOISE_NONE)
+        return state + [out, slot]
+    whole = step(0, units, batch, heads)
+    for at, n in ((0, 1), (units // 2, 300), (units - 200, 200)):
+        assert all(torch.equal(a[at:at + n], b) for a, b in zip(whole, step(at, n, n, 1)))
+    assert (whole[5] >= 0).all() and torch.isfinite(whole[4]).all()
+
+
+def test_beam_select_of_the_most_rows():
+    """65535 rows, and rows of 33 million tokens (thousands of lists per beam), against torch's own sort."""
+    logits = torch.randn(21845, 3, 5, device=DEV, generator=torch.Generator(device=DEV).manual_seed(3))
+    out = [torch.zeros(21845, 15, dtype=t, device=DEV) for t in (torch.float32, torch.int32, torch.int32)]
+    kf.kf_beam_select(logits=logits, scores=torch.zeros(21845, 3, device=DEV), out_scores=out[0], out_parent=out[1], out_token=out[2])
+    value = torch.log_softmax(logits.double(), -1).view(21845, 15)
+    mine = torch.gather(value, 1, (out[1] * 5 + out[2]).long())
+    assert (out[1] * 5 + out[2]).sort(1).values.equal(torch.arange(15, device=DEV, dtype=torch.int32).expand(21845, 15))
+    assert (mine - value.sort(1, descending=True).values).abs().max() <= 1e-6 and (mine - out[0]).abs().max() <= 2e-6
+    V, take = (1 << 25) + 3, 8
+    logits = torch.randn(1, 4, V, device=DEV, generator=torch.Generator(device=DEV).manual_seed(4)).mul_(3).half()
+    scores = torch.tensor([[-1.0, 0.0, -0.5, -9.0]], device=DEV)
+    out = [torch.zeros(1, take, dtype=t, device=DEV) for t in (torch.float32, torch.int32, torch.int32)]
+    kf.kf_beam_select(logits=logits, scores=scores, out_scores=out[0], out_parent=out[1], out_token=out[2])
+    best = []
+    for w in range(4):
+        x = logits[0, w]
+        top, at = torch.sort(x, descending=True, stable=True)              # equal values: the lower token first
+        norm = torch.logsumexp(x.double(), 0)
+        best += [(float(scores[0, w]) + float(top[i].double() - norm), -w, -int(at[i])) for i in range(take)]
+    best = sorted(best, reverse=True)[:take]
+    got = [(float(a), -int(b), -int(c)) for a, b, c in zip(*(t[0] for t in out))]
+    for (value, w, t), (mine, gw, gt) in zip(best, got):
+        # a sum of 33 million exponentials: 8192 partial sums of 8192, each within 2^-20 of its value
+        assert abs(value - mine) <= 2e-6 + 2.0 ** -23 * abs(value) and (w, t) == (gw, gt)
