@@ -12,7 +12,7 @@
 // 8 x 4096 tokens of 32 + 32 heads, d 128, whole heads turned (1.6 GB): 302 us = 5.3 TB/s, 0.83 of a copy; 32 tokens of 32 + 8 heads
 // 3.3 us.  What it took: angles in registers instead of shared memory for every row 908 -> 382, pairs within a lane (no
 // shuffles) 342, six rows requested ahead and streaming stores 302 (three 324, twelve 367: registers).  In bfloat16 the same prompt takes 341 us (halves; 325 in pairs) through the Python call, binary16 320; rows
-// whose squares leave binary32 cost a second pass of their warp, looking for them 1 % (judged row by row where they are met: 8 %).
+// whose squares leave binary32 cost a second pass of their warp, looking for them 1 % (scaling them where they are met: 8 %).
 #include <cuda_bf16.h>
 
 #include <type_traits>
