@@ -442,6 +442,113 @@ int kf_reorder_rows(const kf_row_buffer* buffers, int32_t n_buffers, int32_t bat
  * (KF_ESTATE before its prompt phase); layer = -1: all layers, one launch.  d_parent lies outside the workspace (KF_EINVAL). */
 int kf_reorder_beams(kf_ctx* ctx, int32_t layer, int32_t beams, const int32_t* d_parent, void* stream);
 
+/* ---- Prompts of different lengths, one after the other without padding.  Sequence s owns the rows d_begin[s] .. d_begin[s + 1] - 1
+ * of q, k, v and out; within it, in every head, as kf_prefill_attend:
+ *   out_i = sum_{j <= i} softmax_j(x_ij) v_j,   x_ij = logit_scale q_i k_j (- slope_h (i - j) with KF_BIAS_ALIBI)
+ * Query head h reads key/value head h / (H / Hkv).  Rows of no sequence are left as they were, and what they hold reaches no
+ * output: a sequence ends where its range ends, whatever stands behind it.  Within a sequence a value row that is not finite may make any
+ * earlier row of the same 128 NaN.  A sequence whose range is empty or not within 0 .. tokens has no output; ranges do not descend. */
+typedef struct kf_ragged_args {
+  int32_t tokens, sequences;          /* rows of q, k, v and out (<= 2^28); S (<= 2^20)                           */
+  int32_t n_heads, n_kv_heads;        /* H, Hkv: Hkv divides H                                                    */
+  int32_t head_dim, type;             /* d in {64, 128, 256}; KF_TYPE_FP16 or KF_TYPE_BF16, of all four           */
+  int32_t bias_mode;                  /* KF_BIAS_*                                                                */
+  float   logit_scale;                /* 0 => 1/sqrt(d)                                                           */
+  const float* d_alibi_slopes;        /* DEVICE [H] when bias_mode == KF_BIAS_ALIBI, else ignored                 */
+  int64_t q_token_stride, q_head_stride;      /* in elements, multiples of 8, at least d, below 2^38: any order of */
+  int64_t k_token_stride, k_head_stride;      /* heads and tokens, e.g. the rows of a projection that holds q, k   */
+  int64_t v_token_stride, v_head_stride;      /* and v, or head-major rows.  The features of a head are contiguous */
+  int64_t out_token_stride, out_head_stride;  /* rows of two (token, head) pairs may not share memory             */
+  int32_t debug_fail_first_wait;      /* self-test of the error path, see kf_config                                */
+} kf_ragged_args;
+/*   d_q, d_out : DEVICE [tokens][H] rows of d;  d_k, d_v : DEVICE [tokens][Hkv] rows of d (strides above, 16-byte aligned)
+ *   d_begin    : DEVICE int32 [S + 1]
+ * Output weights are rounded to the type of v (11 or 8 bits), the output once more; sums and references are binary32.  Rows that
+ * did not arrive within the kernel's bounded wait make the output rows that need them NaN. */
+int kf_prefill_attend_ragged(const kf_ragged_args* args, const void* d_q, const void* d_k, const void* d_v, const int32_t* d_begin,
+                             void* d_out, void* stream);
+
+/* ---- Caches in pages of 8 bits.  A page holds page_tokens consecutive tokens of a sequence for every key/value head:
+ *   d_cache : int8 [n_pages][Hkv][2][page_tokens][d]   K codes, then V codes, 16-byte aligned
+ *   d_scale : fp32 [n_pages][Hkv][2]                   a code c stands for c * scale
+ *   d_table : int32 [S][table_width]                   the pages of a sequence in order, -1 where it has none
+ *   d_length: int32 [S]                                tokens in use
+ * kf_pages_write makes scales powers of two: the smallest 2^e with max |x| <= 127 * 2^e over the rows of a page, head and side
+ * (e >= -120), c = rint(x / 2^e) (ties to even).  While a page fills its scale never shrinks; when it grows, the rows that are there already are
+ * brought to it, c <- rint(c * old / new).  As a scale at least doubles then, a row written long before is off by
+ * less than one step of the final scale.  A NaN or an infinity among the rows makes the scale NaN: everything of that page, head and side reads as NaN.
+ * Scales of another origin may be any positive numbers. */
+typedef struct kf_page_cache {
+  int32_t n_pages, page_tokens;       /* page_tokens in {16, 32, 64, 128}; n_pages * Hkv * 2 * page_tokens < 2^31 */
+  int32_t n_kv_heads, head_dim;       /* Hkv; d in {64, 128, 256}                                                  */
+  int32_t sequences, table_width;     /* S (<= 2^20), pages a sequence may have (table_width * page_tokens < 2^30)      */
+} kf_page_cache;
+
+/* Rows of tokens for kf_pages_write and kf_pages_read. */
+typedef struct kf_page_rows {
+  int32_t tokens, type;               /* rows (<= 2^28); KF_TYPE_FP16 or KF_TYPE_BF16                              */
+  int64_t k_token_stride, k_head_stride;      /* in elements, multiples of 8, at least d                          */
+  int64_t v_token_stride, v_head_stride;
+} kf_page_rows;
+/* Rows d_begin[s] .. d_begin[s + 1] - 1 of d_k and d_v become tokens d_length[s], d_length[s] + 1, ... of sequence s.
+ *   d_begin : DEVICE int32 [S + 1], not descending, or NULL: one row per sequence, row s (tokens == S)
+ * d_length is not changed (every layer of a model writes at the same place): the caller adds to it when all layers have written.
+ * The pages that are written belong to one sequence alone.  A row whose page is missing (table entry outside 0 .. n_pages - 1, or
+ * behind the table) is not written; a sequence whose d_length entry is negative is skipped. */
+int kf_pages_write(const kf_page_cache* cache, const kf_page_rows* rows, const void* d_k, const void* d_v, const int32_t* d_begin,
+                   const int32_t* d_length, const int32_t* d_table, void* d_cache, float* d_scale, void* stream);
+/* The way back: rows d_begin[s] .. of d_k and d_v are tokens d_first[s] (NULL: 0), ... of sequence s as the numbers their codes
+ * stand for, rounded once.  Rows whose page is missing are NaN; rows of no sequence are left as they were. */
+int kf_pages_read(const kf_page_cache* cache, const kf_page_rows* rows, const void* d_cache, const float* d_scale, const int32_t* d_table,
+                  const int32_t* d_begin, const int32_t* d_first, void* d_k, void* d_v, void* stream);
+
+/* One query token per sequence, the newest, over the d_length[s] tokens of its pages (its own row among them):
+ *   out = sum_j softmax_j(x_j) v_j,   x_j = logit_scale q k_j (- slope_h (length - 1 - j) with KF_BIAS_ALIBI)
+ * A sequence without tokens gets zeros; one whose length is negative or behind its table, or that needs a missing page, gets NaN. */
+typedef struct kf_pages_attend_args {
+  kf_page_cache cache;
+  int32_t n_heads, type;              /* H: Hkv divides H; of q and out: KF_TYPE_FP16 or KF_TYPE_BF16              */
+  int32_t bias_mode;                  /* KF_BIAS_*                                                                */
+  float   logit_scale;                /* 0 => 1/sqrt(d)                                                           */
+  const float* d_alibi_slopes;        /* DEVICE [H] when bias_mode == KF_BIAS_ALIBI, else ignored                 */
+  int64_t q_sequence_stride, q_head_stride;       /* in elements, multiples of 8, at least d                       */
+  int64_t out_sequence_stride, out_head_stride;   /* rows of two (sequence, head) pairs may not share memory       */
+  int32_t debug_fail_first_wait;      /* self-test of the error path, see kf_config                                */
+} kf_pages_attend_args;
+/*   d_q, d_out : DEVICE [S][H] rows of d, 16-byte aligned
+ *   d_scratch  : DEVICE, kf_pages_attend_scratch_bytes(args) bytes, 256-byte aligned (KF_ENOSPC if `scratch_bytes` is less)
+ * Rows that did not arrive within the kernel's bounded wait make the outputs that need them NaN. */
+size_t kf_pages_attend_scratch_bytes(const kf_pages_attend_args* args);   /* 0 if the arguments are invalid */
+int kf_pages_attend(const kf_pages_attend_args* args, const void* d_q, const void* d_cache, const float* d_scale, const int32_t* d_table,
+                    const int32_t* d_length, void* d_out, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/* Sequences forked, ended and grown, in place.  Sequence s goes on as a copy of what sequence p = d_parent[s] was before the call
+ * (NULL: p = s): full pages are shared; of the sequences that go on from p the first keeps its page that is filled in part, the others get a
+ * page of their own with a copy of its rows, in all layers.  p outside 0 .. S - 1 (-1): s has ended and is empty.  Then
+ * pages are added until s has room for d_grow[s] more tokens (NULL: grow); pages behind those are given back.
+ *   d_refs    : DEVICE int32 [n_pages], how many table entries name a page (plus what the caller counts: a page with
+ *               references is never handed out).  Updated; a page is free when its count is 0.
+ *   d_missing : DEVICE int32 [1], pages that could not be added because none was free or the table too narrow
+ * Free pages are handed out lowest first, in the order of sequences and of the pages of each; where there is none the table
+ * entry is -1; a copy of a page that was missing itself reads as NaN.  d_length[s] becomes the parent's length (0 for an ended one), without the room added.  A length outside 0 ..
+ * table_width * page_tokens counts as 0; negative growth counts as none.  Pages filled in part belong to one sequence alone before and after. */
+typedef struct kf_pages_update_args {
+  kf_page_cache cache;                /* S <= 8192, S * table_width <= 2^28                                       */
+  int32_t n_layers;                   /* d_cache, d_scale: [n_layers] caches one after the other; one table serves all */
+  int32_t grow;                       /* without d_grow                                                           */
+} kf_pages_update_args;
+size_t kf_pages_update_scratch_bytes(const kf_pages_update_args* args);   /* 0 if the arguments are invalid */
+int kf_pages_update(const kf_pages_update_args* args, int32_t* d_table, int32_t* d_length, int32_t* d_refs, const int32_t* d_parent,
+                    const int32_t* d_grow, void* d_cache, float* d_scale, int32_t* d_missing, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/* The rows that a selection kept into new pages: row j of (s, head) in the pages of d_new_table is token d_keep[s][head][j] in those of
+ * d_table, j < d_n_keep[s] (e.g. the positions that a layer's prompt phase kept).  The scale of a new page is the largest of those that
+ * its rows come from, c <- rint(c * old / new).  What lies behind the last row of a page is left as it was.  The new pages are none of those
+ * that the call reads.  A token outside 0 .. d_length[s] - 1, or whose page is missing, makes the scales of its new page and head NaN; a new page that is
+ * missing is not written. */
+int kf_pages_compact(const kf_page_cache* cache, int32_t keep_width, int32_t new_table_width, const int32_t* d_table, const int32_t* d_length,
+                     const int32_t* d_keep, const int32_t* d_n_keep, const int32_t* d_new_table, void* d_cache, float* d_scale, void* stream);
+
 /* Frees host metadata.  The workspace stays with the caller. */
 int kf_destroy(kf_ctx* ctx);
 

@@ -3,6 +3,8 @@ from .binding import (Keyformer, KeyformerError, kf_config, make_config, kf_work
                       kf_decode_step_static, kf_static_step, KF_STATIC_SCRATCH_BYTES,
                       kf_pack_cache, kf_unpack_cache, kf_packed_slot_bytes, kf_packed_scratch_bytes, kf_decode_step_packed, kf_packed_step,
                       kf_qk_norm_rotate, kf_qk_norm_args, kf_beam_select, kf_beam_args, kf_reorder_rows, kf_row_buffer,
+                      kf_prefill_attend_ragged, kf_ragged_args, kf_pages_write, kf_pages_read, kf_pages_attend, kf_pages_attend_scratch_bytes,
+                      kf_pages_attend_args, kf_pages_update, kf_pages_update_scratch_bytes, kf_pages_update_args, kf_pages_compact, kf_page_cache, kf_page_rows,
                       KF_TYPE_FP16, KF_TYPE_BF16, KF_TYPE_FP32, KF_NORM_NONE, KF_NORM_RMS, KF_ROTARY_PAIRS, KF_ROTARY_HALVES,
                       LIB, LIB_PATH, EXPORTS,
                       KF_OK, KF_EINVAL, KF_ENOSPC, KF_ESTATE, KF_ECUDA, KF_ETIMEOUT, KF_EBOUNDS,

@@ -30,7 +30,9 @@ EXPORTS = ("kf_workspace_bytes", "kf_create", "kf_prefill_score_prune", "kf_deco
            "kf_destroy", "kf_strerror", "kf_decode_step_static", "kf_state_bytes", "kf_export_state", "kf_import_state",
            "kf_prefill_attend", "kf_prefill_attend_score_prune", "kf_view_place", "kf_compact_layer", "kf_check_canaries", "kf_describe_decode",
            "kf_packed_slot_bytes", "kf_pack_cache", "kf_unpack_cache", "kf_packed_scratch_bytes", "kf_decode_step_packed",
-           "kf_qk_norm_rotate", "kf_beam_scratch_bytes", "kf_beam_select", "kf_reorder_rows", "kf_reorder_beams")
+           "kf_qk_norm_rotate", "kf_beam_scratch_bytes", "kf_beam_select", "kf_reorder_rows", "kf_reorder_beams",
+           "kf_prefill_attend_ragged", "kf_pages_write", "kf_pages_read", "kf_pages_attend_scratch_bytes", "kf_pages_attend",
+           "kf_pages_update_scratch_bytes", "kf_pages_update", "kf_pages_compact")
 
 
 class kf_config(C.Structure):
@@ -87,6 +89,38 @@ class kf_beam_args(C.Structure):
 
 class kf_row_buffer(C.Structure):
     _fields_ = [("d_base", C.c_void_p), ("row_bytes", C.c_int64), ("outer_stride", C.c_int64), ("outer", C.c_int32)]
+
+
+class kf_ragged_args(C.Structure):
+    _fields_ = [
+        ("tokens", C.c_int32), ("sequences", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+        ("head_dim", C.c_int32), ("type", C.c_int32), ("bias_mode", C.c_int32), ("logit_scale", C.c_float), ("d_alibi_slopes", C.c_void_p),
+        ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64),
+        ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64),
+        ("debug_fail_first_wait", C.c_int32),
+    ]
+
+
+class kf_page_cache(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("sequences", C.c_int32),
+                ("table_width", C.c_int32)]
+
+
+class kf_page_rows(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("type", C.c_int32), ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_token_stride", C.c_int64),
+                ("v_head_stride", C.c_int64)]
+
+
+class kf_pages_attend_args(C.Structure):
+    _fields_ = [
+        ("cache", kf_page_cache), ("n_heads", C.c_int32), ("type", C.c_int32), ("bias_mode", C.c_int32), ("logit_scale", C.c_float),
+        ("d_alibi_slopes", C.c_void_p), ("q_sequence_stride", C.c_int64), ("q_head_stride", C.c_int64), ("out_sequence_stride", C.c_int64),
+        ("out_head_stride", C.c_int64), ("debug_fail_first_wait", C.c_int32),
+    ]
+
+
+class kf_pages_update_args(C.Structure):
+    _fields_ = [("cache", kf_page_cache), ("n_layers", C.c_int32), ("grow", C.c_int32)]
 
 
 def _load() -> C.CDLL:
@@ -151,6 +185,20 @@ def _load() -> C.CDLL:
     lib.kf_reorder_rows.argtypes = [C.POINTER(kf_row_buffer), i32, i32, i32, vp, vp]
     lib.kf_reorder_beams.restype = C.c_int
     lib.kf_reorder_beams.argtypes = [vp, i32, i32, vp, vp]
+    cache = C.POINTER(kf_page_cache)
+    lib.kf_prefill_attend_ragged.restype = C.c_int
+    lib.kf_prefill_attend_ragged.argtypes = [C.POINTER(kf_ragged_args)] + [vp] * 6
+    lib.kf_pages_write.restype = lib.kf_pages_read.restype = C.c_int
+    lib.kf_pages_write.argtypes = lib.kf_pages_read.argtypes = [cache, C.POINTER(kf_page_rows)] + [vp] * 8
+    lib.kf_pages_attend_scratch_bytes.restype = lib.kf_pages_update_scratch_bytes.restype = szt
+    lib.kf_pages_attend_scratch_bytes.argtypes = [C.POINTER(kf_pages_attend_args)]
+    lib.kf_pages_attend.restype = C.c_int
+    lib.kf_pages_attend.argtypes = [C.POINTER(kf_pages_attend_args)] + [vp] * 7 + [szt, vp]
+    lib.kf_pages_update_scratch_bytes.argtypes = [C.POINTER(kf_pages_update_args)]
+    lib.kf_pages_update.restype = C.c_int
+    lib.kf_pages_update.argtypes = [C.POINTER(kf_pages_update_args)] + [vp] * 9 + [szt, vp]
+    lib.kf_pages_compact.restype = C.c_int
+    lib.kf_pages_compact.argtypes = [cache, i32, i32] + [vp] * 8
     lib.kf_destroy.restype = C.c_int
     lib.kf_destroy.argtypes = [vp]
     lib.kf_strerror.restype = C.c_char_p
@@ -314,6 +362,58 @@ def kf_reorder_rows(*, buffers, parent, n_layers=1, stream=None):
     """In every tensor of `buffers` (contiguous [batch * beams, ...], or [n_layers, batch * beams, ...]) row (b, i) becomes what row
     (b, parent[b, i]) was, in place; parent: int32 [batch, beams]."""
     _check(_kf_torch.reorder_rows(buffers, parent, n_layers, stream), "kf_reorder_rows")
+
+
+def kf_prefill_attend_ragged(*, q, k, v, begin, out, bias_mode=KF_BIAS_NONE, alibi_slopes_dev=None, logit_scale=0.0, debug_fail_first_wait=0, stream=None):
+    """Causal attention over prompts that lie one after the other: sequence s has rows begin[s] .. begin[s + 1] - 1 (int32 [S + 1]) of q, out
+    [T, H, d] and k, v [T, Hkv, d] (fp16 or bf16, contiguous features, any strides of tokens and heads: views of a projection's rows, or
+    ``x[0].transpose(0, 1)`` of kf_qk_norm_rotate's head-major rows)."""
+    _check(_kf_torch.attend_ragged(q, k, v, begin, out, bias_mode, alibi_slopes_dev, logit_scale, debug_fail_first_wait, stream), "kf_prefill_attend_ragged")
+
+
+def kf_pages_write(*, k, v, length, table, cache, scale, begin=None, stream=None):
+    """Rows begin[s] .. begin[s + 1] - 1 of k, v [T, Hkv, d] (without `begin` row s) become tokens length[s], ... of sequence s in the 8-bit pages
+    of cache (int8 [pages, Hkv, 2, page, d]) and scale (fp32 [pages, Hkv, 2]) that table (int32 [S, width]) names.  `length` is left as it is."""
+    _check(_kf_torch.pages_write(k, v, begin, length, table, cache, scale, stream), "kf_pages_write")
+
+
+def kf_pages_read(*, table, cache, scale, k, v, begin, first=None, stream=None):
+    """Tokens first[s] (0), ... of every sequence as the values that their codes stand for: rows begin[s] .. of k, v [T, Hkv, d]."""
+    _check(_kf_torch.pages_read(k, v, begin, first, table, cache, scale, stream), "kf_pages_read")
+
+
+def kf_pages_attend(*, q, table, length, cache, scale, out, bias_mode=KF_BIAS_NONE, alibi_slopes_dev=None, logit_scale=0.0, debug_fail_first_wait=0,
+                    scratch=None, stream=None):
+    """One query token per sequence, q and out [S, H, d], over the length[s] tokens of its pages.  `scratch`: a uint8 CUDA tensor of
+    kf_pages_attend_scratch_bytes(...) bytes; without one torch's allocator provides it for the call."""
+    _check(_kf_torch.pages_attend(q, table, length, cache, scale, out, bias_mode, alibi_slopes_dev, logit_scale, debug_fail_first_wait, scratch, stream),
+           "kf_pages_attend")
+
+
+def kf_pages_attend_scratch_bytes(*, sequences, table_width, n_pages, page_tokens, n_heads, n_kv_heads, head_dim) -> int:
+    """Bytes of scratch a kf_pages_attend of this shape needs; 0 if the shape is not supported."""
+    a = kf_pages_attend_args(cache=kf_page_cache(n_pages, page_tokens, n_kv_heads, head_dim, sequences, table_width), n_heads=n_heads)
+    a.q_head_stride = a.out_head_stride = head_dim
+    a.q_sequence_stride = a.out_sequence_stride = head_dim * n_heads
+    return int(LIB.kf_pages_attend_scratch_bytes(C.byref(a)))
+
+
+def kf_pages_update(*, table, length, refs, cache, scale, missing, parent=None, grow=0, scratch=None, stream=None):
+    """Sequences forked (sequence s goes on from parent[s], int32 [S]; -1: it has ended), part-filled pages copied in all layers (cache
+    [layers, pages, ...] or [pages, ...]), pages given back, and room made for grow (a number or int32 [S]) more tokens; table, length, refs (int32 [pages]) in
+    place, `missing` (int32 [1]): pages there were none for.  `scratch`: a uint8 CUDA tensor of kf_pages_update_scratch_bytes(...) bytes."""
+    _check(_kf_torch.pages_update(table, length, refs, cache, scale, parent, grow, missing, scratch, stream), "kf_pages_update")
+
+
+def kf_pages_update_scratch_bytes(*, sequences, table_width, n_pages, page_tokens, n_kv_heads, head_dim, n_layers=1) -> int:
+    """Bytes of scratch a kf_pages_update of this shape needs; 0 if the shape is not supported."""
+    a = kf_pages_update_args(cache=kf_page_cache(n_pages, page_tokens, n_kv_heads, head_dim, sequences, table_width), n_layers=n_layers)
+    return int(LIB.kf_pages_update_scratch_bytes(C.byref(a)))
+
+
+def kf_pages_compact(*, cache, scale, table, length, keep, n_keep, new_table, stream=None):
+    """Row j < n_keep[s] of (s, head) in the pages of new_table becomes token keep[s, head, j] (int32 [S, Hkv, width]) in those of table."""
+    _check(_kf_torch.pages_compact(cache, scale, table, length, keep, n_keep, new_table, stream), "kf_pages_compact")
 
 
 class Keyformer:

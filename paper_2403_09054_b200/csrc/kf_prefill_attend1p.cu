@@ -38,30 +38,6 @@ struct Attend1pParams {
   float a_scale;               // logit scale * log2(e)
 };
 
-__device__ __forceinline__ uint64_t a1_desc_mn(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
-  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) | (1ull << 46) |
-         (2ull << 61);
-}
-
-__device__ __forceinline__ float a1_max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-// (a0, a1) * b + c and (a0, a1) + (b0, b1) as packed binary32 pairs: one instruction for two elements.
-__device__ __forceinline__ void a1_fma2(float& d0, float& d1, float a0, float a1, float b, float c) {
-  asm("{\n\t.reg .b64 ra, rb, rc, rd;\n\t"
-      "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %4};\n\tmov.b64 rc, {%5, %5};\n\t"
-      "fma.rn.f32x2 rd, ra, rb, rc;\n\tmov.b64 {%0, %1}, rd;\n\t}"
-      : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c));
-}
-__device__ __forceinline__ void a1_add2(float& d0, float& d1, float b0, float b1) {
-  asm("{\n\t.reg .b64 ra, rb;\n\t"
-      "mov.b64 ra, {%0, %1};\n\tmov.b64 rb, {%2, %3};\n\t"
-      "add.rn.f32x2 ra, ra, rb;\n\tmov.b64 {%0, %1}, ra;\n\t}"
-      : "+f"(d0), "+f"(d1) : "f"(b0), "f"(b1));
-}
-
 // A thread's row of one key tile: the largest adjusted logit x2 = a_scale x (+ slope (j - i) log2 e), in log2 units,
 // over the columns the causal mask leaves (`diag`: the tile on the diagonal; quarter = the warp's 32-row group, so
 // chunk `quarter` of 32 columns is cut by the diagonal and later chunks are masked altogether).
@@ -86,8 +62,8 @@ __device__ __forceinline__ float a1_tile_max(uint32_t s_addr, float A, float sb,
         if (ALIBI) a4[q] = fmaf(sb, (float)(e + q), fmaf(a4[q], A, bias0));
         if (edge && e + q > lane) a4[q] = -INFINITY;
       }
-      m0 = a1_max3(m0, a4[0], a4[1]);
-      m1 = a1_max3(m1, a4[2], a4[3]);
+      m0 = max3(m0, a4[0], a4[1]);
+      m1 = max3(m1, a4[2], a4[3]);
     }
     const float cm = fmaxf(m0, m1);
     tmax = fmaxf(tmax, ALIBI ? cm : cm * A);   // the scale is positive: maximum of the raw logits first, scale after
@@ -99,25 +75,6 @@ __device__ __forceinline__ float a1_tile_max(uint32_t s_addr, float A, float sb,
 // unrounded values) in `lsum`.  MASK = false is the common case (a tile wholly below the diagonal): it also returns
 // the row's largest x2, so that the caller can tell afterwards whether m_ref was still a valid reference.  MASK =
 // true applies the causal mask of the diagonal tile when `diag` is set (and returns nothing of use).
-#define A1_R32(r) "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),        \
-                  "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),        \
-                  "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),      \
-                  "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-// 32 lanes x 32 columns of tensor memory into r[0..32) WITHOUT waiting: the registers hold the values only after
-// a1_ld_wait(r), which also ties their later uses to the wait for the compiler.
-__device__ __forceinline__ void a1_ld_issue(uint32_t taddr, uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void a1_ld_wait(uint32_t (&r)[32]) { asm volatile("tcgen05.wait::ld.sync.aligned;" : A1_R32(r)::"memory"); }
-
 template <bool ALIBI, bool MASK>
 __device__ __forceinline__ float a1_tile_probs(uint32_t s_addr, float A, float m_ref, float sb, float bias_t, int lane, int quarter,
                                                bool diag, uint32_t (&packed)[64], float& lsum) {
@@ -132,16 +89,16 @@ __device__ __forceinline__ float a1_tile_probs(uint32_t s_addr, float A, float m
       float y0, y1;
       if (ALIBI) {
         const float x0 = fmaf(sb, (float)e, fmaf(v0, A, bias0)), x1 = fmaf(sb, (float)(e + 1), fmaf(v1, A, bias0));
-        if (!MASK) { if (e & 2) m1 = a1_max3(m1, x0, x1); else m0 = a1_max3(m0, x0, x1); }
+        if (!MASK) { if (e & 2) m1 = max3(m1, x0, x1); else m0 = max3(m0, x0, x1); }
         y0 = x0 - m_ref;
         y1 = x1 - m_ref;
       } else {
-        if (!MASK) { if (e & 2) m1 = a1_max3(m1, v0, v1); else m0 = a1_max3(m0, v0, v1); }
-        a1_fma2(y0, y1, v0, v1, A, -m_ref);
+        if (!MASK) { if (e & 2) m1 = max3(m1, v0, v1); else m0 = max3(m0, v0, v1); }
+        fma2(y0, y1, v0, v1, A, -m_ref);
       }
       float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
       if (edge) { p0 = e <= lane ? p0 : 0.f; p1 = e + 1 <= lane ? p1 : 0.f; }
-      a1_add2(l0, l1, p0, p1);
+      add2(l0, l1, p0, p1);
       const __half2 h = __floats2half2_rn(p0, p1);
       packed[c * 16 + (e >> 1)] = *reinterpret_cast<const uint32_t*>(&h);
     }
@@ -155,24 +112,24 @@ __device__ __forceinline__ float a1_tile_probs(uint32_t s_addr, float A, float m
         continue;
       }
       uint32_t r[32];
-      a1_ld_issue(s_addr + (uint32_t)(c * 32), r);
-      a1_ld_wait(r);
+      tmem_ld_issue(s_addr + (uint32_t)(c * 32), r);
+      tmem_ld_wait(r);
       chunk(r, c);
     }
   } else {
     // the logits of the next 32 columns are on their way while the current ones are worked on
     uint32_t ra[32], rb[32];
-    a1_ld_issue(s_addr, ra);
-    a1_ld_wait(ra);
-    a1_ld_issue(s_addr + 32u, rb);
+    tmem_ld_issue(s_addr, ra);
+    tmem_ld_wait(ra);
+    tmem_ld_issue(s_addr + 32u, rb);
     chunk(ra, 0);
-    a1_ld_wait(rb);
-    a1_ld_issue(s_addr + 64u, ra);
+    tmem_ld_wait(rb);
+    tmem_ld_issue(s_addr + 64u, ra);
     chunk(rb, 1);
-    a1_ld_wait(ra);
-    a1_ld_issue(s_addr + 96u, rb);
+    tmem_ld_wait(ra);
+    tmem_ld_issue(s_addr + 96u, rb);
     chunk(ra, 2);
-    a1_ld_wait(rb);
+    tmem_ld_wait(rb);
     chunk(rb, 3);
   }
   lsum = l0 + l1;
@@ -261,7 +218,7 @@ __global__ void __launch_bounds__(A1_THREADS, 1) prefill_attend1p(const __grid_c
     if (lane == 0) {
       bool ok = wait_bar_eager(q_full, 0, abort_flag);
       const uint64_t qd0 = umma_smem_desc(smem_u32(sQ)), kd0 = umma_smem_desc(smem_u32(sR));
-      const uint64_t vd0 = a1_desc_mn(smem_u32(sR), KBOX, 1024);   // descriptors of other slots / offsets: + bytes / 16
+      const uint64_t vd0 = umma_desc_mn(smem_u32(sR), KBOX, 1024);   // descriptors of other slots / offsets: + bytes / 16
       auto kpos = [](int t) { return t == 0 ? 0 : 2 * t - 1; };    // ring positions of K tile t and V tile t
       auto vpos = [](int t) { return 2 * t + 2; };
       // S_b = Q_b K_t^T for tile t (K-major operands, eight MMAs of K = 16 at head_dim 128)

@@ -10,6 +10,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <string>
 
 #include "keyformer.h"
@@ -279,10 +280,193 @@ PyObject* reorder_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// ---- rows with strides: a tensor [rows, heads, d] whose features are contiguous.  The stride of a dimension with one element is never used: any
+// valid number stands for it.
+struct Rows {
+  void* p;
+  int64_t n, heads, d, row_stride, head_stride;
+};
+Rows rows3(PyObject* o, const char* name, const at::Device& device, int64_t n = -1, int64_t heads = -1, int64_t d = -1, const at::ScalarType* type = nullptr) {
+  const at::Tensor& t = tensor(o, name);
+  const auto st = t.scalar_type();
+  if (t.dim() != 3 || (st != at::kHalf && st != at::kBFloat16) || (type && st != *type) || t.device() != device || (t.size(2) > 1 && t.stride(2) != 1) ||
+      (n >= 0 && t.size(0) != n) || (heads >= 0 && t.size(1) != heads) || (d >= 0 && t.size(2) != d) || t.numel() == 0)
+    refuse(std::string(name) + ": expected fp16 or bf16 rows [" + (n >= 0 ? std::to_string(n) : "rows") + ", " + (heads >= 0 ? std::to_string(heads) : "heads") + ", " +
+           (d >= 0 ? std::to_string(d) : "d") + "] with contiguous features, of one type and on " + device.str() + ", " + describe(t));
+  Rows r{t.data_ptr(), t.size(0), t.size(1), t.size(2), t.stride(0), t.stride(1)};
+  const int64_t whole = (r.d + 7) / 8 * 8;
+  if (r.heads == 1) r.head_stride = whole;
+  if (r.n == 1) r.row_stride = whole;
+  return r;
+}
+bool fits32(std::initializer_list<int64_t> v) {
+  for (int64_t x : v)
+    if (x < 0 || x > INT32_MAX) return false;
+  return true;
+}
+
+// The cache of a call: codes int8 [pages, Hkv, 2, page, d] (with `layers` [layers, pages, ...] too), scale fp32 of the leading sizes, table int32 [S, W].
+struct Pages {
+  kf_page_cache c{};
+  void* codes;
+  float* scale;
+  int32_t* table;
+  int64_t layers = 1;
+  bool fits = true;
+};
+Pages pages_of(PyObject* cache, PyObject* scale, PyObject* table, const at::Device& device, bool layers = false) {
+  const at::Tensor &x = tensor(cache, "cache"), &t = tensor(table, "table");
+  Pages r;
+  const int64_t lead = layers && x.dim() == 6 ? 1 : 0;
+  if (x.dim() != 5 + lead || x.size(lead + 2) != 2) refuse(std::string("cache: expected int8 [") + (layers ? "(layers,) " : "") + "pages, key/value heads, 2, page, d], " + describe(x));
+  if (t.dim() != 2) refuse("table: expected int32 [sequences, width], " + describe(t));
+  if (lead) r.layers = x.size(0);
+  r.codes = address(cache, "cache", at::kChar, x.numel(), device);
+  r.scale = static_cast<float*>(address(scale, "scale", at::kFloat, r.layers * x.size(lead) * x.size(lead + 1) * 2, device));
+  r.table = static_cast<int32_t*>(address(table, "table", at::kInt, t.numel(), device));
+  r.fits = fits32({r.layers, x.size(lead), x.size(lead + 1), x.size(lead + 3), x.size(lead + 4), t.size(0), t.size(1)});
+  r.c.n_pages = (int32_t)x.size(lead); r.c.n_kv_heads = (int32_t)x.size(lead + 1);
+  r.c.page_tokens = (int32_t)x.size(lead + 3); r.c.head_dim = (int32_t)x.size(lead + 4);
+  r.c.sequences = (int32_t)t.size(0); r.c.table_width = (int32_t)t.size(1);
+  return r;
+}
+int32_t* ints(PyObject* o, const char* name, int64_t numel, const at::Device& device, bool optional = false) {
+  return static_cast<int32_t*>(address(o, name, at::kInt, numel, device, optional));
+}
+
+// ---- kf_prefill_attend_ragged: (q, k, v, begin, out, bias_mode, slopes, logit_scale, debug_fail_first_wait, stream)
+PyObject* attend_ragged(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 10, [](PyObject* const* a) -> int {
+    const at::Tensor& x = first_tensor(a[0], "q");
+    const at::Device device = x.device();
+    const auto type = x.scalar_type();
+    const Rows q = rows3(a[0], "q", device);
+    const Rows k = rows3(a[1], "k", device, q.n, -1, q.d, &type), v = rows3(a[2], "v", device, q.n, k.heads, q.d, &type);
+    const Rows out = rows3(a[4], "out", device, q.n, q.heads, q.d, &type);
+    const at::Tensor& begin = tensor(a[3], "begin");
+    if (begin.dim() != 1 || begin.numel() < 2) refuse("begin: expected int32 [sequences + 1], " + describe(begin));
+    if (!fits32({q.n, q.heads, k.heads, q.d, begin.numel()})) return KF_EINVAL;
+    kf_ragged_args p{};
+    p.tokens = (int32_t)q.n; p.sequences = (int32_t)begin.numel() - 1;
+    p.n_heads = (int32_t)q.heads; p.n_kv_heads = (int32_t)k.heads; p.head_dim = (int32_t)q.d;
+    p.type = type == at::kHalf ? KF_TYPE_FP16 : KF_TYPE_BF16;
+    p.bias_mode = integer32(a[5]);
+    p.logit_scale = (float)real(a[7]);
+    p.d_alibi_slopes = static_cast<float*>(address(a[6], "alibi_slopes_dev", at::kFloat, q.heads, device, true));
+    p.q_token_stride = q.row_stride; p.q_head_stride = q.head_stride;
+    p.k_token_stride = k.row_stride; p.k_head_stride = k.head_stride;
+    p.v_token_stride = v.row_stride; p.v_head_stride = v.head_stride;
+    p.out_token_stride = out.row_stride; p.out_head_stride = out.head_stride;
+    p.debug_fail_first_wait = integer32(a[8]);
+    const int32_t* b = ints(a[3], "begin", begin.numel(), device);
+    const Where at_(device, a[9]);
+    return kf_prefill_attend_ragged(&p, q.p, k.p, v.p, b, out.p, at_.stream.stream());
+  });
+}
+
+// ---- kf_pages_write: (k, v, begin, length, table, cache, scale, stream); kf_pages_read: (k, v, begin, first, table, cache, scale, stream)
+int page_rows(PyObject* const* a, bool write) {
+  const at::Tensor& x = first_tensor(a[0], "k");
+  const at::Device device = x.device();
+  const auto type = x.scalar_type();
+  const Pages g = pages_of(a[5], a[6], a[4], device);
+  const Rows k = rows3(a[0], "k", device, -1, g.c.n_kv_heads, g.c.head_dim, &type), v = rows3(a[1], "v", device, k.n, k.heads, k.d, &type);
+  const int32_t* begin = ints(a[2], "begin", (int64_t)g.c.sequences + 1, device, write);
+  const int32_t* at_token = ints(a[3], write ? "length" : "first", g.c.sequences, device, !write);
+  if (!g.fits || !fits32({k.n})) return KF_EINVAL;
+  kf_page_rows r{};
+  r.tokens = (int32_t)k.n; r.type = type == at::kHalf ? KF_TYPE_FP16 : KF_TYPE_BF16;
+  r.k_token_stride = k.row_stride; r.k_head_stride = k.head_stride;
+  r.v_token_stride = v.row_stride; r.v_head_stride = v.head_stride;
+  const Where at_(device, a[7]);
+  return write ? kf_pages_write(&g.c, &r, k.p, v.p, begin, at_token, g.table, g.codes, g.scale, at_.stream.stream())
+               : kf_pages_read(&g.c, &r, g.codes, g.scale, g.table, begin, at_token, k.p, v.p, at_.stream.stream());
+}
+PyObject* pages_write(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 8, [](PyObject* const* a) { return page_rows(a, true); });
+}
+PyObject* pages_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 8, [](PyObject* const* a) { return page_rows(a, false); });
+}
+
+// ---- kf_pages_attend: (q, table, length, cache, scale, out, bias_mode, slopes, logit_scale, debug_fail_first_wait, scratch, stream)
+PyObject* pages_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 12, [](PyObject* const* a) -> int {
+    const at::Tensor& x = first_tensor(a[0], "q");
+    const at::Device device = x.device();
+    const auto type = x.scalar_type();
+    const Pages g = pages_of(a[3], a[4], a[1], device);
+    const Rows q = rows3(a[0], "q", device, g.c.sequences, -1, g.c.head_dim), out = rows3(a[5], "out", device, q.n, q.heads, q.d, &type);
+    if (!g.fits || !fits32({q.heads})) return KF_EINVAL;
+    kf_pages_attend_args p{};
+    p.cache = g.c;
+    p.n_heads = (int32_t)q.heads; p.type = type == at::kHalf ? KF_TYPE_FP16 : KF_TYPE_BF16;
+    p.bias_mode = integer32(a[6]);
+    p.d_alibi_slopes = static_cast<float*>(address(a[7], "alibi_slopes_dev", at::kFloat, q.heads, device, true));
+    p.logit_scale = (float)real(a[8]);
+    p.debug_fail_first_wait = integer32(a[9]);
+    p.q_sequence_stride = q.row_stride; p.q_head_stride = q.head_stride;
+    p.out_sequence_stride = out.row_stride; p.out_head_stride = out.head_stride;
+    const int32_t* length = ints(a[2], "length", g.c.sequences, device);
+    const size_t need = kf_pages_attend_scratch_bytes(&p);
+    if (need == 0) return KF_EINVAL;
+    const Where at_(device, a[11]);
+    const Scratch scratch(a[10], need, device, at_);
+    return kf_pages_attend(&p, q.p, g.codes, g.scale, g.table, length, out.p, scratch.p, scratch.bytes, at_.stream.stream());
+  });
+}
+
+// ---- kf_pages_update: (table, length, refs, cache, scale, parent, grow, missing, scratch, stream)
+PyObject* pages_update(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 10, [](PyObject* const* a) -> int {
+    const at::Device device = first_tensor(a[0], "table").device();
+    const Pages g = pages_of(a[3], a[4], a[0], device, true);
+    if (!g.fits) return KF_EINVAL;
+    kf_pages_update_args p{};
+    p.cache = g.c;
+    p.n_layers = (int32_t)g.layers;
+    const bool each = THPVariable_Check(a[6]);
+    if (!each) p.grow = integer32(a[6]);
+    const int64_t S = g.c.sequences;
+    int32_t* length = ints(a[1], "length", S, device);
+    int32_t* refs = ints(a[2], "refs", g.c.n_pages, device);
+    const int32_t* parent = ints(a[5], "parent", S, device, true);
+    const int32_t* grow = each ? ints(a[6], "grow", S, device) : nullptr;
+    int32_t* missing = ints(a[7], "missing", 1, device);
+    const size_t need = kf_pages_update_scratch_bytes(&p);
+    if (need == 0) return KF_EINVAL;
+    const Where at_(device, a[9]);
+    const Scratch scratch(a[8], need, device, at_);
+    return kf_pages_update(&p, g.table, length, refs, parent, grow, g.codes, g.scale, missing, scratch.p, scratch.bytes, at_.stream.stream());
+  });
+}
+
+// ---- kf_pages_compact: (cache, scale, table, length, keep, n_keep, new_table, stream)
+PyObject* pages_compact(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 8, [](PyObject* const* a) -> int {
+    const at::Device device = first_tensor(a[0], "cache").device();
+    const Pages g = pages_of(a[0], a[1], a[2], device);
+    const int64_t S = g.c.sequences, Hkv = g.c.n_kv_heads;
+    const at::Tensor &keep = tensor(a[4], "keep"), &to = tensor(a[6], "new_table");
+    if (keep.dim() != 3 || keep.size(0) != S || keep.size(1) != Hkv) refuse("keep: expected int32 [sequences, key/value heads, width], " + describe(keep));
+    if (to.dim() != 2 || to.size(0) != S) refuse("new_table: expected int32 [sequences, width], " + describe(to));
+    if (!g.fits || !fits32({keep.size(2), to.size(1)})) return KF_EINVAL;
+    const int32_t* length = ints(a[3], "length", S, device);
+    const int32_t* kept = ints(a[4], "keep", keep.numel(), device);
+    const int32_t* count = ints(a[5], "n_keep", S, device);
+    const int32_t* new_table = ints(a[6], "new_table", to.numel(), device);
+    const Where at_(device, a[7]);
+    return kf_pages_compact(&g.c, (int32_t)keep.size(2), (int32_t)to.size(1), g.table, length, kept, count, new_table, g.codes, g.scale, at_.stream.stream());
+  });
+}
+
 #define KF_FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL
 PyMethodDef methods[] = {{"pack_cache", KF_FAST(pack_cache), nullptr},           {"unpack_cache", KF_FAST(unpack_cache), nullptr},
                          {"decode_step_packed", KF_FAST(decode_step_packed), nullptr}, {"qk_norm_rotate", KF_FAST(qk_norm_rotate), nullptr},
                          {"beam_select", KF_FAST(beam_select), nullptr},         {"reorder_rows", KF_FAST(reorder_rows), nullptr},
+                         {"attend_ragged", KF_FAST(attend_ragged), nullptr},     {"pages_write", KF_FAST(pages_write), nullptr},
+                         {"pages_read", KF_FAST(pages_read), nullptr},           {"pages_attend", KF_FAST(pages_attend), nullptr},
+                         {"pages_update", KF_FAST(pages_update), nullptr},       {"pages_compact", KF_FAST(pages_compact), nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kf_torch", nullptr, -1, methods};
 
