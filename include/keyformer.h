@@ -498,7 +498,8 @@ typedef struct kf_page_rows {
 int kf_pages_write(const kf_page_cache* cache, const kf_page_rows* rows, const void* d_k, const void* d_v, const int32_t* d_begin,
                    const int32_t* d_length, const int32_t* d_table, void* d_cache, float* d_scale, void* stream);
 /* The way back: rows d_begin[s] .. of d_k and d_v are tokens d_first[s] (NULL: 0), ... of sequence s as the numbers their codes
- * stand for, rounded once.  Rows whose page is missing are NaN; rows of no sequence are left as they were. */
+ * stand for, rounded once (beyond the type's
+ * largest: infinity).  Rows whose page is missing are NaN; rows of no sequence are left as they were. */
 int kf_pages_read(const kf_page_cache* cache, const kf_page_rows* rows, const void* d_cache, const float* d_scale, const int32_t* d_table,
                   const int32_t* d_begin, const int32_t* d_first, void* d_k, void* d_v, void* stream);
 
@@ -528,7 +529,7 @@ int kf_pages_attend(const kf_pages_attend_args* args, const void* d_q, const voi
  * pages are added until s has room for d_grow[s] more tokens (NULL: grow); pages behind those are given back.
  *   d_refs    : DEVICE int32 [n_pages], how many table entries name a page (plus what the caller counts: a page with
  *               references is never handed out).  Updated; a page is free when its count is 0.
- *   d_missing : DEVICE int32 [1], pages that could not be added because none was free or the table too narrow
+ *   d_missing : DEVICE int32 [1], pages that could not be added because none was free or the table too narrow (at most 2^31 - 1)
  * Free pages are handed out lowest first, in the order of sequences and of the pages of each; where there is none the table
  * entry is -1; a copy of a page that was missing itself reads as NaN.  d_length[s] becomes the parent's length (0 for an ended one), without the room added.  A length outside 0 ..
  * table_width * page_tokens counts as 0; negative growth counts as none.  Pages filled in part belong to one sequence alone before and after. */

@@ -288,7 +288,8 @@ struct UpdateShared {
   int owner[UPDATE_MAX_SEQUENCES];    // lowest sequence that goes on from this one
   int prefix[UPDATE_MAX_SEQUENCES];   // pages handed out to the sequences before
   int scan[UT / 32];
-  int running, found;
+  int found;
+  unsigned long long beyond;
 };
 
 __device__ __forceinline__ int block_exclusive(int v, int* warp_sums, int& total) {
@@ -314,7 +315,8 @@ __device__ __forceinline__ int block_exclusive(int v, int* warp_sums, int& total
 }
 
 struct Sequence {
-  int parent, length, full, part, keeps, stay, need, beyond;   // stay: pages kept from the parent; need: pages in all; beyond: pages there is no room for
+  int parent, length, full, part, keeps, stay, need;   // stay: pages kept from the parent; need: pages in all
+  int64_t beyond;                                      // pages the table has no room for
 };
 
 __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(UT, 1) pages_update_kernel(const __grid_constant__ PagesUpdate U) {
@@ -341,35 +343,33 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(UT, 1) pages_u
     const int64_t tokens = (int64_t)q.length + max(U.grow ? U.grow[s] : U.grow_all, 0);
     const int64_t need = (tokens + c.page - 1) / c.page;
     q.need = (int)min(need, (int64_t)W);
-    q.beyond = (int)min(need - q.need, (int64_t)1 << 17);      // so that all of them together stay within 2^30
+    q.beyond = need - q.need;
     return q;
   };
 
   // ---- who keeps a page that is filled in part; pages to hand out before each sequence
   for (int s = tid; s < S; s += UT) sh.owner[s] = S;
-  if (tid == 0) sh.found = 0;
+  if (tid == 0) sh.beyond = 0;
   __syncthreads();
   for (int s = tid; s < S; s += UT) {
     const int p = parent_of(s);
     if (p >= 0) atomicMin(&sh.owner[p], s);
   }
   __syncthreads();
-  int wanted = 0, beyond = 0;                                    // of all sequences
+  int wanted = 0;                                                // pages to hand out, of all sequences
   for (int base = 0; base < S; base += UT) {
     const int s = base + tid;
     int fresh = 0;
     if (s < S) {
       const Sequence q = look(s);
       fresh = q.need - q.stay;
-      if (q.beyond) atomicAdd(&sh.found, q.beyond);
+      if (q.beyond) atomicAdd(&sh.beyond, (unsigned long long)q.beyond);
     }
     int total;
     const int before = block_exclusive(fresh, sh.scan, total);
     if (s < S) sh.prefix[s] = wanted + before;
     wanted += total;
   }
-  __syncthreads();
-  beyond = sh.found;
 
   // ---- references: what the table names now no longer counts, what stays does
   const uint32_t entries = (uint32_t)S * (uint32_t)W;            // at most 2^28
@@ -457,7 +457,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(UT, 1) pages_u
   cluster.sync();
   k = 0;
   for (int s = rank * UT + tid; s < S; s += CLUSTER * UT) U.length[s] = mine_length[k++];
-  if (rank == 0 && tid == 0) *U.missing = wanted - given + beyond;
+  if (rank == 0 && tid == 0) *U.missing = (int)min((int64_t)(wanted - given) + (int64_t)sh.beyond, (int64_t)INT32_MAX);
 }
 
 // The rows of pages that are filled in part.  Grid: sequences, layers, pieces of the heads.
