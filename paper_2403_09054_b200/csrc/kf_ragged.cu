@@ -21,10 +21,15 @@ namespace kf {
 
 namespace {
 
-constexpr int THREADS = 10 * 32;        // TMA warp, MMA warp, two groups of four compute warps (head_dim 256: one group)
+// A group of four warps for the TMA loads and the MMAs (one warp each), one per block of query rows.  With two blocks the registers of the launch
+// (384 x 168) are dealt out again: a compute thread holds its whole row of logits.
+constexpr int threads_of(int blocks) { return 128 * (blocks + 1); }
+constexpr int FEW_REGS = 72, MANY_REGS = 216;
+static_assert(128 * FEW_REGS + 256 * MANY_REGS <= 384 * 168, "registers of the launch");
 constexpr int RING = 5;                 // slots that K and V tiles go through in the order of use
 constexpr uint32_t TMEM_COLS = 512;
 constexpr float HEADROOM = 7.0f;        // log2 units a weight stands above its distance from the reference
+constexpr float LOWEST = -1e30f;
 constexpr float SLACK = 8.0f;           // log2 units a row's maximum may exceed its reference before the reference moves
 
 struct RaggedParams {
@@ -38,38 +43,6 @@ struct RaggedParams {
   bool fail_first_wait;
 };
 
-// The largest adjusted logit x2 = a_scale x (+ slope (j - i) log2 e), in log2 units, of a thread's row over the columns of a tile that the
-// mask leaves.  MASK: the columns up to `lim`; chunks of 32 columns behind `edge` (the same for the whole warp) hold none.
-template <int KT, bool ALIBI>
-__device__ __forceinline__ float tile_max(uint32_t s_addr, float A, float sb, float bias_t, int lim, int edge, bool mask) {
-  const int nch = mask ? min(edge + 1, KT / 32) : KT / 32;
-  float tmax = -INFINITY;
-#pragma unroll 1
-  for (int c = 0; c < nch; ++c) {
-    float v[32];
-    tmem_ld_32x32(s_addr + (uint32_t)(c * 32), v);
-    const int last = mask && c == edge ? (lim & 31) : 31;
-    float bias0 = 0.f;
-    if (ALIBI) bias0 = fmaf(sb, (float)(c * 32), bias_t);
-    float m0 = -INFINITY, m1 = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < 32; e += 4) {
-      float a4[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        a4[q] = v[e + q];
-        if (ALIBI) a4[q] = fmaf(sb, (float)(e + q), fmaf(a4[q], A, bias0));
-        if (e + q > last) a4[q] = -INFINITY;
-      }
-      m0 = max3(m0, a4[0], a4[1]);
-      m1 = max3(m1, a4[2], a4[3]);
-    }
-    const float cm = fmaxf(m0, m1);
-    tmax = fmaxf(tmax, ALIBI ? cm : cm * A);   // the scale is not negative: maximum of the raw logits first, scale after
-  }
-  return tmax;
-}
-
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   if (BF16) {
@@ -80,73 +53,8 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The row's weights 2^(x2 - m_ref) of one key tile as 16-bit pairs, their sum in binary32 (of the unrounded values) in `lsum`.
-// Without MASK (a tile whose every key every row sees) it also returns the row's largest x2.
-template <int KT, bool ALIBI, bool BF16, bool MASK>
-__device__ __forceinline__ float tile_probs(uint32_t s_addr, float A, float m_ref, float sb, float bias_t, int lim, int edge, uint32_t (&packed)[KT / 2],
-                                            float& lsum) {
-  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-  auto chunk = [&](const uint32_t (&r)[32], int c) {
-    const int last = MASK && c == edge ? (lim & 31) : 31;
-    float bias0 = 0.f;
-    if (ALIBI) bias0 = fmaf(sb, (float)(c * 32), bias_t);
-#pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-      const float v0 = __uint_as_float(r[e]), v1 = __uint_as_float(r[e + 1]);
-      float y0, y1;
-      if (ALIBI) {
-        const float x0 = fmaf(sb, (float)e, fmaf(v0, A, bias0)), x1 = fmaf(sb, (float)(e + 1), fmaf(v1, A, bias0));
-        if (!MASK) { if (e & 2) m1 = max3(m1, x0, x1); else m0 = max3(m0, x0, x1); }
-        y0 = x0 - m_ref;
-        y1 = x1 - m_ref;
-      } else {
-        if (!MASK) { if (e & 2) m1 = max3(m1, v0, v1); else m0 = max3(m0, v0, v1); }
-        fma2(y0, y1, v0, v1, A, -m_ref);
-      }
-      float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
-      if (MASK) { p0 = e <= last ? p0 : 0.f; p1 = e + 1 <= last ? p1 : 0.f; }
-      add2(l0, l1, p0, p1);
-      packed[c * 16 + (e >> 1)] = pack2<BF16>(p0, p1);
-    }
-  };
-  if (MASK) {
-#pragma unroll
-    for (int c = 0; c < KT / 32; ++c) {
-      if (c > edge) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) packed[c * 16 + e] = 0u;
-        continue;
-      }
-      uint32_t r[32];
-      tmem_ld_issue(s_addr + (uint32_t)(c * 32), r);
-      tmem_ld_wait(r);
-      chunk(r, c);
-    }
-  } else {
-    // the logits of the next 32 columns are on their way while the current ones are worked on
-    uint32_t ra[32], rb[32];
-    tmem_ld_issue(s_addr, ra);
-    tmem_ld_wait(ra);
-    tmem_ld_issue(s_addr + 32u, rb);
-    chunk(ra, 0);
-    tmem_ld_wait(rb);
-    if (KT == 128) tmem_ld_issue(s_addr + 64u, ra);
-    chunk(rb, 1);
-    if (KT == 128) {
-      tmem_ld_wait(ra);
-      tmem_ld_issue(s_addr + 96u, rb);
-      chunk(ra, 2);
-      tmem_ld_wait(rb);
-      chunk(rb, 3);
-    }
-  }
-  lsum = l0 + l1;
-  const float m = fmaxf(m0, m1);
-  return ALIBI ? m : m * A;
-}
-
 template <int D, bool ALIBI, bool BF16>
-__global__ void __launch_bounds__(THREADS, 1) ragged_kernel(const __grid_constant__ RaggedParams P) {
+__global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel(const __grid_constant__ RaggedParams P) {
   constexpr int NB = D == 256 ? 1 : 2;     // blocks of 128 query rows
   constexpr int KT = D == 256 ? 64 : 128;  // rows of a key tile
   constexpr int KCH = D / 64;              // 64-feature boxes per row
@@ -166,8 +74,8 @@ __global__ void __launch_bounds__(THREADS, 1) ragged_kernel(const __grid_constan
   uint64_t* r_full = q_full + 1;
   uint64_t* r_empty = r_full + RING;
   uint64_t* s_full = r_empty + RING;      // [2] per block, or per parity of the tile
-  uint64_t* p_full = s_full + 2;          // [2]
-  uint64_t* o_full = p_full + 2;          // [2]
+  uint64_t* p_full = s_full + 2;          // [2][2]: the halves of a tile's weights
+  uint64_t* o_full = p_full + 4;          // [2]
   uint64_t* v_done = o_full + 2;          // one block: the value MMAs of a tile have completed
   uint64_t* v_clean = v_done + 1;         // value rows behind the sequence have been overwritten
   uint64_t* drain = v_clean + 1;
@@ -175,7 +83,7 @@ __global__ void __launch_bounds__(THREADS, 1) ragged_kernel(const __grid_constan
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* issued = const_cast<int*>(abort_flag) + 1;   // ring positions whose loads have been issued
 
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int tb = 128 >> P.log_pack;                // tokens of a block
   constexpr int ROW_SHIFT = NB == 2 ? 8 : 7;       // rows of a CTA
   const int slot = (int)(gridDim.x - 1 - blockIdx.x);   // the longest CTAs of a sequence start first
@@ -189,14 +97,15 @@ __global__ void __launch_bounds__(THREADS, 1) ragged_kernel(const __grid_constan
   const int first = (int)first64;
   const bool has1 = NB == 2 && first + tb < n;
   const int T0 = (min(first + tb, n) + KT - 1) / KT;                              // key tiles of block 0
-  const int T = has1 ? (min(first + 2 * tb, n) + KT - 1) / KT : T0;               // key tiles the CTA walks
-  const bool clean = T * KT > n && row0 + n < P.tokens;                           // rows of others in the last tile
+  const int T = has1 ? (min(first + 2 * tb, n) + KT - 1) / KT : T0;               // key tiles the CTA walks: step u takes tile T - 1 - u
+  const int U0 = T - T0;                                                          // the step at which block 0 joins
+  const bool clean = T * KT > n && row0 + n < P.tokens;                           // rows of others in the last tile, the first to be walked
   const int head0 = blockIdx.y * P.pack, kv_head = head0 / P.group;
 
   if (tid == 0) {
     mbar_init(q_full, 1);
     for (int s = 0; s < RING; ++s) { mbar_init(r_full + s, 1); mbar_init(r_empty + s, 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(s_full + b, 1); mbar_init(p_full + b, 4); mbar_init(o_full + b, 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(s_full + b, 1); mbar_init(p_full + 2 * b, 4); mbar_init(p_full + 2 * b + 1, 4); mbar_init(o_full + b, 1); }
     mbar_init(v_done, 1);
     mbar_init(v_clean, 1);
     mbar_init(drain, 1);
@@ -213,12 +122,11 @@ __global__ void __launch_bounds__(THREADS, 1) ragged_kernel(const __grid_constan
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
-  // Ring position 0 is K tile 0; then, as the MMA warp needs them, K tile t + AHEAD before V tile t.  With one tile of look-ahead
-  // position 2t + 1 is K tile t + 1 and 2t + 2 V tile t; with two, positions 0 and 1 are K tiles, 2t + 2 is V tile t and 2t + 3 K tile t + 2.
-  auto kpos = [](int t) { return AHEAD == 1 ? (t == 0 ? 0 : 2 * t - 1) : (t < 2 ? t : 2 * t - 1); };
-  auto vpos = [](int t) { return 2 * t + 2; };
-
-  if (warp == 0) {
+  // Ring position 0 is the K tile of step 0; then, as the MMA warp needs them, the K tile of step u + AHEAD before the V tile of step u.  With one step of
+  // look-ahead position 2u + 1 is K of step u + 1 and 2u + 2 V of step u; with two, positions 0 and 1 are K, 2u + 2 is V of step u and 2u + 3 K of step u + 2.
+  if (warp < 4) {
+    if (NB == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(FEW_REGS));
+   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     bool ok = true;
     if (lane == 0) {
@@ -227,23 +135,23 @@ __global__ void __launch_bounds__(THREADS, 1) ragged_kernel(const __grid_constan
         for (int kc = 0; kc < KCH; ++kc) tma_load_3d(sQ + b * Q_BYTES + kc * QBOX, &P.tmQ, kc * 64, head0, row0 + first + b * tb, q_full);
       for (int j = 0; ok && j <= 2 * T; ++j) {
         const bool is_v = j >= 2 && (j & 1) == 0;
-        const int t = is_v ? (j - 2) >> 1 : (AHEAD == 1 ? (j == 0 ? 0 : (j + 1) >> 1) : (j < 2 ? j : (j + 1) >> 1));
-        if (t >= T) continue;                                  // a K tile behind the last one
+        const int u = is_v ? (j - 2) >> 1 : (AHEAD == 1 ? (j == 0 ? 0 : (j + 1) >> 1) : (j < 2 ? j : (j + 1) >> 1));
+        if (u >= T) continue;                                  // a K tile behind the last one
         const int s = j % RING;
         if (j >= RING) ok = wait_bar(r_empty + s, (uint32_t)((j / RING - 1) & 1), abort_flag);
         if (!ok) break;
         mbar_expect_tx(r_full + s, SLOT);
         const CUtensorMap* tm = is_v ? &P.tmV : &P.tmK;
-        for (int kc = 0; kc < KCH; ++kc) tma_load_3d(sR + (size_t)s * SLOT + kc * KBOX, tm, kc * 64, row0 + t * KT, kv_head, r_full + s);
+        for (int kc = 0; kc < KCH; ++kc) tma_load_3d(sR + (size_t)s * SLOT + kc * KBOX, tm, kc * 64, row0 + (T - 1 - u) * KT, kv_head, r_full + s);
         issued[0] = j + 1;
       }
       if (!ok) *abort_flag = 1;
     }
-    __syncwarp();
-    if (clean && __shfl_sync(0xffffffffu, ok ? 1 : 0, 0)) {
-      const int j = vpos(T - 1), s = j % RING;
-      const bool here = __all_sync(0xffffffffu, wait_bar(r_full + s, (uint32_t)((j / RING) & 1), abort_flag));
-      if (here) {
+   } else if (warp == 2) {
+    // ------------------------------------------------------------ value rows of others, in the tile of step 0, become zeros
+    if (clean) {
+      constexpr int s = 2;                                     // its ring position
+      if (__all_sync(0xffffffffu, wait_bar_eager(r_full + s, 0, abort_flag))) {
         unsigned char* tile = sR + (size_t)s * SLOT;
         const int from = n - (T - 1) * KT;                     // rows of the tile that are the sequence's
         for (int kc = 0; kc < KCH; ++kc)
@@ -255,158 +163,216 @@ __global__ void __launch_bounds__(THREADS, 1) ragged_kernel(const __grid_constan
         *abort_flag = 1;
       }
     }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------ MMA issuer
-    if (lane == 0) {
-      bool ok = wait_bar_eager(q_full, 0, abort_flag);
-      const uint64_t qd0 = umma_smem_desc(smem_u32(sQ)), kd0 = umma_smem_desc(smem_u32(sR));
-      const uint64_t vd0 = umma_desc_mn(smem_u32(sR), KBOX, 1024);   // descriptors of other slots / offsets: + bytes / 16
-      auto wait_k = [&](int t) { const int j = kpos(t); return wait_bar_eager(r_full + (j % RING), (uint32_t)((j / RING) & 1), abort_flag); };
-      auto free_k = [&](int t) { umma_commit(r_empty + (kpos(t) % RING)); };
-      // S = Q_b K_t^T (K-major operands, 16 features per MMA)
-      auto qk = [&](int b, int t) {
-        const int sb = NB == 2 ? b : (t & 1);
-        const uint64_t kd = kd0 + (uint64_t)(((kpos(t) % RING) * SLOT) >> 4), qd = qd0 + (uint64_t)((b * Q_BYTES) >> 4);
+   } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer: the warp runs along together, one lane issues
+    const uint32_t leader = warp_leader();
+    const int Tu = __shfl_sync(0xffffffffu, T, 0), U0u = __shfl_sync(0xffffffffu, U0, 0);
+    const bool two = __shfl_sync(0xffffffffu, has1 ? 1 : 0, 0) != 0, clean_u = __shfl_sync(0xffffffffu, clean ? 1 : 0, 0) != 0;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bar_eager(bar, parity, abort_flag)) != 0; };
+    // Where a tile lies: its slot of the ring and the parity of the slot's use.  Two positions on is the next tile of its kind.
+    struct Cursor {
+      int slot, parity;
+      __device__ __forceinline__ void next() {
+        slot += 2;
+        if (slot >= RING) { slot -= RING; parity ^= 1; }
+      }
+    };
+    bool ok = wait(q_full, 0);
+    const uint64_t qd0 = umma_smem_desc(smem_u32(sQ)), kd0 = umma_smem_desc(smem_u32(sR));
+    const uint64_t vd0 = umma_desc_mn(smem_u32(sR), KBOX, 1024);   // descriptors of other slots / offsets: + bytes / 16
+    // S = Q_b K_t^T (K-major operands, 16 features per MMA) into tile buffer sb
+    auto qk = [&](int b, int sb, int slot) {
+      const uint64_t kd = kd0 + (uint64_t)((slot * SLOT) >> 4), qd = qd0 + (uint64_t)((b * Q_BYTES) >> 4);
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t in_box = (uint32_t)((kk & 3) * 32);
-          umma_f16(tmem_base + (uint32_t)(sb * KT), qd + ((uint32_t)((kk >> 2) * QBOX) + in_box) / 16, kd + ((uint32_t)((kk >> 2) * KBOX) + in_box) / 16,
-                   IDESC_QK, kk > 0 ? 1u : 0u);
-        }
-        umma_commit(s_full + sb);
-      };
-      // O_b += P V_t (A = P from tensor memory, 16 keys = 8 columns per MMA; B = V, MN-major)
-      auto pv = [&](int b, int t) {
-        const int sb = NB == 2 ? b : (t & 1);
-        const uint64_t vd = vd0 + (uint64_t)(((vpos(t) % RING) * SLOT) >> 4);
+      for (int kk = 0; kk < D / 16; ++kk) {
+        const uint32_t in_box = (uint32_t)((kk & 3) * 32);
+        umma_f16_warp(leader, tmem + (uint32_t)(sb * KT), qd + ((uint32_t)((kk >> 2) * QBOX) + in_box) / 16, kd + ((uint32_t)((kk >> 2) * KBOX) + in_box) / 16,
+                      IDESC_QK, kk > 0 ? 1u : 0u);
+      }
+      umma_commit_warp(leader, s_full + sb);
+    };
+    // O_b += P V_t (A = P from tensor memory, 16 keys = 8 columns per MMA; B = V, MN-major).  The weights arrive in two halves: the first
+    // half's products run while the second is still being formed.
+    auto pv = [&](int b, int sb, int slot, uint32_t parity, bool first) {
+      const uint64_t vd = vd0 + (uint64_t)((slot * SLOT) >> 4);
 #pragma unroll
-        for (int kk = 0; kk < KT / 16; ++kk)
-          umma_f16_ts(tmem_base + O_COL + (uint32_t)(b * D), tmem_base + (uint32_t)(sb * KT + kk * 8), vd + (uint64_t)((kk * 16 * 128) >> 4), IDESC_PV,
-                      (t > 0 || kk > 0) ? 1u : 0u);
-      };
-      // Tile 0, then per tile and block the value MMA and the next logits.  A slot is handed back by a commit placed right after the
-      // last MMA that reads it.
-      for (int t = 0; ok && t < min(AHEAD, T); ++t) {
-        ok = wait_k(t);
-        if (!ok) break;
+      for (int half = 0; half < 2; ++half) {
+        if (!wait(p_full + 2 * sb + half, parity)) return false;
         tc_fence_after();
-        qk(0, t);
-        if (has1) qk(1, t);
-        free_k(t);
+#pragma unroll
+        for (int kk = half * (KT / 32); kk < (half + 1) * (KT / 32); ++kk)
+          umma_f16_ts_warp(leader, tmem + O_COL + (uint32_t)(b * D), tmem + (uint32_t)(sb * KT + kk * 8), vd + (uint64_t)((kk * 16 * 128) >> 4), IDESC_PV,
+                           (!first || kk > 0) ? 1u : 0u);
       }
-      for (int t = 0; ok && t < T; ++t) {
-        const bool more = t + AHEAD < T;
-        const int jv = vpos(t);
-        if (more) ok = wait_k(t + AHEAD);
-        if (ok) ok = wait_bar_eager(r_full + (jv % RING), (uint32_t)((jv / RING) & 1), abort_flag);
-        if (ok && clean && t == T - 1) ok = wait_bar_eager(v_clean, 0, abort_flag);
-        if (!ok) break;
-        if (t < T0) {
-          ok = NB == 2 ? wait_bar_eager(p_full, (uint32_t)(t & 1), abort_flag) : wait_bar_eager(p_full + (t & 1), (uint32_t)((t >> 1) & 1), abort_flag);
-          if (!ok) break;
-          tc_fence_after();
-          pv(0, t);
-          if (!has1) umma_commit(r_empty + (jv % RING));
-          if (NB == 1) umma_commit(v_done);
-          if (t == T0 - 1) umma_commit(o_full);
-          else if (t + AHEAD < T0) qk(0, t + AHEAD);
-        }
-        if (has1) {
-          ok = wait_bar_eager(p_full + 1, (uint32_t)(t & 1), abort_flag);
-          if (!ok) break;
-          tc_fence_after();
-          pv(1, t);
-          umma_commit(r_empty + (jv % RING));                  // both blocks' value MMAs of tile t have been issued
-          if (t == T - 1) umma_commit(o_full + 1);
-          else qk(1, t + 1);
-        }
-        if (more) free_k(t + AHEAD);                           // every logit MMA that reads it has been issued
-      }
-      if (!ok) *abort_flag = 1;
-      umma_commit(drain);
-      (void)wait_bar(drain, 0, abort_flag);
+      return true;
+    };
+    // The tensor pipe must never run dry between two groups of MMAs, so the waits for tiles stand behind the group before the one that
+    // needs them.  A slot is handed back by a commit placed right after the last MMA that reads it.
+    Cursor kc{0, 0}, vc{2, 0};
+    for (int u = 0; ok && u < min(AHEAD, Tu); ++u) {
+      ok = wait(r_full + kc.slot, kc.parity);
+      if (!ok) break;
+      tc_fence_after();
+      if (u >= U0u) qk(0, NB == 2 ? 0 : u, kc.slot);
+      if (two) qk(1, 1, kc.slot);
+      umma_commit_warp(leader, r_empty + kc.slot);
+      kc = Cursor{2 * u + 1, 0};                                   // K of step u + 1 stands at 2u + 1
     }
-  } else if (NB == 2 || warp < 6) {
+    if (ok && AHEAD < Tu) ok = wait(r_full + kc.slot, kc.parity);
+    if (ok) ok = wait(r_full + vc.slot, vc.parity);
+    if (ok && clean_u) ok = wait(v_clean, 0);
+    for (int u = 0; ok && u < Tu; ++u) {
+      const bool more = u + AHEAD < Tu;
+      const int kslot = kc.slot, vslot = vc.slot;
+      kc.next();
+      vc.next();
+      const int own = u - U0u;                                     // block 0's step
+      if (own >= 0) {
+        if (!pv(0, NB == 2 ? 0 : (own & 1), vslot, (uint32_t)(NB == 2 ? own & 1 : own >> 1 & 1), own == 0)) { ok = false; break; }
+        if (!two) umma_commit_warp(leader, r_empty + vslot);
+        if (NB == 1) umma_commit_warp(leader, v_done);
+        if (u == Tu - 1) umma_commit_warp(leader, o_full);
+      }
+      if (more && own + AHEAD >= 0) qk(0, NB == 2 ? 0 : (own & 1), kslot);
+      if (u + AHEAD + 1 < Tu) {
+        ok = wait(r_full + kc.slot, kc.parity);
+        if (!ok) break;
+      }
+      if (two) {
+        if (!pv(1, 1, vslot, (uint32_t)(u & 1), u == 0)) { ok = false; break; }
+        if (more) qk(1, 1, kslot);
+        else umma_commit_warp(leader, o_full + 1);
+        umma_commit_warp(leader, r_empty + vslot);               // both blocks' value MMAs of the step have been issued
+      }
+      if (more) umma_commit_warp(leader, r_empty + kslot);       // every logit MMA that reads it has been issued
+      if (u + 1 < Tu) ok = wait(r_full + vc.slot, vc.parity);
+    }
+    if (!ok && lane == 0) *abort_flag = 1;
+    umma_commit_warp(leader, drain);
+    (void)wait_bar(drain, 0, abort_flag);
+   }
+  } else {
+    if (NB == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MANY_REGS));
     // ------------------------------------------------------------ compute warps: a thread is a query row
-    const int b = NB == 2 ? (warp - 2) >> 2 : 0;
+    const int b = NB == 2 ? (warp - 4) >> 2 : 0;
     const int quarter = warp & 3;
     const int row = quarter * 32 + lane;
     const int block0 = first + b * tb;               // the block's first token within the sequence
     const int i = block0 + (row >> P.log_pack);      // this row's token and head
     const int head = head0 + (row & (P.pack - 1));
     const int warp_i = block0 + ((quarter * 32) >> P.log_pack);
-    const int Tb = b ? T : T0;
+    const int Ub = b ? 0 : U0;                       // the block's first step
     const bool active = b == 0 || has1;
     const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
     const uint32_t o_addr = lane_addr + O_COL + (uint32_t)(b * D);
     const float A = P.a_scale;
     float sb = 0.f;
     if (ALIBI) sb = P.slopes[head] * LOG2E;
+    float bias[32];                                  // ALIBI: slope times the column within 32
+    if (ALIBI) {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) bias[e] = sb * (float)e;
+    }
     bool ok = !P.fail_first_wait;                    // the self-test: as if the first wait had run out
-    float m_ref = 0.f, l = 0.f;
-    for (int t = 0; active && ok && t < Tb; ++t) {
-      const int buf = NB == 2 ? b : (t & 1);
+    float m_ref = 0.f, l0 = 0.f, l1 = 0.f;
+    for (int u = Ub; active && ok && u < T; ++u) {
+      const int t = T - 1 - u, own = u - Ub;         // key tile, and how many the block has done
+      const int buf = NB == 2 ? b : (own & 1);
       const uint32_t s_addr = lane_addr + (uint32_t)(buf * KT);
-      const uint32_t phase = NB == 2 ? (uint32_t)(t & 1) : (uint32_t)((t >> 1) & 1);
-      const bool mask = t * KT + KT - 1 > block0;    // some row of the block does not see the whole tile
-      const int lim = i - t * KT, edge = (warp_i - t * KT) >> 5;
-      ok = __all_sync(0xffffffffu, wait_bar(s_full + buf, phase, abort_flag));
+      const uint32_t phase = NB == 2 ? (uint32_t)(own & 1) : (uint32_t)((own >> 1) & 1);
+      ok = __all_sync(0xffffffffu, wait_bar_eager(s_full + buf, phase, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      const float bias_t = ALIBI ? sb * (float)(t * KT - i) : 0.f;
-      uint32_t packed[KT / 2];
-      float lt = 0.f, tmax;
-      // The common tile: ONE read of S, weights taken against the reference the row already has; the row's maximum comes out of
-      // the same pass and tells whether that was good enough.
-      bool again = t == 0 || mask;
-      if (!again) {
-        tmax = tile_probs<KT, ALIBI, BF16, false>(s_addr, A, m_ref, sb, bias_t, lim, edge, packed, lt);
-        again = __any_sync(0xffffffffu, tmax > m_ref + (HEADROOM + SLACK));
-      } else {
-        tmax = tile_max<KT, ALIBI>(s_addr, A, sb, bias_t, lim, edge, mask);
+      // ---- the row of logits, and its maximum in log2 units (the scale is positive: maximum of the raw logits first, scale after)
+      uint32_t r[KT];
+      tmem_ld_row(s_addr, r);
+      // x2 = a_scale x + slope (j - i) log2 e: the part of the bias that depends on the column within 32 enters here, the rest with the reference
+      if (ALIBI) {
+#pragma unroll
+        for (int e = 0; e < KT; e += 2) {
+          float x0, x1;
+          fma2v(x0, x1, __uint_as_float(r[e]), __uint_as_float(r[e + 1]), A, bias[e & 31], bias[(e & 31) + 1]);
+          r[e] = __float_as_uint(x0);
+          r[e + 1] = __float_as_uint(x1);
+        }
       }
-      if (again) {
-        // The first tile, one with masked keys, or a row whose maximum outgrew its reference: set or move the reference (rescaling the
-        // row of O and its sum), then take the weights from S, which is still whole.
-        float fac = 1.f;
-        bool move = false;
-        if (t == 0) { m_ref = tmax - HEADROOM; }
-        else if (tmax > m_ref + (HEADROOM + SLACK)) { fac = fast_exp2(m_ref - (tmax - HEADROOM)); m_ref = tmax - HEADROOM; move = true; }
+      if (t * KT + KT - 1 > block0) {                // some row of the block does not see the whole tile
+        const int lim = i - t * KT, edge = (warp_i - t * KT) >> 5;      // the mask cuts the same 32 columns for the whole warp
+#pragma unroll
+        for (int c = 0; c < KT / 32; ++c) {
+          const int last = c < edge ? 31 : (c == edge ? (lim & 31) : -1);
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (e > last) r[c * 32 + e] = 0xff800000u;     // -infinity
+        }
+      }
+      const float from = ALIBI ? sb * (float)(t * KT - i) : 0.f;      // of the tile's first column
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < KT / 32; ++c) {
+        float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          m0 = max3(m0, __uint_as_float(r[c * 32 + e]), __uint_as_float(r[c * 32 + e + 1]));
+          m1 = max3(m1, __uint_as_float(r[c * 32 + e + 2]), __uint_as_float(r[c * 32 + e + 3]));
+        }
+        if (ALIBI) tmax = fmaxf(tmax, fmaxf(m0, m1) + fmaf(sb, (float)(c * 32), from));
+        else tmax = max3(tmax, m0, m1);
+      }
+      if (!ALIBI) tmax *= A;
+      // ---- the reference: set by the first tile, moved (the row of O and its sum rescaled) when the maximum exceeds it by more than the slack
+      if (own == 0) {
+        m_ref = fmaxf(tmax, LOWEST) - HEADROOM;      // finite where the tile holds no key for a row yet
+      } else {
+        const bool move = tmax > m_ref + (HEADROOM + SLACK);
         if (__any_sync(0xffffffffu, move)) {
+          const float fac = move ? fast_exp2(m_ref - (tmax - HEADROOM)) : 1.f;
+          if (move) m_ref = tmax - HEADROOM;
+          l0 *= fac;
+          l1 *= fac;
           // rows of O are accumulator lanes of these same threads.  With two blocks the value MMAs of the tiles before have completed (their
           // commit precedes the one that published S); one block that looks ahead has to wait for them.
           if (NB == 1) {
-            ok = __all_sync(0xffffffffu, wait_bar(v_done, (uint32_t)((t - 1) & 1), abort_flag));
+            ok = __all_sync(0xffffffffu, wait_bar(v_done, (uint32_t)((own - 1) & 1), abort_flag));
             if (!ok) break;
             tc_fence_after();
           }
-          l *= fac;
 #pragma unroll 1
-          for (int oc = 0; oc < D / 32; ++oc) {
-            float v[32];
-            tmem_ld_32x32(o_addr + (uint32_t)(oc * 32), v);
+          for (int oc = 0; oc < D / 16; ++oc) {
+            uint32_t w[16];
+            tmem_ld_32x16(o_addr + (uint32_t)(oc * 16), w);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint32_t w[16];
-#pragma unroll
-              for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(v[h * 16 + e] * fac);
-              tmem_st_32x16(o_addr + (uint32_t)(oc * 32 + h * 16), w);
-            }
+            for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * fac);
+            tmem_st_32x16(o_addr + (uint32_t)(oc * 16), w);
           }
           tmem_wait_st();
         }
-        if (mask) (void)tile_probs<KT, ALIBI, BF16, true>(s_addr, A, m_ref, sb, bias_t, lim, edge, packed, lt);
-        else (void)tile_probs<KT, ALIBI, BF16, false>(s_addr, A, m_ref, sb, bias_t, lim, edge, packed, lt);
       }
-      l += lt;
-      // P over the first half of S (every logit of the tile has been read by now)
+      // ---- weights 2^(x2 - m_ref), their sum (of the unrounded values), and P over the first half of S in two steps
 #pragma unroll
-      for (int c = 0; c < KT / 32; ++c) tmem_st_32x16(s_addr + (uint32_t)(c * 16), reinterpret_cast<const uint32_t(&)[16]>(packed[c * 16]));
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(p_full + buf);
+      for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int c = half * (KT / 64); c < (half + 1) * (KT / 64); ++c) {
+          uint32_t packed[16];
+          const float shift = (ALIBI ? fmaf(sb, (float)(c * 32), from) : 0.f) - m_ref;
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            float y0, y1;
+            fma2(y0, y1, __uint_as_float(r[c * 32 + e]), __uint_as_float(r[c * 32 + e + 1]), ALIBI ? 1.f : A, shift);
+            const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
+            add2(l0, l1, p0, p1);
+            packed[e / 2] = pack2<BF16>(p0, p1);
+          }
+          tmem_st_32x16(s_addr + (uint32_t)(c * 16), packed);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + 2 * buf + half);
+      }
     }
+    const float l = l0 + l1;
     // ---- output: O / l; NaN where the rows did not arrive
     if (active && ok) ok = __all_sync(0xffffffffu, wait_bar(o_full + b, 0, abort_flag));
     if (active) {
@@ -443,8 +409,8 @@ __global__ void __launch_bounds__(THREADS, 1) ragged_kernel(const __grid_constan
     const int nj = issued[0];
     for (int j = nj > RING ? nj - RING : 0; j < nj; ++j) {
       const bool is_v = j >= 2 && (j & 1) == 0;
-      const int t = is_v ? (j - 2) >> 1 : (AHEAD == 1 ? (j == 0 ? 0 : (j + 1) >> 1) : (j < 2 ? j : (j + 1) >> 1));
-      if (t >= T) continue;                                    // a position that is never loaded
+      const int u = is_v ? (j - 2) >> 1 : (AHEAD == 1 ? (j == 0 ? 0 : (j + 1) >> 1) : (j < 2 ? j : (j + 1) >> 1));
+      if (u >= T) continue;                                    // a position that is never loaded
       (void)mbar_wait_bounded(r_full + (j % RING), (uint32_t)((j / RING) & 1), TC_WAIT_LIMIT);
     }
     (void)mbar_wait_bounded(q_full, 0, TC_WAIT_LIMIT);
@@ -466,7 +432,7 @@ cudaError_t launch_ragged_d(const RaggedParams& P, int64_t slots, int groups, cu
   auto go = [&](auto kern) -> cudaError_t {
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_req);
     if (e != cudaSuccess) return e;
-    kern<<<dim3((unsigned)slots, (unsigned)groups), THREADS, smem_req, st>>>(P);
+    kern<<<dim3((unsigned)slots, (unsigned)groups), threads_of(NB), smem_req, st>>>(P);
     return cudaGetLastError();
   };
   return P.slopes ? go(ragged_kernel<D, true, BF16>) : go(ragged_kernel<D, false, BF16>);
