@@ -77,8 +77,8 @@ bool attend_ok(const kf_pages_attend_args* a) {
 struct AttendLayout { size_t partials, total; };
 AttendLayout attend_layout(const kf_pages_attend_args* a) {
   const kf_page_cache& c = a->cache;
-  const size_t plan = align_up((size_t)c.sequences * 8);
-  return {plan, plan + align_up(kf::pages_attend_partials(c.sequences, c.n_kv_heads, a->n_heads, c.head_dim) * 4)};
+  const size_t begin = align_up(((size_t)c.sequences + 1) * 8);
+  return {begin, begin + align_up(kf::pages_attend_partials(cache_of(c, nullptr, nullptr), a->n_heads) * 4)};
 }
 
 bool update_ok(const kf_pages_update_args* a) {
@@ -187,7 +187,7 @@ int kf_pages_attend(const kf_pages_attend_args* a, const void* d_q, const void* 
   p.bf16 = a->type == KF_TYPE_BF16;
   p.fail_first_wait = a->debug_fail_first_wait != 0;
   p.scale = a->logit_scale > 0.f ? a->logit_scale : (float)(1.0 / std::sqrt((double)c.head_dim));
-  p.plan = static_cast<int2*>(d_scratch);
+  p.begin = static_cast<int64_t*>(d_scratch);
   p.partials = reinterpret_cast<float*>(static_cast<unsigned char*>(d_scratch) + L.partials);
   return status(kf::launch_pages_attend(p, static_cast<cudaStream_t>(stream)));
 }

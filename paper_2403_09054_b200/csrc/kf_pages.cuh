@@ -65,12 +65,10 @@ struct PagesAttend {
   int32_t H;
   bool bf16, fail_first_wait;
   float scale;
-  int2* plan;                     // scratch [S]: (first chunk, chunks)
-  float* partials;                // scratch, see pages_attend_partials
+  int64_t* begin;                 // scratch [S + 1]: where a sequence begins among all tiles; the tiles of a warp
+  float* partials;                // scratch, pages_attend_partials floats
 };
-// Chunks that the sequences of one (key/value head, block of query heads) are cut into, at most, and floats of partial results in all.
-int pages_attend_chunks(int S, int Hkv, int H);
-size_t pages_attend_partials(int S, int Hkv, int H, int d);
+size_t pages_attend_partials(const PageCache& c, int H);
 cudaError_t launch_pages_attend(const PagesAttend& a, cudaStream_t stream);
 
 #ifdef __CUDACC__

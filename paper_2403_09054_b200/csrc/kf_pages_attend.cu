@@ -8,10 +8,11 @@
 // would have to be written back there first.  A product may take its terms in any order: a lane contracts the features (S) or
 // tokens (O) that its own wide loads bring, and S comes out in the layout in which P goes in, so that no logit passes through shared memory.
 //
-// Work is split by tokens: the tiles of all sequences are dealt out in chunks of about the same size to one wave of CTAs, whatever the
-// lengths are (the host does not know them: every CTA adds them up and finds its chunk).  The four warps of a CTA walk every fourth tile of the
-// chunk, each with a private ring of tiles that TMA fills with swizzled rows (both products' loads are then free of bank conflicts).
-// A chunk that is a whole sequence writes the output; others leave partial results that pages_merge_kernel joins.
+// Work is split by tiles: those of all (sequence, key/value head, block of query heads) units stand one after the other, and every warp of one wave
+// of CTAs gets the same number of consecutive ones, whatever the lengths are (the host does not know them: every CTA adds them up).
+// A warp walks its share with a private ring of tiles that TMA fills with swizzled rows (both products' loads are then free of bank conflicts),
+// across the borders of units.  A unit that lies within one share is written by its warp; others leave a partial result per
+// warp, which pages_merge_kernel joins.
 #include "kf_pages.cuh"
 #include "kf_tc.cuh"
 
@@ -20,8 +21,12 @@ namespace kf {
 namespace {
 
 constexpr int NW = 4, NT = NW * 32;
-constexpr int GB = 8;                       // query heads of a CTA
-constexpr int SMS = 148, RESIDENT = 3;      // CTAs that run at once: the size of a wave
+constexpr int GB = 8;                       // query heads of a unit
+constexpr int SMS = 148;
+constexpr int LEAST = 2;                    // tiles of a share
+constexpr int ENTRIES = 256;                // of a CTA's table of where sequences begin (one per sequence up to 256 of them)
+constexpr int BATCH = 16;                   // tiles a warp looks up at a time
+constexpr int MERGE_WARPS = 8;
 constexpr float FIRST_REF = -1e30f;         // below every logit, but finite
 constexpr float ROOM = 7.0f, GAP = 8.0f;    // weights are taken times 2^7 (binary16 holds 2^-32 to 2^8 of the reference); a reference moves by 2^8
 
@@ -29,15 +34,23 @@ template <int D>
 struct Shape {
   static constexpr int TILE = D == 256 ? 16 : 32;           // tokens
   static constexpr int BYTES = 2 * TILE * D;                // K and V
-  static constexpr int STAGES = 16384 / BYTES;              // per warp
-  static constexpr int HEAD = 8 * (D / 8 + 4) + 4;          // floats between two heads' sums in shared memory: spread over the banks
+  static constexpr int STAGES = D == 256 ? 3 : 16384 / BYTES;   // per warp
+  static constexpr int RESIDENT = D == 256 ? 2 : 3;         // CTAs of an SM, by registers (255 or 168 a thread); all of them are the wave
+};
+
+// What a warp knows of a tile before it comes to it.
+struct __align__(16) Ahead {
+  int row0, row1, rows, pad;        // first K row of its page or pages (-1: the second holds no token); tokens from its first on, may exceed TILE
+  float k0, v0, k1, v1;             // K scale times the logit scale, log2 of the V scale, of both pages
+  int seq, unit, tile, count;       // sequence, unit within it, tile within that, tiles of the unit
 };
 
 struct AttendParams {
   CUtensorMap tm;             // rows of d bytes: [pages][Hkv][2][page]; boxes of min(page, TILE) rows x min(d, 128) bytes, swizzled
   PagesAttend a;
-  int32_t group, blocks;      // query heads per key/value head, CTAs they take
-  int32_t target;             // chunks aimed at, per (key/value head, block of query heads)
+  int32_t group, blocks;      // query heads per key/value head, and units they make up
+  int32_t units;              // per sequence: key/value heads x blocks
+  int32_t rows;               // query heads of a partial result
   int32_t log_page;
   float scale;                // logit scale * log2(e)
 };
@@ -60,18 +73,17 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, i
 }
 
 // Sum over the CTA of one number per thread, and the sum over the threads before.
-__device__ __forceinline__ int cta_scan(int v, int* warp_sums, int& total) {
+__device__ __forceinline__ int64_t cta_scan(int64_t v, int64_t* warp_sums, int64_t& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int x = v;
+  int64_t x = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
-  __syncthreads();
   if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
-  int before = 0;
+  int64_t before = 0;
   total = 0;
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
@@ -82,7 +94,7 @@ __device__ __forceinline__ int cta_scan(int v, int* warp_sums, int& total) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(NT, RESIDENT) pages_attend_kernel(const __grid_constant__ AttendParams P) {
+__global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(const __grid_constant__ AttendParams P) {
   using C = Shape<D>;
   constexpr int TILE = C::TILE, ST = C::STAGES;
   constexpr int GROUPS = TILE / 8;              // groups of eight tokens, the columns of one S product
@@ -91,8 +103,8 @@ __global__ void __launch_bounds__(NT, RESIDENT) pages_attend_kernel(const __grid
   constexpr int HALF = TILE * D;                // bytes of a K tile
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bars_all[NW][ST];
-  __shared__ float sh_m[NW][GB], sh_l[NW][GB], sh_o[NW][GB];
-  __shared__ int sh_scan[NW], sh_at[4];
+  __shared__ int64_t sh_sums[NW], sh_begin[ENTRIES + 1];
+  __shared__ Ahead sh_ahead[NW][2 * BATCH];
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const PagesAttend& a = P.a;
@@ -104,34 +116,43 @@ __global__ void __launch_bounds__(NT, RESIDENT) pages_attend_kernel(const __grid
     return n > 0 && n <= capacity ? (n + TILE - 1) / TILE : 0;
   };
 
-  // ---- this CTA's chunk: size from the tiles of all sequences, sequence from the chunks before
-  int all = 0;
+  // ---- where the sequences begin, in tiles: an entry for every `stride` sequences
+  const int stride = (c.S + ENTRIES - 1) / ENTRIES;
+  int64_t all;
   {
-    int mine = 0;
-    for (int s = tid; s < c.S; s += NT) mine += tiles_of(s);
-    (void)cta_scan(mine, sh_scan, all);
-  }
-  const int size = max((all + P.target - 1) / P.target, 2 * NW) + NW - 1 & ~(NW - 1);   // tiles of a chunk
-  if (tid == 0) sh_at[0] = -1;
-  int chunks_before = 0;
-  for (int base = 0; base < c.S && chunks_before <= (int)blockIdx.x; base += NT) {
-    const int s = base + tid, n = (tiles_of(s) + size - 1) / size;
-    int total;
-    const int first = chunks_before + cta_scan(n, sh_scan, total);
-    if ((int)blockIdx.x >= first && (int)blockIdx.x < first + n) {
-      sh_at[0] = s; sh_at[1] = (int)blockIdx.x - first; sh_at[2] = n; sh_at[3] = first;
+    constexpr int PER = ENTRIES / NT;
+    int64_t own[PER], sum = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      own[i] = 0;
+      const int first = (tid * PER + i) * stride;
+      if (first < c.S)
+        for (int k = 0; k < stride; ++k) own[i] += tiles_of(first + k);
+      sum += own[i];
     }
-    chunks_before += total;
+    int64_t at = cta_scan(sum, sh_sums, all);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      sh_begin[tid * PER + i] = at;
+      at += own[i];
+    }
+    if (tid == NT - 1) sh_begin[ENTRIES] = all;
   }
   __syncthreads();
-  const int s = sh_at[0];
-  if (s < 0) return;
-  const int chunk = sh_at[1], chunks = sh_at[2];
-  const int kv = blockIdx.y / P.blocks, block = blockIdx.y % P.blocks;
-  if (chunk == 0 && blockIdx.y == 0 && tid == 0) a.plan[s] = make_int2(sh_at[3], chunks);
-  const int length = a.length[s];
-  const int tile0 = chunk * size, tile_end = min(tile0 + size, (length + TILE - 1) / TILE);
-  const int heads = min(GB, P.group - block * GB), head0 = kv * P.group + block * GB;
+  const int64_t total = all * P.units, warps = (int64_t)gridDim.x * NW;
+  const int64_t share = max((total + warps - 1) / warps, (int64_t)LEAST);
+  // for the merge: where each sequence begins, and the size of a share
+  for (int e = blockIdx.x + tid * (int)gridDim.x; e < ENTRIES && e * stride < c.S; e += (int)gridDim.x * NT) {
+    int64_t at = sh_begin[e];
+    for (int k = 0; k < stride && e * stride + k < c.S; ++k) {
+      a.begin[e * stride + k] = at;
+      at += tiles_of(e * stride + k);
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) a.begin[c.S] = share;
+  const int64_t me = (int64_t)blockIdx.x * NW + warp, from = me * share;
+  if (from >= total) return;
+  const int mine = (int)(min(from + share, total) - from);      // tiles of this warp
 
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* ring = smem + (size_t)warp * ST * C::BYTES;
@@ -142,44 +163,60 @@ __global__ void __launch_bounds__(NT, RESIDENT) pages_attend_kernel(const __grid
   }
   __syncwarp();
 
-  // ---- pages of the warp's tiles, 32 tiles at a time, a lane one of them: tile w is tile0 + warp + w NW of the sequence
-  const int mine = tile_end > tile0 + warp ? (tile_end - tile0 - warp + NW - 1) / NW : 0;
+  // ---- the tiles of the share, looked up 16 at a time by as many lanes
   const bool two = TILE > 16 && P.log_page == 4;      // a tile spans two pages
-  int id0 = 0, id1 = 0;
-  float ks0 = 0.f, ks1 = 0.f, vs0 = 0.f, vs1 = 0.f;   // K scale times the logit scale; log2 of the V scale
-  auto page_of = [&](int slot, bool used, int& id, float& ks, float& vs) {
-    id = used ? a.table[(size_t)s * c.W + slot] : 0;
+  Ahead* ahead = sh_ahead[warp];
+  auto page_of = [&](int s, int kv, int slot, int& row, float& ks, float& vs) {
+    int id = a.table[(size_t)s * c.W + slot];
     const bool bad = id < 0 || id >= c.pages;
     if (bad) id = 0;
-    float2 sc = make_float2(0.f, 1.f);
-    if (used) sc = *reinterpret_cast<const float2*>(c.scale + ((size_t)id * c.Hkv + kv) * 2);
-    ks = sc.x * P.scale;
-    vs = log2f(sc.y);
-    if (bad) { ks = nan_f32(); vs = ks; }             // a page that is missing: the output is NaN
+    const float2 sc = *reinterpret_cast<const float2*>(c.scale + ((size_t)id * c.Hkv + kv) * 2);
+    ks = bad ? nan_f32() : sc.x * P.scale;            // a page that is missing: the output is NaN
+    vs = bad ? nan_f32() : log2f(sc.y);
+    row = (id * c.Hkv + kv) * 2 << P.log_page;
   };
   auto look_up = [&](int w0) {
-    const int tile = tile0 + warp + (w0 + lane) * NW, token = tile * TILE;
-    const bool used = w0 + lane < mine;
-    page_of(token >> P.log_page, used, id0, ks0, vs0);
-    if (two) page_of((token >> P.log_page) + 1, used && token + 16 < length, id1, ks1, vs1);
+    if (lane < BATCH && w0 + lane < mine) {
+      const int64_t g = from + w0 + lane, in_all = g / P.units;
+      int lo = 0, hi = ENTRIES;                       // the last entry that does not begin behind it
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (sh_begin[mid] <= in_all) lo = mid; else hi = mid;
+      }
+      int64_t at = sh_begin[lo];
+      Ahead t;
+      t.seq = lo * stride;
+      t.count = tiles_of(t.seq);
+      while (at + t.count <= in_all) { at += t.count; t.count = tiles_of(++t.seq); }
+      const int64_t r = g - at * P.units;
+      t.unit = (int)(r / t.count);
+      t.tile = (int)(r - (int64_t)t.unit * t.count);
+      const int token = t.tile * TILE, kv = t.unit / P.blocks;
+      t.rows = a.length[t.seq] - token;
+      page_of(t.seq, kv, token >> P.log_page, t.row0, t.k0, t.v0);
+      t.row0 += token & (c.page - 1);
+      t.row1 = -1;
+      t.k1 = t.v1 = 0.f;
+      t.pad = 0;
+      if (two && t.rows > 16) page_of(t.seq, kv, (token >> P.log_page) + 1, t.row1, t.k1, t.v1);
+      ahead[(w0 + lane) & (2 * BATCH - 1)] = t;
+    }
+    __syncwarp();
   };
   auto issue = [&](int w) {                           // tile w into its slot of the ring
-    const int p0 = __shfl_sync(0xffffffffu, id0, w & 31), p1 = __shfl_sync(0xffffffffu, id1, w & 31);
     if (lane == 0) {
-      const int token = (tile0 + warp + w * NW) * TILE;
+      const int2 at = *reinterpret_cast<const int2*>(&ahead[w & (2 * BATCH - 1)]);
       uint64_t* bar = bars + w % ST;
-      unsigned char* dst = ring + (size_t)(w % ST) * C::BYTES;
-      const int row = ((p0 * c.Hkv + kv) * 2 << P.log_page) + (token & (c.page - 1));
-      mbar_expect_tx(bar, two && token + 16 >= length ? C::BYTES / 2 : C::BYTES);
+      unsigned char* dst = ring + (w % ST) * C::BYTES;
+      mbar_expect_tx(bar, two && at.y < 0 ? C::BYTES / 2 : C::BYTES);
 #pragma unroll
       for (int b = 0; b < D / ROWB; ++b) {
-        tma_load_2d(dst + b * TILE * ROWB, &P.tm, b * ROWB, row, bar);
-        tma_load_2d(dst + HALF + b * TILE * ROWB, &P.tm, b * ROWB, row + c.page, bar);
+        tma_load_2d(dst + b * TILE * ROWB, &P.tm, b * ROWB, at.x, bar);
+        tma_load_2d(dst + HALF + b * TILE * ROWB, &P.tm, b * ROWB, at.x + c.page, bar);
       }
-      if (two && token + 16 < length) {
-        const int row1 = (p1 * c.Hkv + kv) * 2 << P.log_page;
-        tma_load_2d(dst + 16 * ROWB, &P.tm, 0, row1, bar);
-        tma_load_2d(dst + HALF + 16 * ROWB, &P.tm, 0, row1 + c.page, bar);
+      if (at.y >= 0) {
+        tma_load_2d(dst + 16 * ROWB, &P.tm, 0, at.y, bar);
+        tma_load_2d(dst + HALF + 16 * ROWB, &P.tm, 0, at.y + c.page, bar);
       }
     }
   };
@@ -187,274 +224,282 @@ __global__ void __launch_bounds__(NT, RESIDENT) pages_attend_kernel(const __grid
   for (int w = 0; w < ST; ++w)
     if (w < mine) issue(w);
 
-  // ---- queries as the first operand of S: row = head r8, the quarter t4 of the features, four of them per step
-  uint32_t q0[KW], q1[KW];
-  {
-    const unsigned short* q = static_cast<const unsigned short*>(a.q) + (int64_t)s * a.q_sequence + (int64_t)(head0 + min(r8, heads - 1)) * a.q_head + t4 * (D / 4);
-    float top = 0.f;
-    uint2 raw[KW];
-#pragma unroll
-    for (int i = 0; i < KW; i += 2) {
-      const uint4 v = *reinterpret_cast<const uint4*>(q + 4 * i);
-      raw[i] = make_uint2(v.x, v.y);
-      raw[i + 1] = make_uint2(v.z, v.w);
-    }
-    if (a.bf16) {
-      // bfloat16 to binary16: exact after a division by a power of two that brings the head's largest feature to [1, 2), down to
-      // 2^-24 of it.  The power goes back into the logit scale.
-#pragma unroll
-      for (int i = 0; i < KW; ++i) {
-        const float f[4] = {__uint_as_float(raw[i].x << 16), __uint_as_float(raw[i].x & 0xffff0000u), __uint_as_float(raw[i].y << 16), __uint_as_float(raw[i].y & 0xffff0000u)};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(f[e]));
-      }
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    }
-    const int e = a.bf16 ? min(max((int)(__float_as_uint(top) >> 23), 1), 253) - 127 : 0;
-    const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-#pragma unroll
-    for (int i = 0; i < KW; ++i) {
-      if (a.bf16) {
-        q0[i] = h2(__floats2half2_rn(__uint_as_float(raw[i].x << 16) * down, __uint_as_float(raw[i].x & 0xffff0000u) * down));
-        q1[i] = h2(__floats2half2_rn(__uint_as_float(raw[i].y << 16) * down, __uint_as_float(raw[i].y & 0xffff0000u) * down));
-      } else {
-        q0[i] = raw[i].x;
-        q1[i] = raw[i].y;
-      }
-    }
-    top = __uint_as_float((uint32_t)(127 + e) << 23);
-    sh_o[warp][r8] = top;                             // for later: the head's power of two (the same from four lanes)
-  }
-  __syncwarp();
-  const float q_power = sh_o[warp][r8];
-  const float slope = a.slopes ? a.slopes[head0 + min(r8, heads - 1)] * LOG2E : 0.f;
+  bool failed = a.fail_first_wait;                    // the self-test: as if the first wait had run out
+  int w = 0, failed_at = 0;
+  while (w < mine) {
+    // ---- a unit, or the part of it that lies in this share
+    const int4 where = *reinterpret_cast<const int4*>(&ahead[w & (2 * BATCH - 1)].seq);
+    const int s = where.x, y = where.y, first = where.z, tiles = where.w;
+    const int end = min(mine, w + tiles - first);
+    const bool whole = first == 0 && w + tiles <= mine;
+    const int kv = y / P.blocks, block = y - kv * P.blocks;
+    const int heads = min(GB, P.group - block * GB), head0 = kv * P.group + block * GB, head = head0 + min(r8, heads - 1);
 
-  float m_x = FIRST_REF, m_o = FIRST_REF, l = 0.f;    // of head r8, references common to its four lanes; l: this lane's tokens
-  float o[D / 8][4];
-#pragma unroll
-  for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
-
-  // Scales of the tile that is worked on: `mine` may pass 32, then the next 32 pages are looked up before the first of them is fetched.
-  float cur_k0 = ks0, cur_v0 = vs0, cur_k1 = ks1, cur_v1 = vs1;
-  bool failed = a.fail_first_wait && mine > 0;
-  int w = 0;
-  for (; w < mine && !failed; ++w) {
-    if ((w & 31) == 0 && w > 0) { cur_k0 = ks0; cur_v0 = vs0; cur_k1 = ks1; cur_v1 = vs1; }
-    const float k0 = __shfl_sync(0xffffffffu, cur_k0, w & 31) * q_power, v0 = __shfl_sync(0xffffffffu, cur_v0, w & 31);
-    float k1 = k0, v1 = v0;
-    if (two) { k1 = __shfl_sync(0xffffffffu, cur_k1, w & 31) * q_power; v1 = __shfl_sync(0xffffffffu, cur_v1, w & 31); }
-    const int token = (tile0 + warp + w * NW) * TILE;
-    const int rows = length - token;                  // may exceed TILE
-    const unsigned char* buf = ring + (size_t)(w % ST) * C::BYTES;
-    const bool ok = mbar_wait_bounded(bars + w % ST, (uint32_t)(w / ST & 1));
-    if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-
-    // ---- logits: column = token r8 of a group, this lane's quarter of the features
-    float x[GROUPS][2];
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      const int row = g * 8 + r8;
-      uint32_t kw[KW];
-      if (D == 64) {
-        const uint4 v = *reinterpret_cast<const uint4*>(buf + row * 64 + ((t4 ^ (row >> 1 & 3)) << 4));
-        kw[0] = v.x; kw[1] = v.y; kw[2] = v.z; kw[3] = v.w;
-      } else {
-        // 16-byte pieces t4 D/64 + i of the row; those of 256-byte rows lie in two boxes
-#pragma unroll
-        for (int i = 0; i < KW / 4; ++i) {
-          const int piece = t4 * (KW / 4) + i;
-          const uint4 v = *reinterpret_cast<const uint4*>(buf + (piece >> 3) * (TILE * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
-          kw[4 * i] = v.x; kw[4 * i + 1] = v.y; kw[4 * i + 2] = v.z; kw[4 * i + 3] = v.w;
-        }
-      }
-      float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+    // queries as the first operand of S: row = head r8, the quarter t4 of the features, four of them per step in the order 0, 2, 1, 3
+    uint32_t q0[KW], q1[KW];
+    float q_power;
+    {
+      const unsigned short* q = static_cast<const unsigned short*>(a.q) + (int64_t)s * a.q_sequence + (int64_t)head * a.q_head + t4 * (D / 4);
 #pragma unroll
       for (int i = 0; i < KW; i += 2) {
-        mma(s0, q0[i], 0u, q1[i], 0u, code_pair(__byte_perm(kw[i], 0, 0x4140)), code_pair(__byte_perm(kw[i], 0, 0x4342)));
-        mma(s1, q0[i + 1], 0u, q1[i + 1], 0u, code_pair(__byte_perm(kw[i + 1], 0, 0x4140)), code_pair(__byte_perm(kw[i + 1], 0, 0x4342)));
+        const uint4 v = *reinterpret_cast<const uint4*>(q + 4 * i);
+        q0[i] = v.x; q1[i] = v.y;
+        q0[i + 1] = v.z; q1[i + 1] = v.w;
       }
-      const float kf = g >= 2 ? k1 : k0;
-      x[g][0] = (s0[0] + s1[0]) * kf;
-      x[g][1] = (s0[1] + s1[1]) * kf;
-    }
-    // head r8, tokens 8 g + 2 t4 and + 1
-    if (a.slopes) {
-      const float back = (float)(token + 2 * t4 - (length - 1));
+      int e = 0;
+      if (a.bf16) {
+        // bfloat16 to binary16: exact after a division by a power of two that brings the head's largest feature to [1, 2), down to
+        // 2^-24 of it.  The power goes back into the logit scale.
+        uint32_t top = 0;
 #pragma unroll
-      for (int g = 0; g < GROUPS; ++g) {
-        x[g][0] = fmaf(slope, back + (float)(8 * g), x[g][0]);
-        x[g][1] = fmaf(slope, back + (float)(8 * g + 1), x[g][1]);
-      }
-    }
-    if (rows < TILE) {
+        for (int i = 0; i < KW; ++i)
+          top = max(max(top, max(q0[i] & 0x7fffu, q1[i] & 0x7fffu)), max(q0[i] >> 16 & 0x7fffu, q1[i] >> 16 & 0x7fffu));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        e = min(max((int)(top >> 7), 1), 253) - 127;
+        const float down = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
-      for (int g = 0; g < GROUPS; ++g) {
-        if (8 * g + 2 * t4 >= rows) x[g][0] = -INFINITY;
-        if (8 * g + 2 * t4 + 1 >= rows) x[g][1] = -INFINITY;
-      }
-    }
-    // ---- references: of the softmax, and of the weights times the V scale of their page
-    float tx0 = -INFINITY, tx1 = -INFINITY;
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      if (g >= 2) tx1 = max3(tx1, x[g][0], x[g][1]);
-      else tx0 = max3(tx0, x[g][0], x[g][1]);
-    }
-    const float tx = fmaxf(tx0, tx1), to = fmaxf(tx0 + v0, tx1 + v1);
-    if (__any_sync(0xffffffffu, tx > m_x + GAP || to > m_o + GAP)) {
-      float nx = tx, no = to;
-      nx = fmaxf(nx, __shfl_xor_sync(0xffffffffu, nx, 1));
-      no = fmaxf(no, __shfl_xor_sync(0xffffffffu, no, 1));
-      nx = fmaxf(nx, __shfl_xor_sync(0xffffffffu, nx, 2));
-      no = fmaxf(no, __shfl_xor_sync(0xffffffffu, no, 2));
-      if (nx > m_x) { l *= fast_exp2(m_x - nx); m_x = nx; }
-      const float f = no > m_o ? fast_exp2(m_o - no) : 1.f;
-      if (no > m_o) m_o = no;
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][e] *= f;
-    }
-    uint32_t hi[GROUPS], lo[GROUPS];
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      l += fast_exp2(x[g][0] - m_x) + fast_exp2(x[g][1] - m_x);
-      const float up = (g >= 2 ? v1 : v0) - m_o + ROOM;
-      float p0 = fast_exp2(x[g][0] + up), p1 = fast_exp2(x[g][1] + up);
-      if (rows < TILE) {                              // a masked token counts as nothing, whatever its page's scale is
-        p0 = 8 * g + 2 * t4 < rows ? p0 : 0.f;
-        p1 = 8 * g + 2 * t4 + 1 < rows ? p1 : 0.f;
-      }
-      const __half2 h = __floats2half2_rn(p0, p1);
-      const float2 back = __half22float2(h);
-      hi[g] = h2(h);
-      lo[g] = h2(__floats2half2_rn(p0 - back.x, p1 - back.y));
-    }
-    // ---- values: column = feature r8 D/8 + i of product i, tokens 2 t4, + 1, + 8, + 9 of sixteen
-#pragma unroll
-    for (int k = 0; k < TILE / 16; ++k) {
-      constexpr int VW = D / 32;                      // words of V codes per token: an eighth of the features
-      uint32_t vw[4][VW];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = 16 * k + 2 * t4 + (e & 1) + 8 * (e >> 1);
-        if (D == 64) {
-          const uint2 v = *reinterpret_cast<const uint2*>(buf + HALF + row * 64 + (((r8 >> 1) ^ (row >> 1 & 3)) << 4) + (r8 & 1) * 8);
-          vw[e][0] = v.x; vw[e][1] = v.y;
-        } else {
-#pragma unroll
-          for (int i = 0; i < VW / 4; ++i) {
-            const int piece = r8 * (VW / 4) + i;
-            const uint4 v = *reinterpret_cast<const uint4*>(buf + HALF + (piece >> 3) * (TILE * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
-            vw[e][4 * i] = v.x; vw[e][4 * i + 1] = v.y; vw[e][4 * i + 2] = v.z; vw[e][4 * i + 3] = v.w;
-          }
+        for (int i = 0; i < KW; ++i) {
+          q0[i] = h2(__floats2half2_rn(__uint_as_float(q0[i] << 16) * down, __uint_as_float(q0[i] & 0xffff0000u) * down));
+          q1[i] = h2(__floats2half2_rn(__uint_as_float(q1[i] << 16) * down, __uint_as_float(q1[i] & 0xffff0000u) * down));
         }
       }
 #pragma unroll
-      for (int i = 0; i < VW; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          mma(o[4 * i + j], hi[2 * k], lo[2 * k], hi[2 * k + 1], lo[2 * k + 1], code_pair(__byte_perm(vw[0][i], vw[1][i], j | (4 + j) << 8)),
-              code_pair(__byte_perm(vw[2][i], vw[3][i], j | (4 + j) << 8)));
-    }
-    __syncwarp();                                     // the slot has been read by every lane
-    if (w + ST < mine) {
-      if (((w + ST) & 31) == 0) look_up(w + ST);
-      issue(w + ST);
-    }
-  }
-  if (failed)
-    for (int i = w; i < min(w + ST, mine); ++i) (void)mbar_wait_bounded(bars + i % ST, (uint32_t)(i / ST & 1));   // copies in flight
-
-  // ---- join the lanes, then the warps; the sums lie in the ring, which is done with
-  l += __shfl_xor_sync(0xffffffffu, l, 1);
-  l += __shfl_xor_sync(0xffffffffu, l, 2);
-  static_assert(GB * C::HEAD * 4 <= ST * C::BYTES, "a warp's sums fit its ring");
-  __syncwarp();
-  float* sums = reinterpret_cast<float*>(ring);
-#pragma unroll
-  for (int i = 0; i < D / 8; i += 4) {
-    float* at = sums + r8 * C::HEAD + 2 * t4 * (D / 8 + 4) + i;
-    *reinterpret_cast<float4*>(at) = make_float4(o[i][0] + o[i][2], o[i + 1][0] + o[i + 1][2], o[i + 2][0] + o[i + 2][2], o[i + 3][0] + o[i + 3][2]);
-    *reinterpret_cast<float4*>(at + D / 8 + 4) = make_float4(o[i][1] + o[i][3], o[i + 1][1] + o[i + 1][3], o[i + 2][1] + o[i + 2][3], o[i + 3][1] + o[i + 3][3]);
-  }
-  if (t4 == 0) {
-    sh_m[warp][r8] = m_x;
-    sh_o[warp][r8] = m_o;
-    sh_l[warp][r8] = failed ? nan_f32() : l;
-  }
-  __syncthreads();
-  float* partial = a.partials + ((size_t)blockIdx.x * gridDim.y + blockIdx.y) * GB * (D + 2);
-  for (int i = tid; i < heads * (D / 4); i += NT) {
-    const int h = i / (D / 4), f = (i - h * (D / 4)) * 4;
-    float mx = FIRST_REF, mo = FIRST_REF, lx = 0.f;
-#pragma unroll
-    for (int v = 0; v < NW; ++v) { mx = fmaxf(mx, sh_m[v][h]); mo = fmaxf(mo, sh_o[v][h]); }
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int v = 0; v < NW; ++v) {
-      const float fo = fast_exp2(sh_o[v][h] - mo);
-      const float4 t = *reinterpret_cast<const float4*>(smem + (size_t)v * ST * C::BYTES + 4 * (h * C::HEAD + f / (D / 8) * (D / 8 + 4) + f % (D / 8)));
-      acc.x = fmaf(t.x, fo, acc.x); acc.y = fmaf(t.y, fo, acc.y); acc.z = fmaf(t.z, fo, acc.z); acc.w = fmaf(t.w, fo, acc.w);
-      lx = fmaf(sh_l[v][h], fast_exp2(sh_m[v][h] - mx), lx);
-    }
-    // weights were taken against mo and times 2^7, their sum against mx
-    const float bring = fast_exp2(mo - mx - ROOM) * (chunks == 1 ? 1.f / lx : 1.f);
-    acc.x *= bring; acc.y *= bring; acc.z *= bring; acc.w *= bring;
-    if (chunks == 1) {
-      unsigned short* out = static_cast<unsigned short*>(a.out) + (int64_t)s * a.out_sequence + (int64_t)(head0 + h) * a.out_head + f;
-      uint2 r;
-      if (a.bf16) {
-        const __nv_bfloat162 b0 = __floats2bfloat162_rn(acc.x, acc.y), b1 = __floats2bfloat162_rn(acc.z, acc.w);
-        r = make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
-      } else {
-        r = make_uint2(h2(__floats2half2_rn(acc.x, acc.y)), h2(__floats2half2_rn(acc.z, acc.w)));
+      for (int i = 0; i < KW; ++i) {
+        const uint32_t x = q0[i], z = q1[i];
+        q0[i] = __byte_perm(x, z, 0x5410);
+        q1[i] = __byte_perm(x, z, 0x7632);
       }
-      *reinterpret_cast<uint2*>(out) = r;
-    } else {
-      *reinterpret_cast<float4*>(partial + h * D + f) = acc;
-      if (f == 0) { partial[GB * D + 2 * h] = mx; partial[GB * D + 2 * h + 1] = lx; }
+      q_power = __uint_as_float((uint32_t)(127 + e) << 23);
+    }
+    const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.f;
+
+    float m_x = FIRST_REF, m_o = FIRST_REF, l = 0.f;  // of head r8, references common to its four lanes; l: this lane's tokens
+    float o[D / 8][4];
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+
+    for (; w < end; ++w) {
+      const int rows = ahead[w & (2 * BATCH - 1)].rows;
+      const float4 scales = *reinterpret_cast<const float4*>(&ahead[w & (2 * BATCH - 1)].k0);
+      const float k0 = scales.x * q_power, v0 = scales.y;
+      float k1 = k0, v1 = v0;
+      if (two && rows > 16) { k1 = scales.z * q_power; v1 = scales.w; }
+      const unsigned char* buf = ring + (w % ST) * C::BYTES;
+      if (!failed && !__all_sync(0xffffffffu, mbar_wait_bounded(bars + w % ST, (uint32_t)(w / ST & 1)))) { failed = true; failed_at = w; }
+      if (failed) {                                   // nothing more is asked for; the units of the share still have to be gone through
+        if ((w + ST) % BATCH == 0 && w + ST < mine) look_up(w + ST);
+        continue;
+      }
+
+      // ---- logits: column = token r8 of a group, this lane's quarter of the features
+      float x[GROUPS][2];
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        const int row = g * 8 + r8;
+        uint32_t kw[KW];
+        if (D == 64) {
+          const uint4 v = *reinterpret_cast<const uint4*>(buf + row * 64 + ((t4 ^ (row >> 1 & 3)) << 4));
+          kw[0] = v.x; kw[1] = v.y; kw[2] = v.z; kw[3] = v.w;
+        } else {
+          // 16-byte pieces t4 D/64 + i of the row; those of 256-byte rows lie in two boxes
+#pragma unroll
+          for (int i = 0; i < KW / 4; ++i) {
+            const int piece = t4 * (KW / 4) + i;
+            const uint4 v = *reinterpret_cast<const uint4*>(buf + (piece >> 3) * (TILE * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
+            kw[4 * i] = v.x; kw[4 * i + 1] = v.y; kw[4 * i + 2] = v.z; kw[4 * i + 3] = v.w;
+          }
+        }
+        float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < KW; i += 2) {
+          mma(s0, q0[i], 0u, q1[i], 0u, code_pair(kw[i]), code_pair(kw[i] >> 8));
+          mma(s1, q0[i + 1], 0u, q1[i + 1], 0u, code_pair(kw[i + 1]), code_pair(kw[i + 1] >> 8));
+        }
+        const float kf = g >= 2 ? k1 : k0;
+        x[g][0] = (s0[0] + s1[0]) * kf;
+        x[g][1] = (s0[1] + s1[1]) * kf;
+        asm volatile("" ::: "memory");                // the next group's loads stay behind: registers
+      }
+      // head r8, tokens 8 g + 2 t4 and + 1
+      if (a.slopes) {
+        const float back = (float)(2 * t4 + 1 - rows);   // from the newest token to this one
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          x[g][0] = fmaf(slope, back + (float)(8 * g), x[g][0]);
+          x[g][1] = fmaf(slope, back + (float)(8 * g + 1), x[g][1]);
+        }
+      }
+      if (rows < TILE) {
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          if (8 * g + 2 * t4 >= rows) x[g][0] = -INFINITY;
+          if (8 * g + 2 * t4 + 1 >= rows) x[g][1] = -INFINITY;
+        }
+      }
+      // ---- references: of the softmax, and of the weights times the V scale of their page
+      float tx0 = -INFINITY, tx1 = -INFINITY;
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        if (g >= 2) tx1 = max3(tx1, x[g][0], x[g][1]);
+        else tx0 = max3(tx0, x[g][0], x[g][1]);
+      }
+      const float tx = fmaxf(tx0, tx1), to = fmaxf(tx0 + v0, tx1 + v1);
+      if (__any_sync(0xffffffffu, tx > m_x + GAP || to > m_o + GAP)) {
+        float nx = tx, no = to;
+        nx = fmaxf(nx, __shfl_xor_sync(0xffffffffu, nx, 1));
+        no = fmaxf(no, __shfl_xor_sync(0xffffffffu, no, 1));
+        nx = fmaxf(nx, __shfl_xor_sync(0xffffffffu, nx, 2));
+        no = fmaxf(no, __shfl_xor_sync(0xffffffffu, no, 2));
+        if (nx > m_x) { l *= fast_exp2(m_x - nx); m_x = nx; }
+        const float f = no > m_o ? fast_exp2(m_o - no) : 1.f;
+        if (no > m_o) m_o = no;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][e] *= f;
+      }
+      uint32_t hi[GROUPS], lo[GROUPS];
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        l += fast_exp2(x[g][0] - m_x) + fast_exp2(x[g][1] - m_x);
+        const float up = (g >= 2 ? v1 : v0) - m_o + ROOM;
+        float p0 = fast_exp2(x[g][0] + up), p1 = fast_exp2(x[g][1] + up);
+        if (rows < TILE) {                            // a masked token counts as nothing, whatever its page's scale is
+          p0 = 8 * g + 2 * t4 < rows ? p0 : 0.f;
+          p1 = 8 * g + 2 * t4 + 1 < rows ? p1 : 0.f;
+        }
+        const __half2 h = __floats2half2_rn(p0, p1);
+        const float2 back = __half22float2(h);
+        hi[g] = h2(h);
+        lo[g] = h2(__floats2half2_rn(p0 - back.x, p1 - back.y));
+      }
+      // ---- values: column = feature r8 D/8 + i of product i, tokens 2 t4, + 1, + 8, + 9 of sixteen
+#pragma unroll
+      for (int k = 0; k < TILE / 16; ++k) {
+        constexpr int VW = D / 32;                    // words of V codes per token: an eighth of the features
+        uint32_t vw[4][VW];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = 16 * k + 2 * t4 + (e & 1) + 8 * (e >> 1);
+          if (D == 64) {
+            const uint2 v = *reinterpret_cast<const uint2*>(buf + HALF + row * 64 + (((r8 >> 1) ^ (row >> 1 & 3)) << 4) + (r8 & 1) * 8);
+            vw[e][0] = v.x; vw[e][1] = v.y;
+          } else {
+#pragma unroll
+            for (int i = 0; i < VW / 4; ++i) {
+              const int piece = r8 * (VW / 4) + i;
+              const uint4 v = *reinterpret_cast<const uint4*>(buf + HALF + (piece >> 3) * (TILE * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
+              vw[e][4 * i] = v.x; vw[e][4 * i + 1] = v.y; vw[e][4 * i + 2] = v.z; vw[e][4 * i + 3] = v.w;
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < VW; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            mma(o[4 * i + j], hi[2 * k], lo[2 * k], hi[2 * k + 1], lo[2 * k + 1], code_pair(__byte_perm(vw[0][i], vw[1][i], j | (4 + j) << 8)),
+                code_pair(__byte_perm(vw[2][i], vw[3][i], j | (4 + j) << 8)));
+        asm volatile("" ::: "memory");
+      }
+      __syncwarp();                                   // the slot has been read by every lane
+      if (w + ST < mine) {
+        if ((w + ST) % BATCH == 0) look_up(w + ST);
+        issue(w + ST);
+      }
+    }
+
+    // ---- what the warp has of the unit.  Weights were taken against m_o and times 2^7, their sum against m_x; the lane has two runs of D/8 features.
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    if (failed) l = nan_f32();
+    const float bring = fast_exp2(m_o - m_x - ROOM) * (whole ? 1.f / l : 1.f);
+    if (r8 < heads) {
+      if (whole) {
+        unsigned short* out = static_cast<unsigned short*>(a.out) + (int64_t)s * a.out_sequence + (int64_t)head * a.out_head + 2 * t4 * (D / 8);
+#pragma unroll
+        for (int run = 0; run < 2; ++run)
+#pragma unroll
+          for (int i = 0; i < D / 8; i += 8) {
+            uint32_t r[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float u0 = (o[i + 2 * e][run] + o[i + 2 * e][run + 2]) * bring, u1 = (o[i + 2 * e + 1][run] + o[i + 2 * e + 1][run + 2]) * bring;
+              if (a.bf16) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(u0, u1);
+                r[e] = *reinterpret_cast<const uint32_t*>(&b);
+              } else {
+                r[e] = h2(__floats2half2_rn(u0, u1));
+              }
+            }
+            *reinterpret_cast<uint4*>(out + run * (D / 8) + i) = make_uint4(r[0], r[1], r[2], r[3]);
+          }
+      } else {
+        float* part = a.partials + ((me * 2 + (first == 0 ? 1 : 0)) * P.rows + r8) * (D + 4);
+#pragma unroll
+        for (int run = 0; run < 2; ++run)
+#pragma unroll
+          for (int i = 0; i < D / 8; i += 4)
+            *reinterpret_cast<float4*>(part + (2 * t4 + run) * (D / 8) + i) =
+                make_float4((o[i][run] + o[i][run + 2]) * bring, (o[i + 1][run] + o[i + 1][run + 2]) * bring, (o[i + 2][run] + o[i + 2][run + 2]) * bring,
+                            (o[i + 3][run] + o[i + 3][run + 2]) * bring);
+        if (t4 == 0) *reinterpret_cast<float2*>(part + D) = make_float2(m_x, l);
+      }
     }
   }
+  if (failed)                                         // copies in flight get a second bounded wait
+    for (int i = failed_at; i < min(failed_at + ST, mine); ++i) (void)mbar_wait_bounded(bars + i % ST, (uint32_t)(i / ST & 1));
 }
 
-// Joins the chunks of a sequence, and says what a sequence without chunks gets.  Grid: sequences, query heads; four warps take the chunks in turn.
+// Joins the partial results of a sequence's units, and says what a sequence without tokens gets.  Grid: sequences, query heads.
 template <int D>
-__global__ void __launch_bounds__(NT) pages_merge_kernel(const __grid_constant__ AttendParams P) {
-  __shared__ float sh_o[NW][D], sh_m[NW], sh_l[NW];
+__global__ void __launch_bounds__(MERGE_WARPS * 32) pages_merge_kernel(const __grid_constant__ AttendParams P) {
+  constexpr int TILE = Shape<D>::TILE;
+  __shared__ float sh_o[MERGE_WARPS][D], sh_m[MERGE_WARPS], sh_l[MERGE_WARPS];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const PagesAttend& a = P.a;
   const int s = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int length = a.length[s];
   const bool has = length > 0 && length <= a.c.W << P.log_page;
-  const int2 plan = has ? a.plan[s] : make_int2(0, 0);
-  if (has && plan.y == 1) return;
-  const int kv = h / P.group, y = kv * P.blocks + (h - kv * P.group) / GB, row = (h - kv * P.group) % GB;
+  const int kv = h / P.group, in_group = h - kv * P.group, block = in_group / GB, row = in_group % GB;
+  int64_t w0 = 0, w1 = -1;
+  if (has) {
+    const int64_t tiles = (length + TILE - 1) / TILE, share = a.begin[a.c.S];
+    const int64_t first = a.begin[s] * P.units + tiles * (kv * P.blocks + block);
+    w0 = first / share;
+    w1 = (first + tiles - 1) / share;
+    if (w0 == w1) return;                             // its warp has written it
+  }
   constexpr int E = D / 32;
   float m = FIRST_REF, l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int i = warp; i < plan.y; i += NW) {
-    const float* part = a.partials + ((size_t)(plan.x + i) * (a.c.Hkv * P.blocks) + y) * GB * (D + 2);
-    const float pm = part[GB * D + 2 * row], pl = part[GB * D + 2 * row + 1];
-    const float nm = fmaxf(m, pm), fo = fast_exp2(m - nm), fp = fast_exp2(pm - nm);
-    m = nm;
-    l = fmaf(l, fo, pl * fp);
+#pragma unroll 4
+  for (int64_t w = w0 + warp; w <= w1; w += MERGE_WARPS) {
+    const float* part = a.partials + ((w * 2 + (w == w0 ? 1 : 0)) * P.rows + row) * (D + 4);
+    const float2 ml = *reinterpret_cast<const float2*>(part + D);
+    float v[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], fo, part[row * D + lane + 32 * e] * fp);
+    for (int e = 0; e < E; ++e) v[e] = part[lane + 32 * e];
+    const float nm = fmaxf(m, ml.x), fo = fast_exp2(m - nm), fp = fast_exp2(ml.x - nm);
+    m = nm;
+    l = fmaf(l, fo, ml.y * fp);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], fo, v[e] * fp);
   }
   if (lane == 0) { sh_m[warp] = m; sh_l[warp] = l; }
 #pragma unroll
   for (int e = 0; e < E; ++e) sh_o[warp][lane + 32 * e] = o[e];
   __syncthreads();
-  const float top = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
-  for (int f = threadIdx.x; f < D; f += NT) {
+  float top = sh_m[0];
+#pragma unroll
+  for (int w = 1; w < MERGE_WARPS; ++w) top = fmaxf(top, sh_m[w]);
+  for (int f = threadIdx.x; f < D; f += MERGE_WARPS * 32) {
     float acc = 0.f, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
+    for (int w = 0; w < MERGE_WARPS; ++w) {
       const float t = fast_exp2(sh_m[w] - top);
       acc = fmaf(sh_o[w][f], t, acc);
       sum = fmaf(sh_l[w], t, sum);
@@ -467,23 +512,27 @@ __global__ void __launch_bounds__(NT) pages_merge_kernel(const __grid_constant__
 }
 
 int blocks_of(int group) { return (group + GB - 1) / GB; }
-int target_of(int Hkv, int blocks) {
-  const int t = SMS * RESIDENT / (Hkv * blocks);
-  return t > 1 ? t : 1;
+// CTAs of a launch: a wave, or fewer where all tables together could not keep it busy.
+int ctas_of(int S, int W, int page, int Hkv, int group, int d) {
+  const int tile = d == 256 ? 16 : 32;
+  const int64_t most = (int64_t)S * (((int64_t)W * page + tile - 1) / tile) * Hkv * blocks_of(group);
+  const int64_t ctas = (most + NW * LEAST - 1) / (NW * LEAST);
+  const int wave = SMS * (d == 256 ? Shape<256>::RESIDENT : Shape<128>::RESIDENT);
+  return (int)(ctas < wave ? ctas : wave);
 }
 
 template <int D>
 cudaError_t launch_attend_d(const AttendParams& P, cudaStream_t stream) {
   constexpr size_t smem = 1024 + (size_t)NW * Shape<D>::STAGES * Shape<D>::BYTES;
-  static_assert(RESIDENT * (smem + 2048) <= 227 * 1024, "shared memory of the CTAs that are to run at once");
+  static_assert(Shape<D>::RESIDENT * (smem + NW * 2 * BATCH * sizeof(Ahead) + 8 * (ENTRIES + NW * 5 + 1) + 1024) <= 228 * 1024, "shared memory of the CTAs that are to run at once");
   cudaError_t e = cudaFuncSetAttribute(pages_attend_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   const PageCache& c = P.a.c;
-  pages_attend_kernel<D><<<dim3((unsigned)(P.target + c.S), (unsigned)(c.Hkv * P.blocks)), NT, smem, stream>>>(P);
+  pages_attend_kernel<D><<<ctas_of(c.S, c.W, c.page, c.Hkv, P.group, D), NT, smem, stream>>>(P);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)c.S, (unsigned)P.a.H);
-  cfg.blockDim = dim3(NT);
+  cfg.blockDim = dim3(MERGE_WARPS * 32);
   cfg.stream = stream;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -495,9 +544,9 @@ cudaError_t launch_attend_d(const AttendParams& P, cudaStream_t stream) {
 
 }  // namespace
 
-int pages_attend_chunks(int S, int Hkv, int H) { return target_of(Hkv, blocks_of(H / Hkv)) + S; }
-size_t pages_attend_partials(int S, int Hkv, int H, int d) {
-  return (size_t)pages_attend_chunks(S, Hkv, H) * Hkv * blocks_of(H / Hkv) * GB * (d + 2);
+size_t pages_attend_partials(const PageCache& c, int H) {
+  const int group = H / c.Hkv, rows = group < GB ? group : GB;
+  return (size_t)ctas_of(c.S, c.W, c.page, c.Hkv, group, c.d) * NW * 2 * rows * (c.d + 4);
 }
 
 cudaError_t launch_pages_attend(const PagesAttend& a, cudaStream_t stream) {
@@ -505,7 +554,8 @@ cudaError_t launch_pages_attend(const PagesAttend& a, cudaStream_t stream) {
   P.a = a;
   P.group = a.H / a.c.Hkv;
   P.blocks = blocks_of(P.group);
-  P.target = target_of(a.c.Hkv, P.blocks);
+  P.units = a.c.Hkv * P.blocks;
+  P.rows = P.group < GB ? P.group : GB;
   while ((1 << P.log_page) < a.c.page) ++P.log_page;
   P.scale = a.scale * LOG2E;
   const int D = a.c.d, tile = D == 256 ? 16 : 32;
