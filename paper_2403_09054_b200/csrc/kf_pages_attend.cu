@@ -40,13 +40,15 @@ struct Shape {
 
 // What a warp knows of a tile before it comes to it.
 struct __align__(16) Ahead {
-  int row0, row1, rows, pad;        // first K row of its page or pages (-1: the second holds no token); tokens from its first on, may exceed TILE
+  int at0, at1, rows, in_page;      // (page, head) of its page or pages (-1: the second holds no token); tokens from its first on, may exceed TILE; row
+                                    // of its first token in its page
   float k0, v0, k1, v1;             // K scale times the logit scale, log2 of the V scale, of both pages
   int seq, unit, tile, count;       // sequence, unit within it, tile within that, tiles of the unit
 };
 
 struct AttendParams {
-  CUtensorMap tm;             // rows of d bytes: [pages][Hkv][2][page]; boxes of min(page, TILE) rows x min(d, 128) bytes, swizzled
+  CUtensorMap tm;             // [pages x Hkv x 2][page] rows of d bytes; boxes of min(d, 128) bytes x min(page, TILE) rows x K and V (one of them where a
+                              // tile spans two pages), swizzled
   PagesAttend a;
   int32_t group, blocks;      // query heads per key/value head, and units they make up
   int32_t units;              // per sequence: key/value heads x blocks
@@ -59,6 +61,11 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The same onto nothing.
+__device__ __forceinline__ void mma0(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t h2(__half2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
 __device__ __forceinline__ __half2 b2(uint32_t v) { return *reinterpret_cast<const __half2*>(&v); }
 // A pair of codes, moved to [b, x, b', x] by a byte permutation, as binary16 integers: 1024 + (c + 128) has the bits 0x6400 | (c ^ 0x80).
@@ -66,10 +73,6 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t spread) {
   uint32_t r;
   asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(r) : "r"(spread), "r"(0x00ff00ffu), "r"(0x64806480u));   // (a & b) ^ c
   return h2(__hadd2(b2(r), b2(0xe480e480u)));                                                               // - 1152
-}
-__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int c0, int c1, uint64_t* bar) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-               ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1) : "memory");
 }
 
 // Sum over the CTA of one number per thread, and the sum over the threads before.
@@ -100,7 +103,8 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
   constexpr int GROUPS = TILE / 8;              // groups of eight tokens, the columns of one S product
   constexpr int KW = D / 16;                    // words of K codes a lane holds per token: its quarter of the features
   constexpr int ROWB = D < 128 ? D : 128;       // bytes of a shared-memory row
-  constexpr int HALF = TILE * D;                // bytes of a K tile
+  constexpr int VALUES = TILE * ROWB;           // a slot: K rows, V rows, of the first 128 features, then of the others
+  constexpr int COLS = 2 * TILE * ROWB;
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bars_all[NW][ST];
   __shared__ int64_t sh_sums[NW], sh_begin[ENTRIES + 1];
@@ -166,14 +170,14 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
   // ---- the tiles of the share, looked up 16 at a time by as many lanes
   const bool two = TILE > 16 && P.log_page == 4;      // a tile spans two pages
   Ahead* ahead = sh_ahead[warp];
-  auto page_of = [&](int s, int kv, int slot, int& row, float& ks, float& vs) {
+  auto page_of = [&](int s, int kv, int slot, int& at, float& ks, float& vs) {
     int id = a.table[(size_t)s * c.W + slot];
     const bool bad = id < 0 || id >= c.pages;
     if (bad) id = 0;
     const float2 sc = *reinterpret_cast<const float2*>(c.scale + ((size_t)id * c.Hkv + kv) * 2);
     ks = bad ? nan_f32() : sc.x * P.scale;            // a page that is missing: the output is NaN
     vs = bad ? nan_f32() : log2f(sc.y);
-    row = (id * c.Hkv + kv) * 2 << P.log_page;
+    at = id * c.Hkv + kv;
   };
   auto look_up = [&](int w0) {
     if (lane < BATCH && w0 + lane < mine) {
@@ -193,30 +197,31 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
       t.tile = (int)(r - (int64_t)t.unit * t.count);
       const int token = t.tile * TILE, kv = t.unit / P.blocks;
       t.rows = a.length[t.seq] - token;
-      page_of(t.seq, kv, token >> P.log_page, t.row0, t.k0, t.v0);
-      t.row0 += token & (c.page - 1);
-      t.row1 = -1;
+      page_of(t.seq, kv, token >> P.log_page, t.at0, t.k0, t.v0);
+      t.in_page = token & (c.page - 1);
+      t.at1 = -1;
       t.k1 = t.v1 = 0.f;
-      t.pad = 0;
-      if (two && t.rows > 16) page_of(t.seq, kv, (token >> P.log_page) + 1, t.row1, t.k1, t.v1);
+      if (two && t.rows > 16) page_of(t.seq, kv, (token >> P.log_page) + 1, t.at1, t.k1, t.v1);
       ahead[(w0 + lane) & (2 * BATCH - 1)] = t;
     }
     __syncwarp();
   };
   auto issue = [&](int w) {                           // tile w into its slot of the ring
     if (lane == 0) {
-      const int2 at = *reinterpret_cast<const int2*>(&ahead[w & (2 * BATCH - 1)]);
+      const int4 at = *reinterpret_cast<const int4*>(&ahead[w & (2 * BATCH - 1)]);
       uint64_t* bar = bars + w % ST;
       unsigned char* dst = ring + (w % ST) * C::BYTES;
       mbar_expect_tx(bar, two && at.y < 0 ? C::BYTES / 2 : C::BYTES);
+      if (!two) {
 #pragma unroll
-      for (int b = 0; b < D / ROWB; ++b) {
-        tma_load_2d(dst + b * TILE * ROWB, &P.tm, b * ROWB, at.x, bar);
-        tma_load_2d(dst + HALF + b * TILE * ROWB, &P.tm, b * ROWB, at.x + c.page, bar);
-      }
-      if (at.y >= 0) {
-        tma_load_2d(dst + 16 * ROWB, &P.tm, 0, at.y, bar);
-        tma_load_2d(dst + HALF + 16 * ROWB, &P.tm, 0, at.y + c.page, bar);
+        for (int b = 0; b < D / ROWB; ++b) tma_load_3d(dst + b * COLS, &P.tm, b * ROWB, at.w, 2 * at.x, bar);
+      } else {
+        tma_load_3d(dst, &P.tm, 0, 0, 2 * at.x, bar);
+        tma_load_3d(dst + VALUES, &P.tm, 0, 0, 2 * at.x + 1, bar);
+        if (at.y >= 0) {
+          tma_load_3d(dst + 16 * ROWB, &P.tm, 0, 0, 2 * at.y, bar);
+          tma_load_3d(dst + VALUES + 16 * ROWB, &P.tm, 0, 0, 2 * at.y + 1, bar);
+        }
       }
     }
   };
@@ -308,19 +313,19 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
 #pragma unroll
           for (int i = 0; i < KW / 4; ++i) {
             const int piece = t4 * (KW / 4) + i;
-            const uint4 v = *reinterpret_cast<const uint4*>(buf + (piece >> 3) * (TILE * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
+            const uint4 v = *reinterpret_cast<const uint4*>(buf + (piece >> 3) * COLS + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
             kw[4 * i] = v.x; kw[4 * i + 1] = v.y; kw[4 * i + 2] = v.z; kw[4 * i + 3] = v.w;
           }
         }
-        float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+        float sum[4];
 #pragma unroll
-        for (int i = 0; i < KW; i += 2) {
-          mma(s0, q0[i], 0u, q1[i], 0u, code_pair(kw[i]), code_pair(kw[i] >> 8));
-          mma(s1, q0[i + 1], 0u, q1[i + 1], 0u, code_pair(kw[i + 1]), code_pair(kw[i + 1] >> 8));
+        for (int i = 0; i < KW; ++i) {
+          if (i == 0) mma0(sum, q0[i], 0u, q1[i], 0u, code_pair(kw[i]), code_pair(kw[i] >> 8));
+          else mma(sum, q0[i], 0u, q1[i], 0u, code_pair(kw[i]), code_pair(kw[i] >> 8));
         }
         const float kf = g >= 2 ? k1 : k0;
-        x[g][0] = (s0[0] + s1[0]) * kf;
-        x[g][1] = (s0[1] + s1[1]) * kf;
+        x[g][0] = sum[0] * kf;
+        x[g][1] = sum[1] * kf;
         asm volatile("" ::: "memory");                // the next group's loads stay behind: registers
       }
       // head r8, tokens 8 g + 2 t4 and + 1
@@ -385,13 +390,13 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
         for (int e = 0; e < 4; ++e) {
           const int row = 16 * k + 2 * t4 + (e & 1) + 8 * (e >> 1);
           if (D == 64) {
-            const uint2 v = *reinterpret_cast<const uint2*>(buf + HALF + row * 64 + (((r8 >> 1) ^ (row >> 1 & 3)) << 4) + (r8 & 1) * 8);
+            const uint2 v = *reinterpret_cast<const uint2*>(buf + VALUES + row * 64 + (((r8 >> 1) ^ (row >> 1 & 3)) << 4) + (r8 & 1) * 8);
             vw[e][0] = v.x; vw[e][1] = v.y;
           } else {
 #pragma unroll
             for (int i = 0; i < VW / 4; ++i) {
               const int piece = r8 * (VW / 4) + i;
-              const uint4 v = *reinterpret_cast<const uint4*>(buf + HALF + (piece >> 3) * (TILE * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
+              const uint4 v = *reinterpret_cast<const uint4*>(buf + VALUES + (piece >> 3) * COLS + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
               vw[e][4 * i] = v.x; vw[e][4 * i + 1] = v.y; vw[e][4 * i + 2] = v.z; vw[e][4 * i + 3] = v.w;
             }
           }
@@ -559,9 +564,9 @@ cudaError_t launch_pages_attend(const PagesAttend& a, cudaStream_t stream) {
   while ((1 << P.log_page) < a.c.page) ++P.log_page;
   P.scale = a.scale * LOG2E;
   const int D = a.c.d, tile = D == 256 ? 16 : 32;
-  const uint64_t dims[2] = {(uint64_t)D, (uint64_t)a.c.pages * a.c.Hkv * 2 * a.c.page}, strides[1] = {(uint64_t)D};
-  const uint32_t box[2] = {(uint32_t)(D < 128 ? D : 128), (uint32_t)(a.c.page < tile ? a.c.page : tile)};
-  if (!make_tensor_map(&P.tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, a.c.codes, dims, strides, box, D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
+  const uint64_t dims[3] = {(uint64_t)D, (uint64_t)a.c.page, (uint64_t)a.c.pages * a.c.Hkv * 2}, strides[2] = {(uint64_t)D, (uint64_t)a.c.page * D};
+  const uint32_t box[3] = {(uint32_t)(D < 128 ? D : 128), (uint32_t)(a.c.page < tile ? a.c.page : tile), a.c.page < tile ? 1u : 2u};
+  if (!make_tensor_map(&P.tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, a.c.codes, dims, strides, box, D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
     return cudaErrorNotSupported;
   switch (D) {
     case 64: return launch_attend_d<64>(P, stream);
