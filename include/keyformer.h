@@ -507,7 +507,7 @@ int kf_pages_read(const kf_page_cache* cache, const kf_page_rows* rows, const vo
  *   out = sum_j softmax_j(x_j) v_j,   x_j = logit_scale q k_j (- slope_h (length - 1 - j) with KF_BIAS_ALIBI)
  * A sequence without tokens gets zeros; one whose length is negative or behind its table, or that needs a missing page, gets NaN. */
 typedef struct kf_pages_attend_args {
-  kf_page_cache cache;
+  kf_page_cache cache;                /* S * table_width * page_tokens * H < 2^35 is always accepted              */
   int32_t n_heads, type;              /* H: Hkv divides H; of q and out: KF_TYPE_FP16 or KF_TYPE_BF16              */
   int32_t bias_mode;                  /* KF_BIAS_*                                                                */
   float   logit_scale;                /* 0 => 1/sqrt(d)                                                           */

@@ -72,13 +72,14 @@ bool attend_ok(const kf_pages_attend_args* a) {
   if (a->debug_fail_first_wait < 0 || a->debug_fail_first_wait > 1) return false;
   for (int64_t s : {a->q_sequence_stride, a->q_head_stride, a->out_sequence_stride, a->out_head_stride})
     if (!stride_ok(s, a->cache.head_dim)) return false;
+  if (!kf::pages_attend_fits(cache_of(a->cache, nullptr, nullptr), a->n_heads)) return false;
   return apart(a->cache.sequences, a->out_sequence_stride, a->n_heads, a->out_head_stride, a->cache.head_dim);
 }
 struct AttendLayout { size_t partials, total; };
 AttendLayout attend_layout(const kf_pages_attend_args* a) {
   const kf_page_cache& c = a->cache;
-  const size_t begin = align_up(((size_t)c.sequences + 1) * 8);
-  return {begin, begin + align_up(kf::pages_attend_partials(cache_of(c, nullptr, nullptr), a->n_heads) * 4)};
+  const size_t splits = align_up((size_t)kf::pages_attend_shares(cache_of(c, nullptr, nullptr), a->n_heads) * 32);
+  return {splits, splits + align_up(kf::pages_attend_partials(cache_of(c, nullptr, nullptr), a->n_heads) * 4)};
 }
 
 bool update_ok(const kf_pages_update_args* a) {
@@ -187,7 +188,7 @@ int kf_pages_attend(const kf_pages_attend_args* a, const void* d_q, const void* 
   p.bf16 = a->type == KF_TYPE_BF16;
   p.fail_first_wait = a->debug_fail_first_wait != 0;
   p.scale = a->logit_scale > 0.f ? a->logit_scale : (float)(1.0 / std::sqrt((double)c.head_dim));
-  p.begin = static_cast<int64_t*>(d_scratch);
+  p.splits = static_cast<int4*>(d_scratch);
   p.partials = reinterpret_cast<float*>(static_cast<unsigned char*>(d_scratch) + L.partials);
   return status(kf::launch_pages_attend(p, static_cast<cudaStream_t>(stream)));
 }

@@ -65,9 +65,11 @@ struct PagesAttend {
   int32_t H;
   bool bf16, fail_first_wait;
   float scale;
-  int64_t* begin;                 // scratch [S + 1]: where a sequence begins among all tiles; the tiles of a warp
+  int4* splits;                   // scratch, two per share (warp): the unit that begins in it and goes on behind it, and the CTAs that it covers
   float* partials;                // scratch, pages_attend_partials floats
 };
+bool pages_attend_fits(const PageCache& c, int H);     // tiles are counted in 32 bits
+int pages_attend_shares(const PageCache& c, int H);
 size_t pages_attend_partials(const PageCache& c, int H);
 cudaError_t launch_pages_attend(const PagesAttend& a, cudaStream_t stream);
 

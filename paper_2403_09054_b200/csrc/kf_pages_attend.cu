@@ -35,6 +35,7 @@ struct Shape {
   static constexpr int TILE = D == 256 ? 16 : 32;           // tokens
   static constexpr int BYTES = 2 * TILE * D;                // K and V
   static constexpr int STAGES = D == 256 ? 3 : 16384 / BYTES;   // per warp
+  static constexpr int HEAD = 8 * (D / 8 + 4) + 4;          // floats between two heads' sums in shared memory: spread over the banks
   static constexpr int RESIDENT = D == 256 ? 2 : 3;         // CTAs of an SM, by registers (255 or 168 a thread); all of them are the wave
 };
 
@@ -76,17 +77,17 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t spread) {
 }
 
 // Sum over the CTA of one number per thread, and the sum over the threads before.
-__device__ __forceinline__ int64_t cta_scan(int64_t v, int64_t* warp_sums, int64_t& total) {
+__device__ __forceinline__ int cta_scan(int v, int* warp_sums, int& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int64_t x = v;
+  int x = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
   if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
-  int64_t before = 0;
+  int before = 0;
   total = 0;
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
@@ -107,8 +108,9 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
   constexpr int COLS = 2 * TILE * ROWB;
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bars_all[NW][ST];
-  __shared__ int64_t sh_sums[NW], sh_begin[ENTRIES + 1];
+  __shared__ int sh_sums[NW], sh_begin[ENTRIES + 1];
   __shared__ Ahead sh_ahead[NW][2 * BATCH];
+  __shared__ float2 sh_ml[NW][GB];
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const PagesAttend& a = P.a;
@@ -122,10 +124,10 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
 
   // ---- where the sequences begin, in tiles: an entry for every `stride` sequences
   const int stride = (c.S + ENTRIES - 1) / ENTRIES;
-  int64_t all;
+  int all;
   {
     constexpr int PER = ENTRIES / NT;
-    int64_t own[PER], sum = 0;
+    int own[PER], sum = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       own[i] = 0;
@@ -134,7 +136,7 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
         for (int k = 0; k < stride; ++k) own[i] += tiles_of(first + k);
       sum += own[i];
     }
-    int64_t at = cta_scan(sum, sh_sums, all);
+    int at = cta_scan(sum, sh_sums, all);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       sh_begin[tid * PER + i] = at;
@@ -143,20 +145,21 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
     if (tid == NT - 1) sh_begin[ENTRIES] = all;
   }
   __syncthreads();
-  const int64_t total = all * P.units, warps = (int64_t)gridDim.x * NW;
-  const int64_t share = max((total + warps - 1) / warps, (int64_t)LEAST);
-  // for the merge: where each sequence begins, and the size of a share
-  for (int e = blockIdx.x + tid * (int)gridDim.x; e < ENTRIES && e * stride < c.S; e += (int)gridDim.x * NT) {
-    int64_t at = sh_begin[e];
-    for (int k = 0; k < stride && e * stride + k < c.S; ++k) {
-      a.begin[e * stride + k] = at;
-      at += tiles_of(e * stride + k);
-    }
+  const int total = all * P.units, warps = gridDim.x * NW;        // the host makes sure that there are fewer than 2^31 of them
+  const int share = max((int)(((uint32_t)total + warps - 1) / (uint32_t)warps), LEAST);
+  const int me = blockIdx.x * NW + warp;
+  const int from = (int)min((int64_t)me * share, (int64_t)total);
+  // ---- sequences without tiles: zeros, or NaN where the length is not valid
+  for (int i = me; i < c.S; i += warps) {
+    const int n = a.length[i];
+    if (n > 0 && n <= capacity) continue;
+    const uint32_t v = n == 0 ? 0u : 0x7fff7fffu;
+    for (int e = lane; e < a.H * (D / 8); e += 32)
+      *reinterpret_cast<uint4*>(static_cast<unsigned short*>(a.out) + (int64_t)i * a.out_sequence + (int64_t)(e / (D / 8)) * a.out_head + e % (D / 8) * 8) = make_uint4(v, v, v, v);
   }
-  if (blockIdx.x == 0 && tid == 0) a.begin[c.S] = share;
-  const int64_t me = (int64_t)blockIdx.x * NW + warp, from = me * share;
+  if (lane == 0) a.splits[2 * me].x = -1;             // no unit begins in this share and goes on behind it, as far as is known
   if (from >= total) return;
-  const int mine = (int)(min(from + share, total) - from);      // tiles of this warp
+  const int mine = min(share, total - from);      // tiles of this warp
 
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* ring = smem + (size_t)warp * ST * C::BYTES;
@@ -181,20 +184,20 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
   };
   auto look_up = [&](int w0) {
     if (lane < BATCH && w0 + lane < mine) {
-      const int64_t g = from + w0 + lane, in_all = g / P.units;
+      const int g = from + w0 + lane, in_all = (int)((uint32_t)g / (uint32_t)P.units);
       int lo = 0, hi = ENTRIES;                       // the last entry that does not begin behind it
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (sh_begin[mid] <= in_all) lo = mid; else hi = mid;
       }
-      int64_t at = sh_begin[lo];
+      int at = sh_begin[lo];
       Ahead t;
       t.seq = lo * stride;
-      t.count = tiles_of(t.seq);
+      t.count = stride == 1 ? sh_begin[lo + 1] - at : tiles_of(t.seq);
       while (at + t.count <= in_all) { at += t.count; t.count = tiles_of(++t.seq); }
-      const int64_t r = g - at * P.units;
-      t.unit = (int)(r / t.count);
-      t.tile = (int)(r - (int64_t)t.unit * t.count);
+      const int r = g - at * P.units;
+      t.unit = (int)((uint32_t)r / (uint32_t)t.count);
+      t.tile = r - t.unit * t.count;
       const int token = t.tile * TILE, kv = t.unit / P.blocks;
       t.rows = a.length[t.seq] - token;
       page_of(t.seq, kv, token >> P.log_page, t.at0, t.k0, t.v0);
@@ -235,7 +238,7 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
     // ---- a unit, or the part of it that lies in this share
     const int4 where = *reinterpret_cast<const int4*>(&ahead[w & (2 * BATCH - 1)].seq);
     const int s = where.x, y = where.y, first = where.z, tiles = where.w;
-    const int end = min(mine, w + tiles - first);
+    const int begun = w, end = min(mine, w + tiles - first);
     const bool whole = first == 0 && w + tiles <= mine;
     const int kv = y / P.blocks, block = y - kv * P.blocks;
     const int heads = min(GB, P.group - block * GB), head0 = kv * P.group + block * GB, head = head0 + min(r8, heads - 1);
@@ -421,9 +424,9 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
     l += __shfl_xor_sync(0xffffffffu, l, 2);
     if (failed) l = nan_f32();
     const float bring = fast_exp2(m_o - m_x - ROOM) * (whole ? 1.f / l : 1.f);
-    if (r8 < heads) {
-      if (whole) {
-        unsigned short* out = static_cast<unsigned short*>(a.out) + (int64_t)s * a.out_sequence + (int64_t)head * a.out_head + 2 * t4 * (D / 8);
+    if (whole) {
+      unsigned short* out = static_cast<unsigned short*>(a.out) + (int64_t)s * a.out_sequence + (int64_t)head * a.out_head + 2 * t4 * (D / 8);
+      if (r8 < heads) {
 #pragma unroll
         for (int run = 0; run < 2; ++run)
 #pragma unroll
@@ -441,16 +444,51 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
             }
             *reinterpret_cast<uint4*>(out + run * (D / 8) + i) = make_uint4(r[0], r[1], r[2], r[3]);
           }
-      } else {
-        float* part = a.partials + ((me * 2 + (first == 0 ? 1 : 0)) * P.rows + r8) * (D + 4);
+      }
+      continue;
+    }
+    // Where the unit covers all the CTA's shares, its warps' parts become one (a long sequence has hundreds of them).
+    const int cta_from = from - warp * share, begins = from + begun - first, ends = begins + tiles;
+    const bool joined = begins <= cta_from && ends - cta_from >= NW * share;
+    if (first == 0 && lane == 0) {
+      const uint32_t cta_share = NW * (uint32_t)share;
+      a.splits[2 * me + 1] = make_int4((int)(((uint32_t)begins + cta_share - 1) / cta_share), (int)((uint32_t)ends / cta_share), 0, 0);
+      a.splits[2 * me] = make_int4(head0, s, (int)((uint32_t)(ends - 1) / (uint32_t)share), heads);
+    }
+    float* part = a.partials + ((size_t)(me * 2 + (first == 0 ? 1 : 0)) * P.rows + r8) * (D + 4);
+    float* at = joined ? reinterpret_cast<float*>(ring) + r8 * C::HEAD + 2 * t4 * (D / 8 + 4) : part + 2 * t4 * (D / 8);
+    const int run_step = joined ? D / 8 + 4 : D / 8;
+    if (r8 < heads) {
 #pragma unroll
-        for (int run = 0; run < 2; ++run)
+      for (int run = 0; run < 2; ++run)
 #pragma unroll
-          for (int i = 0; i < D / 8; i += 4)
-            *reinterpret_cast<float4*>(part + (2 * t4 + run) * (D / 8) + i) =
-                make_float4((o[i][run] + o[i][run + 2]) * bring, (o[i + 1][run] + o[i + 1][run + 2]) * bring, (o[i + 2][run] + o[i + 2][run + 2]) * bring,
-                            (o[i + 3][run] + o[i + 3][run + 2]) * bring);
-        if (t4 == 0) *reinterpret_cast<float2*>(part + D) = make_float2(m_x, l);
+        for (int i = 0; i < D / 8; i += 4)
+          *reinterpret_cast<float4*>(at + run * run_step + i) =
+              make_float4((o[i][run] + o[i][run + 2]) * bring, (o[i + 1][run] + o[i + 1][run + 2]) * bring, (o[i + 2][run] + o[i + 2][run + 2]) * bring,
+                          (o[i + 3][run] + o[i + 3][run + 2]) * bring);
+      if (t4 == 0) {
+        if (joined) sh_ml[warp][r8] = make_float2(m_x, l);
+        else *reinterpret_cast<float2*>(part + D) = make_float2(m_x, l);
+      }
+    }
+    if (joined) {                                     // all four warps, each with this one part
+      __syncthreads();
+      part = a.partials + (size_t)(blockIdx.x * NW * 2 + (begins == cta_from ? 1 : 0)) * P.rows * (D + 4);
+      for (int i = tid; i < heads * (D / 4); i += NT) {
+        const int h = i / (D / 4), f = i % (D / 4) * 4;
+        float top = FIRST_REF, sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int v = 0; v < NW; ++v) top = fmaxf(top, sh_ml[v][h].x);
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+          const float fo = fast_exp2(sh_ml[v][h].x - top);
+          const float4 u = *reinterpret_cast<const float4*>(smem + (size_t)v * ST * C::BYTES + 4 * (h * C::HEAD + f / (D / 8) * (D / 8 + 4) + f % (D / 8)));
+          acc.x = fmaf(u.x, fo, acc.x); acc.y = fmaf(u.y, fo, acc.y); acc.z = fmaf(u.z, fo, acc.z); acc.w = fmaf(u.w, fo, acc.w);
+          sum = fmaf(sh_ml[v][h].y, fo, sum);
+        }
+        *reinterpret_cast<float4*>(part + h * (D + 4) + f) = acc;
+        if (f == 0) *reinterpret_cast<float2*>(part + h * (D + 4) + D) = make_float2(top, sum);
       }
     }
   }
@@ -458,70 +496,90 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
     for (int i = failed_at; i < min(failed_at + ST, mine); ++i) (void)mbar_wait_bounded(bars + i % ST, (uint32_t)(i / ST & 1));
 }
 
-// Joins the partial results of a sequence's units, and says what a sequence without tokens gets.  Grid: sequences, query heads.
+// Joins the partial results of the units that more than one share has a part of.  A CTA per share in which such a unit begins: its eight warps are dealt
+// out to the query heads, and the partial results of a head to its warps.
 template <int D>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) pages_merge_kernel(const __grid_constant__ AttendParams P) {
-  constexpr int TILE = Shape<D>::TILE;
   __shared__ float sh_o[MERGE_WARPS][D], sh_m[MERGE_WARPS], sh_l[MERGE_WARPS];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const PagesAttend& a = P.a;
-  const int s = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int length = a.length[s];
-  const bool has = length > 0 && length <= a.c.W << P.log_page;
-  const int kv = h / P.group, in_group = h - kv * P.group, block = in_group / GB, row = in_group % GB;
-  int64_t w0 = 0, w1 = -1;
-  if (has) {
-    const int64_t tiles = (length + TILE - 1) / TILE, share = a.begin[a.c.S];
-    const int64_t first = a.begin[s] * P.units + tiles * (kv * P.blocks + block);
-    w0 = first / share;
-    w1 = (first + tiles - 1) / share;
-    if (w0 == w1) return;                             // its warp has written it
-  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, w0 = blockIdx.x;
+  const int4 split = __ldcg(a.splits + 2 * w0);
+  if (split.x < 0) return;
+  // its parts: those of the shares w0 .. w1, of the CTAs c0 .. c1 - 1 one each
+  const int4 ctas = __ldcg(a.splits + 2 * w0 + 1);
+  const int w1 = split.z, heads = split.w, c0 = ctas.x, inner = max(ctas.y - c0, 0), lead = inner ? NW * c0 - w0 : 0;
+  const int parts = w1 - w0 + 1 - inner * (NW - 1);
+  const int per = MERGE_WARPS / heads, row = min(warp / per, heads - 1), part0 = warp - row * per;     // of 8 warps those behind the last head idle
+  const bool used = warp < per * heads;
   constexpr int E = D / 32;
   float m = FIRST_REF, l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-#pragma unroll 4
-  for (int64_t w = w0 + warp; w <= w1; w += MERGE_WARPS) {
-    const float* part = a.partials + ((w * 2 + (w == w0 ? 1 : 0)) * P.rows + row) * (D + 4);
-    const float2 ml = *reinterpret_cast<const float2*>(part + D);
-    float v[E];
+  if (used) {
+    constexpr int AT_ONCE = 4;
+    for (int p = part0; p < parts; p += per * AT_ONCE) {
+      float2 ml[AT_ONCE];
+      float v[AT_ONCE][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = part[lane + 32 * e];
-    const float nm = fmaxf(m, ml.x), fo = fast_exp2(m - nm), fp = fast_exp2(ml.x - nm);
-    m = nm;
-    l = fmaf(l, fo, ml.y * fp);
+      for (int k = 0; k < AT_ONCE; ++k) {
+        const int q = p + k * per, i = w0 + q + (q <= lead ? 0 : min(q - lead, inner) * (NW - 1));
+        ml[k] = make_float2(FIRST_REF, 0.f);
+        if (q < parts) {
+          const float* part = a.partials + (((int64_t)i * 2 + (i == w0 ? 1 : 0)) * P.rows + row) * (D + 4);
+          ml[k] = __ldcg(reinterpret_cast<const float2*>(part + D));
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], fo, v[e] * fp);
+          for (int e = 0; e < E; ++e) v[k][e] = __ldcg(part + lane + 32 * e);
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[k][e] = 0.f;
+        }
+      }
+      float nm = m;
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) nm = fmaxf(nm, ml[k].x);
+      const float fo = fast_exp2(m - nm);
+      m = nm;
+      l *= fo;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= fo;
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) {
+        const float fp = fast_exp2(ml[k].x - nm);
+        l = fmaf(ml[k].y, fp, l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(v[k][e], fp, o[e]);
+      }
+    }
   }
   if (lane == 0) { sh_m[warp] = m; sh_l[warp] = l; }
 #pragma unroll
   for (int e = 0; e < E; ++e) sh_o[warp][lane + 32 * e] = o[e];
   __syncthreads();
-  float top = sh_m[0];
-#pragma unroll
-  for (int w = 1; w < MERGE_WARPS; ++w) top = fmaxf(top, sh_m[w]);
-  for (int f = threadIdx.x; f < D; f += MERGE_WARPS * 32) {
-    float acc = 0.f, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < MERGE_WARPS; ++w) {
+  for (int i = threadIdx.x; i < heads * D; i += MERGE_WARPS * 32) {
+    const int h = i / D, f = i - h * D;
+    float top = FIRST_REF, acc = 0.f, sum = 0.f;
+    for (int w = h * per; w < (h + 1) * per; ++w) top = fmaxf(top, sh_m[w]);
+    for (int w = h * per; w < (h + 1) * per; ++w) {
       const float t = fast_exp2(sh_m[w] - top);
       acc = fmaf(sh_o[w][f], t, acc);
       sum = fmaf(sh_l[w], t, sum);
     }
-    const float r = has ? acc / sum : (length == 0 ? 0.f : nan_f32());
-    unsigned short* out = static_cast<unsigned short*>(a.out) + (int64_t)s * a.out_sequence + (int64_t)h * a.out_head + f;
-    if (a.bf16) *reinterpret_cast<__nv_bfloat16*>(out) = __float2bfloat16_rn(r);
-    else *reinterpret_cast<__half*>(out) = __float2half_rn(r);
+    unsigned short* out = static_cast<unsigned short*>(a.out) + (int64_t)split.y * a.out_sequence + (int64_t)(split.x + h) * a.out_head + f;
+    if (a.bf16) *reinterpret_cast<__nv_bfloat16*>(out) = __float2bfloat16_rn(acc / sum);
+    else *reinterpret_cast<__half*>(out) = __float2half_rn(acc / sum);
   }
 }
 
 int blocks_of(int group) { return (group + GB - 1) / GB; }
+// Tiles that the tables have room for, times units.
+int64_t most_tiles(int S, int W, int page, int Hkv, int group, int d) {
+  const int tile = d == 256 ? 16 : 32;
+  return (int64_t)S * (((int64_t)W * page + tile - 1) / tile) * Hkv * blocks_of(group);
+}
 // CTAs of a launch: a wave, or fewer where all tables together could not keep it busy.
 int ctas_of(int S, int W, int page, int Hkv, int group, int d) {
-  const int tile = d == 256 ? 16 : 32;
-  const int64_t most = (int64_t)S * (((int64_t)W * page + tile - 1) / tile) * Hkv * blocks_of(group);
-  const int64_t ctas = (most + NW * LEAST - 1) / (NW * LEAST);
+  const int64_t ctas = (most_tiles(S, W, page, Hkv, group, d) + NW * LEAST - 1) / (NW * LEAST);
   const int wave = SMS * (d == 256 ? Shape<256>::RESIDENT : Shape<128>::RESIDENT);
   return (int)(ctas < wave ? ctas : wave);
 }
@@ -529,14 +587,16 @@ int ctas_of(int S, int W, int page, int Hkv, int group, int d) {
 template <int D>
 cudaError_t launch_attend_d(const AttendParams& P, cudaStream_t stream) {
   constexpr size_t smem = 1024 + (size_t)NW * Shape<D>::STAGES * Shape<D>::BYTES;
-  static_assert(Shape<D>::RESIDENT * (smem + NW * 2 * BATCH * sizeof(Ahead) + 8 * (ENTRIES + NW * 5 + 1) + 1024) <= 228 * 1024, "shared memory of the CTAs that are to run at once");
+  static_assert(Shape<D>::RESIDENT * (smem + NW * 2 * BATCH * sizeof(Ahead) + 4 * (ENTRIES + 1 + NW) + 8 * NW * (GB + 4) + 1024) <= 228 * 1024, "shared memory of the CTAs that are to run at once");
   cudaError_t e = cudaFuncSetAttribute(pages_attend_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   const PageCache& c = P.a.c;
-  pages_attend_kernel<D><<<ctas_of(c.S, c.W, c.page, c.Hkv, P.group, D), NT, smem, stream>>>(P);
+  static_assert(GB * Shape<D>::HEAD * 4 <= Shape<D>::STAGES * Shape<D>::BYTES, "a warp's sums fit its ring");
+  const int ctas = ctas_of(c.S, c.W, c.page, c.Hkv, P.group, D);
+  pages_attend_kernel<D><<<ctas, NT, smem, stream>>>(P);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)c.S, (unsigned)P.a.H);
+  cfg.gridDim = dim3((unsigned)(ctas * NW));
   cfg.blockDim = dim3(MERGE_WARPS * 32);
   cfg.stream = stream;
   cudaLaunchAttribute attr{};
@@ -549,9 +609,11 @@ cudaError_t launch_attend_d(const AttendParams& P, cudaStream_t stream) {
 
 }  // namespace
 
+bool pages_attend_fits(const PageCache& c, int H) { return most_tiles(c.S, c.W, c.page, c.Hkv, H / c.Hkv, c.d) <= (int64_t)INT32_MAX; }
+int pages_attend_shares(const PageCache& c, int H) { return ctas_of(c.S, c.W, c.page, c.Hkv, H / c.Hkv, c.d) * NW; }
 size_t pages_attend_partials(const PageCache& c, int H) {
   const int group = H / c.Hkv, rows = group < GB ? group : GB;
-  return (size_t)ctas_of(c.S, c.W, c.page, c.Hkv, group, c.d) * NW * 2 * rows * (c.d + 4);
+  return (size_t)pages_attend_shares(c, H) * 2 * rows * (c.d + 4);
 }
 
 cudaError_t launch_pages_attend(const PagesAttend& a, cudaStream_t stream) {
