@@ -216,7 +216,7 @@ int kf_pages_update(const kf_pages_update_args* a, int32_t* d_table, int32_t* d_
   u.layers = a->n_layers; u.grow_all = a->grow;
   u.table = d_table; u.length = d_length; u.refs = d_refs; u.missing = d_missing;
   u.parent = d_parent; u.grow = d_grow;
-  u.fresh_rows = static_cast<int32_t*>(d_scratch);
+  u.stays = static_cast<int32_t*>(d_scratch);
   u.free_list = reinterpret_cast<int32_t*>(scratch + L.list);
   u.copies = reinterpret_cast<int4*>(scratch + L.copies);
   return status(kf::launch_pages_update(u, static_cast<cudaStream_t>(stream)));

@@ -5,6 +5,7 @@
 // whose K and V tiles are contiguous, so that codes move 16 bytes a thread and the scale of a tile is decided by one CTA, without
 // a second pass over memory and without atomics.
 #include "kf_pages.cuh"
+#include "kf_tc.cuh"
 
 #include <cooperative_groups.h>
 
@@ -27,8 +28,26 @@ __device__ __forceinline__ float power_scale(float top) {
   return __uint_as_float((uint32_t)(max(e, -120) + 127) << 23);
 }
 
-__device__ __forceinline__ signed char code_of(float x, float inverse) {
-  return (signed char)(int)fminf(fmaxf(rintf(x * inverse), -127.f), 127.f);
+// Four codes as binary32 integers: 2^23 + (c + 128) has the bits 0x4b000000 | (c ^ 0x80).
+__device__ __forceinline__ void numbers4(uint32_t codes, float (&x)[4]) {
+  const uint32_t u = codes ^ 0x80808080u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 | i));
+  add2(x[0], x[1], -8388736.f, -8388736.f);
+  add2(x[2], x[3], -8388736.f, -8388736.f);
+}
+// rint(x * by), |x * by| <= 127, as four codes: the sum with 1.5 * 2^23 holds the integer (ties to even) in its last bits.
+__device__ __forceinline__ uint32_t codes4(float x0, float x1, float x2, float x3, float by) {
+  float y0, y1, y2, y3;
+  fma2(y0, y1, x0, x1, by, 12582912.f);
+  fma2(y2, y3, x2, x3, by, 12582912.f);
+  return __byte_perm(__byte_perm(__float_as_uint(y0), __float_as_uint(y1), 0x0040), __byte_perm(__float_as_uint(y2), __float_as_uint(y3), 0x0040), 0x5410);
+}
+// Codes of one scale as codes of a larger one, `ratio` = the old one over the new one.
+__device__ __forceinline__ uint32_t rescale4(uint32_t codes, float ratio) {
+  float x[4];
+  numbers4(codes, x);
+  return codes4(x[0], x[1], x[2], x[3], ratio);
 }
 
 template <bool BF16>
@@ -47,15 +66,20 @@ __device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
   }
 }
 
-// The largest |x| of eight values, as the bits of a binary32 number (NaN above infinity above all numbers).
+// The larger |x| of pairs of 16-bit values, NaN if there is one.
 template <bool BF16>
-__device__ __forceinline__ uint32_t top8(const uint4& v) {
-  float x[8];
-  unpack8<BF16>(v, x);
-  uint32_t t = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) t = max(t, __float_as_uint(x[i]) & 0x7fffffffu);
-  return t;
+__device__ __forceinline__ uint32_t top2(uint32_t a, uint32_t b) {
+  b &= 0x7fff7fffu;
+  if (BF16) {
+    const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  }
+  const __half2 m = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t top8(uint32_t top, const uint4& v) {
+  return top2<BF16>(top2<BF16>(top2<BF16>(top2<BF16>(top, v.x), v.y), v.z), v.w);
 }
 
 struct WriteParams {
@@ -68,7 +92,7 @@ struct WriteParams {
 
 // The rows of one page and head.  Grid: slots (see slot_sequence; the new rows of a sequence touch at most rows / page + 2 pages), heads.
 template <bool BF16>
-__global__ void __launch_bounds__(NT) pages_write_kernel(const __grid_constant__ WriteParams P) {
+__global__ void __launch_bounds__(NT, 4) pages_write_kernel(const __grid_constant__ WriteParams P) {
   __shared__ uint32_t sh_top[NT / 32];
   const PageCache& c = P.c;
   const int side = threadIdx.x >= SIDE, tid = threadIdx.x & (SIDE - 1);
@@ -109,9 +133,12 @@ __global__ void __launch_bounds__(NT) pages_write_kernel(const __grid_constant__
     held[h] = i < vecs ? load(i) : make_uint4(0, 0, 0, 0);
   }
 #pragma unroll
-  for (int h = 0; h < HELD; ++h) top = max(top, top8<BF16>(held[h]));
-  for (int i = tid + HELD * SIDE; i < vecs; i += SIDE) top = max(top, top8<BF16>(load(i)));
-  top = __reduce_max_sync(0xffffffffu, top);
+  for (int h = 0; h < HELD; ++h) top = top8<BF16>(top, held[h]);
+  for (int i = tid + HELD * SIDE; i < vecs; i += SIDE) top = top8<BF16>(top, load(i));
+  // the bits of |x| are in order, with NaN above infinity: the larger of the pair as a binary32 number, then the largest of the CTA
+  top = max(top & 0xffffu, top >> 16);
+  top = BF16 ? top << 16 : __float_as_uint(__half2float(__ushort_as_half((unsigned short)top)));
+  top = __reduce_max_sync(0xffffffffu, top & 0x7fffffffu);
   if ((threadIdx.x & 31) == 0) sh_top[threadIdx.x >> 5] = top;
   __syncthreads();
   top = 0;
@@ -125,25 +152,16 @@ __global__ void __launch_bounds__(NT) pages_write_kernel(const __grid_constant__
   if (r0 > 0 && scale > was) {                                   // rows that are there already move to the larger scale
     const float ratio = was > 0.f ? was * inverse : 0.f;
     for (int i = tid; i < r0 * (c.d / 16); i += SIDE) {
-      uint4 v = reinterpret_cast<uint4*>(codes)[i];
-      uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t r = 0;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) r |= (uint32_t)(unsigned char)code_of((float)(signed char)(w[q] >> (8 * b)), ratio) << (8 * b);
-        w[q] = r;
-      }
-      reinterpret_cast<uint4*>(codes)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      const uint4 v = reinterpret_cast<uint4*>(codes)[i];
+      reinterpret_cast<uint4*>(codes)[i] = make_uint4(rescale4(v.x, ratio), rescale4(v.y, ratio), rescale4(v.z, ratio), rescale4(v.w, ratio));
     }
   }
+  const uint32_t valid = scale == scale ? 0xffffffffu : 0u;      // what is not finite has no codes
   auto store = [&](int i, const uint4& v) {
     float x[8];
     unpack8<BF16>(v, x);
-    uint32_t w[2] = {0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e >> 2] |= (uint32_t)(unsigned char)code_of(scale == scale ? x[e] : 0.f, inverse) << (8 * (e & 3));
-    *reinterpret_cast<uint2*>(codes + ((size_t)r0 << (P.log_vec + 3)) + (size_t)i * 8) = make_uint2(w[0], w[1]);
+    *reinterpret_cast<uint2*>(codes + ((size_t)r0 << (P.log_vec + 3)) + (size_t)i * 8) =
+        make_uint2(codes4(x[0], x[1], x[2], x[3], inverse) & valid, codes4(x[4], x[5], x[6], x[7], inverse) & valid);
   };
 #pragma unroll
   for (int h = 0; h < HELD; ++h) {
@@ -163,7 +181,7 @@ struct ReadParams {
 };
 
 template <bool BF16>
-__global__ void __launch_bounds__(NT) pages_read_kernel(const __grid_constant__ ReadParams P) {
+__global__ void __launch_bounds__(NT, 8) pages_read_kernel(const __grid_constant__ ReadParams P) {
   const PageCache& c = P.c;
   const int side = threadIdx.x >= SIDE, tid = threadIdx.x & (SIDE - 1);
   const int s = slot_sequence(P.begin, c.S, blockIdx.x, 1, P.log_page, 2);
@@ -189,10 +207,12 @@ __global__ void __launch_bounds__(NT) pages_read_kernel(const __grid_constant__ 
   for (int i = tid; i < vecs; i += SIDE) {
     const uint2 w = held ? codes[i] : make_uint2(0, 0);
     uint32_t r[4];
+    float x[8];
+    numbers4(w.x, reinterpret_cast<float(&)[4]>(x[0]));
+    numbers4(w.y, reinterpret_cast<float(&)[4]>(x[4]));
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      const uint32_t two = (p < 2 ? w.x : w.y) >> (16 * (p & 1));
-      const float a = (float)(signed char)(two & 0xff) * scale, b = (float)(signed char)(two >> 8 & 0xff) * scale;
+      const float a = x[2 * p] * scale, b = x[2 * p + 1] * scale;
       if (BF16) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
         r[p] = *reinterpret_cast<const uint32_t*>(&h);
@@ -209,10 +229,10 @@ __global__ void __launch_bounds__(NT) pages_read_kernel(const __grid_constant__ 
 struct CompactParams {
   PageCache c;
   const int32_t *table, *length, *keep, *n_keep, *new_table;
-  int32_t keep_width, new_width, log_page;
+  int32_t keep_width, new_width, log_page, log_vec;
 };
 
-__global__ void __launch_bounds__(NT) pages_compact_kernel(const __grid_constant__ CompactParams P) {
+__global__ void __launch_bounds__(NT, 8) pages_compact_kernel(const __grid_constant__ CompactParams P) {
   __shared__ int64_t sh_row[128];             // where a row's K codes stand, -1: nowhere
   __shared__ float sh_scale[2][128];
   __shared__ uint32_t sh_top[2][4];
@@ -255,38 +275,29 @@ __global__ void __launch_bounds__(NT) pages_compact_kernel(const __grid_constant
   const float inverse = scale > 0.f ? 1.f / scale : 0.f;
   const size_t tile = ((size_t)to * c.Hkv + h) * 2 + side;
   uint4* out = reinterpret_cast<uint4*>(c.codes + tile * (size_t)c.page * c.d);
-  const int vec = c.d / 16;
+  const int log_vec = P.log_vec, vec = 1 << log_vec;            // 16-byte pieces of a row
 #pragma unroll 4
-  for (int i = tid; i < rows * vec; i += SIDE) {
-    const int r = i / vec;
+  for (int i = tid; i < rows << log_vec; i += SIDE) {
+    const int r = i >> log_vec;
     const int64_t at = sh_row[r];
     uint4 v = make_uint4(0, 0, 0, 0);
-    if (at >= 0) v = reinterpret_cast<const uint4*>(c.codes + at + (int64_t)side * c.page * c.d)[i - r * vec];
-    const float own = sh_scale[side][r];
-    if (own != scale) {                                          // also where either is NaN: the codes do not matter then
-      const float ratio = own * inverse;
-      uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t n = 0;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) n |= (uint32_t)(unsigned char)code_of((float)(signed char)(w[q] >> (8 * b)), ratio) << (8 * b);
-        w[q] = n;
-      }
-      v = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    if (at >= 0) v = reinterpret_cast<const uint4*>(c.codes + at + (int64_t)side * c.page * c.d)[i & (vec - 1)];
+    const float ratio = sh_scale[side][r] * inverse;
+    if (ratio < 1.f) v = make_uint4(rescale4(v.x, ratio), rescale4(v.y, ratio), rescale4(v.z, ratio), rescale4(v.w, ratio));
     out[i] = v;
   }
   if (tid == 0) c.scale[tile] = scale;
 }
 
-// ---- tables.  One cluster of eight CTAs does the whole update: its barrier stands between counting references, looking for
-// free pages and handing them out.  Every CTA works out the sequences' lengths and where each one's pages begin in the list for itself.
+// ---- tables.  One CTA, or one cluster of eight for large tables, does the whole update: its barrier stands between counting references, looking
+// for free pages and handing them out.  Every CTA works out the sequences' lengths and where each one's pages begin in the list for itself.
 constexpr int CLUSTER = 8, UT = 1024;
 
 struct UpdateShared {
-  int owner[UPDATE_MAX_SEQUENCES];    // lowest sequence that goes on from this one
-  int prefix[UPDATE_MAX_SEQUENCES];   // pages handed out to the sequences before
+  int source[UPDATE_MAX_SEQUENCES];   // whom a sequence goes on from (-1: it has ended)
+  int length[UPDATE_MAX_SEQUENCES];   // its tokens
+  int need[UPDATE_MAX_SEQUENCES];     // pages it is to have; until that is known, the lowest sequence that goes on from this one
+  int prefix[UPDATE_MAX_SEQUENCES];   // pages handed out to the sequences before it, times 2; the last bit: it keeps a page that is filled in part
   int scan[UT / 32];
   int found;
   unsigned long long beyond;
@@ -303,57 +314,48 @@ __device__ __forceinline__ int block_exclusive(int v, int* warp_sums, int& total
   __syncthreads();
   if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
-  int before = 0, all = 0;
+  int sums = lane < UT / 32 ? warp_sums[lane] : 0, before = sums;
 #pragma unroll
-  for (int w = 0; w < UT / 32; ++w) {
-    const int t = warp_sums[w];
-    before += w < warp ? t : 0;
-    all += t;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, before, o);
+    if (lane >= o) before += y;
   }
-  total = all;
-  return before + x - v;
+  total = __shfl_sync(0xffffffffu, before, 31);
+  before -= sums;
+  return __shfl_sync(0xffffffffu, before, warp) + x - v;
 }
 
 struct Sequence {
-  int parent, length, full, part, keeps, stay, need;   // stay: pages kept from the parent; need: pages in all
-  int64_t beyond;                                      // pages the table has no room for
+  int source, full, part, keeps, stay, need, prefix;   // stay: pages kept from the source; need: pages in all
 };
 
-__global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(UT, 1) pages_update_kernel(const __grid_constant__ PagesUpdate U) {
+__global__ void __launch_bounds__(UT, 1) pages_update_kernel(const __grid_constant__ PagesUpdate U) {
   extern __shared__ __align__(16) unsigned char update_smem[];
   UpdateShared& sh = *reinterpret_cast<UpdateShared*>(update_smem);
   cg::cluster_group cluster = cg::this_cluster();
   const PageCache& c = U.c;
-  const int S = c.S, W = c.W, rank = (int)cluster.block_rank(), tid = threadIdx.x;
+  const int S = c.S, W = c.W, rank = (int)cluster.block_rank(), ranks = (int)cluster.num_blocks(), tid = threadIdx.x;
   const int64_t capacity = (int64_t)W * c.page;
+  const int log_page = U.log_page;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  auto parent_of = [&](int s) {
-    const int p = U.parent ? U.parent[s] : s;
-    return p >= 0 && p < S ? p : -1;
-  };
-  auto look = [&](int s) {
-    Sequence q{};
-    q.parent = parent_of(s);
-    q.length = q.parent >= 0 ? U.length[q.parent] : 0;
-    if (q.length < 0 || q.length > capacity) q.length = 0;
-    q.full = q.length / c.page;
-    q.part = q.length - q.full * c.page;
-    q.keeps = q.part > 0 && sh.owner[q.parent] == s;             // a part-filled page implies a parent
-    q.stay = q.full + q.keeps;
-    const int64_t tokens = (int64_t)q.length + max(U.grow ? U.grow[s] : U.grow_all, 0);
-    const int64_t need = (tokens + c.page - 1) / c.page;
-    q.need = (int)min(need, (int64_t)W);
-    q.beyond = need - q.need;
-    return q;
-  };
-
-  // ---- who keeps a page that is filled in part; pages to hand out before each sequence
-  for (int s = tid; s < S; s += UT) sh.owner[s] = S;
+  // ---- lengths, who keeps a page that is filled in part, and the pages to hand out before each sequence
+  for (int s = tid; s < S; s += UT) sh.need[s] = S;
   if (tid == 0) sh.beyond = 0;
   __syncthreads();
   for (int s = tid; s < S; s += UT) {
-    const int p = parent_of(s);
-    if (p >= 0) atomicMin(&sh.owner[p], s);
+    int p = U.parent ? U.parent[s] : s;
+    if (p < 0 || p >= S) p = -1;
+    int n = p >= 0 ? U.length[p] : 0;
+    if (n < 0 || n > capacity) n = 0;
+    sh.source[s] = p;
+    sh.length[s] = n;
+    if (p >= 0) atomicMin(&sh.need[p], s);
+  }
+  __syncthreads();
+  for (int s = tid; s < S; s += UT) {
+    const int p = sh.source[s];
+    sh.prefix[s] = p >= 0 && (sh.length[s] & (c.page - 1)) != 0 && sh.need[p] == s;
   }
   __syncthreads();
   int wanted = 0;                                                // pages to hand out, of all sequences
@@ -361,29 +363,44 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(UT, 1) pages_u
     const int s = base + tid;
     int fresh = 0;
     if (s < S) {
-      const Sequence q = look(s);
-      fresh = q.need - q.stay;
-      if (q.beyond) atomicAdd(&sh.beyond, (unsigned long long)q.beyond);
+      const int64_t tokens = (int64_t)sh.length[s] + max(U.grow ? U.grow[s] : U.grow_all, 0);
+      const int64_t need = (tokens + c.page - 1) >> log_page;
+      sh.need[s] = (int)min(need, (int64_t)W);
+      if (need > W) atomicAdd(&sh.beyond, (unsigned long long)(need - W));      // the table has no room for them
+      fresh = sh.need[s] - (sh.length[s] >> log_page) - sh.prefix[s];
     }
     int total;
     const int before = block_exclusive(fresh, sh.scan, total);
-    if (s < S) sh.prefix[s] = wanted + before;
+    if (s < S) sh.prefix[s] |= (wanted + before) << 1;
     wanted += total;
   }
+  __syncthreads();
+  auto look = [&](int s) {
+    Sequence q;
+    q.source = sh.source[s];
+    q.full = sh.length[s] >> log_page;
+    q.part = sh.length[s] & (c.page - 1);
+    q.keeps = sh.prefix[s] & 1;
+    q.stay = q.full + q.keeps;
+    q.need = sh.need[s];
+    q.prefix = sh.prefix[s] >> 1;
+    return q;
+  };
 
   // ---- references: what the table names now no longer counts, what stays does
   const uint32_t entries = (uint32_t)S * (uint32_t)W;            // at most 2^28
-  const uint32_t thread = (uint32_t)(rank * UT + tid), threads = CLUSTER * UT;
+  const uint32_t thread = (uint32_t)(rank * UT + tid), threads = (uint32_t)ranks * UT;
   for (uint32_t i = thread; i < entries; i += threads) {
     const int s = (int)(i / (uint32_t)W), j = (int)(i - (uint32_t)s * (uint32_t)W);
     const Sequence q = look(s);
+    const bool tail = j == q.full && q.part > 0;                 // the page that is filled in part
     const int old = U.table[i];
     int next = -1;
-    if (j < q.stay || (j == q.full && q.part > 0)) next = q.parent == s ? old : U.table[(int64_t)q.parent * W + j];
+    if (j < q.stay || tail) next = q.source == s ? old : U.table[(size_t)q.source * W + j];
     if (next < 0 || next >= c.pages) next = -1;
-    if (j == q.full && q.part > 0) U.copies[s].x = next;         // the page that is filled in part
+    if (tail) U.copies[s].x = next;
     if (j >= q.stay) next = -1;
-    U.fresh_rows[i] = next;
+    U.stays[i] = next;
     if (next != old) {
       if (old >= 0 && old < c.pages) atomicSub(&U.refs[old], 1);
       if (next >= 0) atomicAdd(&U.refs[next], 1);
@@ -392,8 +409,8 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(UT, 1) pages_u
   __threadfence();
   cluster.sync();
 
-  // ---- free pages, lowest first: counted per CTA, then listed
-  const int per = ((c.pages + CLUSTER - 1) / CLUSTER + 3) & ~3;  // a CTA's stretch of pages
+  // ---- free pages, lowest first: counted per CTA where there are several, then listed
+  const int per = ((c.pages + ranks - 1) / ranks + 3) & ~3;      // a CTA's stretch of pages
   const int lo = (int)min((int64_t)rank * per, (int64_t)c.pages), hi = (int)min((int64_t)lo + per, (int64_t)c.pages);
   auto free_mask = [&](int p) {                                  // pages p .. p + 3
     uint32_t m = 0;
@@ -405,31 +422,33 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(UT, 1) pages_u
     }
     return m;
   };
-  int mine = 0;
-  if (wanted > 0)
-    for (int p = lo + tid * 4; p < hi; p += UT * 4) mine += __popc(free_mask(p));
-  int total;
-  (void)block_exclusive(mine, sh.scan, total);
-  if (tid == 0) sh.found = total;
-  cluster.sync();
-  int rank_before = 0, available = 0;
-  for (int r = 0; r < CLUSTER; ++r) {
-    const int n = *cluster.map_shared_rank(&sh.found, r);
-    rank_before += r < rank ? n : 0;
-    available += n;
+  int at_rank = 0, total;                                        // free pages before the next stretch
+  if (ranks > 1) {
+    int mine = 0;
+    if (wanted > 0)
+      for (int p = lo + tid * 4; p < hi; p += UT * 4) mine += __popc(free_mask(p));
+    (void)block_exclusive(mine, sh.scan, total);
+    if (tid == 0) sh.found = total;
+    cluster.sync();
+    for (int r = 0; r < rank; ++r) at_rank += *cluster.map_shared_rank(&sh.found, r);
   }
-  const int given = min(wanted, available);
-  for (int base = lo; base < hi && rank_before < given; base += UT * 4) {
+  for (int base = lo; base < hi && at_rank < wanted; base += UT * 4) {
     const int p = base + tid * 4;
     const uint32_t m = p < hi ? free_mask(p) : 0;
-    int at = block_exclusive(__popc(m), sh.scan, total) + rank_before;
+    int at = block_exclusive(__popc(m), sh.scan, total) + at_rank;
     for (int e = 0; e < 4; ++e)
       if (m >> e & 1) {
-        if (at < given) { U.free_list[at] = p + e; U.refs[p + e] = 1; }
+        if (at < wanted) { U.free_list[at] = p + e; U.refs[p + e] = 1; }
         ++at;
       }
-    rank_before += total;
+    at_rank += total;
   }
+  int available = at_rank;                                       // of one CTA: all that were looked at, or as many as are wanted
+  if (ranks > 1) {
+    available = 0;
+    for (int r = 0; r < ranks; ++r) available += *cluster.map_shared_rank(&sh.found, r);
+  }
+  const int given = min(wanted, available);
   __threadfence();
   cluster.sync();
 
@@ -437,32 +456,22 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(UT, 1) pages_u
   for (uint32_t i = thread; i < entries; i += threads) {
     const int s = (int)(i / (uint32_t)W), j = (int)(i - (uint32_t)s * (uint32_t)W);
     const Sequence q = look(s);
-    int next = U.fresh_rows[i];
-    if (j >= q.stay && j < q.need) {
-      const int at = sh.prefix[s] + j - q.stay;
-      next = at < given ? __ldcg(U.free_list + at) : -1;
-    }
+    int next = U.stays[i];
+    if (j >= q.stay && j < q.need) next = q.prefix + j - q.stay < given ? __ldcg(U.free_list + q.prefix + j - q.stay) : -1;
     U.table[i] = next;
     if (j == 0) {
-      const bool copy = q.part > 0 && !q.keeps;
-      const int at = sh.prefix[s];                               // its first new page
-      const int from = copy ? __ldcg(&U.copies[s].x) : -1;
-      U.copies[s] = make_int4(from, copy && at < given ? __ldcg(U.free_list + at) : -1, q.part, 0);
+      const bool copy = q.part > 0 && !q.keeps;                  // into its first new page
+      U.copies[s] = make_int4(copy ? __ldcg(&U.copies[s].x) : -1, copy && q.prefix < given ? __ldcg(U.free_list + q.prefix) : -1, q.part, 0);
+      U.length[s] = sh.length[s];                                // every CTA has read the lengths long before
     }
   }
-  // lengths are read by every look(): written when all CTAs are done with them
-  int mine_length[UPDATE_MAX_SEQUENCES / (CLUSTER * UT) + 1];
-  int k = 0;
-  for (int s = rank * UT + tid; s < S; s += CLUSTER * UT) mine_length[k++] = look(s).length;
-  cluster.sync();
-  k = 0;
-  for (int s = rank * UT + tid; s < S; s += CLUSTER * UT) U.length[s] = mine_length[k++];
   if (rank == 0 && tid == 0) *U.missing = (int)min((int64_t)(wanted - given) + (int64_t)sh.beyond, (int64_t)INT32_MAX);
 }
 
 // The rows of pages that are filled in part.  Grid: sequences, layers, pieces of the heads.
 __global__ void __launch_bounds__(NT) pages_copy_kernel(const __grid_constant__ PagesUpdate U) {
-  const int4 copy = U.copies[blockIdx.x];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int4 copy = __ldcg(U.copies + blockIdx.x);
   if (copy.y < 0) return;
   const PageCache& c = U.c;
   const size_t layer = (size_t)blockIdx.y * c.pages;
@@ -516,7 +525,7 @@ cudaError_t launch_pages_compact(const PageCache& c, int keep_width, int new_wid
                                  const int32_t* n_keep, const int32_t* new_table, cudaStream_t stream) {
   CompactParams P{};
   P.c = c; P.table = table; P.length = length; P.keep = keep; P.n_keep = n_keep; P.new_table = new_table;
-  P.keep_width = keep_width; P.new_width = new_width; P.log_page = log2_of(c.page);
+  P.keep_width = keep_width; P.new_width = new_width; P.log_page = log2_of(c.page); P.log_vec = log2_of(c.d / 16);
   pages_compact_kernel<<<dim3((unsigned)c.S * (unsigned)new_width, (unsigned)c.Hkv), NT, 0, stream>>>(P);
   return cudaGetLastError();
 }
@@ -524,12 +533,33 @@ cudaError_t launch_pages_compact(const PageCache& c, int keep_width, int new_wid
 cudaError_t launch_pages_update(const PagesUpdate& u, cudaStream_t stream) {
   cudaError_t e = cudaFuncSetAttribute(pages_update_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(UpdateShared));
   if (e != cudaSuccess) return e;
-  pages_update_kernel<<<CLUSTER, UT, sizeof(UpdateShared), stream>>>(u);
-  e = cudaGetLastError();
+  PagesUpdate U = u;
+  U.log_page = log2_of(u.c.page);
+  // entries and pages one CTA goes through in a few rounds; the barriers of a cluster cost about as much
+  const bool small = (int64_t)u.c.S * u.c.W + u.c.pages / 4 <= 16 * UT;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim = {small ? 1u : (unsigned)CLUSTER, 1u, 1u};
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(small ? 1u : (unsigned)CLUSTER);
+  cfg.blockDim = dim3(UT);
+  cfg.dynamicSmemBytes = sizeof(UpdateShared);
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, pages_update_kernel, U);
   if (e != cudaSuccess || !u.parent) return e;                    // without parents no page has a second owner
   const int pieces = u.c.Hkv * 2 < 8 ? u.c.Hkv * 2 : 8;
-  pages_copy_kernel<<<dim3((unsigned)u.c.S, (unsigned)u.layers, (unsigned)pieces), NT, 0, stream>>>(u);
-  return cudaGetLastError();
+  cudaLaunchAttribute after{};
+  after.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  after.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t copy{};
+  copy.gridDim = dim3((unsigned)u.c.S, (unsigned)u.layers, (unsigned)pieces);
+  copy.blockDim = dim3(NT);
+  copy.stream = stream;
+  copy.attrs = &after;
+  copy.numAttrs = 1;
+  return cudaLaunchKernelEx(&copy, pages_copy_kernel, U);
 }
 
 }  // namespace kf

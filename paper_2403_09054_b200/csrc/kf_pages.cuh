@@ -49,7 +49,8 @@ struct PagesUpdate {
   int32_t layers, grow_all;
   int32_t *table, *length, *refs, *missing;
   const int32_t *parent, *grow;   // or null
-  int32_t *fresh_rows;            // scratch [S][W]: the entries that stay, as read before anything is written
+  int32_t log_page;               // filled in by the launch
+  int32_t *stays;                 // scratch [S][W]: the entries that stay, as read before anything is written
   int32_t *free_list;             // scratch [min(pages, S W)]
   int4* copies;                   // scratch [S]: (from, to, rows, 0) of a page that is filled in part; to = -1: none
 };
