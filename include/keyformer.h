@@ -449,7 +449,7 @@ int kf_reorder_beams(kf_ctx* ctx, int32_t layer, int32_t beams, const int32_t* d
  * output: a sequence ends where its range ends, whatever stands behind it.  Within a sequence a value row that is not finite may make any
  * earlier row of the same 128 NaN.  A sequence whose range is empty or not within 0 .. tokens has no output; ranges do not descend. */
 typedef struct kf_ragged_args {
-  int32_t tokens, sequences;          /* rows of q, k, v and out (<= 2^28); S (<= 2^20)                           */
+  int32_t tokens, sequences;          /* rows of q, k, v and out (<= 2^28); S (<= 2^20); (tokens / 128 + S) H < 2^31 */
   int32_t n_heads, n_kv_heads;        /* H, Hkv: Hkv divides H                                                    */
   int32_t head_dim, type;             /* d in {64, 128, 256}; KF_TYPE_FP16 or KF_TYPE_BF16, of all four           */
   int32_t bias_mode;                  /* KF_BIAS_*                                                                */

@@ -32,6 +32,7 @@ inline bool bias_ok(int32_t mode, const float* slopes) {
 bool ragged_ok(const kf_ragged_args* a) {
   if (!a || a->tokens < 1 || a->tokens > ROWS_MAX || a->sequences < 1 || a->sequences > SEQUENCES_MAX) return false;
   if (a->n_heads < 1 || a->n_heads > 65535 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads != 0 || !head_dim_ok(a->head_dim) || !type16(a->type)) return false;
+  if (((int64_t)a->tokens / 128 + a->sequences) * a->n_heads > INT32_MAX) return false;
   if (!(a->logit_scale >= 0.f) || !std::isfinite(a->logit_scale) || !bias_ok(a->bias_mode, a->d_alibi_slopes)) return false;
   if (a->debug_fail_first_wait < 0 || a->debug_fail_first_wait > 1) return false;
   for (int64_t s : {a->q_token_stride, a->q_head_stride, a->k_token_stride, a->k_head_stride, a->v_token_stride, a->v_head_stride, a->out_token_stride,
