@@ -291,13 +291,16 @@ __global__ void __launch_bounds__(NT, 8) pages_compact_kernel(const __grid_const
 
 // ---- tables.  One CTA, or one cluster of eight for large tables, does the whole update: its barrier stands between counting references, looking
 // for free pages and handing them out.  Every CTA works out the sequences' lengths and where each one's pages begin in the list for itself.
-constexpr int CLUSTER = 8, UT = 1024;
+constexpr int CLUSTER = 8, UT = 1024, UPDATE_LIST = 8192;
+
+constexpr int KEEPS = 1 << 30;         // tokens are fewer
 
 struct UpdateShared {
   int source[UPDATE_MAX_SEQUENCES];   // whom a sequence goes on from (-1: it has ended)
-  int length[UPDATE_MAX_SEQUENCES];   // its tokens
+  int length[UPDATE_MAX_SEQUENCES];   // its tokens; KEEPS: it keeps its source's page that is filled in part
   int need[UPDATE_MAX_SEQUENCES];     // pages it is to have; until that is known, the lowest sequence that goes on from this one
-  int prefix[UPDATE_MAX_SEQUENCES];   // pages handed out to the sequences before it, times 2; the last bit: it keeps a page that is filled in part
+  int prefix[UPDATE_MAX_SEQUENCES];   // the tokens it is to have room for, then the pages handed out to the sequences before it
+  int list[UPDATE_LIST];              // free pages, where one CTA hands out no more than these
   int scan[UT / 32];
   int found;
   unsigned long long beyond;
@@ -345,17 +348,19 @@ __global__ void __launch_bounds__(UT, 1) pages_update_kernel(const __grid_consta
   __syncthreads();
   for (int s = tid; s < S; s += UT) {
     int p = U.parent ? U.parent[s] : s;
+    const int grow = max(U.grow ? U.grow[s] : U.grow_all, 0);
     if (p < 0 || p >= S) p = -1;
     int n = p >= 0 ? U.length[p] : 0;
     if (n < 0 || n > capacity) n = 0;
     sh.source[s] = p;
     sh.length[s] = n;
+    sh.prefix[s] = grow;
     if (p >= 0) atomicMin(&sh.need[p], s);
   }
   __syncthreads();
   for (int s = tid; s < S; s += UT) {
     const int p = sh.source[s];
-    sh.prefix[s] = p >= 0 && (sh.length[s] & (c.page - 1)) != 0 && sh.need[p] == s;
+    if (p >= 0 && (sh.length[s] & (c.page - 1)) != 0 && sh.need[p] == s) sh.length[s] |= KEEPS;
   }
   __syncthreads();
   int wanted = 0;                                                // pages to hand out, of all sequences
@@ -363,27 +368,28 @@ __global__ void __launch_bounds__(UT, 1) pages_update_kernel(const __grid_consta
     const int s = base + tid;
     int fresh = 0;
     if (s < S) {
-      const int64_t tokens = (int64_t)sh.length[s] + max(U.grow ? U.grow[s] : U.grow_all, 0);
-      const int64_t need = (tokens + c.page - 1) >> log_page;
+      const int n = sh.length[s] & ~KEEPS;
+      const int64_t need = ((int64_t)n + sh.prefix[s] + c.page - 1) >> log_page;
       sh.need[s] = (int)min(need, (int64_t)W);
       if (need > W) atomicAdd(&sh.beyond, (unsigned long long)(need - W));      // the table has no room for them
-      fresh = sh.need[s] - (sh.length[s] >> log_page) - sh.prefix[s];
+      fresh = sh.need[s] - (n >> log_page) - (n != sh.length[s]);
     }
     int total;
     const int before = block_exclusive(fresh, sh.scan, total);
-    if (s < S) sh.prefix[s] |= (wanted + before) << 1;
+    if (s < S) sh.prefix[s] = wanted + before;
     wanted += total;
   }
   __syncthreads();
   auto look = [&](int s) {
     Sequence q;
+    const int n = sh.length[s] & ~KEEPS;
     q.source = sh.source[s];
-    q.full = sh.length[s] >> log_page;
-    q.part = sh.length[s] & (c.page - 1);
-    q.keeps = sh.prefix[s] & 1;
+    q.full = n >> log_page;
+    q.part = n & (c.page - 1);
+    q.keeps = n != sh.length[s];
     q.stay = q.full + q.keeps;
     q.need = sh.need[s];
-    q.prefix = sh.prefix[s] >> 1;
+    q.prefix = sh.prefix[s];
     return q;
   };
 
@@ -406,8 +412,7 @@ __global__ void __launch_bounds__(UT, 1) pages_update_kernel(const __grid_consta
       if (next >= 0) atomicAdd(&U.refs[next], 1);
     }
   }
-  __threadfence();
-  cluster.sync();
+  cluster.sync();                                                // releases and acquires: the counts are seen by all
 
   // ---- free pages, lowest first: counted per CTA where there are several, then listed
   const int per = ((c.pages + ranks - 1) / ranks + 3) & ~3;      // a CTA's stretch of pages
@@ -422,6 +427,7 @@ __global__ void __launch_bounds__(UT, 1) pages_update_kernel(const __grid_consta
     }
     return m;
   };
+  int* free_list = ranks == 1 && wanted <= UPDATE_LIST ? sh.list : U.free_list;
   int at_rank = 0, total;                                        // free pages before the next stretch
   if (ranks > 1) {
     int mine = 0;
@@ -438,7 +444,7 @@ __global__ void __launch_bounds__(UT, 1) pages_update_kernel(const __grid_consta
     int at = block_exclusive(__popc(m), sh.scan, total) + at_rank;
     for (int e = 0; e < 4; ++e)
       if (m >> e & 1) {
-        if (at < wanted) { U.free_list[at] = p + e; U.refs[p + e] = 1; }
+        if (at < wanted) { free_list[at] = p + e; U.refs[p + e] = 1; }
         ++at;
       }
     at_rank += total;
@@ -449,7 +455,6 @@ __global__ void __launch_bounds__(UT, 1) pages_update_kernel(const __grid_consta
     for (int r = 0; r < ranks; ++r) available += *cluster.map_shared_rank(&sh.found, r);
   }
   const int given = min(wanted, available);
-  __threadfence();
   cluster.sync();
 
   // ---- the new table
@@ -457,12 +462,12 @@ __global__ void __launch_bounds__(UT, 1) pages_update_kernel(const __grid_consta
     const int s = (int)(i / (uint32_t)W), j = (int)(i - (uint32_t)s * (uint32_t)W);
     const Sequence q = look(s);
     int next = U.stays[i];
-    if (j >= q.stay && j < q.need) next = q.prefix + j - q.stay < given ? __ldcg(U.free_list + q.prefix + j - q.stay) : -1;
+    if (j >= q.stay && j < q.need) next = q.prefix + j - q.stay < given ? *(volatile int*)(free_list + q.prefix + j - q.stay) : -1;
     U.table[i] = next;
     if (j == 0) {
       const bool copy = q.part > 0 && !q.keeps;                  // into its first new page
-      U.copies[s] = make_int4(copy ? __ldcg(&U.copies[s].x) : -1, copy && q.prefix < given ? __ldcg(U.free_list + q.prefix) : -1, q.part, 0);
-      U.length[s] = sh.length[s];                                // every CTA has read the lengths long before
+      U.copies[s] = make_int4(copy ? __ldcg(&U.copies[s].x) : -1, copy && q.prefix < given ? *(volatile int*)(free_list + q.prefix) : -1, q.part, 0);
+      U.length[s] = sh.length[s] & ~KEEPS;                                // every CTA has read the lengths long before
     }
   }
   if (rank == 0 && tid == 0) *U.missing = (int)min((int64_t)(wanted - given) + (int64_t)sh.beyond, (int64_t)INT32_MAX);

@@ -97,7 +97,8 @@ __device__ __forceinline__ int cta_scan(int v, int* warp_sums, int& total) {
   return before + x - v;
 }
 
-template <int D>
+// SHARES: the form described above.  Without it a CTA is a unit, whose tiles its four warps take a quarter each, and joins them itself.
+template <int D, bool SHARES>
 __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(const __grid_constant__ AttendParams P) {
   using C = Shape<D>;
   constexpr int TILE = C::TILE, ST = C::STAGES;
@@ -112,7 +113,7 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
   __shared__ Ahead sh_ahead[NW][2 * BATCH];
   __shared__ float2 sh_ml[NW][GB];
 
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (SHARES) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const PagesAttend& a = P.a;
   const PageCache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r8 = lane >> 2, t4 = lane & 3;
@@ -124,8 +125,8 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
 
   // ---- where the sequences begin, in tiles: an entry for every `stride` sequences
   const int stride = (c.S + ENTRIES - 1) / ENTRIES;
-  int all;
-  {
+  int all = 0;
+  if (SHARES) {
     constexpr int PER = ENTRIES / NT;
     int own[PER], sum = 0;
 #pragma unroll
@@ -144,22 +145,24 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
     }
     if (tid == NT - 1) sh_begin[ENTRIES] = all;
   }
-  __syncthreads();
-  const int total = all * P.units, warps = gridDim.x * NW;        // the host makes sure that there are fewer than 2^31 of them
-  const int share = max((int)(((uint32_t)total + warps - 1) / (uint32_t)warps), LEAST);
-  const int me = blockIdx.x * NW + warp;
+  if (SHARES) __syncthreads();
+  const int own_seq = SHARES ? 0 : blockIdx.x / P.units, own_unit = SHARES ? 0 : blockIdx.x % P.units;
+  const int total = SHARES ? all * P.units : tiles_of(own_seq), warps = SHARES ? gridDim.x * NW : NW;   // the host makes sure that there are fewer than 2^31 tiles
+  const int share = max((int)(((uint32_t)total + warps - 1) / (uint32_t)warps), SHARES ? LEAST : 1);
+  const int me = SHARES ? blockIdx.x * NW + warp : warp;
   const int from = (int)min((int64_t)me * share, (int64_t)total);
   // ---- sequences without tiles: zeros, or NaN where the length is not valid
-  for (int i = me; i < c.S; i += warps) {
+  for (int i = SHARES ? me : own_seq; i < c.S; i += SHARES ? warps : c.S) {
+    if (!SHARES && (own_unit != 0 || warp != 0)) break;
     const int n = a.length[i];
     if (n > 0 && n <= capacity) continue;
     const uint32_t v = n == 0 ? 0u : 0x7fff7fffu;
     for (int e = lane; e < a.H * (D / 8); e += 32)
       *reinterpret_cast<uint4*>(static_cast<unsigned short*>(a.out) + (int64_t)i * a.out_sequence + (int64_t)(e / (D / 8)) * a.out_head + e % (D / 8) * 8) = make_uint4(v, v, v, v);
   }
-  if (lane == 0) a.splits[2 * me].x = -1;             // no unit begins in this share and goes on behind it, as far as is known
-  if (from >= total) return;
-  const int mine = min(share, total - from);      // tiles of this warp
+  if (SHARES && lane == 0) a.splits[2 * me].x = -1;   // no unit begins in this share and goes on behind it, as far as is known
+  if (SHARES ? from >= total : total == 0) return;
+  const int mine = min(share, total - from);          // tiles of this warp
 
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* ring = smem + (size_t)warp * ST * C::BYTES;
@@ -184,20 +187,27 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
   };
   auto look_up = [&](int w0) {
     if (lane < BATCH && w0 + lane < mine) {
-      const int g = from + w0 + lane, in_all = (int)((uint32_t)g / (uint32_t)P.units);
-      int lo = 0, hi = ENTRIES;                       // the last entry that does not begin behind it
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (sh_begin[mid] <= in_all) lo = mid; else hi = mid;
-      }
-      int at = sh_begin[lo];
       Ahead t;
-      t.seq = lo * stride;
-      t.count = stride == 1 ? sh_begin[lo + 1] - at : tiles_of(t.seq);
-      while (at + t.count <= in_all) { at += t.count; t.count = tiles_of(++t.seq); }
-      const int r = g - at * P.units;
-      t.unit = (int)((uint32_t)r / (uint32_t)t.count);
-      t.tile = r - t.unit * t.count;
+      if (SHARES) {
+        const int g = from + w0 + lane, in_all = (int)((uint32_t)g / (uint32_t)P.units);
+        int lo = 0, hi = ENTRIES;                     // the last entry that does not begin behind it
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (sh_begin[mid] <= in_all) lo = mid; else hi = mid;
+        }
+        int at = sh_begin[lo];
+        t.seq = lo * stride;
+        t.count = stride == 1 ? sh_begin[lo + 1] - at : tiles_of(t.seq);
+        while (at + t.count <= in_all) { at += t.count; t.count = tiles_of(++t.seq); }
+        const int r = g - at * P.units;
+        t.unit = (int)((uint32_t)r / (uint32_t)t.count);
+        t.tile = r - t.unit * t.count;
+      } else {
+        t.seq = own_seq;
+        t.unit = own_unit;
+        t.count = total;
+        t.tile = from + w0 + lane;
+      }
       const int token = t.tile * TILE, kv = t.unit / P.blocks;
       t.rows = a.length[t.seq] - token;
       page_of(t.seq, kv, token >> P.log_page, t.at0, t.k0, t.v0);
@@ -234,12 +244,12 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
 
   bool failed = a.fail_first_wait;                    // the self-test: as if the first wait had run out
   int w = 0, failed_at = 0;
-  while (w < mine) {
+  while (SHARES ? w < mine : w == 0) {                // without shares once, even by a warp without tiles
     // ---- a unit, or the part of it that lies in this share
-    const int4 where = *reinterpret_cast<const int4*>(&ahead[w & (2 * BATCH - 1)].seq);
+    const int4 where = SHARES ? *reinterpret_cast<const int4*>(&ahead[w & (2 * BATCH - 1)].seq) : make_int4(own_seq, own_unit, from, total);
     const int s = where.x, y = where.y, first = where.z, tiles = where.w;
     const int begun = w, end = min(mine, w + tiles - first);
-    const bool whole = first == 0 && w + tiles <= mine;
+    const bool whole = SHARES && first == 0 && w + tiles <= mine;
     const int kv = y / P.blocks, block = y - kv * P.blocks;
     const int heads = min(GB, P.group - block * GB), head0 = kv * P.group + block * GB, head = head0 + min(r8, heads - 1);
 
@@ -449,8 +459,8 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
     }
     // Where the unit covers all the CTA's shares, its warps' parts become one (a long sequence has hundreds of them).
     const int cta_from = from - warp * share, begins = from + begun - first, ends = begins + tiles;
-    const bool joined = begins <= cta_from && ends - cta_from >= NW * share;
-    if (first == 0 && lane == 0) {
+    const bool joined = !SHARES || (begins <= cta_from && ends - cta_from >= NW * share);
+    if (SHARES && first == 0 && lane == 0) {
       const uint32_t cta_share = NW * (uint32_t)share;
       a.splits[2 * me + 1] = make_int4((int)(((uint32_t)begins + cta_share - 1) / cta_share), (int)((uint32_t)ends / cta_share), 0, 0);
       a.splits[2 * me] = make_int4(head0, s, (int)((uint32_t)(ends - 1) / (uint32_t)share), heads);
@@ -487,12 +497,25 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
           acc.x = fmaf(u.x, fo, acc.x); acc.y = fmaf(u.y, fo, acc.y); acc.z = fmaf(u.z, fo, acc.z); acc.w = fmaf(u.w, fo, acc.w);
           sum = fmaf(sh_ml[v][h].y, fo, sum);
         }
-        *reinterpret_cast<float4*>(part + h * (D + 4) + f) = acc;
-        if (f == 0) *reinterpret_cast<float2*>(part + h * (D + 4) + D) = make_float2(top, sum);
+        if (SHARES) {
+          *reinterpret_cast<float4*>(part + h * (D + 4) + f) = acc;
+          if (f == 0) *reinterpret_cast<float2*>(part + h * (D + 4) + D) = make_float2(top, sum);
+        } else {
+          const float by = 1.f / sum;
+          uint2 r;
+          if (a.bf16) {
+            const __nv_bfloat162 b0 = __floats2bfloat162_rn(acc.x * by, acc.y * by), b1 = __floats2bfloat162_rn(acc.z * by, acc.w * by);
+            r = make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
+          } else {
+            r = make_uint2(h2(__floats2half2_rn(acc.x * by, acc.y * by)), h2(__floats2half2_rn(acc.z * by, acc.w * by)));
+          }
+          *reinterpret_cast<uint2*>(static_cast<unsigned short*>(a.out) + (int64_t)s * a.out_sequence + (int64_t)(head0 + h) * a.out_head + f) = r;
+        }
       }
     }
+    if (!SHARES) break;
   }
-  if (failed)                                         // copies in flight get a second bounded wait
+  if (failed && mine > 0)                             // copies in flight get a second bounded wait
     for (int i = failed_at; i < min(failed_at + ST, mine); ++i) (void)mbar_wait_bounded(bars + i % ST, (uint32_t)(i / ST & 1));
 }
 
@@ -584,16 +607,31 @@ int ctas_of(int S, int W, int page, int Hkv, int group, int d) {
   return (int)(ctas < wave ? ctas : wave);
 }
 
+// Whether a CTA takes a unit: few units, none of which can have more than a few tiles.  The second kernel, which joins shares, then costs more than
+// their even distribution saves: 8 caches of 64 / 256 / 512 tokens (d 128, four heads each) 4.2 / 5.7 / 8.4 us against 7.6 / 9.8 / 9.9, 512 caches of 256 tokens 15 against
+// 18; but 8 of 1024 tokens 13 against 9.9, and 2048 of 256 tokens 46 against 41.
+constexpr int FEW_TILES = 16, FEW_UNITS = 4 * SMS;
+bool by_unit(const PageCache& c, int units) {
+  const int tile = c.d == 256 ? 16 : 32;
+  return ((int64_t)c.W * c.page + tile - 1) / tile <= FEW_TILES && (int64_t)c.S * units <= FEW_UNITS;
+}
+
 template <int D>
 cudaError_t launch_attend_d(const AttendParams& P, cudaStream_t stream) {
   constexpr size_t smem = 1024 + (size_t)NW * Shape<D>::STAGES * Shape<D>::BYTES;
-  static_assert(Shape<D>::RESIDENT * (smem + NW * 2 * BATCH * sizeof(Ahead) + 4 * (ENTRIES + 1 + NW) + 8 * NW * (GB + 4) + 1024) <= 228 * 1024, "shared memory of the CTAs that are to run at once");
-  cudaError_t e = cudaFuncSetAttribute(pages_attend_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
+  static_assert(Shape<D>::RESIDENT * (smem + NW * 2 * BATCH * sizeof(Ahead) + 4 * (ENTRIES + 1 + NW) + 8 * NW * (GB + 4) + 1024) <= 228 * 1024,
+                "shared memory of the CTAs that are to run at once");
   const PageCache& c = P.a.c;
+  const bool units = by_unit(c, P.units);
+  cudaError_t e = cudaFuncSetAttribute(units ? pages_attend_kernel<D, false> : pages_attend_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  if (units) {
+    pages_attend_kernel<D, false><<<(unsigned)((int64_t)c.S * P.units), NT, smem, stream>>>(P);
+    return cudaGetLastError();
+  }
   static_assert(GB * Shape<D>::HEAD * 4 <= Shape<D>::STAGES * Shape<D>::BYTES, "a warp's sums fit its ring");
   const int ctas = ctas_of(c.S, c.W, c.page, c.Hkv, P.group, D);
-  pages_attend_kernel<D><<<ctas, NT, smem, stream>>>(P);
+  pages_attend_kernel<D, true><<<ctas, NT, smem, stream>>>(P);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(ctas * NW));
