@@ -211,6 +211,26 @@ def test_attention_over_pages(d, page, H, Hkv, dtype, alibi):
     _check(out, q, table, lengths, cache, scale, slopes)
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("H,Hkv,dtype,alibi", [(4, 4, "bf16", True), (16, 2, "fp16", False), (12, 1, "bf16", False)])
+def test_short_sequences_of_few_caches(d, page, H, Hkv, dtype, alibi):
+    """Tables with room for a few tiles only: a CTA takes all of a sequence and cache."""
+    lengths = [0, 1, 15, 16, 17, 33, 64, 100, 127, 128, 255, 256]
+    if d > 64 and page < 128:
+        lengths += [200, 3]
+    pages = sum(-(-n // page) for n in lengths) + 3
+    cache, scale = _pool(pages, Hkv, page, d)
+    table = _table(lengths, page, pages)
+    q = torch.randn(len(lengths), H, d, device=DEV).to(TYPES[dtype])
+    slopes = torch.exp2(-8.0 * torch.arange(1, H + 1, device=DEV) / H) if alibi else None
+    out = _attend(q, table, lengths, cache, scale, slopes)
+    _check(out, q, table, lengths, cache, scale, slopes)
+    # a wider table takes the other form, which splits sequences: the same within both roundings
+    wide = np.concatenate([table, np.full((len(lengths), 40), -1, np.int32)], 1)
+    _check(_attend(q, wide, lengths, cache, scale, slopes), q, wide, lengths, cache, scale, slopes)
+
+
 def test_one_token_is_its_value_row():
     cache, scale = _pool(3, 2, 16, 128)
     q = torch.randn(1, 4, 128, device=DEV).half()
@@ -344,9 +364,12 @@ def test_a_wait_that_runs_out_makes_the_output_nan():
     lengths = [700, 0, 3]
     table = _table(lengths, 16, 100)
     q = torch.randn(3, 4, 64, device=DEV).half()
-    out = _attend(q, table, lengths, cache, scale, debug_fail_first_wait=1)
-    assert torch.isnan(out[[0, 2]]).all() and (out[1] == 0).all()
-    _check(_attend(q, table, lengths, cache, scale), q, table, lengths, cache, scale)
+    for width in (table.shape[1], 10):                          # both forms
+        lengths[0] = min(lengths[0], 16 * width)
+        part = np.ascontiguousarray(table[:, :width])
+        out = _attend(q, part, lengths, cache, scale, debug_fail_first_wait=1)
+        assert torch.isnan(out[[0, 2]]).all() and (out[1] == 0).all()
+        _check(_attend(q, part, lengths, cache, scale), q, part, lengths, cache, scale)
 
 
 def test_attention_on_streams_with_scratch_of_any_content_and_captured():

@@ -35,7 +35,8 @@ def _call_ragged(a, p=None):
                                  dict(n_heads=65536 * 2), dict(head_dim=96), dict(type=2), dict(type=-1), dict(bias_mode=1), dict(bias_mode=2), dict(bias_mode=1, d_alibi_slopes=OK + 2),
                                  dict(logit_scale=-1.0), dict(logit_scale=float("nan")), dict(logit_scale=float("inf")), dict(q_token_stride=0), dict(q_head_stride=0), dict(k_token_stride=132),
                                  dict(k_head_stride=32), dict(v_token_stride=-128), dict(v_head_stride=1 << 38), dict(out_token_stride=128), dict(out_head_stride=256),
-                                 dict(debug_fail_first_wait=2), dict(debug_fail_first_wait=-1)])
+                                 dict(debug_fail_first_wait=2), dict(debug_fail_first_wait=-1),
+                                 dict(sequences=1 << 20, n_heads=4096), dict(tokens=1 << 28, n_heads=2048)])
 def test_ragged_arguments_are_checked(bad):
     assert _call_ragged(_ragged(**bad)) == BAD
 
@@ -133,7 +134,8 @@ def _attend(c=None, **kw):
 
 @pytest.mark.parametrize("bad", [dict(n_heads=0), dict(n_heads=3), dict(n_heads=65536 * 2), dict(type=2), dict(bias_mode=1), dict(bias_mode=-1), dict(logit_scale=-1.0),
                                  dict(logit_scale=float("nan")), dict(q_sequence_stride=60), dict(q_head_stride=0), dict(out_sequence_stride=100), dict(out_head_stride=32),
-                                 dict(out_sequence_stride=64), dict(debug_fail_first_wait=2)])
+                                 dict(out_sequence_stride=64), dict(debug_fail_first_wait=2),
+                                 dict(cache=_cache(sequences=1 << 20, table_width=1 << 16))])
 def test_attend_arguments_are_checked(bad):
     a = _attend(**bad)
     assert kf.LIB.kf_pages_attend_scratch_bytes(C.byref(a)) == 0
