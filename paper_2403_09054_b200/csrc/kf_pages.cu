@@ -11,6 +11,8 @@
 
 #include <cooperative_groups.h>
 
+#include <algorithm>
+
 namespace kf {
 
 namespace {
@@ -97,6 +99,8 @@ template <bool BF16, int NT>
 __global__ void __launch_bounds__(NT, 1024 / NT) pages_write_kernel(const __grid_constant__ WriteParams P) {
   constexpr int SIDE = NT / 2;
   __shared__ uint32_t sh_top[NT / 32];
+  after_earlier_kernels();
+  let_next_kernel_launch();
   const PageCache& c = P.c;
   const int side = threadIdx.x >= SIDE, tid = threadIdx.x & (SIDE - 1);
   int s = blockIdx.x, from = s, count = 1, part = 0;
@@ -186,6 +190,8 @@ struct ReadParams {
 template <bool BF16, int NT>
 __global__ void __launch_bounds__(NT, 2048 / NT) pages_read_kernel(const __grid_constant__ ReadParams P) {
   constexpr int SIDE = NT / 2;
+  after_earlier_kernels();
+  let_next_kernel_launch();
   const PageCache& c = P.c;
   const int side = threadIdx.x >= SIDE, tid = threadIdx.x & (SIDE - 1);
   const int s = slot_sequence(P.begin, c.S, blockIdx.x, 1, P.log_page, 2);
@@ -241,6 +247,8 @@ __global__ void __launch_bounds__(NT, 8) pages_compact_kernel(const __grid_const
   __shared__ float sh_scale[2][128];
   __shared__ uint32_t sh_top[2][4];
   constexpr int SIDE = NT / 2;
+  after_earlier_kernels();
+  let_next_kernel_launch();
   const PageCache& c = P.c;
   const int s = blockIdx.x / P.new_width, j = blockIdx.x % P.new_width, h = blockIdx.y;
   const int kept = min(P.n_keep[s], P.keep_width);
@@ -345,7 +353,8 @@ __global__ void __launch_bounds__(UT, 1) pages_update_kernel(const __grid_consta
   const int S = c.S, W = c.W, rank = (int)cluster.block_rank(), ranks = (int)cluster.num_blocks(), tid = threadIdx.x;
   const int64_t capacity = (int64_t)W * c.page;
   const int log_page = U.log_page;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  after_earlier_kernels();
+  let_next_kernel_launch();
 
   // ---- lengths, who keeps a page that is filled in part, and the pages to hand out before each sequence
   for (int s = tid; s < S; s += UT) sh.need[s] = S;
@@ -480,7 +489,8 @@ __global__ void __launch_bounds__(UT, 1) pages_update_kernel(const __grid_consta
 
 // The rows of pages that are filled in part.  Grid: sequences, layers, pieces of the heads.
 __global__ void __launch_bounds__(NT) pages_copy_kernel(const __grid_constant__ PagesUpdate U) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  after_earlier_kernels();
+  let_next_kernel_launch();
   const int4 copy = __ldcg(U.copies + blockIdx.x);
   if (copy.y < 0) return;
   const PageCache& c = U.c;
@@ -519,13 +529,9 @@ cudaError_t launch_pages_write(const PageCache& c, const PageRows& r, const int3
   const unsigned slots = begin ? (unsigned)((r.tokens >> P.log_page) + 2 * c.S) : (unsigned)c.S;
   const dim3 grid(slots, (unsigned)c.Hkv);
   if (few_rows(r.tokens, slots, c.d)) {
-    if (r.bf16) pages_write_kernel<true, FEW_NT><<<grid, FEW_NT, 0, stream>>>(P);
-    else pages_write_kernel<false, FEW_NT><<<grid, FEW_NT, 0, stream>>>(P);
-  } else {
-    if (r.bf16) pages_write_kernel<true, NT><<<grid, NT, 0, stream>>>(P);
-    else pages_write_kernel<false, NT><<<grid, NT, 0, stream>>>(P);
+    return r.bf16 ? launch_early(pages_write_kernel<true, FEW_NT>, grid, FEW_NT, 0, stream, P) : launch_early(pages_write_kernel<false, FEW_NT>, grid, FEW_NT, 0, stream, P);
   }
-  return cudaGetLastError();
+  return r.bf16 ? launch_early(pages_write_kernel<true, NT>, grid, NT, 0, stream, P) : launch_early(pages_write_kernel<false, NT>, grid, NT, 0, stream, P);
 }
 
 cudaError_t launch_pages_read(const PageCache& c, const PageRows& r, const int32_t* begin, const int32_t* first, const int32_t* table, cudaStream_t stream) {
@@ -536,13 +542,9 @@ cudaError_t launch_pages_read(const PageCache& c, const PageRows& r, const int32
   const unsigned slots = (unsigned)((r.tokens >> P.log_page) + 2 * c.S);
   const dim3 grid(slots, (unsigned)c.Hkv);
   if (few_rows(r.tokens, slots, c.d)) {
-    if (r.bf16) pages_read_kernel<true, FEW_NT><<<grid, FEW_NT, 0, stream>>>(P);
-    else pages_read_kernel<false, FEW_NT><<<grid, FEW_NT, 0, stream>>>(P);
-  } else {
-    if (r.bf16) pages_read_kernel<true, NT><<<grid, NT, 0, stream>>>(P);
-    else pages_read_kernel<false, NT><<<grid, NT, 0, stream>>>(P);
+    return r.bf16 ? launch_early(pages_read_kernel<true, FEW_NT>, grid, FEW_NT, 0, stream, P) : launch_early(pages_read_kernel<false, FEW_NT>, grid, FEW_NT, 0, stream, P);
   }
-  return cudaGetLastError();
+  return r.bf16 ? launch_early(pages_read_kernel<true, NT>, grid, NT, 0, stream, P) : launch_early(pages_read_kernel<false, NT>, grid, NT, 0, stream, P);
 }
 
 cudaError_t launch_pages_compact(const PageCache& c, int keep_width, int new_width, const int32_t* table, const int32_t* length, const int32_t* keep,
@@ -550,8 +552,7 @@ cudaError_t launch_pages_compact(const PageCache& c, int keep_width, int new_wid
   CompactParams P{};
   P.c = c; P.table = table; P.length = length; P.keep = keep; P.n_keep = n_keep; P.new_table = new_table;
   P.keep_width = keep_width; P.new_width = new_width; P.log_page = log2_of(c.page); P.log_vec = log2_of(c.d / 16);
-  pages_compact_kernel<<<dim3((unsigned)c.S * (unsigned)new_width, (unsigned)c.Hkv), NT, 0, stream>>>(P);
-  return cudaGetLastError();
+  return launch_early(pages_compact_kernel, dim3((unsigned)c.S * (unsigned)new_width, (unsigned)c.Hkv), NT, 0, stream, P);
 }
 
 cudaError_t launch_pages_update(const PagesUpdate& u, cudaStream_t stream) {
@@ -561,29 +562,24 @@ cudaError_t launch_pages_update(const PagesUpdate& u, cudaStream_t stream) {
   U.log_page = log2_of(u.c.page);
   // entries and pages one CTA goes through in a few rounds; the barriers of a cluster cost about as much
   const bool small = (int64_t)u.c.S * u.c.W + u.c.pages / 4 <= 16 * UT;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim = {small ? 1u : (unsigned)CLUSTER, 1u, 1u};
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {small ? 1u : (unsigned)CLUSTER, 1u, 1u};
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(small ? 1u : (unsigned)CLUSTER);
   cfg.blockDim = dim3(UT);
   cfg.dynamicSmemBytes = sizeof(UpdateShared);
   cfg.stream = stream;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
   e = cudaLaunchKernelEx(&cfg, pages_update_kernel, U);
   if (e != cudaSuccess || !u.parent) return e;                    // without parents no page has a second owner
-  const int pieces = u.c.Hkv * 2 < 8 ? u.c.Hkv * 2 : 8;
-  cudaLaunchAttribute after{};
-  after.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  after.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t copy{};
-  copy.gridDim = dim3((unsigned)u.c.S, (unsigned)u.layers, (unsigned)pieces);
-  copy.blockDim = dim3(NT);
-  copy.stream = stream;
-  copy.attrs = &after;
-  copy.numAttrs = 1;
-  return cudaLaunchKernelEx(&copy, pages_copy_kernel, U);
+  // most CTAs find nothing to copy: no more of them than a few per SM where there are many sequences
+  const int64_t rows = (int64_t)u.c.S * u.layers;
+  const int pieces = (int)std::min<int64_t>(std::min(8, u.c.Hkv * 2), std::max<int64_t>(1, 1024 / rows));
+  return launch_early(pages_copy_kernel, dim3((unsigned)u.c.S, (unsigned)u.layers, (unsigned)pieces), NT, 0, stream, U);
 }
 
 }  // namespace kf

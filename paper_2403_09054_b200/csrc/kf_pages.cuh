@@ -76,6 +76,27 @@ cudaError_t launch_pages_attend(const PagesAttend& a, cudaStream_t stream);
 
 #ifdef __CUDACC__
 
+// A launch that may begin while the kernel before it on the stream still runs: a token's step is a row of kernels of a few microseconds each, and what a
+// launch costs then hides behind the one before.  Every such kernel calls after_earlier_kernels() before it touches memory.
+template <class Kernel, class... Args>
+cudaError_t launch_early(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t stream, const Args&... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+// Waits until the kernels before have completed and what they wrote is seen.
+__device__ __forceinline__ void after_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The next kernel may be launched (and wait) from here on.
+__device__ __forceinline__ void let_next_kernel_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // The sequence that slot `slot` of a grid belongs to.  A grid that must cover ragged ranges without knowing their lengths on the
 // host gives sequence s the slots from start(s) = (begin[s] >> shift) + extra * s on: as floor(a + b) - floor(a) >= floor(b), every
 // sequence gets ceil(length / 2^shift) + extra - 1 of them at least.  All lanes of a warp call this and get the same answer, found 32 ways at a time;

@@ -119,7 +119,8 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
   __shared__ Ahead sh_ahead[NW][2 * BATCH];
   __shared__ float2 sh_ml[NW][GB];
 
-  if (SHARES) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  after_earlier_kernels();
+  let_next_kernel_launch();
   const PagesAttend& a = P.a;
   const PageCache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r8 = lane >> 2, t4 = lane & 3;
@@ -530,7 +531,8 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
 template <int D>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) pages_merge_kernel(const __grid_constant__ AttendParams P) {
   __shared__ float sh_o[MERGE_WARPS][D], sh_m[MERGE_WARPS], sh_l[MERGE_WARPS];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  after_earlier_kernels();
+  let_next_kernel_launch();
   const PagesAttend& a = P.a;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, w0 = blockIdx.x;
   const int4 split = __ldcg(a.splits + 2 * w0);
@@ -631,24 +633,11 @@ cudaError_t launch_attend_d(const AttendParams& P, cudaStream_t stream) {
   const bool units = by_unit(c, P.units);
   cudaError_t e = cudaFuncSetAttribute(units ? pages_attend_kernel<D, false> : pages_attend_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  if (units) {
-    pages_attend_kernel<D, false><<<(unsigned)((int64_t)c.S * P.units), NT, smem, stream>>>(P);
-    return cudaGetLastError();
-  }
+  if (units) return launch_early(pages_attend_kernel<D, false>, dim3((unsigned)((int64_t)c.S * P.units)), NT, smem, stream, P);
   static_assert(GB * Shape<D>::HEAD * 4 <= Shape<D>::STAGES * Shape<D>::BYTES, "a warp's sums fit its ring");
   const int ctas = ctas_of(c.S, c.W, c.page, c.Hkv, P.group, D);
-  pages_attend_kernel<D, true><<<ctas, NT, smem, stream>>>(P);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(ctas * NW));
-  cfg.blockDim = dim3(MERGE_WARPS * 32);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, pages_merge_kernel<D>, P);
+  e = launch_early(pages_attend_kernel<D, true>, dim3((unsigned)ctas), NT, smem, stream, P);
+  return e != cudaSuccess ? e : launch_early(pages_merge_kernel<D>, dim3((unsigned)(ctas * NW)), MERGE_WARPS * 32, 0, stream, P);
 }
 
 }  // namespace

@@ -166,6 +166,7 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  after_earlier_kernels();
 
   // Every role takes the items in order; number k lies in items[k & 1].  A wait for an item, or for all roles to be done with one, lasts as long as an
   // item may: its limit grows with the tiles.  These waits do not end when a role has given up: all roles then pass over what is left, up to the item
@@ -597,8 +598,7 @@ cudaError_t launch_ragged_d(const RaggedParams& P, cudaStream_t st) {
   auto go = [&](auto kern) -> cudaError_t {
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_req);
     if (e != cudaSuccess) return e;
-    kern<<<(unsigned)(P.slots * P.groups), threads_of(NB), smem_req, st>>>(P);
-    return cudaGetLastError();
+    return launch_early(kern, dim3((unsigned)(P.slots * P.groups)), threads_of(NB), smem_req, st, P);
   };
   return P.slopes ? go(ragged_kernel<D, true, BF16>) : go(ragged_kernel<D, false, BF16>);
 }
