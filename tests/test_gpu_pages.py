@@ -498,6 +498,32 @@ def test_large_tables(S, W, pages):
     _update_case(S, W, 16, pages, 1, 1, 64, rng.integers(-1, S, S).tolist(), length, 1)
 
 
+def test_more_pages_at_once_than_one_cta_lists():
+    _update_case(1, 12000, 16, 14000, 1, 1, 64, None, [100], 11000 * 16)
+
+
+def test_a_row_of_calls_without_a_pause():
+    """Launches begin behind the ones before: what a call wrote is there for the next, and nothing is overwritten that one before still reads."""
+    kf, S, Hkv, d, page, W = _kf(), 6, 2, 64, 16, 20
+    cache, scale = torch.zeros(S * W, Hkv, 2, page, d, device=DEV, dtype=torch.int8), torch.zeros(S * W, Hkv, 2, device=DEV)
+    table, length = torch.full((S, W), -1, device=DEV, dtype=torch.int32), torch.zeros(S, device=DEV, dtype=torch.int32)
+    refs, missing = torch.zeros(S * W, device=DEV, dtype=torch.int32), _ints([0])
+    x = torch.randn(40, 2, S, Hkv, d, device=DEV).half()
+    q, out = torch.randn(40, S, 4, d, device=DEV).half(), torch.zeros(40, S, 4, d, device=DEV).half()
+    for step in range(40):
+        kf.kf_pages_update(table=table, length=length, refs=refs, cache=cache, scale=scale, missing=missing, grow=1)
+        kf.kf_pages_write(k=x[step, 0], v=x[step, 1], length=length, table=table, cache=cache, scale=scale)
+        length.add_(1)
+        kf.kf_pages_attend(q=q[step], table=table, length=length, cache=cache, scale=scale, out=out[step])
+    want_c, want_s = np.zeros(cache.shape, np.int8), np.zeros(scale.shape, np.float32)
+    t = table.cpu().numpy()
+    for step in range(40):
+        ref.write(want_c, want_s, t, [step] * S, x[step].double().cpu().numpy(), list(range(S + 1)))
+        if step % 13 == 0 or step == 39:
+            _check(out[step], q[step], t, [step + 1] * S, torch.from_numpy(want_c), torch.from_numpy(want_s))
+    np.testing.assert_array_equal(cache.cpu().numpy(), want_c)
+
+
 def test_updates_replayed():
     """One captured update steps a beam search on."""
     S, W, page, pages = 4, 6, 16, 64

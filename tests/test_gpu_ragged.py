@@ -144,6 +144,35 @@ def test_references_that_move(d, H, Hkv):
     _check(q, k, v, begin, out, scale=0.5)
 
 
+def test_slopes_of_any_sign():
+    """Biases that grow with the distance make the references move with every tile."""
+    H = 4
+    slopes = torch.tensor([-0.5, -2.0, 0.0, 3.0], device=DEV)
+    for d in (64, 128, 256):
+        q, k, v, begin, out = _inputs([700, 130], H, 2, d, torch.bfloat16)
+        _kf().kf_prefill_attend_ragged(q=q, k=k, v=v, begin=begin, out=out, bias_mode=1, alibi_slopes_dev=slopes)
+        _check(q, k, v, begin, out, slopes)
+
+
+def test_a_very_long_sequence():
+    """150000 tokens: no wait runs out, and rows of every part are right."""
+    n, H, d = 150000, 2, 64
+    q, k, v, begin, out = _inputs([n], H, 1, d, torch.bfloat16)
+    _kf().kf_prefill_attend_ragged(q=q, k=k, v=v, begin=begin, out=out)
+    for i in (0, 127, 128, 40000, 65535, 65536, 99999, n - 2, n - 1):
+        want, weighted, size = ref.attend_rows(q[i:i + 1].double(), k[:i + 1].double(), v[:i + 1].double(), 1 / math.sqrt(d), causal=False)
+        assert ((out[i:i + 1].double() - want).abs() <= ref.bound(want, weighted, size, out.dtype, d, True)).all(), i
+    assert torch.isfinite(out).all()
+
+
+def test_nothing_to_do():
+    q, k, v, _, out = _inputs([50], 4, 2, 128, torch.float16)
+    for begin in ([0, 0], [50, 50, 50], [7] * 300):
+        _kf().kf_prefill_attend_ragged(q=q, k=k, v=v, begin=torch.tensor(begin, device=DEV, dtype=torch.int32), out=out)
+    torch.cuda.synchronize()
+    assert (out == 7.0).all()
+
+
 @pytest.mark.parametrize("dtype,exponent", [("fp16", 20), ("bf16", 30)])
 def test_many_small_weights_count(dtype, exponent):
     """One key with weight 1 and 4000 with 2^-20 or 2^-30: a weight that stands far below the largest is not dropped."""
