@@ -215,7 +215,8 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
         t.count = total;
         t.tile = from + w0 + lane;
       }
-      const int token = t.tile * TILE, kv = t.unit / P.blocks;
+      // from the newest back: with ALiBi the nearest keys have the largest logits, so that references hardly move
+      const int token = (t.count - 1 - t.tile) * TILE, kv = t.unit / P.blocks;
       t.rows = a.length[t.seq] - token;
       page_of(t.seq, kv, token >> P.log_page, t.at0, t.k0, t.v0);
       t.in_page = token & (c.page - 1);
