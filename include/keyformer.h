@@ -307,7 +307,8 @@ int64_t kf_launch_count(const kf_ctx* ctx);
  * caller, work is enqueued on `stream` of the current device, arguments are checked on the host before anything is
  * enqueued, and nothing is allocated.  Scratch holds nothing between calls and need not be cleared; two calls that may run at
  * the same time (other streams, other captured graphs) need scratch of their own.  Nothing that a call
- * writes, its scratch included, may share memory with another of its tensors (KF_EINVAL).
+ * writes, its scratch included, may share memory with another of its tensors (KF_EINVAL; a tensor with strides counts from its first
+ * element to its last, so that two written tensors whose rows alternate within one buffer are refused as well).
  * ------------------------------------------------------------------------------------------------------------------ */
 
 #define KF_TYPE_FP16 0
@@ -531,8 +532,8 @@ int kf_pages_attend(const kf_pages_attend_args* args, const void* d_q, const voi
  *               references is never handed out).  Updated; a page is free when its count is 0.
  *   d_missing : DEVICE int32 [1], pages that could not be added because none was free or the table too narrow (at most 2^31 - 1)
  * Free pages are handed out lowest first, in the order of sequences and of the pages of each; where there is none the table
- * entry is -1; a copy of a page that was missing itself reads as NaN.  d_length[s] becomes the parent's length (0 for an ended one), without the room added.  A length outside 0 ..
- * table_width * page_tokens counts as 0; negative growth counts as none.  Pages filled in part belong to one sequence alone before and after. */
+ * entry is -1; a copy of a page that was missing itself reads as NaN.  d_length[s] becomes the parent's length (0 for an ended one),
+ * without the room added.  A length outside 0 .. table_width * page_tokens counts as 0; negative growth counts as none.  Pages filled in part belong to one sequence alone before and after. */
 typedef struct kf_pages_update_args {
   kf_page_cache cache;                /* S <= 8192, S * table_width <= 2^28                                       */
   int32_t n_layers;                   /* d_cache, d_scale: [n_layers] caches one after the other; one table serves all */

@@ -5,7 +5,8 @@
 // whose K and V tiles are contiguous, so that codes move 16 bytes a thread and the scale of a tile is decided by one CTA, without
 // a second pass over memory and without atomics.  Eight sequences of up to 4096 tokens (32 heads, d 128, pages of 64): written in 70 us and read back in 76,
 // 5.9 and 5.5 TB/s; ALU pipe 65 % and issue slots 65 % busy while writing (codes by conversion instructions instead of one addition: 127 us).
-// 16 prompts of up to 4096 tokens reduced to half: 60 us (4.6 TB/s, scattered rows of 128 bytes).  Tables: 5 to 10 us, four to five dependent trips to memory.
+// 16 prompts of up to 4096 tokens reduced to half: 60 us (4.6 TB/s, scattered rows of 128 bytes).  Tables: 10 to 12 us with the copies, four to five dependent trips to
+// memory.
 #include "kf_pages.cuh"
 #include "kf_tc.cuh"
 

@@ -10,15 +10,19 @@
 //
 // Work is split by tiles: those of all (sequence, key/value head, block of query heads) units stand one after the other, and every warp of one wave
 // of CTAs gets the same number of consecutive ones, whatever the lengths are (the host does not know them: every CTA adds them up).
-// A warp walks its share with a private ring of tiles that TMA fills with swizzled rows (both products' loads are then free of bank conflicts),
-// across the borders of units.  A unit that lies within one share is written by its warp; others leave a partial result per
-// warp, which pages_merge_kernel joins.  (Chunks of one sequence per CTA instead: 271 against 210 us for 32 x 32 caches of 4096 tokens, whose SMs idled for 40 %.)
+// Within a unit tiles go from the newest token back: with ALiBi the nearest keys have the largest logits, so that a reference hardly ever moves (32 x 32
+// caches of 4096 tokens 205 -> 196 us, of d 256 460 -> 417).  A warp walks its share with a private ring of tiles that TMA fills with swizzled rows (both
+// products' loads are then free of bank conflicts), across the borders of units.  A unit that lies within one share is written by its warp; others leave a partial
+// result per warp, which pages_merge_kernel joins.  (Chunks of one sequence per CTA instead: 271 against 210 us for 32 x 32 caches of 4096 tokens, whose SMs
+// idled for 40 %.)
 //
-// What bounds it: 32 x 32 caches of 4096 tokens (1.07 GB) take 197 to 210 us, 5.1 to 5.4 TB/s of 6.57; half of the issue slots are used (815 warp
-// instructions per 32 tokens of d 128, 416 of them conversions), the registers allow 12 warps, and of the 5.6 cycles between two instructions of a warp 1.9 are
-// the fixed latency of the one before, 0.7 a busy pipe and 0.5 memory.  48 sequences of up to 8192 tokens on 8 caches: 84 us, 61 at the copy rate.  Packed binary32
-// arithmetic in the softmax (as many instructions, the pairs have to be moved together) and sums that are corrected for the codes' offset at the end
-// (they would lose the last eleven bits) were not taken.
+// What bounds it: 32 x 32 caches of 4096 tokens (1.07 GB) take 196 us with ALiBi and 194 without, 5.5 TB/s of 6.57; the same loads without any arithmetic take 169.  Half
+// of the issue slots are used (815 warp instructions per 32 tokens of d 128, 416 of them conversions), the registers allow 12 warps, and of the 5.6 cycles between
+// two instructions of a warp 1.9 are the fixed latency of the one before, 0.7 a busy pipe and 0.5 memory.  48 sequences of up to 8192 tokens on 8 caches: 82 to 88 us, 75
+// without arithmetic, 61 at the copy rate.  Not taken, for 32 x 32 caches: 8 warps of 246 registers (195 to 209 us), 16 of 128 and tiles of 16 tokens (290), the table's
+// entries ahead of time by asynchronous copies (198), larger shares for the CTAs that an SM takes first (194 to 199), a record per unit instead of per share for the second
+// kernel (193), packed binary32 arithmetic in the softmax (as many instructions, the pairs have to be moved together), sums that are corrected for the codes'
+// offset at the end (they would lose the last eleven bits).
 #include "kf_pages.cuh"
 #include "kf_tc.cuh"
 
@@ -215,7 +219,6 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
         t.count = total;
         t.tile = from + w0 + lane;
       }
-      // from the newest back: with ALiBi the nearest keys have the largest logits, so that references hardly move
       const int token = (t.count - 1 - t.tile) * TILE, kv = t.unit / P.blocks;
       t.rows = a.length[t.seq] - token;
       page_of(t.seq, kv, token >> P.log_page, t.at0, t.k0, t.v0);
