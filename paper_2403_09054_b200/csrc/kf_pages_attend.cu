@@ -16,7 +16,7 @@
 // result per warp, which pages_merge_kernel joins.  (Chunks of one sequence per CTA instead: 271 against 210 us for 32 x 32 caches of 4096 tokens, whose SMs
 // idled for 40 %.)
 //
-// What bounds it: 32 x 32 caches of 4096 tokens (1.07 GB) take 196 us with ALiBi and 194 without, 5.5 TB/s of 6.57; the same loads without any arithmetic take 169.  Half
+// What bounds it: 32 x 32 caches of 4096 tokens (1.07 GB) take 188 to 196 us with ALiBi, 194 without, 5.5 TB/s of 6.57; the same loads without any arithmetic take 169.  Half
 // of the issue slots are used (815 warp instructions per 32 tokens of d 128, 416 of them conversions), the registers allow 12 warps, and of the 5.6 cycles between
 // two instructions of a warp 1.9 are the fixed latency of the one before, 0.7 a busy pipe and 0.5 memory.  48 sequences of up to 8192 tokens on 8 caches: 82 to 88 us, 75
 // without arithmetic, 61 at the copy rate.  Not taken, for 32 x 32 caches: 8 warps of 246 registers (195 to 209 us), 16 of 128 and tiles of 16 tokens (290), the table's
