@@ -3,9 +3,10 @@
 //
 // All of them are bound by memory (or, for single tokens, by the latency of a few dependent loads): a CTA owns one page of one key/value head,
 // whose K and V tiles are contiguous, so that codes move 16 bytes a thread and the scale of a tile is decided by one CTA, without
-// a second pass over memory and without atomics.  Eight sequences of up to 4096 tokens (32 heads, d 128, pages of 64): written in 70 us and read back in 76,
-// 5.9 and 5.5 TB/s; ALU pipe 65 % and issue slots 65 % busy while writing (codes by conversion instructions instead of one addition: 127 us).
-// 16 prompts of up to 4096 tokens reduced to half: 60 us (4.6 TB/s, scattered rows of 128 bytes).  Tables: 10 to 12 us with the copies, four to five dependent trips to
+// a second pass over memory and without atomics.  Eight sequences of up to 4096 tokens (32 heads, d 128, pages of 64): written in 69 us and read back in 72,
+// 6.0 and 5.8 TB/s; ALU pipe 65 % and issue slots 65 % busy while writing (codes by conversion instructions instead of one addition: 127 us).
+// 16 prompts of up to 4096 tokens reduced to half: 61 us (4.6 TB/s, scattered rows of 128 bytes), and read
+// back in 74.  Tables: 10 to 12 us with the copies, four to five dependent trips to
 // memory.
 #include "kf_pages.cuh"
 #include "kf_tc.cuh"
@@ -13,6 +14,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace kf {
 
@@ -20,8 +22,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int NT = 256;              // threads of a CTA that works on a page: half of them on K, half on V
-constexpr int FEW_NT = 64;           // the same where pages get few rows, as with single tokens (64 tokens of 8 heads, written and read back: 8.4 instead of 11.2 us)
+constexpr int NT = 256;              // threads of a CTA of the copies, and at most of one that works on a page where pages get few rows
 constexpr int HELD = 8;              // 16-byte pieces of rows a thread keeps between the maximum and the codes
 
 // The smallest 2^e with top <= 127 * 2^e, e >= -120, by the exponent and the leading bits of top; NaN where top is not finite.
@@ -185,7 +186,8 @@ struct ReadParams {
   void *k, *v;
   int64_t k_token, k_head, v_token, v_head;
   const int32_t *begin, *first, *table;
-  int32_t tokens, log_page, log_vec;
+  int32_t tokens, log_page, log_vec;   // log2 of the page and of the 16-byte pieces of a row of codes
+  bool wide;                           // rows are aligned to 32 bytes
 };
 
 template <bool BF16, int NT>
@@ -209,20 +211,22 @@ __global__ void __launch_bounds__(NT, 2048 / NT) pages_read_kernel(const __grid_
   const bool held = id >= 0 && id < c.pages;
   const size_t tile = ((size_t)(held ? id : 0) * c.Hkv + blockIdx.y) * 2 + side;
   const float scale = held ? c.scale[tile] : nan_f32();
-  const uint2* codes = reinterpret_cast<const uint2*>(c.codes + (tile * c.page + (size_t)(lo - first_token)) * c.d);
+  const uint4* codes = reinterpret_cast<const uint4*>(c.codes + (tile * c.page + (size_t)(lo - first_token)) * c.d);
   unsigned short* dst = static_cast<unsigned short*>(side ? P.v : P.k) + (from + (lo - start)) * (side ? P.v_token : P.k_token) +
                         (int64_t)blockIdx.y * (side ? P.v_head : P.k_head);
   const int64_t stride = side ? P.v_token : P.k_token;
   const int vecs = (int)(hi - lo) << P.log_vec;
-#pragma unroll 4
+#pragma unroll 2
   for (int i = tid; i < vecs; i += SIDE) {
-    const uint2 w = held ? codes[i] : make_uint2(0, 0);
-    uint32_t r[4];
-    float x[8];
+    const uint4 w = held ? codes[i] : make_uint4(0, 0, 0, 0);
+    uint32_t r[8];
+    float x[16];
     numbers4(w.x, reinterpret_cast<float(&)[4]>(x[0]));
     numbers4(w.y, reinterpret_cast<float(&)[4]>(x[4]));
+    numbers4(w.z, reinterpret_cast<float(&)[4]>(x[8]));
+    numbers4(w.w, reinterpret_cast<float(&)[4]>(x[12]));
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
+    for (int p = 0; p < 8; ++p) {
       const float a = x[2 * p] * scale, b = x[2 * p + 1] * scale;
       if (BF16) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -232,7 +236,13 @@ __global__ void __launch_bounds__(NT, 2048 / NT) pages_read_kernel(const __grid_
         r[p] = *reinterpret_cast<const uint32_t*>(&h);
       }
     }
-    *reinterpret_cast<uint4*>(dst + (int64_t)(i >> P.log_vec) * stride + (i & ((1 << P.log_vec) - 1)) * 8) = make_uint4(r[0], r[1], r[2], r[3]);
+    unsigned short* at = dst + (int64_t)(i >> P.log_vec) * stride + (i & ((1 << P.log_vec) - 1)) * 16;
+    if (P.wide) {                                                // two stores of 16 bytes instead: 75.6 against 71.5 us
+      store_sector(at, r);
+    } else {
+      reinterpret_cast<uint4*>(at)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+      reinterpret_cast<uint4*>(at)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+    }
   }
 }
 
@@ -243,10 +253,11 @@ struct CompactParams {
   int32_t keep_width, new_width, log_page, log_vec;
 };
 
-__global__ void __launch_bounds__(NT, 8) pages_compact_kernel(const __grid_constant__ CompactParams P) {
+template <int NT>
+__global__ void __launch_bounds__(NT, 2048 / NT) pages_compact_kernel(const __grid_constant__ CompactParams P) {
   __shared__ int64_t sh_row[128];             // where a row's K codes stand, -1: nowhere
   __shared__ float sh_scale[2][128];
-  __shared__ uint32_t sh_top[2][4];
+  __shared__ uint32_t sh_top[2][NT / 32];
   constexpr int SIDE = NT / 2;
   after_earlier_kernels();
   let_next_kernel_launch();
@@ -257,34 +268,33 @@ __global__ void __launch_bounds__(NT, 8) pages_compact_kernel(const __grid_const
   if (rows <= 0) return;
   const int to = P.new_table[(size_t)s * P.new_width + j];
   if (to < 0 || to >= c.pages) return;
-  if (threadIdx.x < 128) {
-    float2 scale = make_float2(0.f, 0.f);
+  uint32_t tk = 0, tv = 0;                    // scales carry no sign: their bits are in order, with NaN on top
+  for (int r = threadIdx.x; r < rows; r += NT) {
+    const int token = P.keep[((size_t)s * c.Hkv + h) * P.keep_width + (j << P.log_page) + r];
+    const int slot = token >> P.log_page;
+    int id = -1;
+    if (token >= 0 && token < P.length[s] && slot < c.W) id = P.table[(size_t)s * c.W + slot];
+    float2 scale = make_float2(nan_f32(), nan_f32());
     int64_t at = -1;
-    if ((int)threadIdx.x < rows) {
-      const int token = P.keep[((size_t)s * c.Hkv + h) * P.keep_width + (j << P.log_page) + threadIdx.x];
-      const int slot = token >> P.log_page;
-      int id = -1;
-      if (token >= 0 && token < P.length[s] && slot < c.W) id = P.table[(size_t)s * c.W + slot];
-      if (id >= 0 && id < c.pages) {
-        const size_t tile = ((size_t)id * c.Hkv + h) * 2;
-        scale = *reinterpret_cast<const float2*>(c.scale + tile);
-        at = (int64_t)(tile * c.page + (token & (c.page - 1))) * c.d;
-      } else {
-        scale = make_float2(nan_f32(), nan_f32());
-      }
+    if (id >= 0 && id < c.pages) {
+      const size_t tile = ((size_t)id * c.Hkv + h) * 2;
+      scale = *reinterpret_cast<const float2*>(c.scale + tile);
+      at = (int64_t)(tile * c.page + (token & (c.page - 1))) * c.d;
     }
-    sh_row[threadIdx.x] = at;
-    sh_scale[0][threadIdx.x] = scale.x;
-    sh_scale[1][threadIdx.x] = scale.y;
-    // scales carry no sign: their bits are in order, with NaN on top
-    const uint32_t tk = __reduce_max_sync(0xffffffffu, __float_as_uint(scale.x)), tv = __reduce_max_sync(0xffffffffu, __float_as_uint(scale.y));
-    if ((threadIdx.x & 31) == 0) { sh_top[0][threadIdx.x >> 5] = tk; sh_top[1][threadIdx.x >> 5] = tv; }
+    sh_row[r] = at;
+    sh_scale[0][r] = scale.x;
+    sh_scale[1][r] = scale.y;
+    tk = max(tk, __float_as_uint(scale.x));
+    tv = max(tv, __float_as_uint(scale.y));
   }
+  tk = __reduce_max_sync(0xffffffffu, tk);
+  tv = __reduce_max_sync(0xffffffffu, tv);
+  if ((threadIdx.x & 31) == 0) { sh_top[0][threadIdx.x >> 5] = tk; sh_top[1][threadIdx.x >> 5] = tv; }
   __syncthreads();
   const int side = threadIdx.x >= SIDE, tid = threadIdx.x & (SIDE - 1);
   uint32_t top = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) top = max(top, sh_top[side][w]);
+  for (int w = 0; w < NT / 32; ++w) top = max(top, sh_top[side][w]);
   const float scale = __uint_as_float(top);
   const float inverse = scale > 0.f ? 1.f / scale : 0.f;
   const size_t tile = ((size_t)to * c.Hkv + h) * 2 + side;
@@ -515,12 +525,28 @@ __global__ void __launch_bounds__(NT) pages_copy_kernel(const __grid_constant__ 
   for (int t = from + threadIdx.x; t < to; t += NT) c.scale[b + t] = c.scale[a + t];
 }
 
-// Whether a slot has, on average, no more than one 16-byte piece of a row for each thread of a side.
+// Whether a slot has, on average, no more than one 16-byte piece of a row for each thread of a side: then 64 threads do (64 tokens of 8 heads, written and
+// read back: 8.4 instead of 11.2 us).
 bool few_rows(int tokens, unsigned slots, int d) { return (int64_t)tokens * (d / 8) <= (int64_t)slots * (NT / 2); }
 
 int log2_of(int x) { int n = 0; while ((1 << n) < x) ++n; return n; }
 
 }  // namespace
+
+// Threads of a CTA that works on a page, half of them on K, half on V: `go` with the number (a constant of a type) that deals `pieces` per thread to a page
+// of `all` on each side, within 64 and MOST.  Fewer than the page's rows keep busy leave loads for a second round, more leave threads with the chain of loads to a page
+// and nothing to do: against 256 for every page, 16 prompts of 2048 tokens on 8 heads (d 128, pages of 16) are written in 39 instead of 88 us and read in
+// 38 instead of 47, 8 of 2048 on 32 heads (pages of 32) in 67 instead of 98 and 72 instead of 80, 4 of 4096 on 16 heads (d 256, pages of 128) written in 91 instead of 100.
+template <int MOST, int T = 64, class Go>
+cudaError_t threads_for(int all, int pieces, Go go) {
+  if constexpr (T < MOST)
+    if (all > T / 2 * pieces) return threads_for<MOST, 2 * T>(all, pieces, go);
+  return go(std::integral_constant<int, T>{});
+}
+
+// 16-byte pieces of codes for a thread: four, or two while CTAs of 256 threads for all pages run at once (one prompt of 2047 tokens, 16 heads of 256,
+// reduced and read back: 10.3 instead of 11.5 us).
+int pieces_of(dim3 grid) { return (int64_t)grid.x * grid.y <= 148 * 8 ? 2 : 4; }
 
 cudaError_t launch_pages_write(const PageCache& c, const PageRows& r, const int32_t* begin, const int32_t* length, const int32_t* table, cudaStream_t stream) {
   WriteParams P{};
@@ -529,23 +555,24 @@ cudaError_t launch_pages_write(const PageCache& c, const PageRows& r, const int3
   P.log_page = log2_of(c.page); P.log_vec = log2_of(c.d / 8);
   const unsigned slots = begin ? (unsigned)((r.tokens >> P.log_page) + 2 * c.S) : (unsigned)c.S;
   const dim3 grid(slots, (unsigned)c.Hkv);
-  if (few_rows(r.tokens, slots, c.d)) {
-    return r.bf16 ? launch_early(pages_write_kernel<true, FEW_NT>, grid, FEW_NT, 0, stream, P) : launch_early(pages_write_kernel<false, FEW_NT>, grid, FEW_NT, 0, stream, P);
-  }
-  return r.bf16 ? launch_early(pages_write_kernel<true, NT>, grid, NT, 0, stream, P) : launch_early(pages_write_kernel<false, NT>, grid, NT, 0, stream, P);
+  return threads_for<1024>(few_rows(r.tokens, slots, c.d) ? 0 : c.page * c.d / 8, HELD, [&](auto n) {
+    constexpr int T = decltype(n)::value;
+    return r.bf16 ? launch_early(pages_write_kernel<true, T>, grid, T, 0, stream, P) : launch_early(pages_write_kernel<false, T>, grid, T, 0, stream, P);
+  });
 }
 
 cudaError_t launch_pages_read(const PageCache& c, const PageRows& r, const int32_t* begin, const int32_t* first, const int32_t* table, cudaStream_t stream) {
   ReadParams P{};
   P.c = c; P.k = r.k; P.v = r.v; P.k_token = r.k_token; P.k_head = r.k_head; P.v_token = r.v_token; P.v_head = r.v_head;
   P.begin = begin; P.first = first; P.table = table; P.tokens = r.tokens;
-  P.log_page = log2_of(c.page); P.log_vec = log2_of(c.d / 8);
+  P.log_page = log2_of(c.page); P.log_vec = log2_of(c.d / 16);
+  P.wide = (reinterpret_cast<uintptr_t>(r.k) | reinterpret_cast<uintptr_t>(r.v)) % 32 == 0 && (r.k_token | r.k_head | r.v_token | r.v_head) % 16 == 0;
   const unsigned slots = (unsigned)((r.tokens >> P.log_page) + 2 * c.S);
   const dim3 grid(slots, (unsigned)c.Hkv);
-  if (few_rows(r.tokens, slots, c.d)) {
-    return r.bf16 ? launch_early(pages_read_kernel<true, FEW_NT>, grid, FEW_NT, 0, stream, P) : launch_early(pages_read_kernel<false, FEW_NT>, grid, FEW_NT, 0, stream, P);
-  }
-  return r.bf16 ? launch_early(pages_read_kernel<true, NT>, grid, NT, 0, stream, P) : launch_early(pages_read_kernel<false, NT>, grid, NT, 0, stream, P);
+  return threads_for<256>(few_rows(r.tokens, slots, c.d) ? 0 : c.page * c.d / 16, pieces_of(grid), [&](auto n) {
+    constexpr int T = decltype(n)::value;
+    return r.bf16 ? launch_early(pages_read_kernel<true, T>, grid, T, 0, stream, P) : launch_early(pages_read_kernel<false, T>, grid, T, 0, stream, P);
+  });
 }
 
 cudaError_t launch_pages_compact(const PageCache& c, int keep_width, int new_width, const int32_t* table, const int32_t* length, const int32_t* keep,
@@ -553,7 +580,11 @@ cudaError_t launch_pages_compact(const PageCache& c, int keep_width, int new_wid
   CompactParams P{};
   P.c = c; P.table = table; P.length = length; P.keep = keep; P.n_keep = n_keep; P.new_table = new_table;
   P.keep_width = keep_width; P.new_width = new_width; P.log_page = log2_of(c.page); P.log_vec = log2_of(c.d / 16);
-  return launch_early(pages_compact_kernel, dim3((unsigned)c.S * (unsigned)new_width, (unsigned)c.Hkv), NT, 0, stream, P);
+  const dim3 grid((unsigned)c.S * (unsigned)new_width, (unsigned)c.Hkv);
+  return threads_for<256>(c.page * c.d / 16, pieces_of(grid), [&](auto n) {
+    constexpr int T = decltype(n)::value;
+    return launch_early(pages_compact_kernel<T>, grid, T, 0, stream, P);
+  });
 }
 
 cudaError_t launch_pages_update(const PagesUpdate& u, cudaStream_t stream) {

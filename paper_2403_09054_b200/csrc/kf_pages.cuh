@@ -97,6 +97,11 @@ __device__ __forceinline__ void after_earlier_kernels() { asm volatile("griddepc
 // The next kernel may be launched (and wait) from here on.
 __device__ __forceinline__ void let_next_kernel_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+__device__ __forceinline__ void store_sector(void* at, const uint32_t* w) {   // 32 bytes, aligned to as many
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+               "r"(w[6]), "r"(w[7]) : "memory");
+}
+
 // The sequence that slot `slot` of a grid belongs to.  A grid that must cover ragged ranges without knowing their lengths on the
 // host gives sequence s the slots from start(s) = (begin[s] >> shift) + extra * s on: as floor(a + b) - floor(a) >= floor(b), every
 // sequence gets ceil(length / 2^shift) + extra - 1 of them at least.  All lanes of a warp call this and get the same answer, found 32 ways at a time;

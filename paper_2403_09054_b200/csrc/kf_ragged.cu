@@ -88,11 +88,6 @@ __device__ __forceinline__ void quad_exchange(uint32_t* w) {
   }
 }
 
-__device__ __forceinline__ void store_sector(void* at, const uint32_t* w) {   // 32 bytes, aligned to as many
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
-               "r"(w[6]), "r"(w[7]) : "memory");
-}
-
 // What a CTA works on: one pair of blocks (head_dim 256: one block) of one sequence and group of heads.
 struct Item {
   int valid;                 // 0: there is nothing more
