@@ -84,6 +84,37 @@ def test_rows_written_bit_by_bit(page, d, dtype):
         assert (got[:2] == 5.0).all() and (got[begin[-1]:] == 5.0).all()
 
 
+@pytest.mark.parametrize("page,d", [(16, 64), (16, 128), (16, 256), (32, 128), (64, 64), (128, 128), (128, 256)])
+@pytest.mark.parametrize("shift", [0, 8])
+def test_many_pages_there_and_back_at_any_alignment(page, d, shift):
+    """As many pages as fill the machine several times, in one call; rows that begin on 32 bytes or only on 16."""
+    Hkv, lengths = 16, [2 * page * i + (i * 7) % page for i in range(1, 22)]
+    T, pages = sum(lengths), sum(-(-n // page) for n in lengths)
+    cache, scale = _pool(pages, Hkv, page, d)
+    table = _ints(_table(lengths, page, pages))
+    begin = _ints(np.cumsum([0] + lengths).tolist())
+    x = torch.randn(2, T, Hkv, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(page + d)).half()
+
+    def rows():
+        return torch.full((2, T, Hkv, d + 16), 5.0, device=DEV, dtype=torch.float16)
+    src, dst = rows(), rows()
+    src[..., shift:shift + d] = x
+    _kf().kf_pages_write(k=src[0, ..., shift:shift + d], v=src[1, ..., shift:shift + d], begin=begin, length=torch.zeros_like(begin[1:]), table=table, cache=cache, scale=scale)
+    _kf().kf_pages_read(k=dst[0, ..., shift:shift + d], v=dst[1, ..., shift:shift + d], begin=begin, table=table, cache=cache, scale=scale)
+    for s in range(0, len(lengths), 5):
+        n, b = lengths[s], int(begin[s])
+        for side in range(2):
+            ids = table[s, :-(-n // page)].long()
+            held = (cache[ids, :, side].double() * scale[ids, :, side].double()[..., None, None]).transpose(1, 2).flatten(0, 1)[:n]
+            assert torch.equal(dst[side, b:b + n, :, shift:shift + d], held.half())
+            per = torch.nn.functional.pad(x[side, b:b + n].double().abs().amax(-1).t(), (0, len(ids) * page - n)).view(Hkv, len(ids), page).amax(-1)
+            step = torch.where(per > 0, scale[ids, :, side].double().t(), torch.zeros_like(per))
+            assert (per <= 127 * step).all() and (per > 63.5 * step).all()                        # the smallest power of two that holds the page's rows
+            off = (held - x[side, b:b + n].double()).abs().amax(-1).t()
+            assert (torch.nn.functional.pad(off, (0, len(ids) * page - n)).view(Hkv, len(ids), page).amax(-1) <= step / 2).all()
+    assert (dst[..., :shift] == 5.0).all() and (dst[..., shift + d:] == 5.0).all()
+
+
 def test_one_row_per_sequence():
     page, d, Hkv, S = 16, 128, 8, 50
     cache, scale = _pool(200, Hkv, page, d)
