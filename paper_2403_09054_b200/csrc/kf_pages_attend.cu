@@ -16,13 +16,14 @@
 // result per warp, which pages_merge_kernel joins.  (Chunks of one sequence per CTA instead: 271 against 210 us for 32 x 32 caches of 4096 tokens, whose SMs
 // idled for 40 %.)
 //
-// What bounds it: 32 x 32 caches of 4096 tokens (1.07 GB) take 188 to 196 us with ALiBi, 194 without, 5.5 TB/s of 6.57; the same loads without any arithmetic take 169.  Half
-// of the issue slots are used (815 warp instructions per 32 tokens of d 128, 416 of them conversions), the registers allow 12 warps, and of the 5.6 cycles between
-// two instructions of a warp 1.9 are the fixed latency of the one before, 0.7 a busy pipe and 0.5 memory.  48 sequences of up to 8192 tokens on 8 caches: 82 to 88 us, 75
-// without arithmetic, 61 at the copy rate.  Not taken, for 32 x 32 caches: 8 warps of 246 registers (195 to 209 us), 16 of 128 and tiles of 16 tokens (290), the table's
-// entries ahead of time by asynchronous copies (198), larger shares for the CTAs that an SM takes first (194 to 199), a record per unit instead of per share for the second
-// kernel (193), packed binary32 arithmetic in the softmax (as many instructions, the pairs have to be moved together), sums that are corrected for the codes'
-// offset at the end (they would lose the last eleven bits).
+// What bounds it: 32 x 32 caches of 4096 tokens (1.07 GB) take 195 us, 5.5 TB/s of 6.57; the same loads without any arithmetic take 169.  Half of the issue slots
+// are used (815 warp instructions per 32 tokens of d 128, 416 of them conversions), and the registers allow eight warps, whose products of several groups of tokens the compiler
+// may then mix; twelve of 168 registers, one group of tokens after the other, take as long for many caches and more where a share is short (one sequence of 131072
+// tokens on 8 caches 67 instead of 62 us, 256 of 512 69 instead of 64, units of 74 sequences of 500 24 instead of 18), but for d 64 less (126 instead of 138).  48
+// sequences of up to 8192 tokens on 8 caches: 83 to 88 us, 75 without arithmetic, 61 at the copy rate.  Not taken, for 32 x 32 caches: 16 warps of 128 registers and tiles of 16
+// tokens (290), the table's entries ahead of time by asynchronous copies (198), larger shares for the CTAs that an SM takes first (194 to 199), a record per unit
+// instead of per share for the second kernel (193), packed binary32 arithmetic in the softmax (as many instructions, the pairs have to be moved together), sums that are
+// corrected for the codes' offset at the end (they would lose the last eleven bits).
 #include "kf_pages.cuh"
 #include "kf_tc.cuh"
 
@@ -44,9 +45,9 @@ template <int D>
 struct Shape {
   static constexpr int TILE = D == 256 ? 16 : 32;           // tokens
   static constexpr int BYTES = 2 * TILE * D;                // K and V
-  static constexpr int STAGES = D == 256 ? 3 : 16384 / BYTES;   // per warp
+  static constexpr int STAGES = D == 64 ? 16384 / BYTES : 3;   // per warp
   static constexpr int HEAD = 8 * (D / 8 + 4) + 4;          // floats between two heads' sums in shared memory: spread over the banks
-  static constexpr int RESIDENT = D == 256 ? 2 : 3;         // CTAs of an SM, by registers (255 or 168 a thread); all of them are the wave
+  static constexpr int RESIDENT = D == 64 ? 3 : 2;          // CTAs of an SM, by registers (168 or 255 a thread); all of them are the wave
 };
 
 // What a warp knows of a tile before it comes to it.
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
         const float kf = g >= 2 ? k1 : k0;
         x[g][0] = sum[0] * kf;
         x[g][1] = sum[1] * kf;
-        asm volatile("" ::: "memory");                // the next group's loads stay behind: registers
+        if (D == 64) asm volatile("" ::: "memory");   // the next group's loads stay behind: registers
       }
       // head r8, tokens 8 g + 2 t4 and + 1
       if (a.slopes) {
@@ -431,7 +432,7 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
           for (int j = 0; j < 4; ++j)
             mma(o[4 * i + j], hi[2 * k], lo[2 * k], hi[2 * k + 1], lo[2 * k + 1], code_pair(__byte_perm(vw[0][i], vw[1][i], j | (4 + j) << 8)),
                 code_pair(__byte_perm(vw[2][i], vw[3][i], j | (4 + j) << 8)));
-        asm volatile("" ::: "memory");
+        if (D == 64) asm volatile("" ::: "memory");
       }
       __syncwarp();                                   // the slot has been read by every lane
       if (w + ST < mine) {
@@ -615,14 +616,14 @@ int64_t most_tiles(int S, int W, int page, int Hkv, int group, int d) {
 // CTAs of a launch: a wave, or fewer where all tables together could not keep it busy.
 int ctas_of(int S, int W, int page, int Hkv, int group, int d) {
   const int64_t ctas = (most_tiles(S, W, page, Hkv, group, d) + NW * LEAST - 1) / (NW * LEAST);
-  const int wave = SMS * (d == 256 ? Shape<256>::RESIDENT : Shape<128>::RESIDENT);
+  const int wave = SMS * (d == 64 ? Shape<64>::RESIDENT : Shape<128>::RESIDENT);
   return (int)(ctas < wave ? ctas : wave);
 }
 
 // Whether a CTA takes a unit: few units, none of which can have more than a few tiles.  The second kernel, which joins shares, then costs more than
-// their even distribution saves: 8 caches of 64 / 256 / 512 tokens (d 128, four heads each) 4.2 / 5.7 / 8.4 us against 7.6 / 9.8 / 9.9, 512 caches of 256 tokens 15 against
-// 18; but 8 of 1024 tokens 13 against 9.9, and 2048 of 256 tokens 46 against 41.
-constexpr int FEW_TILES = 16, FEW_UNITS = 4 * SMS;
+// their even distribution saves: 8 caches of 64 / 256 / 512 / 768 tokens (d 128, four heads each) 3.7 / 4.9 / 6.9 / 8.9 us against 7.2 / 9.1 / 9.2 / 9.3, 592 caches
+// of 256 / 768 tokens 12 / 29 against 16 / 31; but 8 of 1024 tokens 10.9 against 9.3, and 2048 of 64 / 256 tokens 26 / 43 against 14 / 38.
+constexpr int FEW_TILES = 24, FEW_UNITS = 4 * SMS;
 bool by_unit(const PageCache& c, int units) {
   const int tile = c.d == 256 ? 16 : 32;
   return ((int64_t)c.W * c.page + tile - 1) / tile <= FEW_TILES && (int64_t)c.S * units <= FEW_UNITS;
