@@ -461,6 +461,8 @@ typedef struct kf_ragged_args {
   int64_t v_token_stride, v_head_stride;      /* and v, or head-major rows.  The features of a head are contiguous */
   int64_t out_token_stride, out_head_stride;  /* rows of two (token, head) pairs may not share memory             */
   int32_t debug_fail_first_wait;      /* self-test of the error path, see kf_config                                */
+  int32_t debug_fail_after;           /* with it: n >= 0: n pieces of work of every CTA go right before a wait fails; -1 - n: n, then the wait */
+                                      /* for the next piece fails                                                 */
 } kf_ragged_args;
 /*   d_q, d_out : DEVICE [tokens][H] rows of d;  d_k, d_v : DEVICE [tokens][Hkv] rows of d (strides above, 16-byte aligned)
  *   d_begin    : DEVICE int32 [S + 1]

@@ -97,7 +97,7 @@ class kf_ragged_args(C.Structure):
         ("head_dim", C.c_int32), ("type", C.c_int32), ("bias_mode", C.c_int32), ("logit_scale", C.c_float), ("d_alibi_slopes", C.c_void_p),
         ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64),
         ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64),
-        ("debug_fail_first_wait", C.c_int32),
+        ("debug_fail_first_wait", C.c_int32), ("debug_fail_after", C.c_int32),
     ]
 
 
@@ -364,11 +364,13 @@ def kf_reorder_rows(*, buffers, parent, n_layers=1, stream=None):
     _check(_kf_torch.reorder_rows(buffers, parent, n_layers, stream), "kf_reorder_rows")
 
 
-def kf_prefill_attend_ragged(*, q, k, v, begin, out, bias_mode=KF_BIAS_NONE, alibi_slopes_dev=None, logit_scale=0.0, debug_fail_first_wait=0, stream=None):
+def kf_prefill_attend_ragged(*, q, k, v, begin, out, bias_mode=KF_BIAS_NONE, alibi_slopes_dev=None, logit_scale=0.0, debug_fail_first_wait=0, debug_fail_after=0,
+                             stream=None):
     """Causal attention over prompts that lie one after the other: sequence s has rows begin[s] .. begin[s + 1] - 1 (int32 [S + 1]) of q, out
     [T, H, d] and k, v [T, Hkv, d] (fp16 or bf16, contiguous features, any strides of tokens and heads: views of a projection's rows, or
     ``x[0].transpose(0, 1)`` of kf_qk_norm_rotate's head-major rows)."""
-    _check(_kf_torch.attend_ragged(q, k, v, begin, out, bias_mode, alibi_slopes_dev, logit_scale, debug_fail_first_wait, stream), "kf_prefill_attend_ragged")
+    _check(_kf_torch.attend_ragged(q, k, v, begin, out, bias_mode, alibi_slopes_dev, logit_scale, debug_fail_first_wait, debug_fail_after, stream),
+           "kf_prefill_attend_ragged")
 
 
 def kf_pages_write(*, k, v, length, table, cache, scale, begin=None, stream=None):

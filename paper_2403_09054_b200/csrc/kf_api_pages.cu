@@ -127,7 +127,9 @@ int kf_prefill_attend_ragged(const kf_ragged_args* a, const void* d_q, const voi
   r.out_token = a->out_token_stride; r.out_head = a->out_head_stride;
   r.tokens = a->tokens; r.sequences = a->sequences; r.H = a->n_heads; r.Hkv = a->n_kv_heads; r.head_dim = d;
   r.bf16 = a->type == KF_TYPE_BF16;
-  r.fail_first_wait = a->debug_fail_first_wait != 0;
+  const bool fails = a->debug_fail_first_wait != 0;
+  r.fail_item = fails && a->debug_fail_after >= 0 ? a->debug_fail_after : -1;
+  r.leave_item = fails && a->debug_fail_after < 0 ? -1 - a->debug_fail_after : -1;
   r.scale = a->logit_scale > 0.f ? a->logit_scale : (float)(1.0 / std::sqrt((double)d));
   return status(kf::launch_ragged(r, static_cast<cudaStream_t>(stream)));
 }

@@ -21,7 +21,8 @@ struct RaggedArgs {
   const float* slopes;         // [H] or null
   int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;   // strides in elements
   int32_t tokens, sequences, H, Hkv, head_dim;
-  bool bf16, fail_first_wait;
+  int32_t fail_item, leave_item;   // the self-test's (-1: none): the items of a CTA from which on waits for logits fail, or at which the wait for it fails
+  bool bf16;
   float scale;
 };
 cudaError_t launch_ragged(const RaggedArgs& a, cudaStream_t stream);

@@ -58,7 +58,7 @@ struct RaggedParams {
   int32_t slots, groups;       // of the grid: places per group of heads, groups
   float a_scale;               // logit scale * log2(e)
   bool wide;                   // output rows are aligned to 32 bytes
-  bool fail_first_wait;
+  int32_t fail_item, leave_item;   // the self-test's: items of a CTA, -1: none
 };
 
 template <bool BF16>
@@ -153,6 +153,8 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* issued = abort_flag + 1;   // loads that have been issued: of the ring, and of queries
+  volatile int* left = issued + 2;         // a role has given up waiting for an item
+  volatile int* looked = left + 1;         // the scheduler's claims when it last met a place that holds nothing
 
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int tb = 128 >> P.log_pack;                // tokens of a block
@@ -174,6 +176,8 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
     mbar_init(drain, 1);
     *abort_flag = 0;
     issued[0] = issued[1] = 0;
+    *left = *looked = 0;
+    items[0].T = items[1].T = 0;
     mbar_fence_init();
   }
   if (warp == 1) {
@@ -186,16 +190,27 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
   const uint32_t tmem_base = *tmem_slot;
   after_earlier_kernels();
 
-  // Every role takes the items in order; number k lies in items[k & 1].  A wait for an item, or for all roles to be done with one, lasts as long as an
-  // item may: its limit grows with the tiles.  These waits do not end when a role has given up: all roles then pass over what is left, up to the item
-  // that says there is no more, so that nothing claimed goes without its output.
-  auto wait_item = [&](uint64_t* bar, int k, int tiles) {
-    for (int i = 0; i <= tiles; ++i)
-      if (mbar_wait_bounded(bar + (k & 1), (uint32_t)(k >> 1 & 1))) return true;
+  // Every role takes the items in order; number k lies in items[k & 1].  A wait for an item, or for all roles to be done with one, lasts as long as the
+  // two items before may (64 times 2^16 polls for every key tile), and begins anew while the scheduler meets places that hold nothing, of which there may be any
+  // number.  It does not end when a role has given up a wait within an item: all roles then pass over what is left, up to the item that says there is no more, so
+  // that nothing claimed goes without its output.  A role that gives up the wait for an item leaves, and so do all others then; rows that not all of them
+  // took become NaN at the end.
+  auto wait_item = [&](uint64_t* bar, int k) {
+    for (int tries = 0, seen = -1;;) {
+      if (__builtin_expect(mbar_wait_bounded(bar + (k & 1), (uint32_t)(k >> 1 & 1), 1u << 16), 1)) return true;
+      const int now = *looked;
+      tries = now == seen ? tries + 1 : 0;
+      seen = now;
+      const volatile Item* two = items;
+      if (*left || tries > 64 * (1 + two[0].T + two[1].T)) return false;
+    }
+  };
+  auto leave = [&]() {
+    if (lane == 0) *left = *abort_flag = 1;
     return false;
   };
-  auto take = [&](int k, Item& item, int tiles) {
-    if (!__all_sync(0xffffffffu, wait_item(item_full, k, tiles))) return false;
+  auto take = [&](int k, Item& item) {
+    if (__builtin_expect(!__all_sync(0xffffffffu, wait_item(item_full, k)), 0)) return leave();
     item = items[k & 1];
     return item.valid != 0;
   };
@@ -204,16 +219,22 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
     if (lane == 0) mbar_arrive(item_empty + (k & 1));
   };
 
+  int handed = 0;                                      // the scheduler's: items
   // The ring's order within an item, as the MMA warp needs the tiles: K of step 0; then K of step u + 1 and V of step u in turn; V of the last step.
   if (warp < 4) {
     if (NB == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(FEW_REGS));
     if (warp == 3) {
       // ---------------------------------------------------------- scheduler: this CTA's own place in the grid, then places that it claims
-      int place = blockIdx.x, claims = 0, tiles = 0, tiles_before = 0;
+      int place = blockIdx.x, claims = 0;
       bool own = true, more = true;
+      constexpr int ROW_SHIFT = NB == 2 ? 8 : 7;           // rows of a place
+      int64_t used = P.slots;                              // slots up to the end of the last sequence: the rows of a buffer need not all be somebody's
       for (int k = 0; more; ++k) {
         // the slot of item k - 2 first: nothing is claimed long before it can be worked on
-        if (k >= 2 && !__all_sync(0xffffffffu, wait_item(item_empty, k - 2, tiles + tiles_before))) break;
+        if (k >= 2 && !__all_sync(0xffffffffu, wait_item(item_empty, k - 2))) {
+          (void)leave();
+          break;
+        }
         Item item{};
         for (;;) {
           if (!own) {
@@ -224,11 +245,14 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
               mbar_expect_tx(claimed, 16);
               claim_issue(claim, claimed);
             }
-            if (!__all_sync(0xffffffffu, mbar_wait_bounded(claimed, (uint32_t)(claims & 1)))) {
-              if (lane == 0) *abort_flag = 1;
-              more = false;
-              break;
+            if (claims == 0) {
+              const int last = P.begin[P.S];
+              if (last >= 0 && last <= P.tokens) used = slot_start(&last, 0, P.pack, ROW_SHIFT, 0) + P.S;
             }
+            // as long as two bounded waits: a place that came after that would be nobody's
+            more = __all_sync(0xffffffffu, mbar_wait_bounded(claimed, (uint32_t)(claims & 1), 1u << 23)) != 0;
+            if (!more && lane == 0) *abort_flag = 1;
+            if (!more) break;
             ++claims;
             more = claim_read(claim, place);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the answer has been read before the next one may come
@@ -236,16 +260,22 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
             if (!more) break;
           }
           own = false;
-          // the place as a pair of blocks of a sequence; some places hold nothing
-          constexpr int ROW_SHIFT = NB == 2 ? 8 : 7;       // rows of a place
+          // The place as a pair of blocks of a sequence; some places hold nothing.
           // All groups of heads of a slot, then the next slot; the slots of a sequence from its end on, so that the longest come first.  (One group
           // after the other, which keeps fewer keys and values in use at a time, ends with a few long places: 416 instead of 373 us for six
           // prompts of up to 4096 tokens and 32 heads, and no gain for 32768 tokens: 8.0 against 7.7 ms.)
           const int slot = P.slots - 1 - place / P.groups, heads = place % P.groups;
+          if (slot >= used) {                              // no search: 430 tokens in a buffer of 131072 take 63 instead of 80 us
+            if (lane == 0) *looked = claims;
+            continue;
+          }
           const int seq = slot_sequence(P.begin, P.S, slot, P.pack, ROW_SHIFT, 1);
           const int row0 = P.begin[seq], row_end = P.begin[seq + 1];
           const int64_t local = (slot - slot_start(P.begin, seq, P.pack, ROW_SHIFT, 1)) * (NB * tb);
-          if (row0 < 0 || row_end > P.tokens || row0 >= row_end || local < 0 || local >= (int64_t)row_end - row0) continue;
+          if (row0 < 0 || row_end > P.tokens || row0 >= row_end || local < 0 || local >= (int64_t)row_end - row0) {
+            if (lane == 0) *looked = claims;
+            continue;
+          }
           item.valid = 1;
           item.row0 = row0;
           item.n = row_end - row0;
@@ -259,22 +289,20 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
           item.kv_head = item.head0 / P.group;
           break;
         }
-        tiles_before = tiles;
-        tiles = item.T;
         if (lane == 0) {
           items[k & 1] = item;
           mbar_arrive(item_full + (k & 1));
         }
+        handed = k + item.valid;
         __syncwarp();
       }
     } else if (warp == 0) {
       // ---------------------------------------------------------- TMA producer
       Item item;
-      item.T = 0;
       int slot = 0, count = 0;                                       // ring slot, and loads before
       uint32_t parity = 1;                                           // of the use of the slot before: none yet, such a wait passes at once
       bool ok = true;
-      for (int k = 0; take(k, item, item.T); ++k) {
+      for (int k = 0; take(k, item); ++k) {
         if (lane == 0 && ok) {
           if (k > 0) ok = wait_bar(q_empty, (uint32_t)((k - 1) & 1), abort_flag);
           if (ok) {
@@ -350,10 +378,9 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
         __syncwarp();
       };
       Item item;
-      item.T = 0;
       int steps0 = 0, steps1 = 0, items0 = 0, items1 = 0;            // of the blocks, over all items
       bool ok = true;
-      for (int k = 0; take(k, item, item.T); ++k) {
+      for (int k = 0; take(k, item); ++k) {
         const int T = __shfl_sync(0xffffffffu, item.T, 0), U0 = __shfl_sync(0xffffffffu, item.U0, 0);
         const bool two = NB == 2 && __shfl_sync(0xffffffffu, item.has1, 0) != 0;
         int kslot = 0, vslot = 0, next_k = 0;
@@ -420,11 +447,13 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
     const uint32_t o_addr = lane_addr + O_COL + (uint32_t)(b * D);
     const float A = P.a_scale;
     Item item;
-    item.T = 0;
     int steps = 0, done = 0;                           // of this block, over all items: steps, items
-    bool ok = !P.fail_first_wait;                      // the self-test: as if the first wait had run out
-    if (!ok && lane == 0) *abort_flag = 1;
-    for (int k = 0; take(k, item, item.T); ++k) {
+    bool ok = true;
+    for (int k = 0; k != P.leave_item ? take(k, item) : leave(); ++k) {
+      if (k == P.fail_item) {                          // the self-test: as if a wait had run out
+        ok = false;
+        if (lane == 0) *abort_flag = 1;
+      }
       if (b == 1 && !item.has1) {
         release(k);
         continue;
@@ -605,9 +634,20 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
     }
   }
 
-  // ---- teardown: on the failure path give the copies still in flight a bounded wait, then free tensor memory
+  // ---- teardown: on the failure path give the copies still in flight a bounded wait and rows that not every role took NaN, then free tensor memory
   tc_fence_before();
   __syncthreads();
+  if (__builtin_expect(warp == 3 && *abort_flag, 0))
+    for (int k = max(handed - 2, 0); k < handed; ++k) {
+      if (mbar_test(item_empty + (k & 1), (uint32_t)(k >> 1 & 1))) continue;
+      const Item item = items[k & 1];                  // of this slot the last one that was handed out: the next would have waited for it
+      const int rows = min(NB * tb, item.n - item.first), pieces = D / 8;
+      for (int e = lane; e < rows * P.pack * pieces; e += 32) {
+        const int row = e / pieces, i = item.row0 + item.first + (row >> P.log_pack), head = item.head0 + (row & (P.pack - 1));
+        *reinterpret_cast<uint4*>(static_cast<unsigned short*>(P.out) + (int64_t)i * P.out_token + (int64_t)head * P.out_head + e % pieces * 8) =
+            make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+      }
+    }
   if (tid == 0 && *abort_flag) {
     for (int j = issued[0] > RING ? issued[0] - RING : 0; j < issued[0]; ++j)
       (void)mbar_wait_bounded(r_full + (j % RING), (uint32_t)((j / RING) & 1), TC_WAIT_LIMIT);
@@ -658,7 +698,8 @@ cudaError_t launch_ragged(const RaggedArgs& a, cudaStream_t stream) {
   P.wide = reinterpret_cast<uintptr_t>(a.out) % 32 == 0 && a.out_token % 16 == 0 && a.out_head % 16 == 0;
   P.tokens = a.tokens; P.S = a.sequences; P.group = group;
   P.a_scale = a.scale * LOG2E;
-  P.fail_first_wait = a.fail_first_wait;
+  P.fail_item = a.fail_item;
+  P.leave_item = a.leave_item;
   const int64_t slots = (((int64_t)a.tokens * P.pack) >> (D == 256 ? 7 : 8)) + a.sequences;
   P.groups = a.H / P.pack;
   if (slots * P.groups > INT32_MAX) return cudaErrorInvalidValue;

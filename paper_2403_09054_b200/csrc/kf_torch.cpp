@@ -334,9 +334,9 @@ int32_t* ints(PyObject* o, const char* name, int64_t numel, const at::Device& de
   return static_cast<int32_t*>(address(o, name, at::kInt, numel, device, optional));
 }
 
-// ---- kf_prefill_attend_ragged: (q, k, v, begin, out, bias_mode, slopes, logit_scale, debug_fail_first_wait, stream)
+// ---- kf_prefill_attend_ragged: (q, k, v, begin, out, bias_mode, slopes, logit_scale, debug_fail_first_wait, debug_fail_after, stream)
 PyObject* attend_ragged(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  return guarded(args, n, 10, [](PyObject* const* a) -> int {
+  return guarded(args, n, 11, [](PyObject* const* a) -> int {
     const at::Tensor& x = first_tensor(a[0], "q");
     const at::Device device = x.device();
     const auto type = x.scalar_type();
@@ -358,8 +358,9 @@ PyObject* attend_ragged(PyObject*, PyObject* const* args, Py_ssize_t n) {
     p.v_token_stride = v.row_stride; p.v_head_stride = v.head_stride;
     p.out_token_stride = out.row_stride; p.out_head_stride = out.head_stride;
     p.debug_fail_first_wait = integer32(a[8]);
+    p.debug_fail_after = integer32(a[9]);
     const int32_t* b = ints(a[3], "begin", begin.numel(), device);
-    const Where at_(device, a[9]);
+    const Where at_(device, a[10]);
     return kf_prefill_attend_ragged(&p, q.p, k.p, v.p, b, out.p, at_.stream.stream());
   });
 }
