@@ -180,6 +180,8 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
     items[0].T = items[1].T = 0;
     mbar_fence_init();
   }
+  // Tensor memory only behind the kernel before: one that lets this one launch early may still have to take its own, and this one waits for its end.
+  after_earlier_kernels();
   if (warp == 1) {
     tmem_alloc(tmem_slot, TMEM_COLS);
     tmem_relinquish();
@@ -188,7 +190,6 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  after_earlier_kernels();
 
   // Every role takes the items in order; number k lies in items[k & 1].  A wait for an item, or for all roles to be done with one, lasts as long as the
   // two items before may (64 times 2^16 polls for every key tile), and begins anew while the scheduler meets places that hold nothing, of which there may be any
