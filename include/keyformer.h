@@ -508,6 +508,7 @@ int kf_pages_read(const kf_page_cache* cache, const kf_page_rows* rows, const vo
 
 /* One query token per sequence, the newest, over the d_length[s] tokens of its pages (its own row among them):
  *   out = sum_j softmax_j(x_j) v_j,   x_j = logit_scale q k_j (- slope_h (length - 1 - j) with KF_BIAS_ALIBI)
+ * Logits may be of any size that binary32 holds in units of log 2 (a row of which all are -infinity, or one is NaN or +infinity, is NaN).
  * A sequence without tokens gets zeros; one whose length is negative or behind its table, or that needs a missing page, gets NaN. */
 typedef struct kf_pages_attend_args {
   kf_page_cache cache;                /* S * table_width * page_tokens * H < 2^35 is always accepted              */

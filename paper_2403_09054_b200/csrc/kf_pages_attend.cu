@@ -38,7 +38,8 @@ constexpr int LEAST = 2;                    // tiles of a share
 constexpr int ENTRIES = 256;                // of a CTA's table of where sequences begin (one per sequence up to 256 of them)
 constexpr int BATCH = 16;                   // tiles a warp looks up at a time
 constexpr int MERGE_WARPS = 8;
-constexpr float FIRST_REF = -1e30f;         // below every logit, but finite
+constexpr float FIRST_REF = -3.402823466e38f;   // no finite logit lies below
+constexpr float LEAST_REF = -1e30f;         // of a reference that counts from another one: 2^this is nothing, and sums with it stay finite
 constexpr float ROOM = 7.0f, GAP = 8.0f;    // weights are taken times 2^7 (binary16 holds 2^-32 to 2^8 of the reference); a reference moves by 2^8
 
 template <int D>
@@ -304,7 +305,9 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
     }
     const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.f;
 
-    float m_x = FIRST_REF, m_o = FIRST_REF, l = 0.f;  // of head r8, references common to its four lanes; l: this lane's tokens
+    // Of head r8: the reference of the logits, and of weights times V scales as it counts from that (so that it is a small number wherever the
+    // logits lie, and loses nothing beside them), both common to its four lanes; l: this lane's tokens.
+    float m_x = FIRST_REF, m_o = 0.f, l = 0.f;
     float o[D / 8][4];
 #pragma unroll
     for (int i = 0; i < D / 8; ++i)
@@ -376,16 +379,20 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
         if (g >= 2) tx1 = max3(tx1, x[g][0], x[g][1]);
         else tx0 = max3(tx0, x[g][0], x[g][1]);
       }
-      const float tx = fmaxf(tx0, tx1), to = fmaxf(tx0 + v0, tx1 + v1);
+      const float tx = fmaxf(tx0, tx1), to = fmaxf(tx0 - m_x + v0, tx1 - m_x + v1);
       if (__any_sync(0xffffffffu, tx > m_x + GAP || to > m_o + GAP)) {
-        float nx = tx, no = to;
+        float nx = tx;
         nx = fmaxf(nx, __shfl_xor_sync(0xffffffffu, nx, 1));
-        no = fmaxf(no, __shfl_xor_sync(0xffffffffu, no, 1));
         nx = fmaxf(nx, __shfl_xor_sync(0xffffffffu, nx, 2));
+        nx = fmaxf(nx, m_x);
+        const float grown = nx - m_x, before = fmaxf(m_o - grown, LEAST_REF);     // grown may be infinite the first time
+        m_x = nx;
+        float no = fmaxf(tx0 - m_x + v0, tx1 - m_x + v1);
+        no = fmaxf(no, __shfl_xor_sync(0xffffffffu, no, 1));
         no = fmaxf(no, __shfl_xor_sync(0xffffffffu, no, 2));
-        if (nx > m_x) { l *= fast_exp2(m_x - nx); m_x = nx; }
-        const float f = no > m_o ? fast_exp2(m_o - no) : 1.f;
-        if (no > m_o) m_o = no;
+        m_o = fmaxf(no, before);
+        l *= fast_exp2(-grown);
+        const float f = fast_exp2(before - m_o);
 #pragma unroll
         for (int i = 0; i < D / 8; ++i)
 #pragma unroll
@@ -394,9 +401,9 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
       uint32_t hi[GROUPS], lo[GROUPS];
 #pragma unroll
       for (int g = 0; g < GROUPS; ++g) {
-        l += fast_exp2(x[g][0] - m_x) + fast_exp2(x[g][1] - m_x);
-        const float up = (g >= 2 ? v1 : v0) - m_o + ROOM;
-        float p0 = fast_exp2(x[g][0] + up), p1 = fast_exp2(x[g][1] + up);
+        const float x0 = x[g][0] - m_x, x1 = x[g][1] - m_x, up = (g >= 2 ? v1 : v0) - m_o + ROOM;
+        l += fast_exp2(x0) + fast_exp2(x1);
+        float p0 = fast_exp2(x0 + up), p1 = fast_exp2(x1 + up);
         if (rows < TILE) {                            // a masked token counts as nothing, whatever its page's scale is
           p0 = 8 * g + 2 * t4 < rows ? p0 : 0.f;
           p1 = 8 * g + 2 * t4 + 1 < rows ? p1 : 0.f;
@@ -441,11 +448,11 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
       }
     }
 
-    // ---- what the warp has of the unit.  Weights were taken against m_o and times 2^7, their sum against m_x; the lane has two runs of D/8 features.
+    // ---- what the warp has of the unit.  Weights were taken against both references and times 2^7, their sum against m_x; the lane has two runs of D/8 features.
     l += __shfl_xor_sync(0xffffffffu, l, 1);
     l += __shfl_xor_sync(0xffffffffu, l, 2);
     if (failed) l = nan_f32();
-    const float bring = fast_exp2(m_o - m_x - ROOM) * (whole ? 1.f / l : 1.f);
+    const float bring = fast_exp2(m_o - ROOM) * (whole ? 1.f / l : 1.f);
     if (whole) {
       unsigned short* out = static_cast<unsigned short*>(a.out) + (int64_t)s * a.out_sequence + (int64_t)head * a.out_head + 2 * t4 * (D / 8);
       if (r8 < heads) {

@@ -1,0 +1,36 @@
+"""The operators on 8-bit pages where logits, scales and ranges lie at the ends of what they may be."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import pages_reference as ref
+from tests.test_gpu_pages import DEV, TYPES, _attend, _check, _ints, _kf, _pool, _table
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("size", [1e4, 1e8, 1e20, 1e32, 1e38])
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("d,page,wide", [(64, 16, 0), (64, 64, 60), (128, 16, 60), (128, 32, 0), (256, 64, 60)])
+def test_rows_whose_logits_are_all_huge(size, sign, d, page, wide):
+    """All logits of a row are equal, finite and far from zero: their softmax is the mean.  Only feature 0 of keys and queries counts, so that a logit is one
+    product, and equal in every tile whatever the binary32 roundings are."""
+    n, Hkv = 200, 2
+    pages = -(-n // page)
+    cache, scale = _pool(pages, Hkv, page, d, seed=1)
+    cache[:, :, 0], cache[:, :, 0, :, 0] = 0, 64
+    scale[:, :, 0] = 2.0 ** -6                                       # keys: 1 in feature 0
+    table = _table([n], page, pages, width=pages + wide)
+    q = torch.zeros(1, 4, d, device=DEV, dtype=torch.bfloat16)
+    q[..., 0] = sign * size
+    out = _attend(q, table, [n], cache, scale, logit=1.0)
+    v = torch.from_numpy(ref.held(cache.cpu().numpy(), scale.cpu().numpy(), table, 0, n)[1]).to(DEV).repeat_interleave(2, 1)
+    want, weighted = v.mean(0), v.abs().mean(0)
+    # all weights are equal: the output's rounding, and the binary32 arithmetic (2^-18)
+    assert ((out[0].double() - want).abs() <= want.abs() * 2.0 ** -8 + weighted * 2.0 ** -18).all()
+    # one key stands above the others by a fifth of the logits' size, far more than a softmax can tell from all
+    cache[table[0, 3 // page], :, 0, 3 % page, 0] += sign * 13
+    out = _attend(q, table, [n], cache, scale, logit=1.0)
+    assert torch.equal(out[0], v[3].bfloat16())
