@@ -452,7 +452,8 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
     l += __shfl_xor_sync(0xffffffffu, l, 1);
     l += __shfl_xor_sync(0xffffffffu, l, 2);
     if (failed) l = nan_f32();
-    const float bring = fast_exp2(m_o - ROOM) * (whole ? 1.f / l : 1.f);
+    // 2^m_o in two factors, the first a power of two: V scales may be as small as 2^-120 and references 2^-128, which the fast exponential takes for zero.
+    const float low = floorf(0.5f * m_o), half = fast_exp2(low), bring = fast_exp2(m_o - low - ROOM) * (whole ? 1.f / l : 1.f);
     if (whole) {
       unsigned short* out = static_cast<unsigned short*>(a.out) + (int64_t)s * a.out_sequence + (int64_t)head * a.out_head + 2 * t4 * (D / 8);
       if (r8 < heads) {
@@ -463,7 +464,8 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
             uint32_t r[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float u0 = (o[i + 2 * e][run] + o[i + 2 * e][run + 2]) * bring, u1 = (o[i + 2 * e + 1][run] + o[i + 2 * e + 1][run + 2]) * bring;
+              const float u0 = (o[i + 2 * e][run] + o[i + 2 * e][run + 2]) * half * bring,
+                          u1 = (o[i + 2 * e + 1][run] + o[i + 2 * e + 1][run + 2]) * half * bring;
               if (a.bf16) {
                 const __nv_bfloat162 b = __floats2bfloat162_rn(u0, u1);
                 r[e] = *reinterpret_cast<const uint32_t*>(&b);
@@ -493,8 +495,8 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
 #pragma unroll
         for (int i = 0; i < D / 8; i += 4)
           *reinterpret_cast<float4*>(at + run * run_step + i) =
-              make_float4((o[i][run] + o[i][run + 2]) * bring, (o[i + 1][run] + o[i + 1][run + 2]) * bring, (o[i + 2][run] + o[i + 2][run + 2]) * bring,
-                          (o[i + 3][run] + o[i + 3][run + 2]) * bring);
+              make_float4((o[i][run] + o[i][run + 2]) * half * bring, (o[i + 1][run] + o[i + 1][run + 2]) * half * bring,
+                          (o[i + 2][run] + o[i + 2][run + 2]) * half * bring, (o[i + 3][run] + o[i + 3][run + 2]) * half * bring);
       if (t4 == 0) {
         if (joined) sh_ml[warp][r8] = make_float2(m_x, l);
         else *reinterpret_cast<float2*>(part + D) = make_float2(m_x, l);

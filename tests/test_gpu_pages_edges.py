@@ -34,3 +34,17 @@ def test_rows_whose_logits_are_all_huge(size, sign, d, page, wide):
     cache[table[0, 3 // page], :, 0, 3 % page, 0] += sign * 13
     out = _attend(q, table, [n], cache, scale, logit=1.0)
     assert torch.equal(out[0], v[3].bfloat16())
+
+
+@pytest.mark.parametrize("wide", [0, 60])
+def test_values_near_the_smallest_scale(wide):
+    """V scales of 2^-120: their outputs are far below one, but bfloat16 holds them."""
+    d, page, n = 128, 32, 300
+    pages = -(-n // page)
+    cache, scale = _pool(pages, 2, page, d)
+    table = _table([n], page, pages, width=pages + wide)
+    q = torch.randn(1, 4, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(0)).bfloat16()
+    scale[:, :, 1] = 2.0 ** -120
+    out = _attend(q, table, [n], cache, scale)
+    assert (out != 0).any()
+    _check(out, q, table, [n], cache, scale)
