@@ -519,6 +519,7 @@ typedef struct kf_pages_attend_args {
   int64_t q_sequence_stride, q_head_stride;       /* in elements, multiples of 8, at least d                       */
   int64_t out_sequence_stride, out_head_stride;   /* rows of two (sequence, head) pairs may not share memory       */
   int32_t debug_fail_first_wait;      /* self-test of the error path, see kf_config                                */
+  int32_t debug_fail_after;           /* with it, >= 0: every warp's waits fail once it has looked up 16 times as many tiles */
 } kf_pages_attend_args;
 /*   d_q, d_out : DEVICE [S][H] rows of d, 16-byte aligned
  *   d_scratch  : DEVICE, kf_pages_attend_scratch_bytes(args) bytes, 256-byte aligned (KF_ENOSPC if `scratch_bytes` is less)

@@ -115,7 +115,7 @@ class kf_pages_attend_args(C.Structure):
     _fields_ = [
         ("cache", kf_page_cache), ("n_heads", C.c_int32), ("type", C.c_int32), ("bias_mode", C.c_int32), ("logit_scale", C.c_float),
         ("d_alibi_slopes", C.c_void_p), ("q_sequence_stride", C.c_int64), ("q_head_stride", C.c_int64), ("out_sequence_stride", C.c_int64),
-        ("out_head_stride", C.c_int64), ("debug_fail_first_wait", C.c_int32),
+        ("out_head_stride", C.c_int64), ("debug_fail_first_wait", C.c_int32), ("debug_fail_after", C.c_int32),
     ]
 
 
@@ -385,11 +385,11 @@ def kf_pages_read(*, table, cache, scale, k, v, begin, first=None, stream=None):
 
 
 def kf_pages_attend(*, q, table, length, cache, scale, out, bias_mode=KF_BIAS_NONE, alibi_slopes_dev=None, logit_scale=0.0, debug_fail_first_wait=0,
-                    scratch=None, stream=None):
+                    debug_fail_after=0, scratch=None, stream=None):
     """One query token per sequence, q and out [S, H, d], over the length[s] tokens of its pages.  `scratch`: a uint8 CUDA tensor of
     kf_pages_attend_scratch_bytes(...) bytes; without one torch's allocator provides it for the call."""
-    _check(_kf_torch.pages_attend(q, table, length, cache, scale, out, bias_mode, alibi_slopes_dev, logit_scale, debug_fail_first_wait, scratch, stream),
-           "kf_pages_attend")
+    _check(_kf_torch.pages_attend(q, table, length, cache, scale, out, bias_mode, alibi_slopes_dev, logit_scale, debug_fail_first_wait, debug_fail_after,
+                                  scratch, stream), "kf_pages_attend")
 
 
 def kf_pages_attend_scratch_bytes(*, sequences, table_width, n_pages, page_tokens, n_heads, n_kv_heads, head_dim) -> int:

@@ -2,6 +2,7 @@
 // before anything is enqueued.
 #include "keyformer.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include "kf_args.cuh"
@@ -70,7 +71,7 @@ kf::PageRows rows_of(const kf_page_rows& r, const void* d_k, const void* d_v) {
 bool attend_ok(const kf_pages_attend_args* a) {
   if (!a || !cache_ok(&a->cache) || a->n_heads < 1 || a->n_heads > 65535 || a->n_heads % a->cache.n_kv_heads != 0 || !type16(a->type)) return false;
   if (!(a->logit_scale >= 0.f) || !std::isfinite(a->logit_scale) || !bias_ok(a->bias_mode, a->d_alibi_slopes)) return false;
-  if (a->debug_fail_first_wait < 0 || a->debug_fail_first_wait > 1) return false;
+  if (a->debug_fail_first_wait < 0 || a->debug_fail_first_wait > 1 || (a->debug_fail_first_wait && a->debug_fail_after < 0)) return false;
   for (int64_t s : {a->q_sequence_stride, a->q_head_stride, a->out_sequence_stride, a->out_head_stride})
     if (!stride_ok(s, a->cache.head_dim)) return false;
   if (!kf::pages_attend_fits(cache_of(a->cache, nullptr, nullptr), a->n_heads)) return false;
@@ -189,7 +190,7 @@ int kf_pages_attend(const kf_pages_attend_args* a, const void* d_q, const void* 
   p.out_sequence = a->out_sequence_stride; p.out_head = a->out_head_stride;
   p.H = a->n_heads;
   p.bf16 = a->type == KF_TYPE_BF16;
-  p.fail_first_wait = a->debug_fail_first_wait != 0;
+  p.fail_at = a->debug_fail_first_wait ? 16 * std::min(a->debug_fail_after, 1 << 26) : -1;   // a warp looks up 16 tiles at a time
   p.scale = a->logit_scale > 0.f ? a->logit_scale : (float)(1.0 / std::sqrt((double)c.head_dim));
   p.splits = static_cast<int4*>(d_scratch);
   p.partials = reinterpret_cast<float*>(static_cast<unsigned char*>(d_scratch) + L.partials);

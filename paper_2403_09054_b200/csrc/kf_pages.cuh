@@ -65,7 +65,8 @@ struct PagesAttend {
   const float* slopes;            // [H] or null
   int64_t q_sequence, q_head, out_sequence, out_head;   // strides in elements
   int32_t H;
-  bool bf16, fail_first_wait;
+  int32_t fail_at;                // the self-test's (-1: none): a tile of every warp
+  bool bf16;
   float scale;
   int4* splits;                   // scratch, two per share (warp): the unit that begins in it and goes on behind it, and the CTAs that it covers
   float* partials;                // scratch, pages_attend_partials floats

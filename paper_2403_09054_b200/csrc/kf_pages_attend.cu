@@ -198,7 +198,9 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
     vs = bad ? nan_f32() : log2f(sc.y);
     at = id * c.Hkv + kv;
   };
+  bool failed = false;
   auto look_up = [&](int w0) {
+    if (w0 == a.fail_at) failed = true;               // the self-test: as if the next wait had run out
     if (lane < BATCH && w0 + lane < mine) {
       Ahead t;
       if (SHARES) {
@@ -255,8 +257,7 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
   for (int w = 0; w < ST; ++w)
     if (w < mine) issue(w);
 
-  bool failed = a.fail_first_wait;                    // the self-test: as if the first wait had run out
-  int w = 0, failed_at = 0;
+  int w = 0, failed_at = mine;                        // the first tile that was not waited for
   while (SHARES ? w < mine : w == 0) {                // without shares once, even by a warp without tiles
     // ---- a unit, or the part of it that lies in this share
     const int4 where = SHARES ? *reinterpret_cast<const int4*>(&ahead[w & (2 * BATCH - 1)].seq) : make_int4(own_seq, own_unit, from, total);
@@ -321,8 +322,9 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
       float k1 = k0, v1 = v0;
       if (two && rows > 16) { k1 = scales.z * q_power; v1 = scales.w; }
       const unsigned char* buf = ring + (w % ST) * C::BYTES;
-      if (!failed && !__all_sync(0xffffffffu, mbar_wait_bounded(bars + w % ST, (uint32_t)(w / ST & 1)))) { failed = true; failed_at = w; }
+      if (!failed && !__all_sync(0xffffffffu, mbar_wait_bounded(bars + w % ST, (uint32_t)(w / ST & 1)))) failed = true;
       if (failed) {                                   // nothing more is asked for; the units of the share still have to be gone through
+        failed_at = min(failed_at, w);
         if ((w + ST) % BATCH == 0 && w + ST < mine) look_up(w + ST);
         continue;
       }

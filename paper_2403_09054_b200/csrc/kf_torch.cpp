@@ -390,9 +390,10 @@ PyObject* pages_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return guarded(args, n, 8, [](PyObject* const* a) { return page_rows(a, false); });
 }
 
-// ---- kf_pages_attend: (q, table, length, cache, scale, out, bias_mode, slopes, logit_scale, debug_fail_first_wait, scratch, stream)
+// ---- kf_pages_attend: (q, table, length, cache, scale, out, bias_mode, slopes, logit_scale, debug_fail_first_wait, debug_fail_after, scratch,
+// stream)
 PyObject* pages_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  return guarded(args, n, 12, [](PyObject* const* a) -> int {
+  return guarded(args, n, 13, [](PyObject* const* a) -> int {
     const at::Tensor& x = first_tensor(a[0], "q");
     const at::Device device = x.device();
     const auto type = x.scalar_type();
@@ -406,13 +407,14 @@ PyObject* pages_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
     p.d_alibi_slopes = static_cast<float*>(address(a[7], "alibi_slopes_dev", at::kFloat, q.heads, device, true));
     p.logit_scale = (float)real(a[8]);
     p.debug_fail_first_wait = integer32(a[9]);
+    p.debug_fail_after = integer32(a[10]);
     p.q_sequence_stride = q.row_stride; p.q_head_stride = q.head_stride;
     p.out_sequence_stride = out.row_stride; p.out_head_stride = out.head_stride;
     const int32_t* length = ints(a[2], "length", g.c.sequences, device);
     const size_t need = kf_pages_attend_scratch_bytes(&p);
     if (need == 0) return KF_EINVAL;
-    const Where at_(device, a[11]);
-    const Scratch scratch(a[10], need, device, at_);
+    const Where at_(device, a[12]);
+    const Scratch scratch(a[11], need, device, at_);
     return kf_pages_attend(&p, q.p, g.codes, g.scale, g.table, length, out.p, scratch.p, scratch.bytes, at_.stream.stream());
   });
 }

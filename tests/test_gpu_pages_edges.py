@@ -36,6 +36,32 @@ def test_rows_whose_logits_are_all_huge(size, sign, d, page, wide):
     assert torch.equal(out[0], v[3].bfloat16())
 
 
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 32), (256, 64)])
+@pytest.mark.parametrize("after", [0, 1, 2, 3, 1000])
+@pytest.mark.parametrize("S,longest,wide", [(400, 700, 0), (1, 100000, 0), (20, 500, 0), (20, 500, 1000)])
+def test_a_wait_that_runs_out_in_the_middle(d, page, after, S, longest, wide):
+    """Sequences and heads that a warp is done with before are right, bit for bit, those that it comes to later NaN; shares of many short sequences, parts of a long one, and
+    a CTA for each."""
+    Hkv = 16
+    lengths = [longest * ((37 * i + 63) % 64) // 63 for i in range(S)]
+    pages = sum(-(-n // page) for n in lengths) + 1
+    cache, scale = _pool(pages, Hkv, page, d)
+    table = _table(lengths, page, pages)
+    table = np.concatenate([table, np.full((S, wide), -1, np.int32)], 1)
+    q = torch.randn(S, 32, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(0)).half()
+    want = _attend(q, table, lengths, cache, scale)
+    got = _attend(q, table, lengths, cache, scale, debug_fail_first_wait=1, debug_fail_after=after)
+    nan, tokens = torch.isnan(got).all(-1), torch.tensor(lengths, device=DEV)
+    assert (nan | (got == want).all(-1)).all() and not nan[tokens == 0].any()
+    assert not torch.isnan(want).any()
+    if after == 0:
+        assert nan[tokens > 0].all()
+    if after == 1000:
+        assert not nan.any()
+    if after in (1, 2) and S == 400:        # shares: 73000 tiles or more of 16 heads over at most 1776 warps, at least 41 each
+        assert nan.any() and not nan[tokens > 0].all()
+
+
 @pytest.mark.parametrize("wide", [0, 60])
 def test_values_near_the_smallest_scale(wide):
     """V scales of 2^-120: their outputs are far below one, but bfloat16 holds them."""
