@@ -364,6 +364,11 @@ def kf_reorder_rows(*, buffers, parent, n_layers=1, stream=None):
     _check(_kf_torch.reorder_rows(buffers, parent, n_layers, stream), "kf_reorder_rows")
 
 
+def _fits32(*sizes) -> bool:
+    """Whether sizes keep their values in the int32 fields of an argument struct (ctypes would drop the upper bits)."""
+    return all(0 <= n < 2 ** 31 for n in sizes)
+
+
 def kf_prefill_attend_ragged(*, q, k, v, begin, out, bias_mode=KF_BIAS_NONE, alibi_slopes_dev=None, logit_scale=0.0, debug_fail_first_wait=0, debug_fail_after=0,
                              stream=None):
     """Causal attention over prompts that lie one after the other: sequence s has rows begin[s] .. begin[s + 1] - 1 (int32 [S + 1]) of q, out
@@ -394,6 +399,8 @@ def kf_pages_attend(*, q, table, length, cache, scale, out, bias_mode=KF_BIAS_NO
 
 def kf_pages_attend_scratch_bytes(*, sequences, table_width, n_pages, page_tokens, n_heads, n_kv_heads, head_dim) -> int:
     """Bytes of scratch a kf_pages_attend of this shape needs; 0 if the shape is not supported."""
+    if not _fits32(sequences, table_width, n_pages, page_tokens, n_heads, n_kv_heads, head_dim):
+        return 0
     a = kf_pages_attend_args(cache=kf_page_cache(n_pages, page_tokens, n_kv_heads, head_dim, sequences, table_width), n_heads=n_heads)
     a.q_head_stride = a.out_head_stride = head_dim
     a.q_sequence_stride = a.out_sequence_stride = head_dim * n_heads
@@ -409,6 +416,8 @@ def kf_pages_update(*, table, length, refs, cache, scale, missing, parent=None, 
 
 def kf_pages_update_scratch_bytes(*, sequences, table_width, n_pages, page_tokens, n_kv_heads, head_dim, n_layers=1) -> int:
     """Bytes of scratch a kf_pages_update of this shape needs; 0 if the shape is not supported."""
+    if not _fits32(sequences, table_width, n_pages, page_tokens, n_kv_heads, head_dim, n_layers):
+        return 0
     a = kf_pages_update_args(cache=kf_page_cache(n_pages, page_tokens, n_kv_heads, head_dim, sequences, table_width), n_layers=n_layers)
     return int(LIB.kf_pages_update_scratch_bytes(C.byref(a)))
 

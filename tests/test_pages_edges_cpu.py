@@ -30,3 +30,14 @@ def test_kernels_that_launch_early_wait_before_they_take_anything_that_lasts():
             at = body.find(taken)
             assert at < 0 or at > wait, (file, name, taken)
     assert seen >= 8
+
+
+def test_scratch_of_sizes_beyond_32_bits():
+    """What does not fit the argument structs is not supported: no bytes, not those of another size."""
+    attend = dict(sequences=3, table_width=4, n_pages=20, page_tokens=16, n_heads=4, n_kv_heads=2, head_dim=64)
+    update = dict(sequences=3, table_width=4, n_pages=20, page_tokens=16, n_kv_heads=2, head_dim=64, n_layers=2)
+    assert kf.kf_pages_attend_scratch_bytes(**attend) > 0 and kf.kf_pages_update_scratch_bytes(**update) > 0
+    for f, base in ((kf.kf_pages_attend_scratch_bytes, attend), (kf.kf_pages_update_scratch_bytes, update)):
+        for name, value in base.items():
+            for far in (value + 2 ** 32, value - 2 ** 32, 2 ** 31, 2 ** 70):
+                assert f(**{**base, name: far}) == 0, (name, far)
