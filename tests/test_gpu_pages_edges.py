@@ -74,3 +74,23 @@ def test_values_near_the_smallest_scale(wide):
     out = _attend(q, table, [n], cache, scale)
     assert (out != 0).any()
     _check(out, q, table, [n], cache, scale)
+
+
+@pytest.mark.parametrize("begin", [[0, 30, 30, 40], [0, 30, 20, 40], [-3, 10, 20, 40], [0, 10, 20, 400], [40, 30, 20, 10], [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1, 7]])
+def test_rows_of_ranges_that_are_not_valid_reach_no_page(begin):
+    page, d, Hkv = 16, 64, 2
+    cache, scale = _pool(12, Hkv, page, d)
+    table = np.arange(12, dtype=np.int32).reshape(3, 4)[::-1].copy()
+    want_c, want_s = cache.cpu().numpy().copy(), scale.cpu().numpy().copy()
+    x = torch.randn(2, 40, Hkv, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(0)).half()
+    b = torch.tensor(begin, device=DEV, dtype=torch.int64).to(torch.int32)
+    _kf().kf_pages_write(k=x[0], v=x[1], begin=b, length=_ints([0, 3, 5]), table=_ints(table), cache=cache, scale=scale)
+    got_c, got_s = cache.cpu().numpy(), scale.cpu().numpy()
+    in_order = all(lo <= hi for lo, hi in zip(begin, begin[1:]))
+    for s, (lo, hi) in enumerate(zip(begin, begin[1:])):
+        if 0 <= lo < hi <= 40:
+            ref.write(want_c, want_s, table[s:s + 1], [[0, 3, 5][s]], x.double().cpu().numpy(), [lo, hi])
+            if not in_order:                    # what belongs to such a range is not said: only its own pages
+                continue
+        np.testing.assert_array_equal(got_c[table[s]], want_c[table[s]])
+        np.testing.assert_array_equal(got_s[table[s]], want_s[table[s]])
