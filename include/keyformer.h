@@ -308,7 +308,8 @@ int64_t kf_launch_count(const kf_ctx* ctx);
  * enqueued, and nothing is allocated.  Scratch holds nothing between calls and need not be cleared; two calls that may run at
  * the same time (other streams, other captured graphs) need scratch of their own.  Nothing that a call
  * writes, its scratch included, may share memory with another of its tensors (KF_EINVAL; a tensor with strides counts from its first
- * element to its last, so that two written tensors whose rows alternate within one buffer are refused as well).
+ * element to its last, so that two written tensors whose rows alternate within one buffer are refused as well; kf_prefill_attend_ragged and
+ * kf_pages_read take rows that alternate within one buffer, where they come at the same strides).
  * ------------------------------------------------------------------------------------------------------------------ */
 
 #define KF_TYPE_FP16 0

@@ -64,7 +64,7 @@ bool rows_ok(const kf_page_cache& c, const kf_page_rows* r, const int32_t* d_beg
 kf::PageCache cache_of(const kf_page_cache& c, void* d_cache, float* d_scale) {
   return {static_cast<signed char*>(d_cache), d_scale, c.n_pages, c.page_tokens, c.n_kv_heads, c.head_dim, c.sequences, c.table_width};
 }
-kf::PageRows rows_of(const kf_page_rows& r, const void* d_k, const void* d_v) {
+kf::PageRows page_rows(const kf_page_rows& r, const void* d_k, const void* d_v) {
   return {const_cast<void*>(d_k), const_cast<void*>(d_v), r.k_token_stride, r.k_head_stride, r.v_token_stride, r.v_head_stride, r.tokens, r.type == KF_TYPE_BF16};
 }
 
@@ -112,10 +112,10 @@ int kf_prefill_attend_ragged(const kf_ragged_args* a, const void* d_q, const voi
   if (misaligned(d_begin, 4)) return KF_EINVAL;
   const int d = a->head_dim;
   const bool alibi = a->bias_mode == KF_BIAS_ALIBI;
-  if (conflict({{d_out, extent(a->tokens, a->out_token_stride, a->n_heads, a->out_head_stride, d)}},
-               {{d_q, extent(a->tokens, a->q_token_stride, a->n_heads, a->q_head_stride, d)},
-                {d_k, extent(a->tokens, a->k_token_stride, a->n_kv_heads, a->k_head_stride, d)},
-                {d_v, extent(a->tokens, a->v_token_stride, a->n_kv_heads, a->v_head_stride, d)},
+  if (conflict({rows_of(d_out, a->tokens, a->out_token_stride, a->n_heads, a->out_head_stride, d)},
+               {rows_of(d_q, a->tokens, a->q_token_stride, a->n_heads, a->q_head_stride, d),
+                rows_of(d_k, a->tokens, a->k_token_stride, a->n_kv_heads, a->k_head_stride, d),
+                rows_of(d_v, a->tokens, a->v_token_stride, a->n_kv_heads, a->v_head_stride, d),
                 {d_begin, ((uint64_t)a->sequences + 1) * 4},
                 {alibi ? a->d_alibi_slopes : nullptr, (uint64_t)a->n_heads * 4}}))
     return KF_EINVAL;
@@ -146,7 +146,7 @@ int kf_pages_write(const kf_page_cache* c, const kf_page_rows* r, const void* d_
                 {d_v, extent(r->tokens, r->v_token_stride, c->n_kv_heads, r->v_head_stride, c->head_dim)},
                 {d_begin, (S + 1) * 4}, {d_length, S * 4}, {d_table, table_bytes(*c)}}))
     return KF_EINVAL;
-  return status(kf::launch_pages_write(cache_of(*c, d_cache, d_scale), rows_of(*r, d_k, d_v), d_begin, d_length, d_table, static_cast<cudaStream_t>(stream)));
+  return status(kf::launch_pages_write(cache_of(*c, d_cache, d_scale), page_rows(*r, d_k, d_v), d_begin, d_length, d_table, static_cast<cudaStream_t>(stream)));
 }
 
 int kf_pages_read(const kf_page_cache* c, const kf_page_rows* r, const void* d_cache, const float* d_scale, const int32_t* d_table, const int32_t* d_begin,
@@ -158,11 +158,11 @@ int kf_pages_read(const kf_page_cache* c, const kf_page_rows* r, const void* d_c
       !apart(r->tokens, r->v_token_stride, c->n_kv_heads, r->v_head_stride, c->head_dim))
     return KF_EINVAL;
   const uint64_t S = (uint64_t)c->sequences;
-  if (conflict({{d_k, extent(r->tokens, r->k_token_stride, c->n_kv_heads, r->k_head_stride, c->head_dim)},
-                {d_v, extent(r->tokens, r->v_token_stride, c->n_kv_heads, r->v_head_stride, c->head_dim)}},
+  if (conflict({rows_of(d_k, r->tokens, r->k_token_stride, c->n_kv_heads, r->k_head_stride, c->head_dim),
+                rows_of(d_v, r->tokens, r->v_token_stride, c->n_kv_heads, r->v_head_stride, c->head_dim)},
                {{d_cache, cache_bytes(*c)}, {d_scale, scale_bytes(*c)}, {d_begin, (S + 1) * 4}, {d_first, S * 4}, {d_table, table_bytes(*c)}}))
     return KF_EINVAL;
-  return status(kf::launch_pages_read(cache_of(*c, const_cast<void*>(d_cache), const_cast<float*>(d_scale)), rows_of(*r, d_k, d_v), d_begin, d_first, d_table,
+  return status(kf::launch_pages_read(cache_of(*c, const_cast<void*>(d_cache), const_cast<float*>(d_scale)), page_rows(*r, d_k, d_v), d_begin, d_first, d_table,
                                       static_cast<cudaStream_t>(stream)));
 }
 

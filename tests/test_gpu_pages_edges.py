@@ -94,3 +94,28 @@ def test_rows_of_ranges_that_are_not_valid_reach_no_page(begin):
                 continue
         np.testing.assert_array_equal(got_c[table[s]], want_c[table[s]])
         np.testing.assert_array_equal(got_s[table[s]], want_s[table[s]])
+
+
+@pytest.mark.parametrize("order", ["side by side", "head by head"])
+def test_keys_and_values_that_alternate_in_one_buffer(order):
+    """Both written into one tensor, as they are taken from one; and prompt attention with its output in the rows that hold q, k and v."""
+    d, page, Hkv, T = 64, 16, 2, 70
+    pages = -(-T // page)
+    cache, scale = _pool(pages, Hkv, page, d)
+    table, begin = _ints([list(range(pages))]), _ints([0, T])
+    rows = torch.full((T, 2, Hkv, d) if order == "side by side" else (T, Hkv, 2, d), 5.0, device=DEV).half()
+    k, v = (rows[:, 0], rows[:, 1]) if order == "side by side" else (rows[:, :, 0], rows[:, :, 1])
+    apart = torch.empty(2, T, Hkv, d, device=DEV).half()
+    _kf().kf_pages_read(table=table, cache=cache, scale=scale, k=k, v=v, begin=begin)
+    _kf().kf_pages_read(table=table, cache=cache, scale=scale, k=apart[0], v=apart[1], begin=begin)
+    assert torch.equal(k, apart[0]) and torch.equal(v, apart[1])
+    with pytest.raises(_kf().KeyformerError):
+        _kf().kf_pages_read(table=table, cache=cache, scale=scale, k=k, v=k, begin=begin)
+    wide = torch.randn(T, 4 + 2 * Hkv + 4, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(0)).half()
+    q, k, v, out = wide[:, :4], wide[:, 4:4 + Hkv], wide[:, 4 + Hkv:4 + 2 * Hkv], wide[:, 4 + 2 * Hkv:]
+    want, before = torch.empty(T, 4, d, device=DEV).half(), wide.clone()
+    _kf().kf_prefill_attend_ragged(q=q, k=k, v=v, begin=begin, out=want)
+    _kf().kf_prefill_attend_ragged(q=q, k=k, v=v, begin=begin, out=out)
+    assert torch.equal(out, want) and torch.equal(wide[:, :4 + 2 * Hkv], before[:, :4 + 2 * Hkv])
+    with pytest.raises(_kf().KeyformerError):
+        _kf().kf_prefill_attend_ragged(q=q, k=k, v=v, begin=begin, out=wide[:, 4 + 2 * Hkv - 1:-1])
