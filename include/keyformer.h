@@ -467,7 +467,9 @@ typedef struct kf_ragged_args {
 } kf_ragged_args;
 /*   d_q, d_out : DEVICE [tokens][H] rows of d;  d_k, d_v : DEVICE [tokens][Hkv] rows of d (strides above, 16-byte aligned)
  *   d_begin    : DEVICE int32 [S + 1]
- * Output weights are rounded to the type of v (11 or 8 bits), the output once more; sums and references are binary32.  Rows that
+ * Output weights are rounded to the type of v (11 or 8 bits), the output once more; sums and references are binary32.  In binary16 a weight below 2^-21
+ * of its row's largest keeps fewer bits: it may be off by 2^-32 of that.  Logits are binary32 too: up to 10^6 in magnitude (with the bias) rows
+ * are as exact as that allows, beyond 4 * 10^6 they may be NaN or off by more.  Rows that
  * did not arrive within the kernel's bounded wait make the output rows that need them NaN. */
 int kf_prefill_attend_ragged(const kf_ragged_args* args, const void* d_q, const void* d_k, const void* d_v, const int32_t* d_begin,
                              void* d_out, void* stream);
@@ -509,6 +511,7 @@ int kf_pages_read(const kf_page_cache* cache, const kf_page_rows* rows, const vo
 
 /* One query token per sequence, the newest, over the d_length[s] tokens of its pages (its own row among them):
  *   out = sum_j softmax_j(x_j) v_j,   x_j = logit_scale q k_j (- slope_h (length - 1 - j) with KF_BIAS_ALIBI)
+ * A weight times the scale of its V rows may be off by 2^-32 of the largest of them, beside binary32 roundings.
  * Logits may be of any size that binary32 holds in units of log 2 (a row of which all are -infinity, or one is NaN or +infinity, is NaN).
  * A sequence without tokens gets zeros; one whose length is negative or behind its table, or that needs a missing page, gets NaN. */
 typedef struct kf_pages_attend_args {

@@ -45,7 +45,7 @@ static_assert(128 * FEW_REGS + 256 * MANY_REGS <= 384 * 168, "registers of the l
 constexpr int RING = 5;                 // slots that K and V tiles go through in the order of use
 constexpr uint32_t TMEM_COLS = 512;
 constexpr float HEADROOM = 7.0f;        // log2 units a weight stands above its distance from the reference
-constexpr float LOWEST = -1e30f;
+constexpr float LOWEST = -1e30f;        // far below every logit that binary32 tells from its neighbours (2^22: there the reference is off by a quarter at most)
 constexpr float SLACK = 8.0f;           // log2 units a row's maximum may exceed its reference before the reference moves
 
 struct RaggedParams {

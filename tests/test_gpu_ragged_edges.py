@@ -48,3 +48,46 @@ def test_a_wait_that_runs_out_in_the_middle(d, H, Hkv, after):
     got.fill_(7.0)
     _kf().kf_prefill_attend_ragged(q=q, k=k, v=v, begin=begin, out=got)
     assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("alibi", [False, True])
+def test_rows_whose_logits_are_all_large(d, dtype, sign, alibi):
+    """Logits of a million, all equal: a row is the mean of the values up to it.  Then one key that stands above all others."""
+    q, k, v, begin, out = _inputs([300, 40], 4, 2, d, TYPES[dtype])
+    q[:], k[:] = 0, 0
+    q[..., 0], k[..., 0] = sign * 1000.0, 1000.0
+    kw = dict(bias_mode=1, alibi_slopes_dev=torch.zeros(4, device=DEV)) if alibi else {}
+    _kf().kf_prefill_attend_ragged(q=q, k=k, v=v, begin=begin, out=out, logit_scale=1.0, **kw)
+    # rounded weights are all the same, so they and the output are off by half a step each; binary32 arithmetic below 2^-18
+    half = torch.finfo(TYPES[dtype]).eps / 2
+    floor = 2.0 ** -25 if dtype == "fp16" else 0.0
+    for lo, hi in ((0, 300), (300, 340)):
+        rows = v[lo:hi].double().repeat_interleave(2, 1)
+        count = torch.arange(1, hi - lo + 1, device=DEV)[:, None, None]
+        want, weighted = rows.cumsum(0) / count, rows.abs().cumsum(0) / count
+        assert ((out[lo:hi].double() - want).abs() <= half * want.abs() + (half + 2.0 ** -18) * weighted + floor).all()
+    k[3, :, 0] += sign * 8.0
+    _kf().kf_prefill_attend_ragged(q=q, k=k, v=v, begin=begin, out=out, logit_scale=1.0, **kw)
+    want = v[3].double().repeat_interleave(2, 0)
+    assert ((out[3:300].double() - want).abs() <= (2 * half + 2.0 ** -18) * want.abs() + floor).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("exponent", [21.3, 24.7, 27.4, 30.2, 31.6])
+@pytest.mark.parametrize("d", [64, 256])
+def test_weights_below_the_normal_numbers(dtype, exponent, d):
+    """One key with weight 1 and no value, thousands with weights between 2^-21 and 2^-32 that are no powers of two: each is off by at most 2^-32 in
+    binary16 (a half step of the subnormal numbers, 2^-25, at 2^7 times the weight), beside its relative rounding."""
+    n, H = 4001, 2
+    q, k, v, begin, out = _inputs([n], H, 1, d, TYPES[dtype])
+    q[:], k[:] = 0, 0
+    q[..., 0], k[1:, :, 0] = 1.0, -exponent
+    v[:], v[1:] = 0, 1000.0
+    _kf().kf_prefill_attend_ragged(q=q, k=k, v=v, begin=begin, out=out, logit_scale=math.log(2.0))
+    want, weighted, size = ref.attend_rows(q[-1:].double(), k.double(), v.double(), math.log(2.0), causal=False)
+    limit = ref.bound(want, weighted, size, out.dtype, d, True) + (2.0 ** -32 * 1000.0 * (n - 1) if dtype == "fp16" else 0)
+    assert ((out[-1:].double() - want).abs() <= limit).all()
+    assert (out[-1] > 0).all()
