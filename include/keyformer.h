@@ -449,7 +449,8 @@ int kf_reorder_beams(kf_ctx* ctx, int32_t layer, int32_t beams, const int32_t* d
  *   out_i = sum_{j <= i} softmax_j(x_ij) v_j,   x_ij = logit_scale q_i k_j (- slope_h (i - j) with KF_BIAS_ALIBI)
  * Query head h reads key/value head h / (H / Hkv).  Rows of no sequence are left as they were, and what they hold reaches no
  * output: a sequence ends where its range ends, whatever stands behind it.  Within a sequence a value row that is not finite may make any
- * earlier row of the same 128 NaN.  A sequence whose range is empty or not within 0 .. tokens has no output; ranges do not descend. */
+ * earlier row of the same 128 NaN.  A prompt sees the rows of its own range only: behind tokens that are in pages already (a prefix) it does not
+ * attend to those.  A sequence whose range is empty or not within 0 .. tokens has no output; ranges do not descend. */
 typedef struct kf_ragged_args {
   int32_t tokens, sequences;          /* rows of q, k, v and out (<= 2^28); S (<= 2^20); (tokens / 128 + S) H < 2^31 */
   int32_t n_heads, n_kv_heads;        /* H, Hkv: Hkv divides H                                                    */
@@ -483,7 +484,7 @@ int kf_prefill_attend_ragged(const kf_ragged_args* args, const void* d_q, const 
  * (e >= -120), c = rint(x / 2^e) (ties to even).  While a page fills its scale never shrinks; when it grows, the rows that are there already are
  * brought to it, c <- rint(c * old / new).  As a scale at least doubles then, a row written long before is off by
  * less than one step of the final scale.  A NaN or an infinity among the rows makes the scale NaN: everything of that page, head and side reads as NaN.
- * Scales of another origin may be any positive numbers. */
+ * Scales of another origin may be any positive normal numbers.  The calls below have at least one row or sequence: a step without any makes none. */
 typedef struct kf_page_cache {
   int32_t n_pages, page_tokens;       /* page_tokens in {16, 32, 64, 128}; n_pages * Hkv * 2 * page_tokens < 2^31 */
   int32_t n_kv_heads, head_dim;       /* Hkv; d in {64, 128, 256}                                                  */
@@ -505,7 +506,7 @@ int kf_pages_write(const kf_page_cache* cache, const kf_page_rows* rows, const v
                    const int32_t* d_length, const int32_t* d_table, void* d_cache, float* d_scale, void* stream);
 /* The way back: rows d_begin[s] .. of d_k and d_v are tokens d_first[s] (NULL: 0), ... of sequence s as the numbers their codes
  * stand for, rounded once (beyond the type's
- * largest: infinity).  Rows whose page is missing are NaN; rows of no sequence are left as they were. */
+ * largest: infinity; with scales of another origin the product of code and scale is rounded to binary32 before).  Rows whose page is missing are NaN; rows of no sequence are left as they were. */
 int kf_pages_read(const kf_page_cache* cache, const kf_page_rows* rows, const void* d_cache, const float* d_scale, const int32_t* d_table,
                   const int32_t* d_begin, const int32_t* d_first, void* d_k, void* d_v, void* stream);
 
@@ -554,7 +555,9 @@ int kf_pages_update(const kf_pages_update_args* args, int32_t* d_table, int32_t*
 /* The rows that a selection kept into new pages: row j of (s, head) in the pages of d_new_table is token d_keep[s][head][j] in those of
  * d_table, j < d_n_keep[s] (e.g. the positions that a layer's prompt phase kept).  The scale of a new page is the largest of those that
  * its rows come from, c <- rint(c * old / new).  What lies behind the last row of a page is left as it was.  The new pages are none of those
- * that the call reads.  A token outside 0 .. d_length[s] - 1, or whose page is missing, makes the scales of its new page and head NaN; a new page that is
+ * that the call reads.  From then on a row's place in the pages is no longer its token's place in the text: KF_BIAS_ALIBI of kf_pages_attend counts places
+ * (as KF_POS_NEW does, not KF_POS_ORIGINAL), keys that were rotated keep the positions at which they were, and rows that follow are rotated by the caller at positions
+ * of the text, not at d_length.  A token outside 0 .. d_length[s] - 1, or whose page is missing, makes the scales of its new page and head NaN; a new page that is
  * missing is not written. */
 int kf_pages_compact(const kf_page_cache* cache, int32_t keep_width, int32_t new_table_width, const int32_t* d_table, const int32_t* d_length,
                      const int32_t* d_keep, const int32_t* d_n_keep, const int32_t* d_new_table, void* d_cache, float* d_scale, void* stream);

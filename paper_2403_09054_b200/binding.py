@@ -373,7 +373,7 @@ def kf_prefill_attend_ragged(*, q, k, v, begin, out, bias_mode=KF_BIAS_NONE, ali
                              stream=None):
     """Causal attention over prompts that lie one after the other: sequence s has rows begin[s] .. begin[s + 1] - 1 (int32 [S + 1]) of q, out
     [T, H, d] and k, v [T, Hkv, d] (fp16 or bf16, contiguous features, any strides of tokens and heads: views of a projection's rows, or
-    ``x[0].transpose(0, 1)`` of kf_qk_norm_rotate's head-major rows)."""
+    ``x[0].transpose(0, 1)`` of kf_qk_norm_rotate's head-major rows).  A prompt sees its own rows only.  T is at least 1."""
     _check(_kf_torch.attend_ragged(q, k, v, begin, out, bias_mode, alibi_slopes_dev, logit_scale, debug_fail_first_wait, debug_fail_after, stream),
            "kf_prefill_attend_ragged")
 
@@ -423,7 +423,8 @@ def kf_pages_update_scratch_bytes(*, sequences, table_width, n_pages, page_token
 
 
 def kf_pages_compact(*, cache, scale, table, length, keep, n_keep, new_table, stream=None):
-    """Row j < n_keep[s] of (s, head) in the pages of new_table becomes token keep[s, head, j] (int32 [S, Hkv, width]) in those of table."""
+    """Row j < n_keep[s] of (s, head) in the pages of new_table becomes token keep[s, head, j] (int32 [S, Hkv, width]) in those of table.  Places in the new pages are
+    not positions in the text: ALiBi then counts kept rows, and what is rotated later keeps its own count of positions."""
     _check(_kf_torch.pages_compact(cache, scale, table, length, keep, n_keep, new_table, stream), "kf_pages_compact")
 
 

@@ -280,8 +280,8 @@ __global__ void __launch_bounds__(NT, Shape<D>::RESIDENT) pages_attend_kernel(co
       }
       int e = 0;
       if (a.bf16) {
-        // bfloat16 to binary16: exact after a division by a power of two that brings the head's largest feature to [1, 2), down to
-        // 2^-24 of it.  The power goes back into the logit scale.
+        // bfloat16 to binary16 after a division by a power of two that brings the head's largest feature to [1, 2): exact down to 2^-17 of it (8 bits above
+        // the last place of 2^-24), below that rounded to multiples of 2^-24.  The power goes back into the logit scale.
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < KW; ++i)

@@ -9,7 +9,7 @@
 //     its rows: row r is token r / pack, head r % pack, which is what a TMA box of 64 features x pack heads x tokens writes.
 //   - The grid is laid out without knowing the lengths (slot_sequence).  A CTA per SM starts with its own place and then claims places that
 //     have not been launched (cluster launch control); its roles run on across the borders, so that the next queries, keys and logits are there
-//     when a block's outputs have been written.  Against a CTA per place: 64 prompts of 256 tokens 152 -> 104 us.
+//     when a block's outputs have been written.  Against a CTA per place: 64 prompts of 256 tokens 152 -> 118 us.
 //   - Key tiles are walked from the diagonal back: with ALiBi the nearest keys have the largest logits, so that a row's reference, which
 //     only moves when a maximum exceeds it by 2^8, hardly ever moves (MPT-like layer 504 -> 440 us).  The bias enters by one packed multiply-add.
 //   - A compute thread reads its whole row of S into registers (the launch's registers are dealt out again between the roles), so that the maximum is
@@ -605,7 +605,7 @@ __global__ void __launch_bounds__(threads_of(D == 256 ? 1 : 2), 1) ragged_kernel
         for (int e = 0; e < PIECE / 2; ++e) w[e] = pack2<BF16>(__uint_as_float(v[2 * e]) * inv_l, __uint_as_float(v[2 * e + 1]) * inv_l);
         if (P.wide && block0 + tb <= n) {
           // Whole blocks: four threads exchange sectors of 32 bytes, so that together they store 128 consecutive bytes of a row, as a store takes as many
-          // cycles as it touches lines (16 prompts of 1024: 195 -> 185 us).  Where rows are missing the exchange costs more than it saves.
+          // cycles as it touches lines (16 prompts of 1024: 192 -> 177 us).  Where rows are missing the exchange costs more than it saves.
 #pragma unroll
           for (int g = 0; g < PIECE / 2; g += 32) {
             quad_exchange<1>(w + g);
