@@ -16,8 +16,8 @@
 // result per warp, which pages_merge_kernel joins.  (Chunks of one sequence per CTA instead: 271 against 210 us for 32 x 32 caches of 4096 tokens, whose SMs
 // idled for 40 %.)
 //
-// What bounds it: 32 x 32 caches of 4096 tokens (1.07 GB) take 195 to 198 us, 5.5 TB/s of 6.57; the same loads without any arithmetic take 169.  Half of the issue slots
-// are used (815 warp instructions per 32 tokens of d 128, 416 of them conversions), and the registers allow eight warps, whose products of several groups of tokens the compiler
+// What bounds it: 32 x 32 caches of 4096 tokens (1.07 GB) take 187 to 198 us, 5.4 to 5.7 TB/s of 6.57; the same loads without any arithmetic take 169.  45 % of the issue
+// slots are used (750 warp instructions per 32 tokens of d 128, 416 of them conversions), and the registers allow eight warps, whose products of several groups of tokens the compiler
 // may then mix; twelve of 168 registers, one group of tokens after the other, take as long for many caches and more where a share is short (one sequence of 131072
 // tokens on 8 caches 67 instead of 62 us, 256 of 512 69 instead of 64, units of 74 sequences of 500 24 instead of 18), but for d 64 less (126 instead of 138).  48
 // sequences of up to 8192 tokens on 8 caches: 83 to 90 us, 75 without arithmetic, 61 at the copy rate.  Not taken, for 32 x 32 caches: 16 warps of 128 registers and tiles of 16

@@ -27,7 +27,7 @@
 // What bounds it: two documents of 8192 tokens (32 heads on 8, d 128) take 815 to 966 us from machine to machine, 1.14 to 1.35 PFLOP/s.  A round of both blocks is
 // 2800 cycles: the chain of one block (logits to registers, maximum, two halves of exponentials, the last products, the next logits), while the tensor pipe
 // is busy for 61 % and the exponential unit for 60 %; back to back the 1000 W limit takes the clock from 1.9 to about 1.5 GHz.  Short prompts (48 of up to
-// 97 tokens, 21 us) are three to four items of 6800 cycles per SM, a third of them the stores of the outputs.  Not taken: a share of the exponentials as polynomials
+// 97 tokens, 22 us) are three to four items of 6800 cycles per SM, a third of them the stores of the outputs.  Not taken: a share of the exponentials as polynomials
 // (1 to 3 % at head_dim 64, nothing at 128); for sequences of one block, the blocks of two groups of heads in one item (200 prompts of 60 tokens, one cache per
 // head, 162 -> 119 us, but 64 of 256 4 % slower, 16 of 1024 and head_dim 64 1 to 3 %).
 #include "kf_pages.cuh"
